@@ -47,7 +47,8 @@ typedef enum {
 
 typedef enum {
     DB_F32 = 0,  /* IEEE binary32 */
-    DB_BF16 = 1  /* bfloat16 (upper half of a binary32) */
+    DB_BF16 = 1, /* bfloat16 (upper half of a binary32) */
+    DB_E4M3 = 2  /* 8-bit float, 4 exponent and 3 mantissa bits, largest value 448 (moments of AdamW only) */
 } db_dtype;
 
 /* Largest number of workers one call combines. */
@@ -166,6 +167,122 @@ db_status db_aggregate_update_multi(db_multi_plan* plan, const int32_t* b,
                                     float lr, float mu, double* grad_sqnorm,
                                     void* cuda_stream);
 db_status db_multi_plan_destroy(db_multi_plan* plan);
+
+/* ------------------------------------------------------------------------
+ * AdamW over a list of tensors, moments in 32 or in 8 bits
+ * (Section 3.1, Eq. 2 for the aggregate; the optimizer is the one that language
+ * models are trained with, for which the paper has no counterpart)
+ *
+ * A plan is built once for a fixed list of T tensors, as for the momentum step
+ * above; each step is then, for every element j of every tensor, with t = step >= 1:
+ *     g = sum_k lambda_k grads[k][j],  lambda_k = b[k] / sum_i b[i]   (as above)
+ *     h = c g,   c = max_norm / norm if max_norm > 0 and norm > max_norm, else 1,
+ *                norm = sqrt(sum of g^2 over all tensors)   (a NaN norm: c = 1)
+ *     m <- beta1 m + (1 - beta1) h        u <- beta2 u + (1 - beta2) h^2
+ *     p <- p (1 - lr wd) - lr (m / (1 - beta1^t)) / (sqrt(u / (1 - beta2^t)) + eps)
+ * wd is the tensor's weight decay; p takes m and u before they are rounded to
+ * 8 bits.  All arithmetic is fp32, the norm's sum is held in fp64.
+ *
+ *   grads        host array of K*T device pointers, grads[k*T + t] = worker k's
+ *                gradient of tensor t (sizes[t] elements of grad_dtype, fp32 or bf16)
+ *   sizes        host, T element counts >= 0
+ *   params       host array of T device pointers, fp32, updated in place
+ *   params_bf16  host array of T device pointers that receive the updated
+ *                parameters rounded to bf16 (a working copy), or NULL for none
+ *   first_moment, second_moment   host arrays of T device pointers to sizes[t]
+ *                elements of state_dtype, updated in place (zero before step 1)
+ *   state_dtype  DB_F32, or DB_E4M3: a moment's value is then code * scale with
+ *                one fp32 scale for each DB_ADAMW_BLOCK consecutive elements of a
+ *                tensor (the last block may be shorter)
+ *   first_scale, second_scale     DB_E4M3: host arrays of T device pointers to
+ *                ceil(sizes[t] / DB_ADAMW_BLOCK) fp32 scales, updated in place
+ *                (before step 1: codes and scales zero); DB_F32: ignored, NULL
+ *   weight_decay host, T finite coefficients, or NULL for none
+ *   flags        DB_ADAMW_CLIP if steps may clip (max_norm > 0); the device table
+ *                then also holds 4 bytes for each element when K * sizeof(grad) > 8
+ *   device_table device scratch of >= db_adamw_plan_device_bytes(...) bytes (0 for
+ *                invalid arguments), 256-byte aligned; must outlive the plan
+ *   cuda_stream  (create) the table is uploaded on it and the call waits for the
+ *                upload, so no capture may be under way; (step) the launch stream
+ *   b            host, K mini-batch sizes, each >= 0, sum > 0; b[k] == 0: worker
+ *                k's buffers are not read
+ *   max_norm     0 (no clipping) or the finite bound > 0
+ *   seed         DB_E4M3: seed of the stochastic rounding; ignored for DB_F32
+ *   grad_norm    device, one float that receives norm (before clipping), or NULL
+ *                (no elements in the whole list: nothing is enqueued, it stays)
+ *
+ * 8-bit moments.  For a block with a = max |x|, s = max(a, 2^-100): scale = s / 448,
+ * y = |x| 448 / s, q = 2^(max(floor(log2 y), -6) - 3), and the code's magnitude is
+ * q floor(y / q + r / 65536), at most 448: rounded up with the probability of the
+ * distance, so that a moving average whose change is far below a code's step still
+ * moves, on the average, as it should.  r has 16 random bits: the low (first moment)
+ * or high (second moment) half of hash(256 * blocks of the tensors before + index in
+ * the tensor), keyed by seed and step; the same seed and step give the same bits
+ * whatever the alignment or the launch.  A second moment > 0 is never stored as
+ * code 0 (it gets 2^-9).  A block with a value that is not finite gets a NaN scale
+ * and codes 0: NaN and Inf spread to their block of 256.
+ *
+ * Any alignment down to the element size is accepted; a tensor's accesses are 256-bit
+ * wide when its fp32 buffers are 32-byte, its bf16 buffers 16-byte and its 8-bit
+ * buffers 8-byte aligned, otherwise element-wise.  Results do not depend on it.  No
+ * buffer that a step writes may overlap another one of the plan (DB_ERR_ARG).  Steps
+ * on one plan must not overlap on the device (two captured graphs of steps on one plan
+ * neither); a captured step replays its b, lr, step and seed.
+ * A clipped step is three launches (norm, fold, update), one without clipping is one,
+ * or two with grad_norm (three beyond 2^24 elements).
+ * ------------------------------------------------------------------------ */
+#define DB_ADAMW_BLOCK 256
+#define DB_ADAMW_CLIP 1u
+
+typedef struct db_adamw_plan db_adamw_plan;
+
+size_t db_adamw_plan_device_bytes(int32_t K, db_dtype grad_dtype,
+                                  const int64_t* sizes, int32_t T,
+                                  uint32_t flags);
+db_status db_adamw_plan_create(db_adamw_plan** out, const void* const* grads,
+                               db_dtype grad_dtype, int32_t K,
+                               const int64_t* sizes, int32_t T,
+                               float* const* params, void* const* params_bf16,
+                               void* const* first_moment,
+                               void* const* second_moment,
+                               db_dtype state_dtype, float* const* first_scale,
+                               float* const* second_scale,
+                               const float* weight_decay, uint32_t flags,
+                               void* device_table, size_t device_table_bytes,
+                               void* cuda_stream);
+db_status db_aggregate_adamw_multi(db_adamw_plan* plan, const int32_t* b,
+                                   float lr, float beta1, float beta2,
+                                   float eps, int64_t step, float max_norm,
+                                   uint64_t seed, float* grad_norm,
+                                   void* cuda_stream);
+db_status db_adamw_plan_destroy(db_adamw_plan* plan);
+
+/* ------------------------------------------------------------------------
+ * The global norm of the weighted gradient over a list of tensors
+ * (Section 3.1, Eq. 2 for the aggregate)
+ *
+ *     *grad_norm = sqrt(sum over all tensors and elements of (sum_k lambda_k g_k)^2)
+ * What a clipped AdamW step computes first, for callers that log it, decide by
+ * it or use another optimizer.  The aggregate is formed in fp32 as above; squares
+ * that would overflow or vanish in fp32 are taken in fp64, the sum is held in
+ * fp64, and its order depends on the device and the list alone.
+ * Arguments are those of the AdamW plan; grad_norm: device, one float.  Calls on
+ * one plan must not overlap on the device.  Two launches.
+ * ------------------------------------------------------------------------ */
+typedef struct db_grad_norm_plan db_grad_norm_plan;
+
+size_t db_grad_norm_plan_device_bytes(int32_t K, db_dtype grad_dtype,
+                                      const int64_t* sizes, int32_t T);
+db_status db_grad_norm_plan_create(db_grad_norm_plan** out,
+                                   const void* const* grads,
+                                   db_dtype grad_dtype, int32_t K,
+                                   const int64_t* sizes, int32_t T,
+                                   void* device_table,
+                                   size_t device_table_bytes,
+                                   void* cuda_stream);
+db_status db_grad_norm_multi(db_grad_norm_plan* plan, const int32_t* b,
+                             float* grad_norm, void* cuda_stream);
+db_status db_grad_norm_plan_destroy(db_grad_norm_plan* plan);
 
 /* ------------------------------------------------------------------------
  * The same step for callers that cannot provide scratch memory

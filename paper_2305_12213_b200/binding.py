@@ -16,9 +16,11 @@ from typing import Optional, Sequence
 import torch
 
 DB_OK, DB_ERR_NULL, DB_ERR_ARG, DB_ERR_UNSUPPORTED, DB_ERR_INFEASIBLE, DB_ERR_CUDA = range(6)
-DB_F32, DB_BF16 = 0, 1
+DB_F32, DB_BF16, DB_E4M3 = 0, 1, 2
 DB_MAX_K = 64
 DB_STATIC_SCRATCH_BYTES = 1 << 20     # the built-in scratch of aggregate_update_static
+DB_ADAMW_BLOCK = 256                  # elements that share a scale of an 8-bit moment
+DB_ADAMW_CLIP = 1
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "csrc", "libdynbatch.so")
 
@@ -48,6 +50,18 @@ _SIGNATURES = {
                                        c_void_p, c_size_t, c_void_p]),
     "db_aggregate_update_multi": (c_int32, [c_void_p, c_void_p, c_float, c_float, c_void_p, c_void_p]),
     "db_multi_plan_destroy": (c_int32, [c_void_p]),
+    "db_adamw_plan_device_bytes": (c_size_t, [c_int32, c_int32, c_void_p, c_int32, ctypes.c_uint32]),
+    "db_adamw_plan_create": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_void_p,
+                                       c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, ctypes.c_uint32,
+                                       c_void_p, c_size_t, c_void_p]),
+    "db_aggregate_adamw_multi": (c_int32, [c_void_p, c_void_p, c_float, c_float, c_float, c_float, c_int64, c_float,
+                                           ctypes.c_uint64, c_void_p, c_void_p]),
+    "db_adamw_plan_destroy": (c_int32, [c_void_p]),
+    "db_grad_norm_plan_device_bytes": (c_size_t, [c_int32, c_int32, c_void_p, c_int32]),
+    "db_grad_norm_plan_create": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_size_t,
+                                           c_void_p]),
+    "db_grad_norm_multi": (c_int32, [c_void_p, c_void_p, c_void_p, c_void_p]),
+    "db_grad_norm_plan_destroy": (c_int32, [c_void_p]),
     "db_aggregate_update_static": (c_int32, [c_void_p, c_int32, c_void_p, c_int32, c_int64, c_void_p,
                                              c_void_p, c_float, c_float, c_void_p, c_void_p]),
     "db_shard_range": (c_int32, [c_int64, c_int32, c_int32, c_int32, c_void_p, c_void_p]),
@@ -520,3 +534,152 @@ class MultiTensorPlan:
             self.close()
         except Exception:
             pass
+
+
+class _ListPlan:
+    """What the plans over a tensor list share: the buffers' device, the worker table and the handle's life."""
+
+    _destroy = ""
+
+    def __init__(self, grads: Sequence[Sequence[torch.Tensor]], shapes: Optional[Sequence[torch.Tensor]]):
+        if len(grads) < 1 or len(grads[0]) < 1:
+            raise ValueError("at least one worker and one tensor")
+        self.K, self.T = len(grads), len(grads[0])
+        like = grads[0] if shapes is None else shapes
+        if len(like) != self.T or any(len(g) != self.T for g in grads):
+            raise ValueError("every worker has one gradient for each tensor")
+        self.grad_dtype = grads[0][0].dtype
+        self._code = _dtype_code(self.grad_dtype)
+        self.device = like[0].device
+        self.sizes = [int(t.numel()) for t in like]
+        self._sizes = (c_int64 * self.T)(*self.sizes)
+        self._keep = []                                  # the plan stores raw pointers: the buffers stay alive
+        for g in grads:
+            if any(x.numel() != n for x, n in zip(g, self.sizes)):
+                raise ValueError("gradient and parameter sizes differ")
+        self._grads = (c_void_p * (self.K * self.T))(
+            *[p for g in grads for p in self._pointers(g, self.grad_dtype, "grads[k]")])
+        self._b = (c_int32 * self.K)()
+        self._h = c_void_p()
+
+    def _pointers(self, tensors, dtype, name, sizes=None):
+        tensors = list(tensors)
+        if len(tensors) != self.T:
+            raise ValueError(f"{name} must have one tensor for each parameter tensor")
+        for t, n in zip(tensors, self.sizes if sizes is None else sizes):
+            if t.device != self.device:
+                raise ValueError(f"{name}[t] is on {t.device}, the plan's first tensor on {self.device}")
+            if t.numel() != n:
+                raise ValueError(f"{name}[t] must have {n} elements")
+        self._keep.append(tensors)
+        return [_dev_ptr(t, dtype, f"{name}[t]") for t in tensors]
+
+    def _array(self, tensors, dtype, name, sizes=None):
+        return None if tensors is None else (c_void_p * self.T)(*self._pointers(tensors, dtype, name, sizes))
+
+    def _stream(self, stream: Optional[torch.cuda.Stream]) -> int:
+        return (torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream
+
+    def _on_device(self):
+        return torch.cuda.device(self.device)
+
+    def _workers(self, b: Sequence[int]):
+        if len(b) != self.K:
+            raise ValueError("len(b) != K")
+        self._b[:] = b
+        return self._b
+
+    def _scalar(self, t: Optional[torch.Tensor]) -> Optional[int]:
+        if t is not None and (t.device != self.device or t.numel() < 1):
+            raise ValueError("grad_norm must hold one element on the plan's device")
+        return _dev_ptr(t, torch.float32, "grad_norm")
+
+    def close(self) -> None:
+        if self._h:
+            getattr(lib(), self._destroy)(self._h)
+            self._h = c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class AdamWPlan(_ListPlan):
+    """db_adamw_plan: AdamW over a fixed list of tensors, with optional clipping by the global norm.
+
+    grads[k][t] is worker k's gradient of tensor t (all float32 or all bfloat16); params[t] float32;
+    first_moment[t], second_moment[t] all float32, or all float8_e4m3fn with first_scale[t], second_scale[t] of
+    adamw_scale_elems(numel) float32 elements; params_bf16[t] optional bfloat16 working copies, weight_decay
+    one coefficient for each tensor.  clip: whether steps may pass max_norm > 0.
+    """
+
+    _destroy = "db_adamw_plan_destroy"
+
+    def __init__(self, grads: Sequence[Sequence[torch.Tensor]], params: Sequence[torch.Tensor],
+                 first_moment: Sequence[torch.Tensor], second_moment: Sequence[torch.Tensor],
+                 first_scale: Optional[Sequence[torch.Tensor]] = None,
+                 second_scale: Optional[Sequence[torch.Tensor]] = None,
+                 params_bf16: Optional[Sequence[torch.Tensor]] = None,
+                 weight_decay: Optional[Sequence[float]] = None, clip: bool = False,
+                 stream: Optional[torch.cuda.Stream] = None):
+        super().__init__(grads, params)
+        if len(first_moment) < 1:
+            raise ValueError("first_moment must have one tensor for each parameter tensor")
+        state = first_moment[0].dtype
+        if state not in (torch.float32, torch.float8_e4m3fn):
+            raise TypeError("moments must be float32 or float8_e4m3fn")
+        blocks = [adamw_scale_elems(n) for n in self.sizes]
+        if weight_decay is not None and len(weight_decay) != self.T:
+            raise ValueError("weight_decay must have one coefficient for each parameter tensor")
+        p = self._array(params, torch.float32, "params")
+        w = self._array(params_bf16, torch.bfloat16, "params_bf16")
+        m = self._array(first_moment, state, "first_moment")
+        u = self._array(second_moment, state, "second_moment")
+        ms = self._array(first_scale, torch.float32, "first_scale", blocks)
+        us = self._array(second_scale, torch.float32, "second_scale", blocks)
+        wd = None if weight_decay is None else (c_float * self.T)(*[float(x) for x in weight_decay])
+        flags = DB_ADAMW_CLIP if clip else 0
+        nbytes = int(lib().db_adamw_plan_device_bytes(self.K, self._code, self._sizes, self.T, flags))
+        self.table = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+        with self._on_device():
+            _check(lib().db_adamw_plan_create(
+                ctypes.byref(self._h), self._grads, self._code, self.K, self._sizes, self.T, p, w, m, u,
+                DB_F32 if state == torch.float32 else DB_E4M3, ms, us, wd, flags, self.table.data_ptr(),
+                self.table.numel(), self._stream(stream)))
+        self._fn = lib().db_aggregate_adamw_multi
+
+    def step(self, b: Sequence[int], lr: float, beta1: float, beta2: float, eps: float, step: int,
+             max_norm: float = 0.0, seed: int = 0, grad_norm: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None) -> None:
+        """db_aggregate_adamw_multi: one step of every tensor, in place; grad_norm receives the norm before clipping."""
+        with self._on_device():
+            _check(self._fn(self._h, self._workers(b), lr, beta1, beta2, eps, step, max_norm, seed,
+                            self._scalar(grad_norm), self._stream(stream)))
+
+
+class GradNormPlan(_ListPlan):
+    """db_grad_norm_plan: the global norm of the workers' weighted gradient over a fixed list of tensors."""
+
+    _destroy = "db_grad_norm_plan_destroy"
+
+    def __init__(self, grads: Sequence[Sequence[torch.Tensor]], stream: Optional[torch.cuda.Stream] = None):
+        super().__init__(grads, None)
+        nbytes = int(lib().db_grad_norm_plan_device_bytes(self.K, self._code, self._sizes, self.T))
+        self.table = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+        with self._on_device():
+            _check(lib().db_grad_norm_plan_create(ctypes.byref(self._h), self._grads, self._code, self.K, self._sizes,
+                                                  self.T, self.table.data_ptr(), self.table.numel(),
+                                                  self._stream(stream)))
+        self._fn = lib().db_grad_norm_multi
+
+    def run(self, b: Sequence[int], grad_norm: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """db_grad_norm_multi: grad_norm (one float32) receives the norm."""
+        with self._on_device():
+            _check(self._fn(self._h, self._workers(b), self._scalar(grad_norm), self._stream(stream)))
+
+
+def adamw_scale_elems(n: int) -> int:
+    """Scales of an 8-bit moment of n elements: one for each DB_ADAMW_BLOCK."""
+    return -(-int(n) // DB_ADAMW_BLOCK)

@@ -1,0 +1,468 @@
+// AdamW over a list of parameter tensors for K workers' batch-weighted gradients, moments in 32 or 8 bits, with
+// optional clipping by the global norm; and that norm alone.  A plan holds one record per tile of 2048 elements
+// in device memory, as for the momentum step over a list; each step is one launch, three when it clips (norm of
+// the aggregate, fold, update).
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <exception>
+#include <new>
+#include <utility>
+#include <vector>
+
+#include "adamw_kernels.cuh"
+#include "common.h"
+
+namespace dynbatch {
+namespace {
+
+using namespace adamw;
+
+size_t round256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+size_t grad_bytes(db_dtype dt) { return dt == DB_F32 ? 4 : 2; }
+
+// The fold sums up to kFoldPer partials with one CTA; beyond that a first stage of CTAs takes kFoldPer each.
+constexpr int kFoldPer = 8192;
+
+// Elements of the list in tiles; false if a size is negative or there are more tiles than a grid takes.
+bool count_tiles(const int64_t* sizes, int32_t T, long long* tiles) {
+    long long sum = 0;
+    for (int32_t t = 0; t < T; ++t) {
+        if (sizes[t] < 0) return false;
+        sum += sizes[t] / kTile + (sizes[t] % kTile != 0);
+        if (sum > 0x7fffffffLL) return false;
+    }
+    *tiles = sum;
+    return true;
+}
+
+// Whether a clipped step lets the norm kernel leave the aggregate (4 bytes written, 4 read for each element)
+// instead of reading the K gradients a second time.
+bool stages(int K, db_dtype dt) { return static_cast<size_t>(K) * grad_bytes(dt) > 8; }
+
+struct Layout {
+    long long tiles;
+    int stride;                       // words of a record
+    size_t recs, partials, sums, factor, staged, end;
+};
+
+bool make_layout(int32_t K, db_dtype dt, const int64_t* sizes, int32_t T, int header, bool clip, Layout* L) {
+    if (!count_tiles(sizes, T, &L->tiles)) return false;
+    const size_t n = static_cast<size_t>(L->tiles > 0 ? L->tiles : 1);
+    L->stride = (header + K + 1) & ~1;                             // records stay 16-byte aligned
+    L->recs = 0;
+    L->partials = round256(8 * static_cast<size_t>(L->stride) * n);
+    L->sums = L->partials + round256(8 * n);
+    L->factor = L->sums + round256(8 * (n / kFoldPer + 1));
+    L->staged = L->factor + 256;
+    L->end = L->staged + (clip && stages(K, dt) ? 4 * static_cast<size_t>(kTile) * n : 0);
+    return true;
+}
+
+// Norm kernel: CTAs that stay and take every grid-th tile; few enough that their partials fold in one stage.
+int norm_grid(long long tiles) {
+    const long long most = static_cast<long long>(sm_count()) * 8;
+    return static_cast<int>(tiles < most ? tiles : most);
+}
+
+struct Range {
+    uintptr_t begin, end;
+    bool operator<(const Range& o) const { return begin < o.begin; }
+};
+
+// Buffers that a step writes may not overlap one another, nor a gradient one of them.
+bool overlaps(std::vector<Range>& written, const std::vector<Range>& read) {
+    std::sort(written.begin(), written.end());
+    for (size_t i = 1; i < written.size(); ++i)
+        if (written[i].begin < written[i - 1].end) return true;
+    for (const Range& r : read) {
+        const auto it = std::lower_bound(written.begin(), written.end(), Range{r.end, 0});   // the first that begins at or behind r's end
+        if (it != written.begin() && std::prev(it)->end > r.begin) return true;
+    }
+    return false;
+}
+
+void add_range(std::vector<Range>& v, const void* p, long long n, size_t elem) {
+    if (n > 0 && p) v.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + static_cast<size_t>(n) * elem});
+}
+
+long long word(const void* p) { return static_cast<long long>(reinterpret_cast<uintptr_t>(p)); }
+bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
+
+// Uploads the records and waits for it: plan creation is not on the hot path, and not possible in a capture.
+db_status upload(const std::vector<long long>& recs, void* to, cudaStream_t stream, const char* where) {
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (stream) DB_CUDA_TRY(cudaStreamIsCapturing(stream, &capture));
+    if (capture != cudaStreamCaptureStatusNone) {
+        record_message("a plan cannot be created while its stream is being captured");
+        return DB_ERR_UNSUPPORTED;
+    }
+    cudaError_t err = cudaSuccess;
+    if (!recs.empty()) err = cudaMemcpyAsync(to, recs.data(), 8 * recs.size(), cudaMemcpyHostToDevice, stream);
+    if (err == cudaSuccess) err = cudaStreamSynchronize(stream);
+    return err == cudaSuccess ? DB_OK : record_cuda_error(err, where);
+}
+
+// The workers of a call: weights of those with samples.  DB_ERR_ARG if a batch is negative or all are empty.
+db_status set_workers(const int32_t* b, int K, Source* s) {
+    long long total = 0;
+    for (int k = 0; k < K; ++k) {
+        if (b[k] < 0) return DB_ERR_ARG;
+        total += b[k];
+    }
+    if (total <= 0) return DB_ERR_ARG;
+    s->K = 0;
+    for (int k = 0; k < K; ++k) {
+        if (b[k] == 0) continue;
+        s->lambda[s->K] = static_cast<float>(static_cast<double>(b[k]) / static_cast<double>(total));
+        s->worker[s->K++] = static_cast<unsigned char>(k);
+    }
+    return DB_OK;
+}
+
+// Every kernel may be scheduled while its predecessor in the stream still runs; it waits before its first access.
+template <typename... Params, typename... Args>
+cudaError_t launch(void (*fn)(Params...), long long grid, int block, cudaStream_t stream, Args... args) {
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[1]{};
+    cfg.gridDim = dim3(static_cast<unsigned int>(grid));
+    cfg.blockDim = dim3(block);
+    cfg.stream = stream;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, fn, args...);
+}
+
+db_status launch_fold(double* partials, long long n, double* sums, float* norm, float* factor, float max_norm,
+                      cudaStream_t stream) {
+    if (n > kFoldPer) {
+        const long long stage = (n + kFoldPer - 1) / kFoldPer;
+        DB_CUDA_TRY(launch(fold_kernel, stage, 1024, stream, static_cast<const double*>(partials), n, kFoldPer, sums,
+                           static_cast<float*>(nullptr), static_cast<float*>(nullptr), 0.0f));
+        partials = sums;
+        n = stage;
+    }
+    DB_CUDA_TRY(launch(fold_kernel, 1, n > 256 ? 1024 : 256, stream, static_cast<const double*>(partials), n,
+                       static_cast<int>(n), static_cast<double*>(nullptr), norm, factor, max_norm));
+    return DB_OK;
+}
+
+using NormFn = void (*)(const NormArgs);
+template <typename GT>
+NormFn pick_norm(int K) {
+    if (K <= 1) return grad_norm_kernel<GT, 1>;
+    if (K <= 2) return grad_norm_kernel<GT, 2>;
+    if (K <= 4) return grad_norm_kernel<GT, 4>;
+    return grad_norm_kernel<GT, 8>;
+}
+
+db_status launch_norm(db_dtype dt, const NormArgs& a, int grid, cudaStream_t stream) {
+    const NormFn fn = dt == DB_F32 ? pick_norm<float>(a.src.K) : pick_norm<__nv_bfloat16>(a.src.K);
+    DB_CUDA_TRY(launch(fn, grid, kThreads, stream, a));
+    return DB_OK;
+}
+
+using StepFn = void (*)(const StepArgs);
+template <typename GT, bool STATE8, bool CLIP, bool NORM>
+StepFn pick_workers(int K) {
+    if (K <= 1) return adamw_kernel<GT, 1, STATE8, CLIP, NORM>;
+    if (K <= 2) return adamw_kernel<GT, 2, STATE8, CLIP, NORM>;
+    if (K <= 4) return adamw_kernel<GT, 4, STATE8, CLIP, NORM>;
+    return adamw_kernel<GT, 8, STATE8, CLIP, NORM>;
+}
+template <typename GT, bool STATE8>
+StepFn pick_step(int K, bool clip, bool staged, bool norm) {
+    if (clip) return pick_workers<GT, STATE8, true, false>(staged ? 1 : K);
+    return norm ? pick_workers<GT, STATE8, false, true>(K) : pick_workers<GT, STATE8, false, false>(K);
+}
+
+}  // namespace
+}  // namespace dynbatch
+
+struct db_adamw_plan {
+    dynbatch::Layout layout{};
+    char* table = nullptr;
+    db_dtype grad_dtype = DB_F32, state_dtype = DB_F32;
+    int32_t K = 0;
+    bool clip = false;
+};
+
+struct db_grad_norm_plan {
+    dynbatch::Layout layout{};
+    char* table = nullptr;
+    db_dtype grad_dtype = DB_F32;
+    int32_t K = 0;
+};
+
+namespace dynbatch {
+namespace {
+
+bool known(db_dtype dt) { return dt == DB_F32 || dt == DB_BF16; }
+
+// Checks of the gradient table shared by both plans; fills one tensor's part of `read` and tells whether all
+// its gradients reach the alignment of a lane's vector (32 bytes fp32, 16 bf16).
+db_status check_grads(const void* const* grads, db_dtype dt, int32_t K, int32_t T, int32_t t, long long n,
+                      std::vector<Range>* read, bool* aligned) {
+    const size_t size = grad_bytes(dt);
+    *aligned = true;
+    for (int32_t k = 0; k < K; ++k) {
+        const void* g = grads[static_cast<size_t>(k) * T + t];
+        if (n > 0 && !g) return DB_ERR_NULL;
+        if (misaligned(g, size)) return DB_ERR_ARG;
+        *aligned = *aligned && !misaligned(g, size * kLaneElems);
+        add_range(*read, g, n, size);
+    }
+    return DB_OK;
+}
+
+}  // namespace
+}  // namespace dynbatch
+
+extern "C" size_t db_adamw_plan_device_bytes(int32_t K, db_dtype grad_dtype, const int64_t* sizes, int32_t T,
+                                             uint32_t flags) {
+    using namespace dynbatch;
+    if (!sizes || K < 1 || K > DB_MAX_K || T < 1 || !known(grad_dtype) || (flags & ~DB_ADAMW_CLIP)) return 0;
+    Layout L;
+    return make_layout(K, grad_dtype, sizes, T, kRecGrads, flags & DB_ADAMW_CLIP, &L) ? L.end : 0;
+}
+
+extern "C" db_status db_adamw_plan_create(db_adamw_plan** out, const void* const* grads, db_dtype grad_dtype,
+                                          int32_t K, const int64_t* sizes, int32_t T, float* const* params,
+                                          void* const* params_bf16, void* const* first_moment,
+                                          void* const* second_moment, db_dtype state_dtype,
+                                          float* const* first_scale, float* const* second_scale,
+                                          const float* weight_decay, uint32_t flags, void* device_table,
+                                          size_t device_table_bytes, void* cuda_stream) {
+    using namespace dynbatch;
+    if (!out) return DB_ERR_NULL;
+    *out = nullptr;
+    if (!grads || !sizes || !params || !first_moment || !second_moment || !device_table) return DB_ERR_NULL;
+    if (K < 1 || K > DB_MAX_K || T < 1 || (flags & ~DB_ADAMW_CLIP)) return DB_ERR_ARG;
+    if (!known(grad_dtype) || (state_dtype != DB_F32 && state_dtype != DB_E4M3)) return DB_ERR_UNSUPPORTED;
+    const bool state8 = state_dtype == DB_E4M3, clip = flags & DB_ADAMW_CLIP;
+    if (state8 && (!first_scale || !second_scale)) return DB_ERR_NULL;
+    try {
+        Layout L;
+        if (!make_layout(K, grad_dtype, sizes, T, kRecGrads, clip, &L)) return DB_ERR_ARG;
+        if (misaligned(device_table, 256) || device_table_bytes < L.end) return DB_ERR_ARG;
+        const size_t state_size = state8 ? 1 : 4;
+        std::vector<Range> written, read;
+        std::vector<long long> recs(static_cast<size_t>(L.stride) * static_cast<size_t>(L.tiles), 0);
+        add_range(written, device_table, static_cast<long long>(L.end), 1);
+        long long* r = recs.data();
+        long long position = 0;
+        for (int32_t t = 0; t < T; ++t) {
+            const long long n = sizes[t], blocks = n / kWarpElems + (n % kWarpElems != 0);
+            const float wd = weight_decay ? weight_decay[t] : 0.0f;
+            if (!std::isfinite(wd)) return DB_ERR_ARG;
+            float* p = params[t];
+            char *m = static_cast<char*>(first_moment[t]), *u = static_cast<char*>(second_moment[t]);
+            char* w = params_bf16 ? static_cast<char*>(params_bf16[t]) : nullptr;
+            float *ms = state8 ? first_scale[t] : nullptr, *us = state8 ? second_scale[t] : nullptr;
+            if (n > 0 && (!p || !m || !u || (params_bf16 && !w) || (state8 && (!ms || !us)))) return DB_ERR_NULL;
+            if (misaligned(p, 4) || misaligned(m, state_size) || misaligned(u, state_size) || misaligned(w, 2) ||
+                misaligned(ms, 4) || misaligned(us, 4))
+                return DB_ERR_ARG;
+            add_range(written, p, n, 4);
+            add_range(written, m, n, state_size);
+            add_range(written, u, n, state_size);
+            add_range(written, w, n, 2);
+            add_range(written, ms, blocks, 4);
+            add_range(written, us, blocks, 4);
+            bool grads_aligned;
+            const db_status st = check_grads(grads, grad_dtype, K, T, t, n, &read, &grads_aligned);
+            if (st != DB_OK) return st;
+            const bool state_aligned = !misaligned(p, 32) && !misaligned(m, kLaneElems * state_size) &&
+                                       !misaligned(u, kLaneElems * state_size) && !misaligned(w, 16);
+            const long long bits = (state_aligned ? kStateAligned : 0) | (grads_aligned ? kGradsAligned : 0);
+            uint32_t wd_bits;
+            static_assert(sizeof wd_bits == sizeof wd, "binary32");
+            __builtin_memcpy(&wd_bits, &wd, 4);
+            for (long long e = 0; e < n; e += kTile, r += L.stride) {
+                r[kRecParam] = word(p + e);
+                r[kRecFirst] = word(m + e * state_size);
+                r[kRecSecond] = word(u + e * state_size);
+                r[kRecCount] = (n - e < kTile ? n - e : kTile) | bits << 32;
+                if (state8) {
+                    r[kRecFirstScale] = word(ms + e / kWarpElems);
+                    r[kRecSecondScale] = word(us + e / kWarpElems);
+                }
+                r[kRecCopy] = w ? word(w + 2 * e) : 0;
+                r[kRecDecay] = wd_bits;
+                r[kRecPosition] = position + e;
+                for (int32_t k = 0; k < K; ++k)
+                    r[kRecGrads + k] = word(static_cast<const char*>(grads[static_cast<size_t>(k) * T + t]) + e * grad_bytes(grad_dtype));
+            }
+            position += blocks * kWarpElems;
+        }
+        if (overlaps(written, read)) return DB_ERR_ARG;
+        db_adamw_plan* plan = new db_adamw_plan();
+        plan->layout = L;
+        plan->table = static_cast<char*>(device_table);
+        plan->grad_dtype = grad_dtype;
+        plan->state_dtype = state_dtype;
+        plan->K = K;
+        plan->clip = clip;
+        const db_status st = upload(recs, plan->table + L.recs, static_cast<cudaStream_t>(cuda_stream), "db_adamw_plan_create");
+        if (st != DB_OK) {
+            delete plan;
+            return st;
+        }
+        *out = plan;
+        return DB_OK;
+    } catch (const std::exception&) {
+        record_message("db_adamw_plan_create: out of host memory");
+        return DB_ERR_UNSUPPORTED;
+    }
+}
+
+extern "C" db_status db_adamw_plan_destroy(db_adamw_plan* plan) {
+    delete plan;
+    return DB_OK;
+}
+
+extern "C" db_status db_aggregate_adamw_multi(db_adamw_plan* plan, const int32_t* b, float lr, float beta1, float beta2,
+                                              float eps, int64_t step, float max_norm, uint64_t seed, float* grad_norm,
+                                              void* cuda_stream) {
+    using namespace dynbatch;
+    if (!plan || !b) return DB_ERR_NULL;
+    if (!std::isfinite(lr) || !std::isfinite(eps) || !(eps >= 0.0f) || step < 1) return DB_ERR_ARG;
+    if (!(beta1 >= 0.0f) || !(beta1 < 1.0f) || !(beta2 >= 0.0f) || !(beta2 < 1.0f)) return DB_ERR_ARG;
+    if (!std::isfinite(max_norm) || !(max_norm >= 0.0f) || (max_norm > 0.0f && !plan->clip)) return DB_ERR_ARG;
+    if (misaligned(grad_norm, 4)) return DB_ERR_ARG;
+    StepArgs a{};
+    const db_status st = set_workers(b, plan->K, &a.src);
+    if (st != DB_OK) return st;
+    const Layout& L = plan->layout;
+    if (L.tiles == 0) return DB_OK;
+    const bool clip = max_norm > 0.0f, norm = !clip && grad_norm, staged = clip && stages(a.src.K, plan->grad_dtype);
+    a.src.recs = reinterpret_cast<const long long*>(plan->table + L.recs);
+    a.src.stride = L.stride;
+    a.src.tiles = L.tiles;
+    a.src.staged = staged ? reinterpret_cast<float*>(plan->table + L.staged) : nullptr;
+    a.partials = reinterpret_cast<double*>(plan->table + L.partials);
+    double* sums = reinterpret_cast<double*>(plan->table + L.sums);
+    float* factor = reinterpret_cast<float*>(plan->table + L.factor);
+    a.factor = factor;
+    a.beta1 = beta1;
+    a.beta2 = beta2;
+    a.one_minus_beta1 = 1.0f - beta1;
+    a.one_minus_beta2 = 1.0f - beta2;
+    // bias corrections in fp64, once per call
+    a.step_size = static_cast<float>(static_cast<double>(lr) / (1.0 - std::pow(static_cast<double>(beta1), static_cast<double>(step))));
+    a.inv_sqrt_c2 = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(static_cast<double>(beta2), static_cast<double>(step))));
+    a.eps = eps;
+    a.lr = lr;
+    // keys of the stochastic rounding: the finalizer of splitmix64 (Steele, Lea and Flood 2014) over seed and step
+    uint64_t z = seed + 0x9E3779B97F4A7C15ull * static_cast<uint64_t>(step);
+    z = (z ^ z >> 30) * 0xBF58476D1CE4E5B9ull;
+    z = (z ^ z >> 27) * 0x94D049BB133111EBull;
+    z ^= z >> 31;
+    a.key0 = static_cast<uint32_t>(z);
+    a.key1 = static_cast<uint32_t>(z >> 32);
+
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (clip) {
+        NormArgs n{};
+        n.src = a.src;
+        n.count_word = kRecCount;
+        n.grads_word = kRecGrads;
+        n.partials = a.partials;
+        const int grid = norm_grid(L.tiles);
+        db_status s = launch_norm(plan->grad_dtype, n, grid, stream);
+        if (s == DB_OK) s = launch_fold(a.partials, grid, sums, grad_norm, factor, max_norm, stream);
+        if (s != DB_OK) return s;
+    }
+    const bool state8 = plan->state_dtype == DB_E4M3;
+    StepFn fn;
+    if (plan->grad_dtype == DB_F32)
+        fn = state8 ? pick_step<float, true>(a.src.K, clip, staged, norm) : pick_step<float, false>(a.src.K, clip, staged, norm);
+    else
+        fn = state8 ? pick_step<__nv_bfloat16, true>(a.src.K, clip, staged, norm)
+                    : pick_step<__nv_bfloat16, false>(a.src.K, clip, staged, norm);
+    DB_CUDA_TRY(launch(fn, L.tiles, kThreads, stream, a));
+    return norm ? launch_fold(a.partials, L.tiles, sums, grad_norm, nullptr, 0.0f, stream) : DB_OK;
+}
+
+extern "C" size_t db_grad_norm_plan_device_bytes(int32_t K, db_dtype grad_dtype, const int64_t* sizes, int32_t T) {
+    using namespace dynbatch;
+    if (!sizes || K < 1 || K > DB_MAX_K || T < 1 || !known(grad_dtype)) return 0;
+    Layout L;
+    return make_layout(K, grad_dtype, sizes, T, kNormGrads, false, &L) ? L.end : 0;
+}
+
+extern "C" db_status db_grad_norm_plan_create(db_grad_norm_plan** out, const void* const* grads, db_dtype grad_dtype,
+                                              int32_t K, const int64_t* sizes, int32_t T, void* device_table,
+                                              size_t device_table_bytes, void* cuda_stream) {
+    using namespace dynbatch;
+    if (!out) return DB_ERR_NULL;
+    *out = nullptr;
+    if (!grads || !sizes || !device_table) return DB_ERR_NULL;
+    if (K < 1 || K > DB_MAX_K || T < 1) return DB_ERR_ARG;
+    if (!known(grad_dtype)) return DB_ERR_UNSUPPORTED;
+    try {
+        Layout L;
+        if (!make_layout(K, grad_dtype, sizes, T, kNormGrads, false, &L)) return DB_ERR_ARG;
+        if (misaligned(device_table, 256) || device_table_bytes < L.end) return DB_ERR_ARG;
+        std::vector<Range> written, read;
+        std::vector<long long> recs(static_cast<size_t>(L.stride) * static_cast<size_t>(L.tiles), 0);
+        add_range(written, device_table, static_cast<long long>(L.end), 1);
+        long long* r = recs.data();
+        for (int32_t t = 0; t < T; ++t) {
+            const long long n = sizes[t];
+            bool aligned;
+            const db_status st = check_grads(grads, grad_dtype, K, T, t, n, &read, &aligned);
+            if (st != DB_OK) return st;
+            for (long long e = 0; e < n; e += kTile, r += L.stride) {
+                r[kNormCount] = (n - e < kTile ? n - e : kTile) | static_cast<long long>(aligned ? kGradsAligned : 0) << 32;
+                for (int32_t k = 0; k < K; ++k)
+                    r[kNormGrads + k] = word(static_cast<const char*>(grads[static_cast<size_t>(k) * T + t]) + e * grad_bytes(grad_dtype));
+            }
+        }
+        if (overlaps(written, read)) return DB_ERR_ARG;
+        db_grad_norm_plan* plan = new db_grad_norm_plan();
+        plan->layout = L;
+        plan->table = static_cast<char*>(device_table);
+        plan->grad_dtype = grad_dtype;
+        plan->K = K;
+        const db_status st = upload(recs, plan->table + L.recs, static_cast<cudaStream_t>(cuda_stream), "db_grad_norm_plan_create");
+        if (st != DB_OK) {
+            delete plan;
+            return st;
+        }
+        *out = plan;
+        return DB_OK;
+    } catch (const std::exception&) {
+        record_message("db_grad_norm_plan_create: out of host memory");
+        return DB_ERR_UNSUPPORTED;
+    }
+}
+
+extern "C" db_status db_grad_norm_plan_destroy(db_grad_norm_plan* plan) {
+    delete plan;
+    return DB_OK;
+}
+
+extern "C" db_status db_grad_norm_multi(db_grad_norm_plan* plan, const int32_t* b, float* grad_norm, void* cuda_stream) {
+    using namespace dynbatch;
+    if (!plan || !b || !grad_norm) return DB_ERR_NULL;
+    if (misaligned(grad_norm, 4)) return DB_ERR_ARG;
+    NormArgs a{};
+    const db_status st = set_workers(b, plan->K, &a.src);
+    if (st != DB_OK) return st;
+    const Layout& L = plan->layout;
+    if (L.tiles == 0) return DB_OK;
+    a.src.recs = reinterpret_cast<const long long*>(plan->table + L.recs);
+    a.src.stride = L.stride;
+    a.src.tiles = L.tiles;
+    a.count_word = kNormCount;
+    a.grads_word = kNormGrads;
+    a.partials = reinterpret_cast<double*>(plan->table + L.partials);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const int grid = norm_grid(L.tiles);
+    const db_status s = launch_norm(plan->grad_dtype, a, grid, stream);
+    if (s != DB_OK) return s;
+    return launch_fold(a.partials, grid, reinterpret_cast<double*>(plan->table + L.sums), grad_norm, nullptr, 0.0f, stream);
+}
