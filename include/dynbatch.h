@@ -175,13 +175,17 @@ db_status db_multi_plan_destroy(db_multi_plan* plan);
  *
  * A plan is built once for a fixed list of T tensors, as for the momentum step
  * above; each step is then, for every element j of every tensor, with t = step >= 1:
- *     g = sum_k lambda_k grads[k][j],  lambda_k = b[k] / sum_i b[i]   (as above)
+ *     g = sum_k lambda_k grads[k][j],  lambda_k = b[k] / sum_i b[i]
  *     h = c g,   c = max_norm / norm if max_norm > 0 and norm > max_norm, else 1,
  *                norm = sqrt(sum of g^2 over all tensors)   (a NaN norm: c = 1)
  *     m <- beta1 m + (1 - beta1) h        u <- beta2 u + (1 - beta2) h^2
  *     p <- p (1 - lr wd) - lr (m / (1 - beta1^t)) / (sqrt(u / (1 - beta2^t)) + eps)
  * wd is the tensor's weight decay; p takes m and u before they are rounded to
- * 8 bits.  All arithmetic is fp32, the norm's sum is held in fp64.
+ * 8 bits.  All arithmetic is fp32, squares and sum of the norm are fp64.  g adds
+ * the rounded products of the workers with b[k] > 0 in four partial sums (every
+ * fourth of them, k ascending), joined in order; in m and u every product and sum
+ * is rounded on its own, as written.  So they, and with them the 8-bit codes, are
+ * the same bits on any device and at any alignment.
  *
  *   grads        host array of K*T device pointers, grads[k*T + t] = worker k's
  *                gradient of tensor t (sizes[t] elements of grad_dtype, fp32 or bf16)
@@ -211,7 +215,7 @@ db_status db_multi_plan_destroy(db_multi_plan* plan);
  *   grad_norm    device, one float that receives norm (before clipping), or NULL
  *                (no elements in the whole list: nothing is enqueued, it stays)
  *
- * 8-bit moments.  For a block with a = max |x|, s = max(a, 2^-100): scale = s / 448,
+ * 8-bit moments.  For a block with a = max |x|, s = max(a, 2^-100): scale = s (1/448),
  * y = |x| 448 / s, q = 2^(max(floor(log2 y), -6) - 3), and the code's magnitude is
  * q floor(y / q + r / 65536), at most 448: rounded up with the probability of the
  * distance, so that a moving average whose change is far below a code's step still
@@ -263,9 +267,8 @@ db_status db_adamw_plan_destroy(db_adamw_plan* plan);
  *
  *     *grad_norm = sqrt(sum over all tensors and elements of (sum_k lambda_k g_k)^2)
  * What a clipped AdamW step computes first, for callers that log it, decide by
- * it or use another optimizer.  The aggregate is formed in fp32 as above; squares
- * that would overflow or vanish in fp32 are taken in fp64, the sum is held in
- * fp64, and its order depends on the device and the list alone.
+ * it or use another optimizer.  The aggregate is formed in fp32 as above, squares
+ * and their sum in fp64; the sum's order depends on the device and the list alone.
  * Arguments are those of the AdamW plan; grad_norm: device, one float.  Calls on
  * one plan must not overlap on the device.  Two launches.
  * ------------------------------------------------------------------------ */

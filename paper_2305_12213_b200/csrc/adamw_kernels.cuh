@@ -41,6 +41,7 @@ struct Source {                  // where the weighted gradient comes from
     int stride;
     long long tiles;
     float* staged;               // kTile fp32 aggregates for each tile, or NULL
+    float one;                   // 1, see add()
 };
 
 struct NormArgs {
@@ -60,48 +61,72 @@ struct StepArgs {
     uint32_t key0, key1;
 };
 
+// ---- pairs of fp32 ---------------------------------------------------------------------------------
+// Two elements in a 64-bit register: one instruction multiplies or adds both, each rounded on its own.
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair pack(float lo, float hi) {
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float lo(Pair x) { return __uint_as_float(static_cast<uint32_t>(x)); }
+__device__ __forceinline__ float hi(Pair x) { return __uint_as_float(static_cast<uint32_t>(x >> 32)); }
+__device__ __forceinline__ Pair both(float x) { return pack(x, x); }
+__device__ __forceinline__ Pair mul(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Pair mul_add(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+// a + b, as an FMA with a one that the compiler does not know (`one`, both halves, comes from the host).  ptxas 12.9
+// joins a packed product and a packed sum into one FMA, rounded once, even with .rn on both and --fmad=false
+// (measured: 26 % of a b + c d then differ from the separately rounded sum); this it cannot join.
+__device__ __forceinline__ Pair add(Pair a, Pair b, Pair one) { return mul_add(a, one, b); }
+
 // ---- memory access of one lane's eight elements --------------------------------------------------
 // ALIGNED: elements 8 lane .. 8 lane + 7.  Otherwise elements lane + 32 i, those below n.
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-    asm volatile("ld.global.cs.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
-                 : "l"(p));
-}
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-    asm volatile("st.global.cs.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]),
-                 "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7])
-                 : "memory");
-}
-
 template <bool ALIGNED>
-__device__ __forceinline__ void load_f32(const float* p, int lane, int n, float (&x)[8]) {
+__device__ __forceinline__ void load_f32(const float* p, int lane, int n, Pair (&x)[4]) {
     if (ALIGNED) {
-        load8(p + 8 * lane, x);
+        asm volatile("ld.global.cs.v4.b64 {%0,%1,%2,%3}, [%4];"
+                     : "=l"(x[0]), "=l"(x[1]), "=l"(x[2]), "=l"(x[3])
+                     : "l"(p + 8 * lane));
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = lane + 32 * i < n ? __ldcs(p + lane + 32 * i) : 0.0f;
+        for (int i = 0; i < 4; ++i) {
+            const int j = lane + 64 * i;
+            x[i] = pack(j < n ? __ldcs(p + j) : 0.0f, j + 32 < n ? __ldcs(p + j + 32) : 0.0f);
+        }
     }
 }
 template <bool ALIGNED>
-__device__ __forceinline__ void store_f32(float* p, int lane, int n, const float (&x)[8]) {
+__device__ __forceinline__ void store_f32(float* p, int lane, int n, const Pair (&x)[4]) {
     if (ALIGNED) {
-        store8(p + 8 * lane, x);
+        asm volatile("st.global.cs.v4.b64 [%0], {%1,%2,%3,%4};" ::"l"(p + 8 * lane), "l"(x[0]), "l"(x[1]), "l"(x[2]), "l"(x[3])
+                     : "memory");
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (lane + 32 * i < n) __stcs(p + lane + 32 * i, x[i]);
+        for (int i = 0; i < 4; ++i) {
+            const int j = lane + 64 * i;
+            if (j < n) __stcs(p + j, lo(x[i]));
+            if (j + 32 < n) __stcs(p + j + 32, hi(x[i]));
+        }
     }
 }
 
 // Raw gradient vectors, widened only when they are used, so that several workers' loads are in flight at once.
 template <typename GT> struct GradRaw;
 template <> struct GradRaw<float> {
-    float x[8];
+    Pair x[4];
     template <bool ALIGNED>
     __device__ __forceinline__ void load(const void* base, int lane, int n) {
         load_f32<ALIGNED>(static_cast<const float*>(base), lane, n, x);
     }
-    __device__ __forceinline__ float get(int i) const { return x[i]; }
+    __device__ __forceinline__ Pair get(int i) const { return x[i]; }
 };
 template <> struct GradRaw<__nv_bfloat16> {
     uint32_t x[4];               // bf16 is the high half of a binary32: widening is a shift, exact
@@ -115,22 +140,25 @@ template <> struct GradRaw<__nv_bfloat16> {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int j = lane + 64 * i;
-                const uint32_t lo = j < n ? __ldcs(p + j) : 0u, hi = j + 32 < n ? __ldcs(p + j + 32) : 0u;
-                x[i] = lo | hi << 16;
+                const uint32_t l = j < n ? __ldcs(p + j) : 0u, h = j + 32 < n ? __ldcs(p + j + 32) : 0u;
+                x[i] = l | h << 16;
             }
         }
     }
-    __device__ __forceinline__ float get(int i) const {
-        return __uint_as_float(i & 1 ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16);
+    __device__ __forceinline__ Pair get(int i) const {
+        return pack(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u));
     }
 };
 
-// g = sum over the active workers of lambda_k g_k: fp32 FMAs, k ascending, from zero.  KU workers' loads at once.
+// g = sum over the active workers of lambda_k g_k: products rounded to fp32, added in four partial sums (k mod 4,
+// k ascending) that are joined in order.  Shorter chains than one sum, and a pair's product and sum cost what two
+// FMAs do.  KU workers' loads at once.
 template <typename GT, int KU, bool ALIGNED>
 __device__ __forceinline__ void aggregate(const Source& s, const long long* grads, int offset, int lane, int n,
-                                          float (&g)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) g[i] = 0.0f;
+                                          Pair (&g)[4]) {
+    constexpr int kSums = KU < 4 ? KU : 4;
+    const Pair one = both(s.one);
+    Pair sum[kSums][4];
     for (int k0 = 0; k0 < s.K; k0 += KU) {
         GradRaw<GT> raw[KU];
 #pragma unroll
@@ -139,29 +167,35 @@ __device__ __forceinline__ void aggregate(const Source& s, const long long* grad
                 raw[j].template load<ALIGNED>(reinterpret_cast<const GT*>(__ldg(grads + s.worker[k0 + j])) + offset, lane, n);
 #pragma unroll
         for (int j = 0; j < KU; ++j) {
-            if (k0 + j < s.K) {
-                const float w = s.lambda[k0 + j];
+            const bool in = k0 + j < s.K;
+            const Pair w = both(in ? s.lambda[k0 + j] : 0.0f);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = fmaf(w, raw[j].get(i), g[i]);
+            for (int i = 0; i < 4; ++i) {
+                const Pair x = in ? mul(w, raw[j].get(i)) : both(-0.0f);      // -0 adds nothing to anything
+                if (j < 4) sum[j % kSums][i] = k0 == 0 ? x : add(sum[j % kSums][i], x, one);
+                else sum[j % kSums][i] = add(sum[j % kSums][i], x, one);
             }
         }
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        g[i] = sum[0][i];
+#pragma unroll
+        for (int j = 1; j < kSums; ++j) g[i] = add(g[i], sum[j][i], one);
+    }
 }
 
-// Sum of the squares of a lane's eight aggregates.  In fp32 where every square that matters is a normal number,
-// in fp64 otherwise (a finite gradient beyond 1.8e19 has no fp32 square).
-__device__ __forceinline__ double sum_squares(const float (&g)[8]) {
-    float top = 0.0f, part = 0.0f;
+// Sum of the squares of a lane's eight aggregates, in fp64: a finite gradient beyond 1.8e19 or below 1e-19 has
+// no fp32 square, and the clipping factor is then the correctly rounded one but for the sum's 2^-53.
+__device__ __forceinline__ double sum_squares(const Pair (&g)[4]) {
+    double s = 0.0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        top = fmaxf(top, fabsf(g[i]));
-        part = fmaf(g[i], g[i], part);
+    for (int i = 0; i < 4; ++i) {
+        const double a = lo(g[i]), b = hi(g[i]);
+        s = fma(a, a, s);
+        s = fma(b, b, s);
     }
-    if (top < 1e15f && (top > 1e-15f || top == 0.0f)) return static_cast<double>(part);
-    double wide = 0.0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) wide = fma(static_cast<double>(g[i]), static_cast<double>(g[i]), wide);
-    return wide;
+    return s;
 }
 
 // ---- 8-bit moments --------------------------------------------------------------------------------
@@ -175,33 +209,48 @@ __device__ __forceinline__ uint32_t random_bits(uint32_t position_low, uint32_t 
     return fold_multiply(fold_multiply(position_low ^ key0, 0xAC4C1B51u) ^ key1, 0xD6E8FEB5u);
 }
 
-// e4m3 code of magnitude y in [0, 448], taken up to the next value with probability (distance below y) / (step):
-// `chance` has 16 random bits.  Scaled by 2^-120, the 8-bit type's exponents (subnormals included) are binary32's
-// lowest ones, so one step is 2^20 units of the bit pattern: add the chance below it and cut off.
-__device__ __forceinline__ uint32_t encode(float y, uint32_t chance) {
-    const uint32_t bits = __float_as_uint(y * 0x1p-120f) + (chance << 4);
-    return min(bits >> 20, 0x7eu);
+// e4m3 code of magnitude y in [0, 448], taken up to the next value with probability (distance below y) / (step).
+// Scaled by 2^-120, the 8-bit type's exponents (subnormals included) are binary32's lowest ones, so the code is
+// bits 20 .. 26 of the pattern and what is below them the distance.  Both are kept four bits further up: the code
+// is then the word's top byte, and 16 random bits belong into bytes 1 and 2.
+__device__ __forceinline__ uint32_t encode(float y_scaled, uint32_t chance) { return (__float_as_uint(y_scaled) << 4) + chance; }
+
+// y = |x| (448 / s) has two fp32 roundings, at most two units in the last place (16 each in the word above): where the word is
+// within three of a carry, it cannot tell which code the exact y would get.
+__device__ __forceinline__ uint32_t distance_to_carry(uint32_t word) { return (word << 8) + (48u << 8); }
+constexpr uint32_t kUnsure = 96u << 8;
+
+// The same word's top byte by fp64: q floor(y / q + r / 65536), q = 2^(max(exponent of y, -6) - 3).
+__device__ __noinline__ uint32_t encode_exactly(float magnitude, float top, uint32_t chance) {
+    const double y = static_cast<double>(magnitude) * 448.0 / static_cast<double>(top);
+    int exponent = static_cast<int>(__double_as_longlong(y) >> 52) - 1023;
+    exponent = max(exponent, -6);
+    const double steps = floor(y * __longlong_as_double(static_cast<long long>(1023 + 3 - exponent) << 52) +
+                               static_cast<double>(chance >> 8) * 0x1p-16);
+    const float value = fminf(static_cast<float>(steps) * __uint_as_float(static_cast<uint32_t>(127 + exponent - 3) << 23), 448.0f);
+    return __float_as_uint(value * 0x1p-120f) << 4;
 }
 
-// Block scale: a = max |x| over the warp's 256 elements.  Returns 448 / s for s = max(a, 2^-100) and s / 448; a
-// block with a value that is not finite gets a NaN scale and keep = 0 (codes are masked to zero).
+// Block scale: a = max |x| over the warp's 256 elements, s = max(a, 2^-100).  A block with a value that is not
+// finite gets a NaN scale and keep = 0 (codes are masked to zero).
 struct BlockScale {
-    float to_code, scale;
+    float top, scale;
+    Pair to_code;
     uint32_t keep;
 };
 __device__ __forceinline__ BlockScale block_scale(uint32_t lane_top) {
     const uint32_t top = max(__reduce_max_sync(0xffffffffu, lane_top), 0x0d800000u);      // bits of 2^-100
     const bool finite = top < 0x7f800000u;
-    const float s = __uint_as_float(top);
     BlockScale r;
-    r.to_code = 448.0f / s;
-    r.scale = finite ? s / 448.0f : __uint_as_float(0x7fffffffu);
+    r.top = __uint_as_float(top);
+    r.to_code = both(448.0f / r.top);
+    r.scale = finite ? r.top * (1.0f / 448.0f) : __uint_as_float(0x7fffffffu);
     r.keep = finite ? 0xffffffffu : 0u;
     return r;
 }
 
 template <bool ALIGNED>
-__device__ __forceinline__ void load_codes(const uint8_t* p, int lane, int n, float scale, float (&x)[8]) {
+__device__ __forceinline__ void load_codes(const uint8_t* p, int lane, int n, float scale, Pair (&x)[4]) {
     uint32_t c[2] = {0u, 0u};
     if (ALIGNED) {
         const uint2 r = __ldcs(reinterpret_cast<const uint2*>(p + 8 * lane));
@@ -212,15 +261,20 @@ __device__ __forceinline__ void load_codes(const uint8_t* p, int lane, int n, fl
             if (lane + 32 * i < n) c[i >> 2] |= static_cast<uint32_t>(__ldcs(p + lane + 32 * i)) << (8 * (i & 3));
     }
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(c[i >> 2] >> (8 * (i & 3))), __NV_E4M3);
+    for (int i = 0; i < 4; ++i) {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(c[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
         const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-        x[i] = f.x * scale;
-        x[i + 1] = f.y * scale;
+        x[i] = mul(pack(f.x, f.y), both(scale));
     }
 }
+
+// Codes of eight moments: the words' top bytes.
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
 template <bool ALIGNED>
-__device__ __forceinline__ void store_codes(uint8_t* p, int lane, int n, const uint32_t (&c)[2]) {
+__device__ __forceinline__ void store_codes(uint8_t* p, int lane, int n, const uint32_t (&w)[8], uint32_t keep) {
+    const uint32_t c[2] = {top_bytes(w[0], w[1], w[2], w[3]) & keep, top_bytes(w[4], w[5], w[6], w[7]) & keep};
     if (ALIGNED) {
         __stcs(reinterpret_cast<uint2*>(p + 8 * lane), make_uint2(c[0], c[1]));
     } else {
@@ -231,11 +285,25 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int lane, int n, const u
 }
 
 // ---- one block of elements ------------------------------------------------------------------------
+// Approximate square root and reciprocal (relative error 2^-23 each): they enter the parameter only, through a
+// move that is a small part of it.  The reciprocal flushes subnormals; a denominator is 0 or above 3e-23, the host
+// having raised an eps below the normal numbers to the least of them.
+__device__ __forceinline__ float root(float x) {
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 template <typename GT, int KU, bool STATE8, bool CLIP, bool NORM, bool ALIGNED>
 __device__ __forceinline__ void step_block(const StepArgs& a, const long long* rec, long long tile, int offset, int lane,
                                            int n, float factor, double& sq) {
     float* param = reinterpret_cast<float*>(__ldg(rec + kRecParam)) + offset;
-    float p[8], m[8], u[8], g[8];
+    Pair p[4], m[4], u[4], g[4];
     load_f32<ALIGNED>(param, lane, n, p);
     const long long first = __ldg(rec + kRecFirst), second = __ldg(rec + kRecSecond);
     float *first_scale = nullptr, *second_scale = nullptr;
@@ -254,60 +322,80 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const long long* r
         aggregate<GT, KU, ALIGNED>(a.src, rec + kRecGrads, offset, lane, n, g);
     if (NORM) sq += sum_squares(g);
 
-    const float decay = 1.0f - a.lr * __uint_as_float(static_cast<uint32_t>(__ldg(rec + kRecDecay)));
+    const Pair one = both(a.src.one), decay = both(1.0f - a.lr * __uint_as_float(static_cast<uint32_t>(__ldg(rec + kRecDecay))));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float h = CLIP ? g[i] * factor : g[i];
-        m[i] = fmaf(a.beta1, m[i], a.one_minus_beta1 * h);
-        u[i] = fmaf(a.beta2, u[i], a.one_minus_beta2 * (h * h));
-        p[i] = fmaf(-a.step_size, m[i] / fmaf(sqrtf(u[i]), a.inv_sqrt_c2, a.eps), p[i] * decay);
+    for (int i = 0; i < 4; ++i) {
+        // every product and sum of the moments is rounded on its own: 8-bit codes depend on the last bit
+        const Pair h = CLIP ? mul(g[i], both(factor)) : g[i];
+        m[i] = add(mul(m[i], both(a.beta1)), mul(h, both(a.one_minus_beta1)), one);
+        u[i] = add(mul(u[i], both(a.beta2)), mul(mul(h, h), both(a.one_minus_beta2)), one);
+        const Pair d = mul_add(pack(root(lo(u[i])), root(hi(u[i]))), both(a.inv_sqrt_c2), both(a.eps));
+        const Pair move = mul(m[i], pack(reciprocal(lo(d)), reciprocal(hi(d))));
+        p[i] = mul_add(both(-a.step_size), move, mul(p[i], decay));
     }
     store_f32<ALIGNED>(param, lane, n, p);
     if (const long long copy = __ldg(rec + kRecCopy)) {
         __nv_bfloat16* w = reinterpret_cast<__nv_bfloat16*>(copy) + offset;
         if (ALIGNED) {
-            uint4 r;
-            __nv_bfloat162 h[4];
+            uint32_t r[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(p[2 * i], p[2 * i + 1]);
-            r.x = *reinterpret_cast<uint32_t*>(&h[0]); r.y = *reinterpret_cast<uint32_t*>(&h[1]);
-            r.z = *reinterpret_cast<uint32_t*>(&h[2]); r.w = *reinterpret_cast<uint32_t*>(&h[3]);
-            *reinterpret_cast<uint4*>(w + 8 * lane) = r;
+            for (int i = 0; i < 4; ++i) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(lo(p[i]), hi(p[i]));
+                r[i] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            *reinterpret_cast<uint4*>(w + 8 * lane) = make_uint4(r[0], r[1], r[2], r[3]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (lane + 32 * i < n) w[lane + 32 * i] = __float2bfloat16_rn(p[i]);
+            for (int i = 0; i < 4; ++i) {
+                const int j = lane + 64 * i;
+                if (j < n) w[j] = __float2bfloat16_rn(lo(p[i]));
+                if (j + 32 < n) w[j + 32] = __float2bfloat16_rn(hi(p[i]));
+            }
         }
     }
     if (STATE8) {
+        // elements beyond n have zero moments: they leave the maximum alone
         uint32_t top_m = 0u, top_u = 0u;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (!ALIGNED && lane + 32 * i >= n) continue;
-            top_m = max(top_m, __float_as_uint(m[i]) & 0x7fffffffu);
-            top_u = max(top_u, __float_as_uint(u[i]) & 0x7fffffffu);
+        for (int i = 0; i < 4; ++i) {
+            top_m = max(top_m, max(__float_as_uint(lo(m[i])) & 0x7fffffffu, __float_as_uint(hi(m[i])) & 0x7fffffffu));
+            top_u = max(top_u, max(__float_as_uint(lo(u[i])) & 0x7fffffffu, __float_as_uint(hi(u[i])) & 0x7fffffffu));
         }
         const BlockScale sm = block_scale(top_m), su = block_scale(top_u);
         const long long position = __ldg(rec + kRecPosition) + offset;      // a multiple of 256: the high word is the block's
         const uint32_t low = static_cast<uint32_t>(position) + (ALIGNED ? 8 * lane : lane);
         const uint32_t key1 = a.key1 ^ (static_cast<uint32_t>(position >> 32) * 0x85EBCA6Bu);
-        uint32_t cm[2] = {0u, 0u}, cu[2] = {0u, 0u};
+        uint32_t wm[8], wu[8], nearest = 0xffffffffu;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t r = random_bits(low + (ALIGNED ? i : 32 * i), a.key0, key1);
-            const uint32_t em = encode(fabsf(m[i]) * sm.to_code, r & 0xffffu) | (__float_as_uint(m[i]) >> 24 & 0x80u);
+        for (int i = 0; i < 4; ++i) {
+            const Pair ym = mul(mul(m[i], sm.to_code), both(0x1p-120f)), yu = mul(mul(u[i], su.to_code), both(0x1p-120f));
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int j = 2 * i + e;
+                const uint32_t r = random_bits(low + (ALIGNED ? j : 32 * j), a.key0, key1);
+                wm[j] = encode(fabsf(e ? hi(ym) : lo(ym)), __byte_perm(r, 0u, 0x4104));
+                wu[j] = encode(fabsf(e ? hi(yu) : lo(yu)), __byte_perm(r, 0u, 0x4324));
+                nearest = min(nearest, min(distance_to_carry(wm[j]), distance_to_carry(wu[j])));
+            }
+        }
+        if (nearest < kUnsure) {             // one lane in ten thousand, with its sixteen codes
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t r = random_bits(low + (ALIGNED ? j : 32 * j), a.key0, key1);
+                const float xm = fabsf(j & 1 ? hi(m[j >> 1]) : lo(m[j >> 1])), xu = fabsf(j & 1 ? hi(u[j >> 1]) : lo(u[j >> 1]));
+                if (distance_to_carry(wm[j]) < kUnsure) wm[j] = encode_exactly(xm, sm.top, __byte_perm(r, 0u, 0x4104));
+                if (distance_to_carry(wu[j]) < kUnsure) wu[j] = encode_exactly(xu, su.top, __byte_perm(r, 0u, 0x4324));
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float xm = j & 1 ? hi(m[j >> 1]) : lo(m[j >> 1]), xu = j & 1 ? hi(u[j >> 1]) : lo(u[j >> 1]);
+            wm[j] |= __float_as_uint(xm) & 0x80000000u;
             // a second moment that is not zero is never held as zero: the next step divides by its root
-            const uint32_t eu = max(encode(u[i] * su.to_code, r >> 16), min(__float_as_uint(u[i]), 1u));
-            cm[i >> 2] |= em << (8 * (i & 3));
-            cu[i >> 2] |= eu << (8 * (i & 3));
+            if (xu != 0.0f) wu[j] = max(wu[j], 1u << 24);
         }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            cm[i] &= sm.keep;
-            cu[i] &= su.keep;
-        }
-        store_codes<ALIGNED>(reinterpret_cast<uint8_t*>(first) + offset, lane, n, cm);
-        store_codes<ALIGNED>(reinterpret_cast<uint8_t*>(second) + offset, lane, n, cu);
+        store_codes<ALIGNED>(reinterpret_cast<uint8_t*>(first) + offset, lane, n, wm, sm.keep);
+        store_codes<ALIGNED>(reinterpret_cast<uint8_t*>(second) + offset, lane, n, wu, su.keep);
         if (lane == 0) {
             *first_scale = sm.scale;
             *second_scale = su.scale;
@@ -320,7 +408,7 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const long long* r
 
 // One CTA per tile.
 template <typename GT, int KU, bool STATE8, bool CLIP, bool NORM>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ StepArgs a) {
+__global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 3) adamw_kernel(const __grid_constant__ StepArgs a) {
     agg::griddep_launch_dependents();
     agg::griddep_wait();
     const int lane = threadIdx.x & 31, offset = (threadIdx.x >> 5) * kWarpElems;
@@ -343,7 +431,7 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
 // The norm of the weighted gradient alone: a CTA takes tiles blockIdx.x, blockIdx.x + gridDim.x, ...; with a
 // staging buffer it also leaves the aggregates there, for the step that follows.
 template <typename GT, int KU>
-__global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_constant__ NormArgs a) {
+__global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 3) grad_norm_kernel(const __grid_constant__ NormArgs a) {
     agg::griddep_launch_dependents();
     agg::griddep_wait();
     const int lane = threadIdx.x & 31, offset = (threadIdx.x >> 5) * kWarpElems;
@@ -353,11 +441,11 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_consta
         const long long cf = __ldg(rec + a.count_word);
         const int n = static_cast<int>(cf & 0xffffffffLL) - offset, flags = static_cast<int>(cf >> 32);
         if (n <= 0) continue;
-        float g[8];
+        Pair g[4];
         float* staged = a.src.staged ? a.src.staged + tile * kTile + offset : nullptr;
         if (flags & kGradsAligned && n >= kWarpElems) {
             aggregate<GT, KU, true>(a.src, rec + a.grads_word, offset, lane, kWarpElems, g);
-            if (staged) store8(staged + 8 * lane, g);
+            if (staged) store_f32<true>(staged, lane, kWarpElems, g);
         } else {
             aggregate<GT, KU, false>(a.src, rec + a.grads_word, offset, lane, min(n, kWarpElems), g);
             if (staged) store_f32<false>(staged, lane, min(n, kWarpElems), g);

@@ -111,6 +111,7 @@ db_status set_workers(const int32_t* b, int K, Source* s) {
         total += b[k];
     }
     if (total <= 0) return DB_ERR_ARG;
+    s->one = 1.0f;
     s->K = 0;
     for (int k = 0; k < K; ++k) {
         if (b[k] == 0) continue;
@@ -353,7 +354,7 @@ extern "C" db_status db_aggregate_adamw_multi(db_adamw_plan* plan, const int32_t
     // bias corrections in fp64, once per call
     a.step_size = static_cast<float>(static_cast<double>(lr) / (1.0 - std::pow(static_cast<double>(beta1), static_cast<double>(step))));
     a.inv_sqrt_c2 = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(static_cast<double>(beta2), static_cast<double>(step))));
-    a.eps = eps;
+    a.eps = eps > 0.0f ? std::max(eps, 1.17549435e-38f) : 0.0f;    // a normal number: see the kernel's reciprocal
     a.lr = lr;
     // keys of the stochastic rounding: the finalizer of splitmix64 (Steele, Lea and Flood 2014) over seed and step
     uint64_t z = seed + 0x9E3779B97F4A7C15ull * static_cast<uint64_t>(step);

@@ -520,3 +520,38 @@ def test_training_the_classifier_with_workers_clipping_and_adamw(state8):
         assert abs(seen.item() - norm) <= norm_tolerance(3) * norm and abs(inside.item() - norm) <= norm_tolerance(3) * norm
         check_step(prob, before, grads, bs, 1e-2, B1, B2, EPS, t, min(1.0, limit / norm), norm_tolerance(3) + 2 * ref.EPS32, seed=t)
     assert binding.worker_grad_status(ws) == 0
+
+
+@pytest.mark.parametrize("grad", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("K", [1, 3, 8, 13])
+def test_codes_are_the_definitions_exactly(K, grad):
+    """The same step with 32-bit moments, from the values that the codes stand for, gives the moments before they are
+    rounded, bit for bit; from them the definition in fp64 gives every code, with no element left over, and every
+    scale is the maximum times fp32's 1/448.  Elements next to a border between two codes, and the block's maximum, are among them:
+    two million elements."""
+    n = 1_000_003
+    a = Problem([n, 1_000_000], K, grad, True, 91, fresh=False)
+    wide = object.__new__(Problem)
+    wide.__dict__.update(a.__dict__)
+    wide.p = [x.clone() for x in a.p]
+    vals = a.state()
+    wide.m, wide.u = ([torch.tensor(v[i], dtype=torch.float32, device=DEV) for v in vals] for i in (1, 2))
+    wide.ms = wide.us = None
+    b = batches(K)
+    for prob in (a, wide):
+        prob.plan(clip=True).step(b, LR, B1, B2, EPS, 6, max_norm=0.5, seed=12)
+    torch.cuda.synchronize()
+    position = 0
+    for t, size in enumerate(a.sizes):
+        assert torch.equal(a.p[t], wide.p[t])
+        for codes, scales, x, second in ((a.m[t], a.ms[t], f64(wide.m[t]), False), (a.u[t], a.us[t], f64(wide.u[t]), True)):
+            top = ref.block_max(x)
+            r = ref.random_bits(position + np.arange(size), 12, 6)
+            chance = (r >> np.uint64(16) if second else r & np.uint64(0xFFFF)).astype(np.float64)
+            want = ref.round_up_by_chance(np.abs(x) * 448 / np.repeat(top, 256)[:size], chance)
+            if second:
+                want = np.where(x > 0, np.maximum(want, 2.0**-9), want)
+            got = ref.e4m3_values(codes.view(torch.uint8).cpu().numpy())
+            assert np.array_equal(got, np.where(x < 0, -want, want))
+            assert np.array_equal(f64(scales), (top.astype(np.float32) * np.float32(1 / 448)).astype(np.float64))
+        position += -(-size // 256) * 256
