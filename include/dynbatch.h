@@ -227,13 +227,13 @@ db_status db_multi_plan_destroy(db_multi_plan* plan);
  * and codes 0: NaN and Inf spread to their block of 256.
  *
  * Any alignment down to the element size is accepted; a tensor's accesses are 256-bit
- * wide when its fp32 buffers are 32-byte, its bf16 buffers 16-byte and its 8-bit
- * buffers 8-byte aligned, otherwise element-wise.  Results do not depend on it.  No
+ * wide when its fp32 buffers are 32-byte, its bf16 and 8-bit buffers 16-byte aligned,
+ * otherwise element-wise.  Results do not depend on it.  No
  * buffer that a step writes may overlap another one of the plan (DB_ERR_ARG).  Steps
  * on one plan must not overlap on the device (two captured graphs of steps on one plan
  * neither); a captured step replays its b, lr, step and seed.
- * A clipped step is three launches (norm, fold, update), one without clipping is one,
- * or two with grad_norm (three beyond 2^24 elements).
+ * A clipped step is two launches (norm, update), one without clipping is one, or two or
+ * three with grad_norm.
  * ------------------------------------------------------------------------ */
 #define DB_ADAMW_BLOCK 256
 #define DB_ADAMW_CLIP 1u
@@ -241,8 +241,8 @@ db_status db_multi_plan_destroy(db_multi_plan* plan);
 typedef struct db_adamw_plan db_adamw_plan;
 
 size_t db_adamw_plan_device_bytes(int32_t K, db_dtype grad_dtype,
-                                  const int64_t* sizes, int32_t T,
-                                  uint32_t flags);
+                                  db_dtype state_dtype, const int64_t* sizes,
+                                  int32_t T, uint32_t flags);
 db_status db_adamw_plan_create(db_adamw_plan** out, const void* const* grads,
                                db_dtype grad_dtype, int32_t K,
                                const int64_t* sizes, int32_t T,
@@ -270,7 +270,7 @@ db_status db_adamw_plan_destroy(db_adamw_plan* plan);
  * it or use another optimizer.  The aggregate is formed in fp32 as above, squares
  * and their sum in fp64; the sum's order depends on the device and the list alone.
  * Arguments are those of the AdamW plan; grad_norm: device, one float.  Calls on
- * one plan must not overlap on the device.  Two launches.
+ * one plan must not overlap on the device.  One launch.
  * ------------------------------------------------------------------------ */
 typedef struct db_grad_norm_plan db_grad_norm_plan;
 

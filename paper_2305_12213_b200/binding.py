@@ -50,7 +50,7 @@ _SIGNATURES = {
                                        c_void_p, c_size_t, c_void_p]),
     "db_aggregate_update_multi": (c_int32, [c_void_p, c_void_p, c_float, c_float, c_void_p, c_void_p]),
     "db_multi_plan_destroy": (c_int32, [c_void_p]),
-    "db_adamw_plan_device_bytes": (c_size_t, [c_int32, c_int32, c_void_p, c_int32, ctypes.c_uint32]),
+    "db_adamw_plan_device_bytes": (c_size_t, [c_int32, c_int32, c_int32, c_void_p, c_int32, ctypes.c_uint32]),
     "db_adamw_plan_create": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_void_p,
                                        c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, ctypes.c_uint32,
                                        c_void_p, c_size_t, c_void_p]),
@@ -641,13 +641,13 @@ class AdamWPlan(_ListPlan):
         us = self._array(second_scale, torch.float32, "second_scale", blocks)
         wd = None if weight_decay is None else (c_float * self.T)(*[float(x) for x in weight_decay])
         flags = DB_ADAMW_CLIP if clip else 0
-        nbytes = int(lib().db_adamw_plan_device_bytes(self.K, self._code, self._sizes, self.T, flags))
+        state_code = DB_F32 if state == torch.float32 else DB_E4M3
+        nbytes = int(lib().db_adamw_plan_device_bytes(self.K, self._code, state_code, self._sizes, self.T, flags))
         self.table = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
         with self._on_device():
             _check(lib().db_adamw_plan_create(
                 ctypes.byref(self._h), self._grads, self._code, self.K, self._sizes, self.T, p, w, m, u,
-                DB_F32 if state == torch.float32 else DB_E4M3, ms, us, wd, flags, self.table.data_ptr(),
-                self.table.numel(), self._stream(stream)))
+                state_code, ms, us, wd, flags, self.table.data_ptr(), self.table.numel(), self._stream(stream)))
         self._fn = lib().db_aggregate_adamw_multi
 
     def step(self, b: Sequence[int], lr: float, beta1: float, beta2: float, eps: float, step: int,

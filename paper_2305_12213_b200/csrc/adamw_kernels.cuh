@@ -2,10 +2,11 @@
 // (Section 3.1, Eq. 2 for the aggregate; AdamW and the clipping are what language models train with).
 //
 // Work is laid out in blocks of 256 consecutive elements of one tensor, one warp each: the unit that shares a
-// scale when the moments are held in 8 bits.  A CTA's eight warps take one tile of eight blocks; a record in
-// device memory holds the tile's pointers.  Lanes own eight elements: consecutive ones when every buffer of the
-// tensor is aligned (one 32-byte access for fp32, 16 for bf16, 8 for e4m3), otherwise every 32nd one, element by
-// element.  What is computed for an element does not depend on which lane has it.
+// scale when the moments are held in 8 bits.  A record in device memory holds the pointers of a run of up to
+// `run` elements (a multiple of 2048, one step of a CTA's eight warps) of one tensor; a CTA takes a record.
+// Lanes own eight elements: consecutive ones when every buffer of the tensor is aligned (one 32-byte access for
+// fp32, 16 for bf16, 8 for e4m3), otherwise every 32nd one, element by element.  What is computed for an element
+// does not depend on which lane has it.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
@@ -21,33 +22,37 @@ namespace adamw {
 constexpr int kThreads = 256;
 constexpr int kLaneElems = 8;
 constexpr int kWarpElems = DB_ADAMW_BLOCK;                       // 32 lanes x 8 elements
-constexpr int kTile = kThreads * kLaneElems;
+constexpr int kSpan = kThreads * kLaneElems;                       // elements of a CTA's step
+constexpr int kWarps = kThreads / 32;
 static_assert(kWarpElems == 32 * kLaneElems, "one warp per block of elements");
 
-// Words of 8 bytes of a tile's record; the K gradient pointers follow at kRecGrads.
+// Words of 8 bytes of a run's record; the K gradient pointers follow at kRecGrads.
 enum RecordWord {
     kRecParam = 0, kRecFirst, kRecSecond, kRecCount,             // count | flags << 32
     kRecFirstScale, kRecSecondScale, kRecCopy, kRecDecay,        // bits of the fp32 weight decay
     kRecPosition, kRecSpare, kRecGrads
 };
-enum NormRecordWord { kNormCount = 0, kNormSpare, kNormGrads };
-constexpr int kStateAligned = 1, kGradsAligned = 2;
+enum NormRecordWord { kNormCount = 0, kNormPosition, kNormGrads };
+constexpr int kStateAligned = 1, kGradsAligned = 2;              // flags: buffers aligned to a lane's vector
 
 struct Source {                  // where the weighted gradient comes from
     const long long* recs;       // records, `stride` words apart
+    long long records;
     float lambda[DB_MAX_K];      // weights of the active workers (b_k > 0), in worker order
     unsigned char worker[DB_MAX_K];   // their indexes
     int K;                       // how many
     int stride;
-    long long tiles;
-    float* staged;               // kTile fp32 aggregates for each tile, or NULL
+    float* staged;               // fp32 aggregates by position (256 a block), or NULL
     float one;                   // 1, see add()
 };
 
 struct NormArgs {
     Source src;
-    int count_word, grads_word;
     double* partials;            // one per CTA
+    unsigned int* ticket;        // CTAs that have left their partial; 0 between launches
+    float* norm;                 // or NULL
+    float* factor;               // or NULL
+    float max_norm;
 };
 
 struct StepArgs {
@@ -58,6 +63,7 @@ struct StepArgs {
     float step_size;             // lr / (1 - beta1^t)
     float inv_sqrt_c2;           // 1 / sqrt(1 - beta2^t)
     float eps, lr;
+    int item_workers;            // 8-bit moments: a multiple of 4, or all workers
     uint32_t key0, key1;
 };
 
@@ -211,8 +217,8 @@ __device__ __forceinline__ uint32_t random_bits(uint32_t position_low, uint32_t 
 
 // e4m3 code of magnitude y in [0, 448], taken up to the next value with probability (distance below y) / (step).
 // Scaled by 2^-120, the 8-bit type's exponents (subnormals included) are binary32's lowest ones, so the code is
-// bits 20 .. 26 of the pattern and what is below them the distance.  Both are kept four bits further up: the code
-// is then the word's top byte, and 16 random bits belong into bytes 1 and 2.
+// bits 20 .. 26 of the pattern and what is below them the distance.  Both are kept four bits further up, which also
+// drops the sign: the code is then the word's top byte, and 16 random bits belong into bytes 1 and 2.
 __device__ __forceinline__ uint32_t encode(float y_scaled, uint32_t chance) { return (__float_as_uint(y_scaled) << 4) + chance; }
 
 // y = |x| (448 / s) has two fp32 roundings, at most two units in the last place (16 each in the word above): where the word is
@@ -250,8 +256,8 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t lane_top) {
 }
 
 template <bool ALIGNED>
-__device__ __forceinline__ void load_codes(const uint8_t* p, int lane, int n, float scale, Pair (&x)[4]) {
-    uint32_t c[2] = {0u, 0u};
+__device__ __forceinline__ void load_codes(const uint8_t* p, int lane, int n, uint32_t (&c)[2]) {
+    c[0] = c[1] = 0u;
     if (ALIGNED) {
         const uint2 r = __ldcs(reinterpret_cast<const uint2*>(p + 8 * lane));
         c[0] = r.x; c[1] = r.y;
@@ -260,6 +266,8 @@ __device__ __forceinline__ void load_codes(const uint8_t* p, int lane, int n, fl
         for (int i = 0; i < 8; ++i)
             if (lane + 32 * i < n) c[i >> 2] |= static_cast<uint32_t>(__ldcs(p + lane + 32 * i)) << (8 * (i & 3));
     }
+}
+__device__ __forceinline__ void decode(const uint32_t (&c)[2], float scale, Pair (&x)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(c[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
@@ -299,30 +307,11 @@ __device__ __forceinline__ float reciprocal(float x) {
     return r;
 }
 
-template <typename GT, int KU, bool STATE8, bool CLIP, bool NORM, bool ALIGNED>
-__device__ __forceinline__ void step_block(const StepArgs& a, const long long* rec, long long tile, int offset, int lane,
-                                           int n, float factor, double& sq) {
-    float* param = reinterpret_cast<float*>(__ldg(rec + kRecParam)) + offset;
-    Pair p[4], m[4], u[4], g[4];
-    load_f32<ALIGNED>(param, lane, n, p);
-    const long long first = __ldg(rec + kRecFirst), second = __ldg(rec + kRecSecond);
-    float *first_scale = nullptr, *second_scale = nullptr;
-    if (STATE8) {
-        first_scale = reinterpret_cast<float*>(__ldg(rec + kRecFirstScale)) + offset / kWarpElems;
-        second_scale = reinterpret_cast<float*>(__ldg(rec + kRecSecondScale)) + offset / kWarpElems;
-        load_codes<ALIGNED>(reinterpret_cast<const uint8_t*>(first) + offset, lane, n, *first_scale, m);
-        load_codes<ALIGNED>(reinterpret_cast<const uint8_t*>(second) + offset, lane, n, *second_scale, u);
-    } else {
-        load_f32<ALIGNED>(reinterpret_cast<const float*>(first) + offset, lane, n, m);
-        load_f32<ALIGNED>(reinterpret_cast<const float*>(second) + offset, lane, n, u);
-    }
-    if (CLIP && a.src.staged)
-        load_f32<ALIGNED>(a.src.staged + tile * kTile + offset, lane, n, g);
-    else
-        aggregate<GT, KU, ALIGNED>(a.src, rec + kRecGrads, offset, lane, n, g);
-    if (NORM) sq += sum_squares(g);
-
-    const Pair one = both(a.src.one), decay = both(1.0f - a.lr * __uint_as_float(static_cast<uint32_t>(__ldg(rec + kRecDecay))));
+// One step of the optimizer on a lane's eight elements, given the aggregate.
+template <bool CLIP>
+__device__ __forceinline__ void update(const StepArgs& a, float factor, Pair decay, const Pair (&g)[4], Pair (&p)[4],
+                                       Pair (&m)[4], Pair (&u)[4]) {
+    const Pair one = both(a.src.one);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         // every product and sum of the moments is rounded on its own: 8-bit codes depend on the last bit
@@ -333,87 +322,139 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const long long* r
         const Pair move = mul(m[i], pack(reciprocal(lo(d)), reciprocal(hi(d))));
         p[i] = mul_add(both(-a.step_size), move, mul(p[i], decay));
     }
-    store_f32<ALIGNED>(param, lane, n, p);
-    if (const long long copy = __ldg(rec + kRecCopy)) {
-        __nv_bfloat16* w = reinterpret_cast<__nv_bfloat16*>(copy) + offset;
-        if (ALIGNED) {
-            uint32_t r[4];
+}
+__device__ __forceinline__ Pair decay_of(const StepArgs& a, const long long* rec) {
+    return both(1.0f - a.lr * __uint_as_float(static_cast<uint32_t>(__ldg(rec + kRecDecay))));
+}
+
+template <bool ALIGNED>
+__device__ __forceinline__ void store_copy(long long to, int offset, int lane, int n, const Pair (&p)[4]) {
+    __nv_bfloat16* w = reinterpret_cast<__nv_bfloat16*>(to) + offset;
+    if (ALIGNED) {
+        uint32_t r[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(lo(p[i]), hi(p[i]));
-                r[i] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            *reinterpret_cast<uint4*>(w + 8 * lane) = make_uint4(r[0], r[1], r[2], r[3]);
-        } else {
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(lo(p[i]), hi(p[i]));
+            r[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        __stcs(reinterpret_cast<uint4*>(w + 8 * lane), make_uint4(r[0], r[1], r[2], r[3]));
+    } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int j = lane + 64 * i;
-                if (j < n) w[j] = __float2bfloat16_rn(lo(p[i]));
-                if (j + 32 < n) w[j + 32] = __float2bfloat16_rn(hi(p[i]));
-            }
+        for (int i = 0; i < 4; ++i) {
+            const int j = lane + 64 * i;
+            if (j < n) w[j] = __float2bfloat16_rn(lo(p[i]));
+            if (j + 32 < n) w[j + 32] = __float2bfloat16_rn(hi(p[i]));
         }
     }
-    if (STATE8) {
-        // elements beyond n have zero moments: they leave the maximum alone
-        uint32_t top_m = 0u, top_u = 0u;
+}
+
+// Both moments of a block to 8 bits: codes at `first`, `second`, scales by lane 0.
+template <bool ALIGNED>
+__device__ __forceinline__ void store_moments(const StepArgs& a, uint8_t* first, uint8_t* second, float* first_scale,
+                                              float* second_scale, long long position, int lane, int n,
+                                              const Pair (&m)[4], const Pair (&u)[4]) {
+    // elements beyond n have zero moments: they leave the maximum alone
+    uint32_t top_m = 0u, top_u = 0u;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            top_m = max(top_m, max(__float_as_uint(lo(m[i])) & 0x7fffffffu, __float_as_uint(hi(m[i])) & 0x7fffffffu));
-            top_u = max(top_u, max(__float_as_uint(lo(u[i])) & 0x7fffffffu, __float_as_uint(hi(u[i])) & 0x7fffffffu));
+    for (int i = 0; i < 4; ++i) {
+        top_m = max(top_m, max(__float_as_uint(lo(m[i])) & 0x7fffffffu, __float_as_uint(hi(m[i])) & 0x7fffffffu));
+        top_u = max(top_u, max(__float_as_uint(lo(u[i])) & 0x7fffffffu, __float_as_uint(hi(u[i])) & 0x7fffffffu));
+    }
+    const BlockScale sm = block_scale(top_m), su = block_scale(top_u);
+    // position is a multiple of 256: its high word is the whole block's
+    const uint32_t low = static_cast<uint32_t>(position) + (ALIGNED ? 8 * lane : lane);
+    const uint32_t key1 = a.key1 ^ (static_cast<uint32_t>(position >> 32) * 0x85EBCA6Bu);
+    uint32_t wm[8], wu[8], nearest = 0xffffffffu;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const Pair ym = mul(mul(m[i], sm.to_code), both(0x1p-120f)), yu = mul(mul(u[i], su.to_code), both(0x1p-120f));
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int j = 2 * i + e;
+            const uint32_t r = random_bits(low + (ALIGNED ? j : 32 * j), a.key0, key1);
+            wm[j] = encode(e ? hi(ym) : lo(ym), __byte_perm(r, 0u, 0x4104));
+            wu[j] = encode(e ? hi(yu) : lo(yu), __byte_perm(r, 0u, 0x4324));
+            nearest = min(nearest, min(distance_to_carry(wm[j]), distance_to_carry(wu[j])));
         }
-        const BlockScale sm = block_scale(top_m), su = block_scale(top_u);
-        const long long position = __ldg(rec + kRecPosition) + offset;      // a multiple of 256: the high word is the block's
-        const uint32_t low = static_cast<uint32_t>(position) + (ALIGNED ? 8 * lane : lane);
-        const uint32_t key1 = a.key1 ^ (static_cast<uint32_t>(position >> 32) * 0x85EBCA6Bu);
-        uint32_t wm[8], wu[8], nearest = 0xffffffffu;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const Pair ym = mul(mul(m[i], sm.to_code), both(0x1p-120f)), yu = mul(mul(u[i], su.to_code), both(0x1p-120f));
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int j = 2 * i + e;
-                const uint32_t r = random_bits(low + (ALIGNED ? j : 32 * j), a.key0, key1);
-                wm[j] = encode(fabsf(e ? hi(ym) : lo(ym)), __byte_perm(r, 0u, 0x4104));
-                wu[j] = encode(fabsf(e ? hi(yu) : lo(yu)), __byte_perm(r, 0u, 0x4324));
-                nearest = min(nearest, min(distance_to_carry(wm[j]), distance_to_carry(wu[j])));
-            }
-        }
-        if (nearest < kUnsure) {             // one lane in ten thousand, with its sixteen codes
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t r = random_bits(low + (ALIGNED ? j : 32 * j), a.key0, key1);
-                const float xm = fabsf(j & 1 ? hi(m[j >> 1]) : lo(m[j >> 1])), xu = fabsf(j & 1 ? hi(u[j >> 1]) : lo(u[j >> 1]));
-                if (distance_to_carry(wm[j]) < kUnsure) wm[j] = encode_exactly(xm, sm.top, __byte_perm(r, 0u, 0x4104));
-                if (distance_to_carry(wu[j]) < kUnsure) wu[j] = encode_exactly(xu, su.top, __byte_perm(r, 0u, 0x4324));
-            }
-        }
+    }
+    if (nearest < kUnsure) {             // one lane in ten thousand, with its sixteen codes
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float xm = j & 1 ? hi(m[j >> 1]) : lo(m[j >> 1]), xu = j & 1 ? hi(u[j >> 1]) : lo(u[j >> 1]);
-            wm[j] |= __float_as_uint(xm) & 0x80000000u;
-            // a second moment that is not zero is never held as zero: the next step divides by its root
-            if (xu != 0.0f) wu[j] = max(wu[j], 1u << 24);
+            const uint32_t r = random_bits(low + (ALIGNED ? j : 32 * j), a.key0, key1);
+            const float xm = fabsf(j & 1 ? hi(m[j >> 1]) : lo(m[j >> 1])), xu = fabsf(j & 1 ? hi(u[j >> 1]) : lo(u[j >> 1]));
+            if (distance_to_carry(wm[j]) < kUnsure) wm[j] = encode_exactly(xm, sm.top, __byte_perm(r, 0u, 0x4104));
+            if (distance_to_carry(wu[j]) < kUnsure) wu[j] = encode_exactly(xu, su.top, __byte_perm(r, 0u, 0x4324));
         }
-        store_codes<ALIGNED>(reinterpret_cast<uint8_t*>(first) + offset, lane, n, wm, sm.keep);
-        store_codes<ALIGNED>(reinterpret_cast<uint8_t*>(second) + offset, lane, n, wu, su.keep);
-        if (lane == 0) {
-            *first_scale = sm.scale;
-            *second_scale = su.scale;
-        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float xm = j & 1 ? hi(m[j >> 1]) : lo(m[j >> 1]), xu = j & 1 ? hi(u[j >> 1]) : lo(u[j >> 1]);
+        wm[j] |= __float_as_uint(xm) & 0x80000000u;
+        // a second moment that is not zero is never held as zero: the next step divides by its root
+        if (xu != 0.0f) wu[j] = max(wu[j], 1u << 24);
+    }
+    store_codes<ALIGNED>(first, lane, n, wm, sm.keep);
+    store_codes<ALIGNED>(second, lane, n, wu, su.keep);
+    if (lane == 0) {
+        *first_scale = sm.scale;
+        *second_scale = su.scale;
+    }
+}
+
+// A block straight from global memory to registers and back.
+template <typename GT, int KU, bool STATE8, bool CLIP, bool NORM, bool ALIGNED>
+__device__ __forceinline__ void step_block(const StepArgs& a, const long long* rec, int offset, int lane, int n, float factor,
+                                           double& sq) {
+    float* param = reinterpret_cast<float*>(__ldg(rec + kRecParam)) + offset;
+    Pair p[4], m[4], u[4], g[4];
+    load_f32<ALIGNED>(param, lane, n, p);
+    const long long first = __ldg(rec + kRecFirst), second = __ldg(rec + kRecSecond);
+    float *first_scale = nullptr, *second_scale = nullptr;
+    if (STATE8) {
+        first_scale = reinterpret_cast<float*>(__ldg(rec + kRecFirstScale)) + offset / kWarpElems;
+        second_scale = reinterpret_cast<float*>(__ldg(rec + kRecSecondScale)) + offset / kWarpElems;
+        uint32_t c[2];
+        load_codes<ALIGNED>(reinterpret_cast<const uint8_t*>(first) + offset, lane, n, c);
+        decode(c, *first_scale, m);
+        load_codes<ALIGNED>(reinterpret_cast<const uint8_t*>(second) + offset, lane, n, c);
+        decode(c, *second_scale, u);
+    } else {
+        load_f32<ALIGNED>(reinterpret_cast<const float*>(first) + offset, lane, n, m);
+        load_f32<ALIGNED>(reinterpret_cast<const float*>(second) + offset, lane, n, u);
+    }
+    const long long position = __ldg(rec + kRecPosition) + offset;
+    if (CLIP && a.src.staged)
+        load_f32<ALIGNED>(a.src.staged + position, lane, n, g);
+    else
+        aggregate<GT, KU, ALIGNED>(a.src, rec + kRecGrads, offset, lane, n, g);
+    if (NORM) sq += sum_squares(g);
+    update<CLIP>(a, factor, decay_of(a, rec), g, p, m, u);
+    store_f32<ALIGNED>(param, lane, n, p);
+    if (const long long copy = __ldg(rec + kRecCopy)) store_copy<ALIGNED>(copy, offset, lane, n, p);
+    if (STATE8) {
+        store_moments<ALIGNED>(a, reinterpret_cast<uint8_t*>(first) + offset, reinterpret_cast<uint8_t*>(second) + offset,
+                               first_scale, second_scale, position, lane, n, m, u);
     } else {
         store_f32<ALIGNED>(reinterpret_cast<float*>(first) + offset, lane, n, m);
         store_f32<ALIGNED>(reinterpret_cast<float*>(second) + offset, lane, n, u);
     }
 }
 
-// One CTA per tile.
-template <typename GT, int KU, bool STATE8, bool CLIP, bool NORM>
+// The same for a block off the vector grid or shorter than 256, kept out of the kernels' registers.
+template <typename GT, bool STATE8, bool CLIP, bool NORM>
+__device__ __noinline__ double step_block_slow(const StepArgs& a, const long long* rec, int offset, int lane, int n, float factor) {
+    double sq = 0.0;
+    step_block<GT, 4, STATE8, CLIP, NORM, false>(a, rec, offset, lane, n, factor, sq);
+    return sq;
+}
+
+// 32-bit moments: one CTA per record, one block per warp.
+template <typename GT, int KU, bool CLIP, bool NORM>
 __global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 3) adamw_kernel(const __grid_constant__ StepArgs a) {
     agg::griddep_launch_dependents();
     agg::griddep_wait();
     const int lane = threadIdx.x & 31, offset = (threadIdx.x >> 5) * kWarpElems;
-    const long long tile = blockIdx.x;
-    const long long* rec = a.src.recs + tile * a.src.stride;
+    const long long* rec = a.src.recs + blockIdx.x * static_cast<long long>(a.src.stride);
     const long long cf = __ldg(rec + kRecCount);
     const int n = static_cast<int>(cf & 0xffffffffLL) - offset, flags = static_cast<int>(cf >> 32);
     const float factor = CLIP ? __ldcg(a.factor) : 1.0f;
@@ -421,45 +462,261 @@ __global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 3) adamw_kernel(const 
     if (n > 0) {
         const bool aligned = flags & kStateAligned && (flags & kGradsAligned || (CLIP && a.src.staged));
         if (aligned && n >= kWarpElems)
-            step_block<GT, KU, STATE8, CLIP, NORM, true>(a, rec, tile, offset, lane, kWarpElems, factor, sq);
+            step_block<GT, KU, false, CLIP, NORM, true>(a, rec, offset, lane, kWarpElems, factor, sq);
         else
-            step_block<GT, KU, STATE8, CLIP, NORM, false>(a, rec, tile, offset, lane, min(n, kWarpElems), factor, sq);
+            sq = step_block_slow<GT, false, CLIP, NORM>(a, rec, offset, lane, min(n, kWarpElems), factor);
     }
     if (NORM) agg::store_norm_partial(a.partials, sq);
 }
 
-// The norm of the weighted gradient alone: a CTA takes tiles blockIdx.x, blockIdx.x + gridDim.x, ...; with a
-// staging buffer it also leaves the aggregates there, for the step that follows.
-template <typename GT, int KU>
-__global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 3) grad_norm_kernel(const __grid_constant__ NormArgs a) {
-    agg::griddep_launch_dependents();
-    agg::griddep_wait();
-    const int lane = threadIdx.x & 31, offset = (threadIdx.x >> 5) * kWarpElems;
-    double sq = 0.0;
-    for (long long tile = blockIdx.x; tile < a.src.tiles; tile += gridDim.x) {
-        const long long* rec = a.src.recs + tile * a.src.stride;
-        const long long cf = __ldg(rec + a.count_word);
-        const int n = static_cast<int>(cf & 0xffffffffLL) - offset, flags = static_cast<int>(cf >> 32);
-        if (n <= 0) continue;
-        Pair g[4];
-        float* staged = a.src.staged ? a.src.staged + tile * kTile + offset : nullptr;
-        if (flags & kGradsAligned && n >= kWarpElems) {
-            aggregate<GT, KU, true>(a.src, rec + a.grads_word, offset, lane, kWarpElems, g);
-            if (staged) store_f32<true>(staged, lane, kWarpElems, g);
-        } else {
-            aggregate<GT, KU, false>(a.src, rec + a.grads_word, offset, lane, min(n, kWarpElems), g);
-            if (staged) store_f32<false>(staged, lane, min(n, kWarpElems), g);
-        }
-        sq += sum_squares(g);
-    }
-    agg::store_norm_partial(a.partials, sq);
+// ---- 8-bit moments: blocks through shared memory ------------------------------------------------------
+// Sixty instructions an element keep a warp busy for as long as its loads take, and the registers that this needs
+// leave few warps: with loads and arithmetic in turn the kernel reached 47 % of the DRAM's rate (issue slots 43 %
+// busy).  So every warp copies blocks ahead into shared memory of its own (cp.async, kept in order by commit
+// groups; nobody waits for another warp) and computes on one that has arrived.
+// An item is one block's parameters, codes and scales with up to `item_workers` gradients; further workers of the
+// block follow as items of gradients alone.
+
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
+    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Bytes of a stage of one warp: parameters, codes, scales (padded to 16), gradients.
+constexpr int kStageCodes = 4 * kWarpElems, kStageScales = kStageCodes + 2 * kWarpElems, kStageGrads = kStageScales + 16;
+__host__ __device__ constexpr int stage_bytes(int workers, int grad_size) {
+    return kStageGrads + workers * grad_size * kWarpElems;
 }
 
-// Folds the partials: CTA c sums partials [c per, (c + 1) per).  The last stage (one CTA) writes the norm and the
-// clipping factor max_norm / norm where the norm is larger than max_norm, else 1 (a NaN norm does not clip).
+// One worker's 256 gradients to shared memory, in order, by the widest copy that the address allows.
+template <typename GT>
+__device__ __forceinline__ void copy_block(uint32_t to, const GT* from, int lane) {
+    constexpr int kBytes = static_cast<int>(sizeof(GT)) * kWarpElems;
+    const char* src = reinterpret_cast<const char*>(from);
+    const uint32_t low = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(src));
+    if ((low & 15u) == 0u) {
+#pragma unroll
+        for (int i = 0; i < kBytes; i += 512) copy_async<16>(to + i + 16 * lane, src + i + 16 * lane);
+    } else if ((low & 3u) == 0u) {
+#pragma unroll
+        for (int i = 0; i < kBytes; i += 128) copy_async<4>(to + i + 4 * lane, src + i + 4 * lane);
+    } else {                                  // bf16 at an odd element
+#pragma unroll
+        for (int i = 0; i < kBytes; i += 64) {
+            const uint16_t x = __ldcs(reinterpret_cast<const uint16_t*>(src + i) + lane);
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + i + 2 * lane), "h"(x) : "memory");
+        }
+    }
+}
+
+__device__ __forceinline__ void read_pairs(uint32_t from, Pair (&x)[4]) {
+    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(x[0]), "=l"(x[1]) : "r"(from) : "memory");
+    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(x[2]), "=l"(x[3]) : "r"(from + 16) : "memory");
+}
+template <typename GT> __device__ __forceinline__ void read_grads(uint32_t from, int lane, Pair (&x)[4]);
+template <> __device__ __forceinline__ void read_grads<float>(uint32_t from, int lane, Pair (&x)[4]) { read_pairs(from + 32 * lane, x); }
+template <> __device__ __forceinline__ void read_grads<__nv_bfloat16>(uint32_t from, int lane, Pair (&x)[4]) {
+    uint32_t r[4];
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(from + 16 * lane) : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = pack(__uint_as_float(r[i] << 16), __uint_as_float(r[i] & 0xffff0000u));
+}
+
+// SUMS: partial sums of the aggregate, min(K, 4) rounded up to 1, 2 or 4.  STAGES: items in shared memory.
+template <typename GT, int SUMS, int STAGES, bool CLIP, bool NORM>
+__global__ void __launch_bounds__(kThreads, 3) adamw8_kernel(const __grid_constant__ StepArgs a) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    agg::griddep_launch_dependents();
+    agg::griddep_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long* rec = a.src.recs + blockIdx.x * static_cast<long long>(a.src.stride);
+    const long long cf = __ldg(rec + kRecCount);
+    const int count = static_cast<int>(cf & 0xffffffffLL);
+    const float factor = CLIP ? __ldcg(a.factor) : 1.0f;
+    const Pair one = both(a.src.one);
+    const int K = CLIP && a.src.staged ? 1 : a.src.K;
+    double sq = 0.0;
+
+    // blocks warp, warp + 8, ... of the run; whole ones of aligned tensors take the staged path
+    const int mine = (count - warp * kWarpElems + kSpan - 1) / kSpan;                        // blocks that begin in the run
+    int whole = cf >> 32 & kStateAligned ? (count - (warp + 1) * kWarpElems + kSpan) / kSpan : 0;
+    if (whole < 0) whole = 0;
+    const int chunks = (K + a.item_workers - 1) / a.item_workers;
+    const int items = whole * chunks, stage = stage_bytes(min(K, a.item_workers), CLIP && a.src.staged ? 4 : static_cast<int>(sizeof(GT)));
+    const uint32_t ring = shared_address(smem) + warp * STAGES * stage;
+    const float* params = reinterpret_cast<const float*>(__ldg(rec + kRecParam));
+    const long long first = __ldg(rec + kRecFirst), second = __ldg(rec + kRecSecond);
+    float* first_scale = reinterpret_cast<float*>(__ldg(rec + kRecFirstScale));
+    float* second_scale = reinterpret_cast<float*>(__ldg(rec + kRecSecondScale));
+    const long long position = __ldg(rec + kRecPosition);
+
+    int next = 0, next_offset = warp * kWarpElems, next_chunk = 0, next_slot = 0;            // the item to copy
+    auto issue = [&]() {
+        if (next < items) {
+            const uint32_t to = ring + next_slot * stage;
+            if (next_chunk == 0) {
+                const char* p = reinterpret_cast<const char*>(params + next_offset);
+                copy_async<16>(to + 16 * lane, p + 16 * lane);
+                copy_async<16>(to + 512 + 16 * lane, p + 512 + 16 * lane);
+                const char* codes = reinterpret_cast<const char*>(lane < 16 ? first : second) + next_offset;
+                copy_async<16>(to + kStageCodes + 16 * lane, codes + 16 * (lane & 15));
+                const float* scale = lane == 0 ? first_scale : second_scale;
+                if (lane < 2) copy_async<4>(to + kStageScales + 4 * lane, scale + next_offset / kWarpElems);
+            }
+            if (CLIP && a.src.staged) {
+                copy_block<float>(to + kStageGrads, a.src.staged + position + next_offset, lane);
+            } else {
+                const int k0 = next_chunk * a.item_workers, k1 = min(K, k0 + a.item_workers);
+                for (int k = k0; k < k1; ++k)
+                    copy_block<GT>(to + kStageGrads + (k - k0) * static_cast<int>(sizeof(GT)) * kWarpElems,
+                                   reinterpret_cast<const GT*>(__ldg(rec + kRecGrads + a.src.worker[k])) + next_offset, lane);
+            }
+            ++next;
+            next_slot = next_slot + 1 == STAGES ? 0 : next_slot + 1;
+            if (++next_chunk == chunks) {
+                next_chunk = 0;
+                next_offset += kSpan;
+            }
+        }
+        copy_commit();                       // an empty group where nothing is left: the count of groups stays right
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) issue();
+
+    const Pair decay = decay_of(a, rec);
+    const long long copy = __ldg(rec + kRecCopy);
+    int slot = 0, offset = warp * kWarpElems;
+    for (int block = 0; block < whole; ++block, offset += kSpan) {
+        Pair sum[SUMS][4], p[4];
+        uint32_t codes[4];
+        float scales[2];
+#pragma unroll
+        for (int j = 0; j < SUMS; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[j][i] = both(-0.0f);                             // adds nothing to anything
+        for (int chunk = 0; chunk < chunks; ++chunk) {
+            issue();
+            copy_wait<STAGES - 1>();
+            __syncwarp();
+            const uint32_t from = ring + slot * stage;
+            if (chunk == 0) {
+                read_pairs(from + 32 * lane, p);
+                asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(codes[0]), "=r"(codes[1]) : "r"(from + kStageCodes + 8 * lane) : "memory");
+                asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];"
+                             : "=r"(codes[2]), "=r"(codes[3]) : "r"(from + kStageCodes + kWarpElems + 8 * lane) : "memory");
+                asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(scales[0]), "=f"(scales[1]) : "r"(from + kStageScales) : "memory");
+            }
+            if (CLIP && a.src.staged) {
+                read_grads<float>(from + kStageGrads, lane, sum[0]);
+            } else {
+                const int k0 = chunk * a.item_workers, here = min(K - k0, a.item_workers);
+                for (int k = 0; k < here; k += SUMS) {
+#pragma unroll
+                    for (int j = 0; j < SUMS; ++j) {
+                        if (k + j < here) {
+                            Pair x[4];
+                            read_grads<GT>(from + kStageGrads + (k + j) * static_cast<int>(sizeof(GT)) * kWarpElems, lane, x);
+                            const Pair w = both(a.src.lambda[k0 + k + j]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) sum[j][i] = add(mul(w, x[i]), sum[j][i], one);
+                        }
+                    }
+                }
+            }
+            __syncwarp();                    // everybody has read the slot before anybody's copy overwrites it
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
+        }
+#pragma unroll
+        for (int j = 1; j < SUMS; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[0][i] = add(sum[0][i], sum[j][i], one);
+        if (NORM) sq += sum_squares(sum[0]);
+        Pair m[4], u[4];
+        const uint32_t cm[2] = {codes[0], codes[1]}, cu[2] = {codes[2], codes[3]};
+        decode(cm, scales[0], m);
+        decode(cu, scales[1], u);
+        update<CLIP>(a, factor, decay, sum[0], p, m, u);
+        store_f32<true>(const_cast<float*>(params) + offset, lane, kWarpElems, p);
+        if (copy) store_copy<true>(copy, offset, lane, kWarpElems, p);
+        store_moments<true>(a, reinterpret_cast<uint8_t*>(first) + offset, reinterpret_cast<uint8_t*>(second) + offset,
+                            first_scale + offset / kWarpElems, second_scale + offset / kWarpElems, position + offset, lane,
+                            kWarpElems, m, u);
+    }
+    // a tensor's last, shorter block, and tensors off the grid
+#pragma unroll 1
+    for (int block = whole; block < mine; ++block, offset += kSpan)
+        sq += step_block_slow<GT, true, CLIP, NORM>(a, rec, offset, lane, min(count - offset, kWarpElems), factor);
+    if (NORM) agg::store_norm_partial(a.partials, sq);
+}
+
+// ---- the norm of the weighted gradient ------------------------------------------------------------------
+// CTAs take records blockIdx.x, blockIdx.x + gridDim.x, ...; with a staging buffer they also leave the aggregates
+// there, for the step that follows.  The CTA that arrives last adds the partials, in their order, and writes the
+// norm and the clipping factor max_norm / norm where the norm is larger than max_norm, else 1 (NaN does not clip).
+template <typename GT>
+__device__ __noinline__ double norm_block_slow(const Source& s, const long long* grads, int offset, int lane, int n, float* staged) {
+    Pair g[4];
+    aggregate<GT, 4, false>(s, grads, offset, lane, n, g);
+    if (staged) store_f32<false>(staged, lane, n, g);
+    return sum_squares(g);
+}
+
+template <typename GT, int KU>
+__global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 3) grad_norm_kernel(const __grid_constant__ NormArgs a) {
+    __shared__ double smem[kWarps];
+    __shared__ bool last;
+    agg::griddep_launch_dependents();
+    agg::griddep_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    double sq = 0.0;
+    for (long long r = blockIdx.x; r < a.src.records; r += gridDim.x) {
+        const long long* rec = a.src.recs + r * a.src.stride;
+        const long long cf = __ldg(rec + kNormCount), position = __ldg(rec + kNormPosition);
+        const int count = static_cast<int>(cf & 0xffffffffLL);
+        const bool aligned = cf >> 32 & kGradsAligned;
+#pragma unroll 1
+        for (int offset = warp * kWarpElems; offset < count; offset += kSpan) {
+            const int n = min(count - offset, kWarpElems);
+            float* staged = a.src.staged ? a.src.staged + position + offset : nullptr;
+            if (aligned && n == kWarpElems) {
+                Pair g[4];
+                aggregate<GT, KU, true>(a.src, rec + kNormGrads, offset, lane, n, g);
+                if (staged) store_f32<true>(staged, lane, n, g);
+                sq += sum_squares(g);
+            } else {
+                sq += norm_block_slow<GT>(a.src, rec + kNormGrads, offset, lane, n, staged);
+            }
+        }
+    }
+    const double mine = agg::block_sum(sq, smem);
+    if (threadIdx.x == 0) {
+        a.partials[blockIdx.x] = mine;
+        __threadfence();
+        last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double acc = 0.0;
+    for (int i = threadIdx.x; i < static_cast<int>(gridDim.x); i += kThreads) acc += __ldcg(a.partials + i);
+    const double total = agg::block_sum(acc, smem);
+    if (threadIdx.x != 0) return;
+    *a.ticket = 0u;
+    const double root = sqrt(total);
+    if (a.norm) *a.norm = static_cast<float>(root);
+    if (a.factor) *a.factor = root > static_cast<double>(a.max_norm) ? static_cast<float>(a.max_norm / root) : 1.0f;
+}
+
+// Norm as the by-product of a step: folds its CTAs' partials, CTA c sums [c per, (c + 1) per); the last stage (one
+// CTA) writes the norm.
 static __global__ void __launch_bounds__(1024) fold_kernel(const double* __restrict__ partials, long long n, int per,
-                                                           double* __restrict__ sums, float* __restrict__ norm,
-                                                           float* __restrict__ factor, float max_norm) {
+                                                           double* __restrict__ sums, float* __restrict__ norm) {
     __shared__ double smem[32];
     agg::griddep_launch_dependents();
     agg::griddep_wait();
@@ -469,13 +726,8 @@ static __global__ void __launch_bounds__(1024) fold_kernel(const double* __restr
     for (long long i = begin + threadIdx.x; i < end; i += blockDim.x) acc += __ldcg(partials + i);
     const double total = agg::block_sum(acc, smem);
     if (threadIdx.x != 0) return;
-    if (sums) {
-        sums[blockIdx.x] = total;
-        return;
-    }
-    const double root = sqrt(total);
-    if (norm) *norm = static_cast<float>(root);
-    if (factor) *factor = root > static_cast<double>(max_norm) ? static_cast<float>(max_norm / root) : 1.0f;
+    if (sums) sums[blockIdx.x] = total;
+    else *norm = static_cast<float>(sqrt(total));
 }
 
 }  // namespace adamw

@@ -1,7 +1,6 @@
 // AdamW over a list of parameter tensors for K workers' batch-weighted gradients, moments in 32 or 8 bits, with
-// optional clipping by the global norm; and that norm alone.  A plan holds one record per tile of 2048 elements
-// in device memory, as for the momentum step over a list; each step is one launch, three when it clips (norm of
-// the aggregate, fold, update).
+// optional clipping by the global norm; and that norm alone.  A plan holds records in device memory, as for the
+// momentum step over a list; each step is one launch, two when it clips (norm of the aggregate, update).
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
@@ -19,20 +18,21 @@ namespace {
 using namespace adamw;
 
 size_t round256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+long long blocks_of(long long n) { return n / kWarpElems + (n % kWarpElems != 0); }
 size_t grad_bytes(db_dtype dt) { return dt == DB_F32 ? 4 : 2; }
 
 // The fold sums up to kFoldPer partials with one CTA; beyond that a first stage of CTAs takes kFoldPer each.
 constexpr int kFoldPer = 8192;
 
-// Elements of the list in tiles; false if a size is negative or there are more tiles than a grid takes.
-bool count_tiles(const int64_t* sizes, int32_t T, long long* tiles) {
+// CTA steps (kSpan elements) in the list; false if a size is negative or there are more than a grid takes.
+bool count_spans(const int64_t* sizes, int32_t T, long long* spans) {
     long long sum = 0;
     for (int32_t t = 0; t < T; ++t) {
         if (sizes[t] < 0) return false;
-        sum += sizes[t] / kTile + (sizes[t] % kTile != 0);
+        sum += sizes[t] / kSpan + (sizes[t] % kSpan != 0);
         if (sum > 0x7fffffffLL) return false;
     }
-    *tiles = sum;
+    *spans = sum;
     return true;
 }
 
@@ -40,29 +40,50 @@ bool count_tiles(const int64_t* sizes, int32_t T, long long* tiles) {
 // instead of reading the K gradients a second time.
 bool stages(int K, db_dtype dt) { return static_cast<size_t>(K) * grad_bytes(dt) > 8; }
 
-struct Layout {
-    long long tiles;
-    int stride;                       // words of a record
-    size_t recs, partials, sums, factor, staged, end;
-};
-
-bool make_layout(int32_t K, db_dtype dt, const int64_t* sizes, int32_t T, int header, bool clip, Layout* L) {
-    if (!count_tiles(sizes, T, &L->tiles)) return false;
-    const size_t n = static_cast<size_t>(L->tiles > 0 ? L->tiles : 1);
-    L->stride = (header + K + 1) & ~1;                             // records stay 16-byte aligned
-    L->recs = 0;
-    L->partials = round256(8 * static_cast<size_t>(L->stride) * n);
-    L->sums = L->partials + round256(8 * n);
-    L->factor = L->sums + round256(8 * (n / kFoldPer + 1));
-    L->staged = L->factor + 256;
-    L->end = L->staged + (clip && stages(K, dt) ? 4 * static_cast<size_t>(kTile) * n : 0);
-    return true;
+// Elements of a record: as many CTA steps, up to eight, as leave 2400 records (16 for each of 148 SMs) where the
+// list has so many.
+int run_of(long long spans) {
+    const long long steps = spans / 2400;
+    return kSpan * static_cast<int>(steps < 1 ? 1 : steps > 8 ? 8 : steps);
 }
 
-// Norm kernel: CTAs that stay and take every grid-th tile; few enough that their partials fold in one stage.
-int norm_grid(long long tiles) {
-    const long long most = static_cast<long long>(sm_count()) * 8;
-    return static_cast<int>(tiles < most ? tiles : most);
+// One kind of records: `run` elements each, `stride` words apart.
+struct Records {
+    int run, stride;
+    long long count;
+    size_t at;
+};
+
+Records records_of(const int64_t* sizes, int32_t T, int run, int words, size_t* end) {
+    Records r{run, (words + 1) & ~1, 0, *end};                      // an even stride: records stay 16-byte aligned
+    for (int32_t t = 0; t < T; ++t) r.count += sizes[t] / run + (sizes[t] % run != 0);
+    *end += round256(8 * static_cast<size_t>(r.stride) * static_cast<size_t>(r.count));
+    return r;
+}
+
+struct Layout {
+    Records step, norm;
+    size_t partials, sums, scalars, staged, end;                    // scalars: ticket, clipping factor
+};
+
+// step: records of the optimizer step (state8: several CTA steps each); norm: records of the norm kernel.
+bool make_layout(int32_t K, db_dtype dt, bool state8, const int64_t* sizes, int32_t T, bool step, bool norm, Layout* L) {
+    long long spans;
+    if (!count_spans(sizes, T, &spans)) return false;
+    L->end = 0;
+    L->step = L->norm = Records{};
+    if (step) L->step = records_of(sizes, T, state8 ? run_of(spans) : kSpan, kRecGrads + K, &L->end);
+    if (norm) L->norm = records_of(sizes, T, run_of(spans), kNormGrads + K, &L->end);
+    const size_t n = static_cast<size_t>(std::max<long long>(1, std::max(L->step.count, L->norm.count)));
+    L->partials = L->end;
+    L->sums = L->partials + round256(8 * n);
+    L->scalars = L->sums + round256(8 * (n / kFoldPer + 1));
+    L->staged = L->scalars + 256;
+    size_t staged = 0;
+    if (step && norm && stages(K, dt))
+        for (int32_t t = 0; t < T; ++t) staged += static_cast<size_t>(blocks_of(sizes[t])) * kWarpElems * 4;
+    L->end = L->staged + staged;
+    return true;
 }
 
 struct Range {
@@ -89,17 +110,24 @@ void add_range(std::vector<Range>& v, const void* p, long long n, size_t elem) {
 long long word(const void* p) { return static_cast<long long>(reinterpret_cast<uintptr_t>(p)); }
 bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
 
-// Uploads the records and waits for it: plan creation is not on the hot path, and not possible in a capture.
-db_status upload(const std::vector<long long>& recs, void* to, cudaStream_t stream, const char* where) {
+// Uploads records and the cleared ticket and waits for it: plan creation is not on the hot path, and not possible
+// in a capture.
+db_status upload(const Layout& L, const std::vector<long long>& step, const std::vector<long long>& norm, char* table,
+                 cudaStream_t stream, const char* where) {
     cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
     if (stream) DB_CUDA_TRY(cudaStreamIsCapturing(stream, &capture));
     if (capture != cudaStreamCaptureStatusNone) {
         record_message("a plan cannot be created while its stream is being captured");
         return DB_ERR_UNSUPPORTED;
     }
-    cudaError_t err = cudaSuccess;
-    if (!recs.empty()) err = cudaMemcpyAsync(to, recs.data(), 8 * recs.size(), cudaMemcpyHostToDevice, stream);
-    if (err == cudaSuccess) err = cudaStreamSynchronize(stream);
+    cudaError_t err = cudaMemsetAsync(table + L.scalars, 0, 256, stream);
+    if (err == cudaSuccess && !step.empty())
+        err = cudaMemcpyAsync(table + L.step.at, step.data(), 8 * step.size(), cudaMemcpyHostToDevice, stream);
+    if (err == cudaSuccess && !norm.empty())
+        err = cudaMemcpyAsync(table + L.norm.at, norm.data(), 8 * norm.size(), cudaMemcpyHostToDevice, stream);
+    // the host vectors go away when the caller returns
+    const cudaError_t done = cudaStreamSynchronize(stream);
+    if (err == cudaSuccess) err = done;
     return err == cudaSuccess ? DB_OK : record_cuda_error(err, where);
 }
 
@@ -123,11 +151,12 @@ db_status set_workers(const int32_t* b, int K, Source* s) {
 
 // Every kernel may be scheduled while its predecessor in the stream still runs; it waits before its first access.
 template <typename... Params, typename... Args>
-cudaError_t launch(void (*fn)(Params...), long long grid, int block, cudaStream_t stream, Args... args) {
+cudaError_t launch(void (*fn)(Params...), long long grid, int block, size_t shared, cudaStream_t stream, Args... args) {
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute attr[1]{};
     cfg.gridDim = dim3(static_cast<unsigned int>(grid));
     cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = shared;
     cfg.stream = stream;
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -136,17 +165,16 @@ cudaError_t launch(void (*fn)(Params...), long long grid, int block, cudaStream_
     return cudaLaunchKernelEx(&cfg, fn, args...);
 }
 
-db_status launch_fold(double* partials, long long n, double* sums, float* norm, float* factor, float max_norm,
-                      cudaStream_t stream) {
+db_status launch_fold(double* partials, long long n, double* sums, float* norm, cudaStream_t stream) {
     if (n > kFoldPer) {
         const long long stage = (n + kFoldPer - 1) / kFoldPer;
-        DB_CUDA_TRY(launch(fold_kernel, stage, 1024, stream, static_cast<const double*>(partials), n, kFoldPer, sums,
-                           static_cast<float*>(nullptr), static_cast<float*>(nullptr), 0.0f));
+        DB_CUDA_TRY(launch(fold_kernel, stage, 1024, 0, stream, static_cast<const double*>(partials), n, kFoldPer, sums,
+                           static_cast<float*>(nullptr)));
         partials = sums;
         n = stage;
     }
-    DB_CUDA_TRY(launch(fold_kernel, 1, n > 256 ? 1024 : 256, stream, static_cast<const double*>(partials), n,
-                       static_cast<int>(n), static_cast<double*>(nullptr), norm, factor, max_norm));
+    DB_CUDA_TRY(launch(fold_kernel, 1, n > 256 ? 1024 : 256, 0, stream, static_cast<const double*>(partials), n,
+                       static_cast<int>(n), static_cast<double*>(nullptr), norm));
     return DB_OK;
 }
 
@@ -155,28 +183,87 @@ template <typename GT>
 NormFn pick_norm(int K) {
     if (K <= 1) return grad_norm_kernel<GT, 1>;
     if (K <= 2) return grad_norm_kernel<GT, 2>;
-    if (K <= 4) return grad_norm_kernel<GT, 4>;
+    if (K <= 4 || sizeof(GT) == 4) return grad_norm_kernel<GT, 4>;
     return grad_norm_kernel<GT, 8>;
 }
 
-db_status launch_norm(db_dtype dt, const NormArgs& a, int grid, cudaStream_t stream) {
-    const NormFn fn = dt == DB_F32 ? pick_norm<float>(a.src.K) : pick_norm<__nv_bfloat16>(a.src.K);
-    DB_CUDA_TRY(launch(fn, grid, kThreads, stream, a));
+// Norm (and aggregate, and clipping factor) of a plan's gradients: CTAs stay and take every grid-th record.
+db_status launch_norm(const Layout& L, char* table, db_dtype dt, Source src, float* norm, float* factor, float max_norm,
+                      cudaStream_t stream) {
+    NormArgs a{};
+    a.src = src;
+    a.src.recs = reinterpret_cast<const long long*>(table + L.norm.at);
+    a.src.records = L.norm.count;
+    a.src.stride = L.norm.stride;
+    a.partials = reinterpret_cast<double*>(table + L.partials);
+    a.ticket = reinterpret_cast<unsigned int*>(table + L.scalars);
+    a.norm = norm;
+    a.factor = factor;
+    a.max_norm = max_norm;
+    const NormFn fn = dt == DB_F32 ? pick_norm<float>(src.K) : pick_norm<__nv_bfloat16>(src.K);
+    const long long resident = static_cast<long long>(sm_count()) * 8;
+    DB_CUDA_TRY(launch(fn, std::min(L.norm.count, resident), kThreads, 0, stream, a));
     return DB_OK;
 }
 
 using StepFn = void (*)(const StepArgs);
-template <typename GT, bool STATE8, bool CLIP, bool NORM>
+template <typename GT, bool CLIP, bool NORM>
 StepFn pick_workers(int K) {
-    if (K <= 1) return adamw_kernel<GT, 1, STATE8, CLIP, NORM>;
-    if (K <= 2) return adamw_kernel<GT, 2, STATE8, CLIP, NORM>;
-    if (K <= 4) return adamw_kernel<GT, 4, STATE8, CLIP, NORM>;
-    return adamw_kernel<GT, 8, STATE8, CLIP, NORM>;
+    if (K <= 1) return adamw_kernel<GT, 1, CLIP, NORM>;
+    if (K <= 2) return adamw_kernel<GT, 2, CLIP, NORM>;
+    if (K <= 4) return adamw_kernel<GT, 4, CLIP, NORM>;
+    return adamw_kernel<GT, 8, CLIP, NORM>;
 }
-template <typename GT, bool STATE8>
-StepFn pick_step(int K, bool clip, bool staged, bool norm) {
-    if (clip) return pick_workers<GT, STATE8, true, false>(staged ? 1 : K);
-    return norm ? pick_workers<GT, STATE8, false, true>(K) : pick_workers<GT, STATE8, false, false>(K);
+template <typename GT>
+StepFn pick_step(int K, bool clip, bool norm) {
+    if (clip) return pick_workers<GT, true, false>(K);
+    return norm ? pick_workers<GT, false, true>(K) : pick_workers<GT, false, false>(K);
+}
+
+// 8-bit moments: how many workers' gradients an item takes, how many items a warp keeps in shared memory.
+struct Ring {
+    int item_workers, stages;
+    size_t shared;
+};
+Ring ring_of(int K, size_t gsize) {
+    Ring r;
+    r.item_workers = gsize == 4 ? 4 : 8;
+    const int stage = stage_bytes(std::min(K, r.item_workers), static_cast<int>(gsize));
+    r.stages = 4;
+    while (r.stages > 2 && kWarps * r.stages * stage > 74 << 10) --r.stages;
+    r.shared = static_cast<size_t>(kWarps) * r.stages * stage;
+    return r;
+}
+constexpr int kMaxShared = kWarps * 2 * stage_bytes(4, 4);
+static_assert(stage_bytes(4, 4) == stage_bytes(8, 2) && kMaxShared > 74 << 10 && kMaxShared <= 227 << 10, "ring");
+
+template <typename GT, int SUMS, bool CLIP, bool NORM>
+StepFn pick_stages(int n) {
+    return n == 2 ? adamw8_kernel<GT, SUMS, 2, CLIP, NORM> : n == 3 ? adamw8_kernel<GT, SUMS, 3, CLIP, NORM>
+                                                                   : adamw8_kernel<GT, SUMS, 4, CLIP, NORM>;
+}
+template <typename GT, bool CLIP, bool NORM>
+StepFn pick_sums(int K, int n) {
+    return K <= 1 ? pick_stages<GT, 1, CLIP, NORM>(n) : K <= 2 ? pick_stages<GT, 2, CLIP, NORM>(n)
+                                                                : pick_stages<GT, 4, CLIP, NORM>(n);
+}
+template <typename GT>
+StepFn pick_step8(int K, int n, bool clip, bool norm) {
+    if (clip) return pick_sums<GT, true, false>(K, n);
+    return norm ? pick_sums<GT, false, true>(K, n) : pick_sums<GT, false, false>(K, n);
+}
+
+// Every 8-bit kernel of a gradient type may use as much shared memory as its ring takes (per device: at plan creation).
+template <typename GT>
+cudaError_t allow_shared() {
+    for (int K : {1, 2, 4})
+        for (int n : {2, 3, 4})
+            for (int mode = 0; mode < 3; ++mode) {
+                const cudaError_t err = cudaFuncSetAttribute(reinterpret_cast<const void*>(pick_step8<GT>(K, n, mode == 1, mode == 2)),
+                                                             cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxShared);
+                if (err != cudaSuccess) return err;
+            }
+    return cudaSuccess;
 }
 
 }  // namespace
@@ -218,15 +305,28 @@ db_status check_grads(const void* const* grads, db_dtype dt, int32_t K, int32_t 
     return DB_OK;
 }
 
+// Norm records of one tensor; returns the place of the next.
+long long* norm_records(long long* r, const Records& kind, const void* const* grads, db_dtype dt, int32_t K, int32_t T,
+                        int32_t t, long long n, long long position, bool aligned) {
+    for (long long e = 0; e < n; e += kind.run, r += kind.stride) {
+        r[kNormCount] = std::min<long long>(n - e, kind.run) | static_cast<long long>(aligned ? kGradsAligned : 0) << 32;
+        r[kNormPosition] = position + e;
+        for (int32_t k = 0; k < K; ++k)
+            r[kNormGrads + k] = word(static_cast<const char*>(grads[static_cast<size_t>(k) * T + t]) + e * grad_bytes(dt));
+    }
+    return r;
+}
+
 }  // namespace
 }  // namespace dynbatch
 
-extern "C" size_t db_adamw_plan_device_bytes(int32_t K, db_dtype grad_dtype, const int64_t* sizes, int32_t T,
-                                             uint32_t flags) {
+extern "C" size_t db_adamw_plan_device_bytes(int32_t K, db_dtype grad_dtype, db_dtype state_dtype, const int64_t* sizes,
+                                             int32_t T, uint32_t flags) {
     using namespace dynbatch;
     if (!sizes || K < 1 || K > DB_MAX_K || T < 1 || !known(grad_dtype) || (flags & ~DB_ADAMW_CLIP)) return 0;
+    if (state_dtype != DB_F32 && state_dtype != DB_E4M3) return 0;
     Layout L;
-    return make_layout(K, grad_dtype, sizes, T, kRecGrads, flags & DB_ADAMW_CLIP, &L) ? L.end : 0;
+    return make_layout(K, grad_dtype, state_dtype == DB_E4M3, sizes, T, true, flags & DB_ADAMW_CLIP, &L) ? L.end : 0;
 }
 
 extern "C" db_status db_adamw_plan_create(db_adamw_plan** out, const void* const* grads, db_dtype grad_dtype,
@@ -246,16 +346,17 @@ extern "C" db_status db_adamw_plan_create(db_adamw_plan** out, const void* const
     if (state8 && (!first_scale || !second_scale)) return DB_ERR_NULL;
     try {
         Layout L;
-        if (!make_layout(K, grad_dtype, sizes, T, kRecGrads, clip, &L)) return DB_ERR_ARG;
+        if (!make_layout(K, grad_dtype, state8, sizes, T, true, clip, &L)) return DB_ERR_ARG;
         if (misaligned(device_table, 256) || device_table_bytes < L.end) return DB_ERR_ARG;
         const size_t state_size = state8 ? 1 : 4;
         std::vector<Range> written, read;
-        std::vector<long long> recs(static_cast<size_t>(L.stride) * static_cast<size_t>(L.tiles), 0);
+        std::vector<long long> step(static_cast<size_t>(L.step.stride) * static_cast<size_t>(L.step.count), 0);
+        std::vector<long long> norm(static_cast<size_t>(L.norm.stride) * static_cast<size_t>(L.norm.count), 0);
         add_range(written, device_table, static_cast<long long>(L.end), 1);
-        long long* r = recs.data();
+        long long *r = step.data(), *q = norm.data();
         long long position = 0;
         for (int32_t t = 0; t < T; ++t) {
-            const long long n = sizes[t], blocks = n / kWarpElems + (n % kWarpElems != 0);
+            const long long n = sizes[t], blocks = blocks_of(n);
             const float wd = weight_decay ? weight_decay[t] : 0.0f;
             if (!std::isfinite(wd)) return DB_ERR_ARG;
             float* p = params[t];
@@ -275,17 +376,19 @@ extern "C" db_status db_adamw_plan_create(db_adamw_plan** out, const void* const
             bool grads_aligned;
             const db_status st = check_grads(grads, grad_dtype, K, T, t, n, &read, &grads_aligned);
             if (st != DB_OK) return st;
-            const bool state_aligned = !misaligned(p, 32) && !misaligned(m, kLaneElems * state_size) &&
-                                       !misaligned(u, kLaneElems * state_size) && !misaligned(w, 16);
+            // a lane's vector: 32 bytes of fp32; 8-bit moments are copied 16 bytes at a time
+            const size_t state_vec = state8 ? 16 : 32;
+            const bool state_aligned = !misaligned(p, 32) && !misaligned(m, state_vec) && !misaligned(u, state_vec) &&
+                                       !misaligned(w, 16);
             const long long bits = (state_aligned ? kStateAligned : 0) | (grads_aligned ? kGradsAligned : 0);
             uint32_t wd_bits;
             static_assert(sizeof wd_bits == sizeof wd, "binary32");
             __builtin_memcpy(&wd_bits, &wd, 4);
-            for (long long e = 0; e < n; e += kTile, r += L.stride) {
+            for (long long e = 0; e < n; e += L.step.run, r += L.step.stride) {
                 r[kRecParam] = word(p + e);
                 r[kRecFirst] = word(m + e * state_size);
                 r[kRecSecond] = word(u + e * state_size);
-                r[kRecCount] = (n - e < kTile ? n - e : kTile) | bits << 32;
+                r[kRecCount] = std::min<long long>(n - e, L.step.run) | bits << 32;
                 if (state8) {
                     r[kRecFirstScale] = word(ms + e / kWarpElems);
                     r[kRecSecondScale] = word(us + e / kWarpElems);
@@ -296,6 +399,7 @@ extern "C" db_status db_adamw_plan_create(db_adamw_plan** out, const void* const
                 for (int32_t k = 0; k < K; ++k)
                     r[kRecGrads + k] = word(static_cast<const char*>(grads[static_cast<size_t>(k) * T + t]) + e * grad_bytes(grad_dtype));
             }
+            if (clip) q = norm_records(q, L.norm, grads, grad_dtype, K, T, t, n, position, grads_aligned);
             position += blocks * kWarpElems;
         }
         if (overlaps(written, read)) return DB_ERR_ARG;
@@ -306,7 +410,11 @@ extern "C" db_status db_adamw_plan_create(db_adamw_plan** out, const void* const
         plan->state_dtype = state_dtype;
         plan->K = K;
         plan->clip = clip;
-        const db_status st = upload(recs, plan->table + L.recs, static_cast<cudaStream_t>(cuda_stream), "db_adamw_plan_create");
+        db_status st = upload(L, step, norm, plan->table, static_cast<cudaStream_t>(cuda_stream), "db_adamw_plan_create");
+        if (st == DB_OK && state8) {
+            const cudaError_t err = grad_dtype == DB_F32 ? allow_shared<float>() : allow_shared<__nv_bfloat16>();
+            if (err != cudaSuccess) st = record_cuda_error(err, "db_adamw_plan_create");
+        }
         if (st != DB_OK) {
             delete plan;
             return st;
@@ -337,15 +445,14 @@ extern "C" db_status db_aggregate_adamw_multi(db_adamw_plan* plan, const int32_t
     const db_status st = set_workers(b, plan->K, &a.src);
     if (st != DB_OK) return st;
     const Layout& L = plan->layout;
-    if (L.tiles == 0) return DB_OK;
+    if (L.step.count == 0) return DB_OK;
     const bool clip = max_norm > 0.0f, norm = !clip && grad_norm, staged = clip && stages(a.src.K, plan->grad_dtype);
-    a.src.recs = reinterpret_cast<const long long*>(plan->table + L.recs);
-    a.src.stride = L.stride;
-    a.src.tiles = L.tiles;
+    a.src.recs = reinterpret_cast<const long long*>(plan->table + L.step.at);
+    a.src.records = L.step.count;
+    a.src.stride = L.step.stride;
     a.src.staged = staged ? reinterpret_cast<float*>(plan->table + L.staged) : nullptr;
     a.partials = reinterpret_cast<double*>(plan->table + L.partials);
-    double* sums = reinterpret_cast<double*>(plan->table + L.sums);
-    float* factor = reinterpret_cast<float*>(plan->table + L.factor);
+    float* factor = reinterpret_cast<float*>(plan->table + L.scalars) + 1;
     a.factor = factor;
     a.beta1 = beta1;
     a.beta2 = beta2;
@@ -366,32 +473,30 @@ extern "C" db_status db_aggregate_adamw_multi(db_adamw_plan* plan, const int32_t
 
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (clip) {
-        NormArgs n{};
-        n.src = a.src;
-        n.count_word = kRecCount;
-        n.grads_word = kRecGrads;
-        n.partials = a.partials;
-        const int grid = norm_grid(L.tiles);
-        db_status s = launch_norm(plan->grad_dtype, n, grid, stream);
-        if (s == DB_OK) s = launch_fold(a.partials, grid, sums, grad_norm, factor, max_norm, stream);
+        const db_status s = launch_norm(L, plan->table, plan->grad_dtype, a.src, grad_norm, factor, max_norm, stream);
         if (s != DB_OK) return s;
     }
-    const bool state8 = plan->state_dtype == DB_E4M3;
+    const int K = staged ? 1 : a.src.K;
     StepFn fn;
-    if (plan->grad_dtype == DB_F32)
-        fn = state8 ? pick_step<float, true>(a.src.K, clip, staged, norm) : pick_step<float, false>(a.src.K, clip, staged, norm);
-    else
-        fn = state8 ? pick_step<__nv_bfloat16, true>(a.src.K, clip, staged, norm)
-                    : pick_step<__nv_bfloat16, false>(a.src.K, clip, staged, norm);
-    DB_CUDA_TRY(launch(fn, L.tiles, kThreads, stream, a));
-    return norm ? launch_fold(a.partials, L.tiles, sums, grad_norm, nullptr, 0.0f, stream) : DB_OK;
+    size_t shared = 0;
+    if (plan->state_dtype == DB_E4M3) {
+        const Ring ring = ring_of(K, staged ? 4 : grad_bytes(plan->grad_dtype));
+        a.item_workers = ring.item_workers;
+        shared = ring.shared;
+        fn = plan->grad_dtype == DB_F32 ? pick_step8<float>(K, ring.stages, clip, norm)
+                                        : pick_step8<__nv_bfloat16>(K, ring.stages, clip, norm);
+    } else {
+        fn = plan->grad_dtype == DB_F32 ? pick_step<float>(K, clip, norm) : pick_step<__nv_bfloat16>(K, clip, norm);
+    }
+    DB_CUDA_TRY(launch(fn, L.step.count, kThreads, shared, stream, a));
+    return norm ? launch_fold(a.partials, L.step.count, reinterpret_cast<double*>(plan->table + L.sums), grad_norm, stream) : DB_OK;
 }
 
 extern "C" size_t db_grad_norm_plan_device_bytes(int32_t K, db_dtype grad_dtype, const int64_t* sizes, int32_t T) {
     using namespace dynbatch;
     if (!sizes || K < 1 || K > DB_MAX_K || T < 1 || !known(grad_dtype)) return 0;
     Layout L;
-    return make_layout(K, grad_dtype, sizes, T, kNormGrads, false, &L) ? L.end : 0;
+    return make_layout(K, grad_dtype, false, sizes, T, false, true, &L) ? L.end : 0;
 }
 
 extern "C" db_status db_grad_norm_plan_create(db_grad_norm_plan** out, const void* const* grads, db_dtype grad_dtype,
@@ -405,22 +510,19 @@ extern "C" db_status db_grad_norm_plan_create(db_grad_norm_plan** out, const voi
     if (!known(grad_dtype)) return DB_ERR_UNSUPPORTED;
     try {
         Layout L;
-        if (!make_layout(K, grad_dtype, sizes, T, kNormGrads, false, &L)) return DB_ERR_ARG;
+        if (!make_layout(K, grad_dtype, false, sizes, T, false, true, &L)) return DB_ERR_ARG;
         if (misaligned(device_table, 256) || device_table_bytes < L.end) return DB_ERR_ARG;
         std::vector<Range> written, read;
-        std::vector<long long> recs(static_cast<size_t>(L.stride) * static_cast<size_t>(L.tiles), 0);
+        std::vector<long long> norm(static_cast<size_t>(L.norm.stride) * static_cast<size_t>(L.norm.count), 0);
         add_range(written, device_table, static_cast<long long>(L.end), 1);
-        long long* r = recs.data();
+        long long *r = norm.data(), position = 0;
         for (int32_t t = 0; t < T; ++t) {
             const long long n = sizes[t];
             bool aligned;
             const db_status st = check_grads(grads, grad_dtype, K, T, t, n, &read, &aligned);
             if (st != DB_OK) return st;
-            for (long long e = 0; e < n; e += kTile, r += L.stride) {
-                r[kNormCount] = (n - e < kTile ? n - e : kTile) | static_cast<long long>(aligned ? kGradsAligned : 0) << 32;
-                for (int32_t k = 0; k < K; ++k)
-                    r[kNormGrads + k] = word(static_cast<const char*>(grads[static_cast<size_t>(k) * T + t]) + e * grad_bytes(grad_dtype));
-            }
+            r = norm_records(r, L.norm, grads, grad_dtype, K, T, t, n, position, aligned);
+            position += blocks_of(n) * kWarpElems;
         }
         if (overlaps(written, read)) return DB_ERR_ARG;
         db_grad_norm_plan* plan = new db_grad_norm_plan();
@@ -428,7 +530,7 @@ extern "C" db_status db_grad_norm_plan_create(db_grad_norm_plan** out, const voi
         plan->table = static_cast<char*>(device_table);
         plan->grad_dtype = grad_dtype;
         plan->K = K;
-        const db_status st = upload(recs, plan->table + L.recs, static_cast<cudaStream_t>(cuda_stream), "db_grad_norm_plan_create");
+        const db_status st = upload(L, {}, norm, plan->table, static_cast<cudaStream_t>(cuda_stream), "db_grad_norm_plan_create");
         if (st != DB_OK) {
             delete plan;
             return st;
@@ -450,20 +552,10 @@ extern "C" db_status db_grad_norm_multi(db_grad_norm_plan* plan, const int32_t* 
     using namespace dynbatch;
     if (!plan || !b || !grad_norm) return DB_ERR_NULL;
     if (misaligned(grad_norm, 4)) return DB_ERR_ARG;
-    NormArgs a{};
-    const db_status st = set_workers(b, plan->K, &a.src);
+    Source src{};
+    const db_status st = set_workers(b, plan->K, &src);
     if (st != DB_OK) return st;
-    const Layout& L = plan->layout;
-    if (L.tiles == 0) return DB_OK;
-    a.src.recs = reinterpret_cast<const long long*>(plan->table + L.recs);
-    a.src.stride = L.stride;
-    a.src.tiles = L.tiles;
-    a.count_word = kNormCount;
-    a.grads_word = kNormGrads;
-    a.partials = reinterpret_cast<double*>(plan->table + L.partials);
-    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const int grid = norm_grid(L.tiles);
-    const db_status s = launch_norm(plan->grad_dtype, a, grid, stream);
-    if (s != DB_OK) return s;
-    return launch_fold(a.partials, grid, reinterpret_cast<double*>(plan->table + L.sums), grad_norm, nullptr, 0.0f, stream);
+    if (plan->layout.norm.count == 0) return DB_OK;
+    return launch_norm(plan->layout, plan->table, plan->grad_dtype, src, grad_norm, nullptr, 0.0f,
+                       static_cast<cudaStream_t>(cuda_stream));
 }

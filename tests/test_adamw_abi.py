@@ -55,15 +55,17 @@ def test_constants_are_the_headers():
 
 
 def test_device_bytes(lib):
-    def need(sizes, K=2, dt=E.DB_F32, flags=0):
-        return lib.db_adamw_plan_device_bytes(K, dt, (ctypes.c_int64 * max(1, len(sizes)))(*sizes), len(sizes), flags)
+    def need(sizes, K=2, dt=E.DB_F32, flags=0, state=E.DB_F32):
+        return lib.db_adamw_plan_device_bytes(K, dt, state, (ctypes.c_int64 * max(1, len(sizes)))(*sizes), len(sizes), flags)
     n = 100_000
-    assert need([n]) > 0 and need([n], flags=E.DB_ADAMW_CLIP) == need([n])              # 8 bytes of gradient: read twice
-    assert need([n], K=3, flags=E.DB_ADAMW_CLIP) >= need([n], K=3) + 4 * n               # more: staged
-    assert need([n], K=4, dt=E.DB_BF16, flags=E.DB_ADAMW_CLIP) == need([n], K=4, dt=E.DB_BF16)
-    assert need([0, 0]) > 0
+    C = E.DB_ADAMW_CLIP
+    assert need([n]) > 0 and need([n], flags=C) < need([n]) + 4 * n                      # 8 bytes of gradient: read twice
+    assert need([n], K=3, flags=C) >= need([n], K=3) + 4 * n                              # more: staged
+    assert need([n], K=4, dt=E.DB_BF16, flags=C) < need([n], K=4, dt=E.DB_BF16) + 4 * n
+    assert need([n], state=E.DB_E4M3) > 0 and need([0, 0]) > 0
     assert need([n], K=0) == need([n], K=65) == need([-1]) == need([]) == need([n], dt=E.DB_E4M3) == need([n], flags=2) == 0
-    assert need([2**63 - 1]) == 0 and need([2**62, 2**62, 2**62]) == 0                   # more tiles than a grid has
+    assert need([n], state=E.DB_BF16) == 0
+    assert need([2**63 - 1]) == 0 and need([2**62, 2**62, 2**62]) == 0                   # more steps than a grid has
     norm = lambda K, dt, s: lib.db_grad_norm_plan_device_bytes(K, dt, (ctypes.c_int64 * len(s))(*s), len(s))  # noqa: E731
     assert norm(1, E.DB_BF16, [1]) > 0 and norm(1, 7, [1]) == 0 and norm(1, E.DB_F32, [2**63 - 1]) == 0
 
