@@ -181,7 +181,7 @@ db_status db_multi_plan_destroy(db_multi_plan* plan);
  *     m <- beta1 m + (1 - beta1) h        u <- beta2 u + (1 - beta2) h^2
  *     p <- p (1 - lr wd) - lr (m / (1 - beta1^t)) / (sqrt(u / (1 - beta2^t)) + eps)
  * wd is the tensor's weight decay; p takes m and u before they are rounded to
- * 8 bits.  All arithmetic is fp32, squares and sum of the norm are fp64.  g adds
+ * 8 bits; a u below 2^-126 counts as 0 under the root.  All arithmetic is fp32, squares and sum of the norm are fp64.  g adds
  * the rounded products of the workers with b[k] > 0 in four partial sums (every
  * fourth of them, k ascending), joined in order; in m and u every product and sum
  * is rounded on its own, as written.  So they, and with them the 8-bit codes, are

@@ -43,7 +43,7 @@ struct Source {                  // where the weighted gradient comes from
     int K;                       // how many
     int stride;
     float* staged;               // fp32 aggregates by position (256 a block), or NULL
-    float one;                   // 1, see add()
+    unsigned long long one;      // a pair of ones, see add()
 };
 
 struct NormArgs {
@@ -59,11 +59,12 @@ struct StepArgs {
     Source src;
     double* partials;            // norm partials (NORM only)
     const float* factor;         // clipping factor in device memory (CLIP only)
-    float beta1, one_minus_beta1, beta2, one_minus_beta2;
-    float step_size;             // lr / (1 - beta1^t)
-    float inv_sqrt_c2;           // 1 / sqrt(1 - beta2^t)
-    float eps, lr;
-    int item_workers;            // 8-bit moments: a multiple of 4, or all workers
+    // pairs of fp32, both halves alike, as the packed arithmetic takes them
+    unsigned long long beta1, one_minus_beta1, beta2, one_minus_beta2;
+    unsigned long long minus_step_size;   // -lr / (1 - beta1^t)
+    unsigned long long inv_sqrt_c2;       // 1 / sqrt(1 - beta2^t)
+    unsigned long long eps;
+    float lr;
     uint32_t key0, key1;
 };
 
@@ -92,6 +93,20 @@ __device__ __forceinline__ Pair mul_add(Pair a, Pair b, Pair c) {
 // joins a packed product and a packed sum into one FMA, rounded once, even with .rn on both and --fmad=false
 // (measured: 26 % of a b + c d then differ from the separately rounded sum); this it cannot join.
 __device__ __forceinline__ Pair add(Pair a, Pair b, Pair one) { return mul_add(a, one, b); }
+
+// Approximate square root and reciprocal (relative error 2^-23 each): they enter the parameter only, through a
+// move that is a small part of it.  Both flush subnormals: a second moment below 2^-126 counts as 0 in the
+// denominator; a denominator is 0 or normal, the host having raised a subnormal eps to the least normal number.
+__device__ __forceinline__ float root(float x) {
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 
 // ---- memory access of one lane's eight elements --------------------------------------------------
 // ALIGNED: elements 8 lane .. 8 lane + 7.  Otherwise elements lane + 32 i, those below n.
@@ -163,7 +178,7 @@ template <typename GT, int KU, bool ALIGNED>
 __device__ __forceinline__ void aggregate(const Source& s, const long long* grads, int offset, int lane, int n,
                                           Pair (&g)[4]) {
     constexpr int kSums = KU < 4 ? KU : 4;
-    const Pair one = both(s.one);
+    const Pair one = s.one;
     Pair sum[kSums][4];
     for (int k0 = 0; k0 < s.K; k0 += KU) {
         GradRaw<GT> raw[KU];
@@ -211,8 +226,8 @@ __device__ __forceinline__ uint32_t fold_multiply(uint32_t x, uint32_t m) {
     const uint64_t z = static_cast<uint64_t>(x) * m;
     return static_cast<uint32_t>(z >> 32) ^ static_cast<uint32_t>(z);
 }
-__device__ __forceinline__ uint32_t random_bits(uint32_t position_low, uint32_t key0, uint32_t key1) {
-    return fold_multiply(fold_multiply(position_low ^ key0, 0xAC4C1B51u) ^ key1, 0xD6E8FEB5u);
+__device__ __forceinline__ uint32_t random_bits(uint32_t position_and_key, uint32_t key1) {
+    return fold_multiply(fold_multiply(position_and_key, 0xAC4C1B51u) ^ key1, 0xD6E8FEB5u);
 }
 
 // e4m3 code of magnitude y in [0, 448], taken up to the next value with probability (distance below y) / (step).
@@ -221,10 +236,13 @@ __device__ __forceinline__ uint32_t random_bits(uint32_t position_low, uint32_t 
 // drops the sign: the code is then the word's top byte, and 16 random bits belong into bytes 1 and 2.
 __device__ __forceinline__ uint32_t encode(float y_scaled, uint32_t chance) { return (__float_as_uint(y_scaled) << 4) + chance; }
 
-// y = |x| (448 / s) has two fp32 roundings, at most two units in the last place (16 each in the word above): where the word is
-// within three of a carry, it cannot tell which code the exact y would get.
-__device__ __forceinline__ uint32_t distance_to_carry(uint32_t word) { return (word << 8) + (48u << 8); }
-constexpr uint32_t kUnsure = 96u << 8;
+// The random bits' byte 0 holds 128, so that the word is eight units in the last place (16 each) too high:
+// y = |x| 2^-120 (448 / s) is off by less than five (an approximate reciprocal and two roundings), and where bytes 1
+// and 2 of the word are zero, the word is within eight of a carry and cannot tell which code the exact y would get.
+__device__ __forceinline__ uint32_t chance_low(uint32_t r) { return __byte_perm(r, 0x80u, 0x5104); }
+__device__ __forceinline__ uint32_t chance_high(uint32_t r) { return __byte_perm(r, 0x80u, 0x5324); }
+__device__ __forceinline__ uint32_t middle_bytes(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x6521); }
+__device__ __forceinline__ bool unsure(uint32_t word) { return (word & 0x00ffff00u) == 0u; }
 
 // The same word's top byte by fp64: q floor(y / q + r / 65536), q = 2^(max(exponent of y, -6) - 3).
 __device__ __noinline__ uint32_t encode_exactly(float magnitude, float top, uint32_t chance) {
@@ -232,7 +250,7 @@ __device__ __noinline__ uint32_t encode_exactly(float magnitude, float top, uint
     int exponent = static_cast<int>(__double_as_longlong(y) >> 52) - 1023;
     exponent = max(exponent, -6);
     const double steps = floor(y * __longlong_as_double(static_cast<long long>(1023 + 3 - exponent) << 52) +
-                               static_cast<double>(chance >> 8) * 0x1p-16);
+                               static_cast<double>(chance >> 8) * 0x1p-16);      // byte 0 dropped
     const float value = fminf(static_cast<float>(steps) * __uint_as_float(static_cast<uint32_t>(127 + exponent - 3) << 23), 448.0f);
     return __float_as_uint(value * 0x1p-120f) << 4;
 }
@@ -241,18 +259,39 @@ __device__ __noinline__ uint32_t encode_exactly(float magnitude, float top, uint
 // finite gets a NaN scale and keep = 0 (codes are masked to zero).
 struct BlockScale {
     float top, scale;
-    Pair to_code;
     uint32_t keep;
 };
-__device__ __forceinline__ BlockScale block_scale(uint32_t lane_top) {
-    const uint32_t top = max(__reduce_max_sync(0xffffffffu, lane_top), 0x0d800000u);      // bits of 2^-100
+__device__ __forceinline__ BlockScale block_scale(float lane_top) {
+    const uint32_t top = max(__reduce_max_sync(0xffffffffu, __float_as_uint(lane_top)), 0x0d800000u);   // bits of 2^-100
     const bool finite = top < 0x7f800000u;
     BlockScale r;
     r.top = __uint_as_float(top);
-    r.to_code = both(448.0f / r.top);
     r.scale = finite ? r.top * (1.0f / 448.0f) : __uint_as_float(0x7fffffffu);
     r.keep = finite ? 0xffffffffu : 0u;
     return r;
+}
+// max(|a|, |b|, |c|), NaN if one is
+__device__ __forceinline__ float top_of(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float top_of(const Pair (&x)[4]) {
+    return top_of(top_of(lo(x[0]), hi(x[0]), lo(x[1])), top_of(hi(x[1]), lo(x[2]), hi(x[2])), top_of(lo(x[3]), hi(x[3]), 0.0f));
+}
+
+// x 2^-120 (448 / s).  The factor is a normal number up to s = 2^14; above, x and s are brought down first (an x that
+// this makes subnormal is far below the smallest code's distance to the next).
+__device__ __forceinline__ void scale_down(const Pair (&x)[4], float s, Pair (&y)[4]) {
+    if (s < 0x1p14f) {
+        const Pair factor = both(reciprocal(s) * (448.0f * 0x1p-120f));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = mul(x[i], factor);
+    } else {
+        const Pair factor = both(reciprocal(s * 0x1p-114f) * (448.0f * 0x1p-120f));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = mul(mul(x[i], both(0x1p-114f)), factor);
+    }
 }
 
 template <bool ALIGNED>
@@ -281,8 +320,7 @@ __device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c
     return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
 template <bool ALIGNED>
-__device__ __forceinline__ void store_codes(uint8_t* p, int lane, int n, const uint32_t (&w)[8], uint32_t keep) {
-    const uint32_t c[2] = {top_bytes(w[0], w[1], w[2], w[3]) & keep, top_bytes(w[4], w[5], w[6], w[7]) & keep};
+__device__ __forceinline__ void store_codes(uint8_t* p, int lane, int n, const uint32_t (&c)[2]) {
     if (ALIGNED) {
         __stcs(reinterpret_cast<uint2*>(p + 8 * lane), make_uint2(c[0], c[1]));
     } else {
@@ -293,34 +331,20 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int lane, int n, const u
 }
 
 // ---- one block of elements ------------------------------------------------------------------------
-// Approximate square root and reciprocal (relative error 2^-23 each): they enter the parameter only, through a
-// move that is a small part of it.  The reciprocal flushes subnormals; a denominator is 0 or above 3e-23, the host
-// having raised an eps below the normal numbers to the least of them.
-__device__ __forceinline__ float root(float x) {
-    float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-__device__ __forceinline__ float reciprocal(float x) {
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-
 // One step of the optimizer on a lane's eight elements, given the aggregate.
 template <bool CLIP>
 __device__ __forceinline__ void update(const StepArgs& a, float factor, Pair decay, const Pair (&g)[4], Pair (&p)[4],
                                        Pair (&m)[4], Pair (&u)[4]) {
-    const Pair one = both(a.src.one);
+    const Pair one = a.src.one;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         // every product and sum of the moments is rounded on its own: 8-bit codes depend on the last bit
         const Pair h = CLIP ? mul(g[i], both(factor)) : g[i];
-        m[i] = add(mul(m[i], both(a.beta1)), mul(h, both(a.one_minus_beta1)), one);
-        u[i] = add(mul(u[i], both(a.beta2)), mul(mul(h, h), both(a.one_minus_beta2)), one);
-        const Pair d = mul_add(pack(root(lo(u[i])), root(hi(u[i]))), both(a.inv_sqrt_c2), both(a.eps));
+        m[i] = add(mul(m[i], a.beta1), mul(h, a.one_minus_beta1), one);
+        u[i] = add(mul(u[i], a.beta2), mul(mul(h, h), a.one_minus_beta2), one);
+        const Pair d = mul_add(pack(root(lo(u[i])), root(hi(u[i]))), a.inv_sqrt_c2, a.eps);
         const Pair move = mul(m[i], pack(reciprocal(lo(d)), reciprocal(hi(d))));
-        p[i] = mul_add(both(-a.step_size), move, mul(p[i], decay));
+        p[i] = mul_add(a.minus_step_size, move, mul(p[i], decay));
     }
 }
 __device__ __forceinline__ Pair decay_of(const StepArgs& a, const long long* rec) {
@@ -354,47 +378,48 @@ __device__ __forceinline__ void store_moments(const StepArgs& a, uint8_t* first,
                                               float* second_scale, long long position, int lane, int n,
                                               const Pair (&m)[4], const Pair (&u)[4]) {
     // elements beyond n have zero moments: they leave the maximum alone
-    uint32_t top_m = 0u, top_u = 0u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        top_m = max(top_m, max(__float_as_uint(lo(m[i])) & 0x7fffffffu, __float_as_uint(hi(m[i])) & 0x7fffffffu));
-        top_u = max(top_u, max(__float_as_uint(lo(u[i])) & 0x7fffffffu, __float_as_uint(hi(u[i])) & 0x7fffffffu));
-    }
-    const BlockScale sm = block_scale(top_m), su = block_scale(top_u);
-    // position is a multiple of 256: its high word is the whole block's
-    const uint32_t low = static_cast<uint32_t>(position) + (ALIGNED ? 8 * lane : lane);
+    const BlockScale sm = block_scale(top_of(m)), su = block_scale(top_of(u));
+    Pair ym[4], yu[4];
+    scale_down(m, sm.top, ym);
+    scale_down(u, su.top, yu);
+    // position is a multiple of 256: its high word is the whole block's, and the lane's index does not carry
+    const uint32_t base = (static_cast<uint32_t>(position) + (ALIGNED ? 8 * lane : lane)) ^ a.key0;
     const uint32_t key1 = a.key1 ^ (static_cast<uint32_t>(position >> 32) * 0x85EBCA6Bu);
-    uint32_t wm[8], wu[8], nearest = 0xffffffffu;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const Pair ym = mul(mul(m[i], sm.to_code), both(0x1p-120f)), yu = mul(mul(u[i], su.to_code), both(0x1p-120f));
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int j = 2 * i + e;
-            const uint32_t r = random_bits(low + (ALIGNED ? j : 32 * j), a.key0, key1);
-            wm[j] = encode(e ? hi(ym) : lo(ym), __byte_perm(r, 0u, 0x4104));
-            wu[j] = encode(e ? hi(yu) : lo(yu), __byte_perm(r, 0u, 0x4324));
-            nearest = min(nearest, min(distance_to_carry(wm[j]), distance_to_carry(wu[j])));
-        }
-    }
-    if (nearest < kUnsure) {             // one lane in ten thousand, with its sixteen codes
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t r = random_bits(low + (ALIGNED ? j : 32 * j), a.key0, key1);
-            const float xm = fabsf(j & 1 ? hi(m[j >> 1]) : lo(m[j >> 1])), xu = fabsf(j & 1 ? hi(u[j >> 1]) : lo(u[j >> 1]));
-            if (distance_to_carry(wm[j]) < kUnsure) wm[j] = encode_exactly(xm, sm.top, __byte_perm(r, 0u, 0x4104));
-            if (distance_to_carry(wu[j]) < kUnsure) wu[j] = encode_exactly(xu, su.top, __byte_perm(r, 0u, 0x4324));
-        }
-    }
+    uint32_t wm[8], wu[8], clear = 0xffffffffu;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float xm = j & 1 ? hi(m[j >> 1]) : lo(m[j >> 1]), xu = j & 1 ? hi(u[j >> 1]) : lo(u[j >> 1]);
-        wm[j] |= __float_as_uint(xm) & 0x80000000u;
-        // a second moment that is not zero is never held as zero: the next step divides by its root
-        if (xu != 0.0f) wu[j] = max(wu[j], 1u << 24);
+        const uint32_t r = random_bits(base ^ (ALIGNED ? j : 32 * j), key1);
+        wm[j] = encode(j & 1 ? hi(ym[j >> 1]) : lo(ym[j >> 1]), chance_low(r));
+        wu[j] = encode(j & 1 ? hi(yu[j >> 1]) : lo(yu[j >> 1]), chance_high(r));
+        clear = __vminu2(clear, middle_bytes(wm[j], wu[j]));
     }
-    store_codes<ALIGNED>(first, lane, n, wm, sm.keep);
-    store_codes<ALIGNED>(second, lane, n, wu, su.keep);
+    if ((clear & 0xffffu) == 0u || clear < 0x10000u) {            // one lane in 4,000, with its sixteen codes
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t r = random_bits(base ^ (ALIGNED ? j : 32 * j), key1);
+            const float xm = fabsf(j & 1 ? hi(m[j >> 1]) : lo(m[j >> 1])), xu = fabsf(j & 1 ? hi(u[j >> 1]) : lo(u[j >> 1]));
+            if (unsure(wm[j])) wm[j] = encode_exactly(xm, sm.top, chance_low(r));
+            if (unsure(wu[j])) wu[j] = encode_exactly(xu, su.top, chance_high(r));
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) wm[j] |= __float_as_uint(j & 1 ? hi(m[j >> 1]) : lo(m[j >> 1])) & 0x80000000u;
+    const uint32_t cm[2] = {top_bytes(wm[0], wm[1], wm[2], wm[3]) & sm.keep, top_bytes(wm[4], wm[5], wm[6], wm[7]) & sm.keep};
+    uint32_t cu[2] = {top_bytes(wu[0], wu[1], wu[2], wu[3]), top_bytes(wu[4], wu[5], wu[6], wu[7])};
+    // A second moment that is not zero is never held as zero: the next step divides by its root.  Codes are below
+    // 128, so a byte is zero where subtracting one borrows into its top bit.
+    if (((cu[0] - 0x01010101u) | (cu[1] - 0x01010101u)) & 0x80808080u) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float x = j & 1 ? hi(u[j >> 1]) : lo(u[j >> 1]);
+            const uint32_t least = x != 0.0f ? 1u << (8 * (j & 3)) : 0u;
+            if ((cu[j >> 2] >> (8 * (j & 3)) & 0xffu) == 0u) cu[j >> 2] |= least;
+        }
+    }
+    cu[0] &= su.keep;
+    cu[1] &= su.keep;
+    store_codes<ALIGNED>(first, lane, n, cm);
+    store_codes<ALIGNED>(second, lane, n, cu);
     if (lane == 0) {
         *first_scale = sm.scale;
         *second_scale = su.scale;
@@ -474,8 +499,8 @@ __global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 3) adamw_kernel(const 
 // leave few warps: with loads and arithmetic in turn the kernel reached 47 % of the DRAM's rate (issue slots 43 %
 // busy).  So every warp copies blocks ahead into shared memory of its own (cp.async, kept in order by commit
 // groups; nobody waits for another warp) and computes on one that has arrived.
-// An item is one block's parameters, codes and scales with up to `item_workers` gradients; further workers of the
-// block follow as items of gradients alone.
+// An item is one block's parameters, codes and scales with up to KI gradients; further workers of the block follow
+// as items of gradients alone.
 
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 template <int BYTES>
@@ -495,11 +520,11 @@ __host__ __device__ constexpr int stage_bytes(int workers, int grad_size) {
 
 // One worker's 256 gradients to shared memory, in order, by the widest copy that the address allows.
 template <typename GT>
-__device__ __forceinline__ void copy_block(uint32_t to, const GT* from, int lane) {
+__device__ __forceinline__ void copy_block(bool aligned, uint32_t to, const GT* from, int lane) {
     constexpr int kBytes = static_cast<int>(sizeof(GT)) * kWarpElems;
     const char* src = reinterpret_cast<const char*>(from);
     const uint32_t low = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(src));
-    if ((low & 15u) == 0u) {
+    if (aligned) {
 #pragma unroll
         for (int i = 0; i < kBytes; i += 512) copy_async<16>(to + i + 16 * lane, src + i + 16 * lane);
     } else if ((low & 3u) == 0u) {
@@ -518,6 +543,12 @@ __device__ __forceinline__ void read_pairs(uint32_t from, Pair (&x)[4]) {
     asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(x[0]), "=l"(x[1]) : "r"(from) : "memory");
     asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(x[2]), "=l"(x[3]) : "r"(from + 16) : "memory");
 }
+__device__ __forceinline__ void read_words(uint32_t from, uint32_t (&x)[2]) {
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(from) : "memory");
+}
+__device__ __forceinline__ void read_floats(uint32_t from, float (&x)[2]) {
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(x[0]), "=f"(x[1]) : "r"(from) : "memory");
+}
 template <typename GT> __device__ __forceinline__ void read_grads(uint32_t from, int lane, Pair (&x)[4]);
 template <> __device__ __forceinline__ void read_grads<float>(uint32_t from, int lane, Pair (&x)[4]) { read_pairs(from + 32 * lane, x); }
 template <> __device__ __forceinline__ void read_grads<__nv_bfloat16>(uint32_t from, int lane, Pair (&x)[4]) {
@@ -528,125 +559,147 @@ template <> __device__ __forceinline__ void read_grads<__nv_bfloat16>(uint32_t f
     for (int i = 0; i < 4; ++i) x[i] = pack(__uint_as_float(r[i] << 16), __uint_as_float(r[i] & 0xffff0000u));
 }
 
-// SUMS: partial sums of the aggregate, min(K, 4) rounded up to 1, 2 or 4.  STAGES: items in shared memory.
-template <typename GT, int SUMS, int STAGES, bool CLIP, bool NORM>
-__global__ void __launch_bounds__(kThreads, 3) adamw8_kernel(const __grid_constant__ StepArgs a) {
+// One kernel for each number KI of gradients in an item (1, 2, 4 or 8; MANY: more workers than that).  In flight
+// for each SM, with two CTAs on it: (stages - 1) * 16 items, 70 to 100 KB.
+__host__ __device__ constexpr int ring_stages(int workers, int grad_size) {
+    const int stage = stage_bytes(workers, grad_size);
+    return stage <= 2600 ? 4 : stage <= 3600 ? 3 : 2;
+}
+__host__ __device__ constexpr size_t ring_bytes(int workers, int grad_size) {
+    return static_cast<size_t>(kWarps) * ring_stages(workers, grad_size) * stage_bytes(workers, grad_size);
+}
+
+template <typename GT, int KI, bool MANY, bool CLIP, bool NORM>
+__global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_constant__ StepArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
+    constexpr int kGrad = static_cast<int>(sizeof(GT)), kStages = ring_stages(KI, kGrad), kStage = stage_bytes(KI, kGrad);
+    constexpr int kSums = KI < 4 ? KI : 4;
     agg::griddep_launch_dependents();
     agg::griddep_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long* rec = a.src.recs + blockIdx.x * static_cast<long long>(a.src.stride);
     const long long cf = __ldg(rec + kRecCount);
     const int count = static_cast<int>(cf & 0xffffffffLL);
+    const bool grads_aligned = cf >> 32 & kGradsAligned || (CLIP && a.src.staged);
     const float factor = CLIP ? __ldcg(a.factor) : 1.0f;
-    const Pair one = both(a.src.one);
-    const int K = CLIP && a.src.staged ? 1 : a.src.K;
+    const int K = a.src.K, chunks = MANY ? (K + KI - 1) / KI : 1;
     double sq = 0.0;
 
     // blocks warp, warp + 8, ... of the run; whole ones of aligned tensors take the staged path
     const int mine = (count - warp * kWarpElems + kSpan - 1) / kSpan;                        // blocks that begin in the run
     int whole = cf >> 32 & kStateAligned ? (count - (warp + 1) * kWarpElems + kSpan) / kSpan : 0;
     if (whole < 0) whole = 0;
-    const int chunks = (K + a.item_workers - 1) / a.item_workers;
-    const int items = whole * chunks, stage = stage_bytes(min(K, a.item_workers), CLIP && a.src.staged ? 4 : static_cast<int>(sizeof(GT)));
-    const uint32_t ring = shared_address(smem) + warp * STAGES * stage;
-    const float* params = reinterpret_cast<const float*>(__ldg(rec + kRecParam));
-    const long long first = __ldg(rec + kRecFirst), second = __ldg(rec + kRecSecond);
-    float* first_scale = reinterpret_cast<float*>(__ldg(rec + kRecFirstScale));
-    float* second_scale = reinterpret_cast<float*>(__ldg(rec + kRecSecondScale));
+    const uint32_t ring = shared_address(smem) + warp * (kStages * kStage);
+    const char* params = reinterpret_cast<const char*>(__ldg(rec + kRecParam));
+    const char* first = reinterpret_cast<const char*>(__ldg(rec + kRecFirst));
+    const char* second = reinterpret_cast<const char*>(__ldg(rec + kRecSecond));
+    const char* first_scale = reinterpret_cast<const char*>(__ldg(rec + kRecFirstScale));
+    const char* second_scale = reinterpret_cast<const char*>(__ldg(rec + kRecSecondScale));
     const long long position = __ldg(rec + kRecPosition);
+    // what a lane copies of every block, at the run's first element
+    const char* my_params = params + 16 * lane;
+    const char* my_codes = (lane < 16 ? first : second) + 16 * (lane & 15);
+    const char* my_scale = lane == 0 ? first_scale : second_scale;
+    const char* only = KI == 1 ? (CLIP && a.src.staged ? reinterpret_cast<const char*>(a.src.staged + position)
+                                                        : reinterpret_cast<const char*>(__ldg(rec + kRecGrads + a.src.worker[0])))
+                               : nullptr;
 
-    int next = 0, next_offset = warp * kWarpElems, next_chunk = 0, next_slot = 0;            // the item to copy
+    auto copy_item = [&](int offset, int chunk, uint32_t to) {
+        if (!MANY || chunk == 0) {
+            copy_async<16>(to + 16 * lane, my_params + 4 * offset);
+            copy_async<16>(to + 512 + 16 * lane, my_params + 4 * offset + 512);
+            copy_async<16>(to + kStageCodes + 16 * lane, my_codes + offset);
+            if (lane < 2) copy_async<4>(to + kStageScales + 4 * lane, my_scale + offset / (kWarpElems / 4));
+        }
+#pragma unroll
+        for (int j = 0; j < KI; ++j) {
+            const int k = MANY ? chunk * KI + j : j;
+            if (KI == 1 || k < K) {
+                const char* g = KI == 1 ? only : reinterpret_cast<const char*>(__ldg(rec + kRecGrads + a.src.worker[k]));
+                copy_block<GT>(grads_aligned, to + kStageGrads + j * kGrad * kWarpElems,
+                               reinterpret_cast<const GT*>(g) + offset, lane);
+            }
+        }
+    };
+
+    int next_offset = warp * kWarpElems, next_chunk = 0, left = whole * chunks;              // the item to copy
+    uint32_t to = ring, from = ring;
     auto issue = [&]() {
-        if (next < items) {
-            const uint32_t to = ring + next_slot * stage;
-            if (next_chunk == 0) {
-                const char* p = reinterpret_cast<const char*>(params + next_offset);
-                copy_async<16>(to + 16 * lane, p + 16 * lane);
-                copy_async<16>(to + 512 + 16 * lane, p + 512 + 16 * lane);
-                const char* codes = reinterpret_cast<const char*>(lane < 16 ? first : second) + next_offset;
-                copy_async<16>(to + kStageCodes + 16 * lane, codes + 16 * (lane & 15));
-                const float* scale = lane == 0 ? first_scale : second_scale;
-                if (lane < 2) copy_async<4>(to + kStageScales + 4 * lane, scale + next_offset / kWarpElems);
-            }
-            if (CLIP && a.src.staged) {
-                copy_block<float>(to + kStageGrads, a.src.staged + position + next_offset, lane);
-            } else {
-                const int k0 = next_chunk * a.item_workers, k1 = min(K, k0 + a.item_workers);
-                for (int k = k0; k < k1; ++k)
-                    copy_block<GT>(to + kStageGrads + (k - k0) * static_cast<int>(sizeof(GT)) * kWarpElems,
-                                   reinterpret_cast<const GT*>(__ldg(rec + kRecGrads + a.src.worker[k])) + next_offset, lane);
-            }
-            ++next;
-            next_slot = next_slot + 1 == STAGES ? 0 : next_slot + 1;
-            if (++next_chunk == chunks) {
+        if (left > 0) {
+            copy_item(next_offset, next_chunk, to);
+            --left;
+            if (!MANY || ++next_chunk == chunks) {
                 next_chunk = 0;
                 next_offset += kSpan;
             }
         }
         copy_commit();                       // an empty group where nothing is left: the count of groups stays right
+        to = to == ring + (kStages - 1) * kStage ? ring : to + kStage;
     };
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) issue();
+    for (int i = 0; i < kStages - 1; ++i) issue();
 
     const Pair decay = decay_of(a, rec);
     const long long copy = __ldg(rec + kRecCopy);
-    int slot = 0, offset = warp * kWarpElems;
+    int offset = warp * kWarpElems;
+#pragma unroll 1
     for (int block = 0; block < whole; ++block, offset += kSpan) {
-        Pair sum[SUMS][4], p[4];
-        uint32_t codes[4];
+        Pair sum[kSums][4], p[4];
+        uint32_t cm[2], cu[2];
         float scales[2];
+        if (MANY) {
 #pragma unroll
-        for (int j = 0; j < SUMS; ++j)
+            for (int j = 0; j < kSums; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[j][i] = both(-0.0f);                             // adds nothing to anything
+                for (int i = 0; i < 4; ++i) sum[j][i] = both(-0.0f);                         // adds nothing to anything
+        }
+#pragma unroll 1
         for (int chunk = 0; chunk < chunks; ++chunk) {
             issue();
-            copy_wait<STAGES - 1>();
+            copy_wait<kStages - 1>();
             __syncwarp();
-            const uint32_t from = ring + slot * stage;
-            if (chunk == 0) {
+            if (!MANY || chunk == 0) {
                 read_pairs(from + 32 * lane, p);
-                asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(codes[0]), "=r"(codes[1]) : "r"(from + kStageCodes + 8 * lane) : "memory");
-                asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];"
-                             : "=r"(codes[2]), "=r"(codes[3]) : "r"(from + kStageCodes + kWarpElems + 8 * lane) : "memory");
-                asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(scales[0]), "=f"(scales[1]) : "r"(from + kStageScales) : "memory");
+                read_words(from + kStageCodes + 8 * lane, cm);
+                read_words(from + kStageCodes + kWarpElems + 8 * lane, cu);
+                read_floats(from + kStageScales, scales);
             }
-            if (CLIP && a.src.staged) {
-                read_grads<float>(from + kStageGrads, lane, sum[0]);
-            } else {
-                const int k0 = chunk * a.item_workers, here = min(K - k0, a.item_workers);
-                for (int k = 0; k < here; k += SUMS) {
 #pragma unroll
-                    for (int j = 0; j < SUMS; ++j) {
-                        if (k + j < here) {
-                            Pair x[4];
-                            read_grads<GT>(from + kStageGrads + (k + j) * static_cast<int>(sizeof(GT)) * kWarpElems, lane, x);
-                            const Pair w = both(a.src.lambda[k0 + k + j]);
+            for (int j = 0; j < KI; ++j) {
+                const int k = MANY ? chunk * KI + j : j;
+                Pair x[4];
+                read_grads<GT>(from + kStageGrads + j * kGrad * kWarpElems, lane, x);        // beyond K: not used
+                if (KI == 1) {               // the only weight is 1
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) sum[j][i] = add(mul(w, x[i]), sum[j][i], one);
-                        }
+                    for (int i = 0; i < 4; ++i) sum[0][i] = x[i];
+                } else {
+                    const Pair w = both(k < K ? a.src.lambda[k] : 0.0f);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const Pair y = k < K ? mul(w, x[i]) : both(-0.0f);
+                        sum[j % kSums][i] = !MANY && j < kSums ? y : add(y, sum[j % kSums][i], a.src.one);
                     }
                 }
             }
             __syncwarp();                    // everybody has read the slot before anybody's copy overwrites it
-            slot = slot + 1 == STAGES ? 0 : slot + 1;
+            from = from == ring + (kStages - 1) * kStage ? ring : from + kStage;
         }
 #pragma unroll
-        for (int j = 1; j < SUMS; ++j)
+        for (int j = 1; j < kSums; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[0][i] = add(sum[0][i], sum[j][i], one);
+            for (int i = 0; i < 4; ++i) sum[0][i] = add(sum[0][i], sum[j][i], a.src.one);
         if (NORM) sq += sum_squares(sum[0]);
         Pair m[4], u[4];
-        const uint32_t cm[2] = {codes[0], codes[1]}, cu[2] = {codes[2], codes[3]};
         decode(cm, scales[0], m);
         decode(cu, scales[1], u);
         update<CLIP>(a, factor, decay, sum[0], p, m, u);
-        store_f32<true>(const_cast<float*>(params) + offset, lane, kWarpElems, p);
+        store_f32<true>(reinterpret_cast<float*>(const_cast<char*>(params)) + offset, lane, kWarpElems, p);
         if (copy) store_copy<true>(copy, offset, lane, kWarpElems, p);
-        store_moments<true>(a, reinterpret_cast<uint8_t*>(first) + offset, reinterpret_cast<uint8_t*>(second) + offset,
-                            first_scale + offset / kWarpElems, second_scale + offset / kWarpElems, position + offset, lane,
-                            kWarpElems, m, u);
+        store_moments<true>(a, reinterpret_cast<uint8_t*>(const_cast<char*>(first)) + offset,
+                            reinterpret_cast<uint8_t*>(const_cast<char*>(second)) + offset,
+                            reinterpret_cast<float*>(const_cast<char*>(first_scale)) + offset / kWarpElems,
+                            reinterpret_cast<float*>(const_cast<char*>(second_scale)) + offset / kWarpElems, position + offset,
+                            lane, kWarpElems, m, u);
     }
     // a tensor's last, shorter block, and tensors off the grid
 #pragma unroll 1

@@ -131,6 +131,13 @@ db_status upload(const Layout& L, const std::vector<long long>& step, const std:
     return err == cudaSuccess ? DB_OK : record_cuda_error(err, where);
 }
 
+// Both halves of a packed pair.
+unsigned long long pair_of(float x) {
+    uint32_t bits;
+    __builtin_memcpy(&bits, &x, 4);
+    return static_cast<unsigned long long>(bits) << 32 | bits;
+}
+
 // The workers of a call: weights of those with samples.  DB_ERR_ARG if a batch is negative or all are empty.
 db_status set_workers(const int32_t* b, int K, Source* s) {
     long long total = 0;
@@ -139,7 +146,7 @@ db_status set_workers(const int32_t* b, int K, Source* s) {
         total += b[k];
     }
     if (total <= 0) return DB_ERR_ARG;
-    s->one = 1.0f;
+    s->one = pair_of(1.0f);
     s->K = 0;
     for (int k = 0; k < K; ++k) {
         if (b[k] == 0) continue;
@@ -183,7 +190,8 @@ template <typename GT>
 NormFn pick_norm(int K) {
     if (K <= 1) return grad_norm_kernel<GT, 1>;
     if (K <= 2) return grad_norm_kernel<GT, 2>;
-    if (K <= 4 || sizeof(GT) == 4) return grad_norm_kernel<GT, 4>;
+    if constexpr (sizeof(GT) == 4) return grad_norm_kernel<GT, 4>;
+    if (K <= 4) return grad_norm_kernel<GT, 4>;
     return grad_norm_kernel<GT, 8>;
 }
 
@@ -220,49 +228,34 @@ StepFn pick_step(int K, bool clip, bool norm) {
     return norm ? pick_workers<GT, false, true>(K) : pick_workers<GT, false, false>(K);
 }
 
-// 8-bit moments: how many workers' gradients an item takes, how many items a warp keeps in shared memory.
-struct Ring {
-    int item_workers, stages;
-    size_t shared;
-};
-Ring ring_of(int K, size_t gsize) {
-    Ring r;
-    r.item_workers = gsize == 4 ? 4 : 8;
-    const int stage = stage_bytes(std::min(K, r.item_workers), static_cast<int>(gsize));
-    r.stages = 4;
-    while (r.stages > 2 && kWarps * r.stages * stage > 74 << 10) --r.stages;
-    r.shared = static_cast<size_t>(kWarps) * r.stages * stage;
-    return r;
-}
-constexpr int kMaxShared = kWarps * 2 * stage_bytes(4, 4);
-static_assert(stage_bytes(4, 4) == stage_bytes(8, 2) && kMaxShared > 74 << 10 && kMaxShared <= 227 << 10, "ring");
-
-template <typename GT, int SUMS, bool CLIP, bool NORM>
-StepFn pick_stages(int n) {
-    return n == 2 ? adamw8_kernel<GT, SUMS, 2, CLIP, NORM> : n == 3 ? adamw8_kernel<GT, SUMS, 3, CLIP, NORM>
-                                                                   : adamw8_kernel<GT, SUMS, 4, CLIP, NORM>;
-}
+// 8-bit moments: the kernel for K workers and the shared memory of its ring.  An item holds up to 4 KB of gradients.
 template <typename GT, bool CLIP, bool NORM>
-StepFn pick_sums(int K, int n) {
-    return K <= 1 ? pick_stages<GT, 1, CLIP, NORM>(n) : K <= 2 ? pick_stages<GT, 2, CLIP, NORM>(n)
-                                                                : pick_stages<GT, 4, CLIP, NORM>(n);
+StepFn pick_workers8(int K, size_t* shared) {
+    constexpr int kSize = static_cast<int>(sizeof(GT)), kMost = 16 / kSize;
+    *shared = ring_bytes(K <= 1 ? 1 : K <= 2 ? 2 : K <= 4 ? 4 : kMost, kSize);
+    if (K <= 1) return adamw8_kernel<GT, 1, false, CLIP, NORM>;
+    if (K <= 2) return adamw8_kernel<GT, 2, false, CLIP, NORM>;
+    if (K <= 4) return adamw8_kernel<GT, 4, false, CLIP, NORM>;
+    if (kMost == 8 && K <= 8) return adamw8_kernel<GT, kMost, false, CLIP, NORM>;
+    return adamw8_kernel<GT, kMost, true, CLIP, NORM>;
 }
 template <typename GT>
-StepFn pick_step8(int K, int n, bool clip, bool norm) {
-    if (clip) return pick_sums<GT, true, false>(K, n);
-    return norm ? pick_sums<GT, false, true>(K, n) : pick_sums<GT, false, false>(K, n);
+StepFn pick_step8(int K, bool clip, bool norm, size_t* shared) {
+    if (clip) return pick_workers8<GT, true, false>(K, shared);
+    return norm ? pick_workers8<GT, false, true>(K, shared) : pick_workers8<GT, false, false>(K, shared);
 }
 
 // Every 8-bit kernel of a gradient type may use as much shared memory as its ring takes (per device: at plan creation).
 template <typename GT>
 cudaError_t allow_shared() {
-    for (int K : {1, 2, 4})
-        for (int n : {2, 3, 4})
-            for (int mode = 0; mode < 3; ++mode) {
-                const cudaError_t err = cudaFuncSetAttribute(reinterpret_cast<const void*>(pick_step8<GT>(K, n, mode == 1, mode == 2)),
-                                                             cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxShared);
-                if (err != cudaSuccess) return err;
-            }
+    for (int K : {1, 2, 4, 8, 9})
+        for (int mode = 0; mode < 3; ++mode) {
+            size_t shared;
+            const StepFn fn = pick_step8<GT>(K, mode == 1, mode == 2, &shared);
+            const cudaError_t err = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn),
+                                                         cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
+            if (err != cudaSuccess) return err;
+        }
     return cudaSuccess;
 }
 
@@ -412,7 +405,8 @@ extern "C" db_status db_adamw_plan_create(db_adamw_plan** out, const void* const
         plan->clip = clip;
         db_status st = upload(L, step, norm, plan->table, static_cast<cudaStream_t>(cuda_stream), "db_adamw_plan_create");
         if (st == DB_OK && state8) {
-            const cudaError_t err = grad_dtype == DB_F32 ? allow_shared<float>() : allow_shared<__nv_bfloat16>();
+            cudaError_t err = allow_shared<float>();
+            if (err == cudaSuccess && grad_dtype == DB_BF16) err = allow_shared<__nv_bfloat16>();
             if (err != cudaSuccess) st = record_cuda_error(err, "db_adamw_plan_create");
         }
         if (st != DB_OK) {
@@ -454,14 +448,16 @@ extern "C" db_status db_aggregate_adamw_multi(db_adamw_plan* plan, const int32_t
     a.partials = reinterpret_cast<double*>(plan->table + L.partials);
     float* factor = reinterpret_cast<float*>(plan->table + L.scalars) + 1;
     a.factor = factor;
-    a.beta1 = beta1;
-    a.beta2 = beta2;
-    a.one_minus_beta1 = 1.0f - beta1;
-    a.one_minus_beta2 = 1.0f - beta2;
+    a.beta1 = pair_of(beta1);
+    a.beta2 = pair_of(beta2);
+    a.one_minus_beta1 = pair_of(1.0f - beta1);
+    a.one_minus_beta2 = pair_of(1.0f - beta2);
     // bias corrections in fp64, once per call
-    a.step_size = static_cast<float>(static_cast<double>(lr) / (1.0 - std::pow(static_cast<double>(beta1), static_cast<double>(step))));
-    a.inv_sqrt_c2 = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(static_cast<double>(beta2), static_cast<double>(step))));
-    a.eps = eps > 0.0f ? std::max(eps, 1.17549435e-38f) : 0.0f;    // a normal number: see the kernel's reciprocal
+    const double c1 = 1.0 - std::pow(static_cast<double>(beta1), static_cast<double>(step));
+    const double c2 = 1.0 - std::pow(static_cast<double>(beta2), static_cast<double>(step));
+    a.minus_step_size = pair_of(static_cast<float>(-static_cast<double>(lr) / c1));
+    a.inv_sqrt_c2 = pair_of(static_cast<float>(1.0 / std::sqrt(c2)));
+    a.eps = pair_of(eps > 0.0f ? std::max(eps, 1.17549435e-38f) : 0.0f);      // never subnormal: see the kernel's reciprocal
     a.lr = lr;
     // keys of the stochastic rounding: the finalizer of splitmix64 (Steele, Lea and Flood 2014) over seed and step
     uint64_t z = seed + 0x9E3779B97F4A7C15ull * static_cast<uint64_t>(step);
@@ -480,11 +476,9 @@ extern "C" db_status db_aggregate_adamw_multi(db_adamw_plan* plan, const int32_t
     StepFn fn;
     size_t shared = 0;
     if (plan->state_dtype == DB_E4M3) {
-        const Ring ring = ring_of(K, staged ? 4 : grad_bytes(plan->grad_dtype));
-        a.item_workers = ring.item_workers;
-        shared = ring.shared;
-        fn = plan->grad_dtype == DB_F32 ? pick_step8<float>(K, ring.stages, clip, norm)
-                                        : pick_step8<__nv_bfloat16>(K, ring.stages, clip, norm);
+        // a staged aggregate is one fp32 gradient, whatever the workers' are
+        fn = plan->grad_dtype == DB_F32 || staged ? pick_step8<float>(K, clip, norm, &shared)
+                                                  : pick_step8<__nv_bfloat16>(K, clip, norm, &shared);
     } else {
         fn = plan->grad_dtype == DB_F32 ? pick_step<float>(K, clip, norm) : pick_step<__nv_bfloat16>(K, clip, norm);
     }
