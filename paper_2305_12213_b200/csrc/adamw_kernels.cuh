@@ -38,7 +38,7 @@ constexpr int kStateAligned = 1, kGradsAligned = 2;              // flags: buffe
 struct Source {                  // where the weighted gradient comes from
     const long long* recs;       // records, `stride` words apart
     long long records;
-    float lambda[DB_MAX_K];      // weights of the active workers (b_k > 0), in worker order
+    unsigned long long lambda[DB_MAX_K];   // weights of the active workers (b_k > 0), in worker order, as pairs
     unsigned char worker[DB_MAX_K];   // their indexes
     int K;                       // how many
     int stride;
@@ -49,7 +49,7 @@ struct Source {                  // where the weighted gradient comes from
 struct NormArgs {
     Source src;
     double* partials;            // one per CTA
-    unsigned int* ticket;        // CTAs that have left their partial; 0 between launches
+    unsigned int* ticket;        // LAST: CTAs that have left their partial; 0 between launches
     float* norm;                 // or NULL
     float* factor;               // or NULL
     float max_norm;
@@ -171,38 +171,67 @@ template <> struct GradRaw<__nv_bfloat16> {
     }
 };
 
+template <int SUMS>
+__device__ __forceinline__ void join_sums(Pair (&sum)[SUMS][4], Pair one) {
+#pragma unroll
+    for (int j = 1; j < SUMS; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[0][i] = add(sum[0][i], sum[j][i], one);
+}
+
 // g = sum over the active workers of lambda_k g_k: products rounded to fp32, added in four partial sums (k mod 4,
 // k ascending) that are joined in order.  Shorter chains than one sum, and a pair's product and sum cost what two
-// FMAs do.  KU workers' loads at once.
+// FMAs do.  KU workers' loads at once; MANY: more than KU workers, in rounds.
 template <typename GT, int KU, bool ALIGNED>
-__device__ __forceinline__ void aggregate(const Source& s, const long long* grads, int offset, int lane, int n,
-                                          Pair (&g)[4]) {
-    constexpr int kSums = KU < 4 ? KU : 4;
-    const Pair one = s.one;
-    Pair sum[kSums][4];
-    for (int k0 = 0; k0 < s.K; k0 += KU) {
-        GradRaw<GT> raw[KU];
+__device__ __forceinline__ void load_round(const Source& s, const long long* grads, int k0, int offset, int lane, int n,
+                                           GradRaw<GT> (&raw)[KU]) {
 #pragma unroll
-        for (int j = 0; j < KU; ++j)
-            if (k0 + j < s.K)
-                raw[j].template load<ALIGNED>(reinterpret_cast<const GT*>(__ldg(grads + s.worker[k0 + j])) + offset, lane, n);
+    for (int j = 0; j < KU; ++j)
+        if (k0 + j < s.K)
+            raw[j].template load<ALIGNED>(reinterpret_cast<const GT*>(__ldg(grads + s.worker[k0 + j])) + offset, lane, n);
+}
+// All workers of a sum that fits one round: partial sum by partial sum.
+template <typename GT, int KU>
+__device__ __forceinline__ void weigh_round(const Source& s, const GradRaw<GT> (&raw)[KU], Pair (&g)[4]) {
 #pragma unroll
-        for (int j = 0; j < KU; ++j) {
-            const bool in = k0 + j < s.K;
-            const Pair w = both(in ? s.lambda[k0 + j] : 0.0f);
+    for (int j = 0; j < (KU < 4 ? KU : 4); ++j) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const Pair x = in ? mul(w, raw[j].get(i)) : both(-0.0f);      // -0 adds nothing to anything
-                if (j < 4) sum[j % kSums][i] = k0 == 0 ? x : add(sum[j % kSums][i], x, one);
-                else sum[j % kSums][i] = add(sum[j % kSums][i], x, one);
-            }
+        for (int i = 0; i < 4; ++i) {
+            Pair x = j < s.K ? mul(s.lambda[j], raw[j].get(i)) : both(-0.0f);                // -0 adds nothing to anything
+#pragma unroll
+            for (int l = j + 4; l < KU; l += 4)
+                if (l < s.K) x = add(mul(s.lambda[l], raw[l].get(i)), x, s.one);
+            g[i] = j == 0 ? x : add(x, g[i], s.one);
         }
     }
+}
+template <typename GT, int KU, bool MANY, bool ALIGNED>
+__device__ __forceinline__ void aggregate(const Source& s, const long long* grads, int offset, int lane, int n,
+                                          Pair (&g)[4]) {
+    GradRaw<GT> raw[KU];
+    if constexpr (!MANY) {
+        load_round<GT, KU, ALIGNED>(s, grads, 0, offset, lane, n, raw);
+        weigh_round<GT, KU>(s, raw, g);
+    } else {
+        static_assert(KU % 4 == 0, "worker k belongs to sum k mod 4");
+        Pair sum[4][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        g[i] = sum[0][i];
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int j = 1; j < kSums; ++j) g[i] = add(g[i], sum[j][i], one);
+            for (int i = 0; i < 4; ++i) sum[j][i] = both(-0.0f);
+#pragma unroll 1
+        for (int k0 = 0; k0 < s.K; k0 += KU) {
+            load_round<GT, KU, ALIGNED>(s, grads, k0, offset, lane, n, raw);
+#pragma unroll
+            for (int j = 0; j < KU; ++j)
+                if (k0 + j < s.K) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[j & 3][i] = add(mul(s.lambda[k0 + j], raw[j].get(i)), sum[j & 3][i], s.one);
+                }
+        }
+        join_sums<4>(sum, s.one);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g[i] = sum[0][i];
     }
 }
 
@@ -427,7 +456,7 @@ __device__ __forceinline__ void store_moments(const StepArgs& a, uint8_t* first,
 }
 
 // A block straight from global memory to registers and back.
-template <typename GT, int KU, bool STATE8, bool CLIP, bool NORM, bool ALIGNED>
+template <typename GT, int KU, bool MANY, bool STATE8, bool CLIP, bool NORM, bool ALIGNED>
 __device__ __forceinline__ void step_block(const StepArgs& a, const long long* rec, int offset, int lane, int n, float factor,
                                            double& sq) {
     float* param = reinterpret_cast<float*>(__ldg(rec + kRecParam)) + offset;
@@ -451,7 +480,7 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const long long* r
     if (CLIP && a.src.staged)
         load_f32<ALIGNED>(a.src.staged + position, lane, n, g);
     else
-        aggregate<GT, KU, ALIGNED>(a.src, rec + kRecGrads, offset, lane, n, g);
+        aggregate<GT, KU, MANY, ALIGNED>(a.src, rec + kRecGrads, offset, lane, n, g);
     if (NORM) sq += sum_squares(g);
     update<CLIP>(a, factor, decay_of(a, rec), g, p, m, u);
     store_f32<ALIGNED>(param, lane, n, p);
@@ -469,13 +498,13 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const long long* r
 template <typename GT, bool STATE8, bool CLIP, bool NORM>
 __device__ __noinline__ double step_block_slow(const StepArgs& a, const long long* rec, int offset, int lane, int n, float factor) {
     double sq = 0.0;
-    step_block<GT, 4, STATE8, CLIP, NORM, false>(a, rec, offset, lane, n, factor, sq);
+    step_block<GT, 4, true, STATE8, CLIP, NORM, false>(a, rec, offset, lane, n, factor, sq);
     return sq;
 }
 
 // 32-bit moments: one CTA per record, one block per warp.
-template <typename GT, int KU, bool CLIP, bool NORM>
-__global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 3) adamw_kernel(const __grid_constant__ StepArgs a) {
+template <typename GT, int KU, bool MANY, bool CLIP, bool NORM>
+__global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 4) adamw_kernel(const __grid_constant__ StepArgs a) {
     agg::griddep_launch_dependents();
     agg::griddep_wait();
     const int lane = threadIdx.x & 31, offset = (threadIdx.x >> 5) * kWarpElems;
@@ -487,7 +516,7 @@ __global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 3) adamw_kernel(const 
     if (n > 0) {
         const bool aligned = flags & kStateAligned && (flags & kGradsAligned || (CLIP && a.src.staged));
         if (aligned && n >= kWarpElems)
-            step_block<GT, KU, false, CLIP, NORM, true>(a, rec, offset, lane, kWarpElems, factor, sq);
+            step_block<GT, KU, MANY, false, CLIP, NORM, true>(a, rec, offset, lane, kWarpElems, factor, sq);
         else
             sq = step_block_slow<GT, false, CLIP, NORM>(a, rec, offset, lane, min(n, kWarpElems), factor);
     }
@@ -559,6 +588,28 @@ template <> __device__ __forceinline__ void read_grads<__nv_bfloat16>(uint32_t f
     for (int i = 0; i < 4; ++i) x[i] = pack(__uint_as_float(r[i] << 16), __uint_as_float(r[i] & 0xffff0000u));
 }
 
+// The aggregate's partial sums (worker k in sum k mod 4) with an item's gradients added; KI == 1: one worker, whose
+// weight is 1.
+template <typename GT, int KI, bool MANY, int SUMS>
+__device__ __forceinline__ void add_item(const Source& s, uint32_t from, int chunk, int K, int lane, Pair (&sum)[SUMS][4]) {
+#pragma unroll
+    for (int j = 0; j < KI; ++j) {
+        const int k = MANY ? chunk * KI + j : j;
+        Pair x[4];
+        read_grads<GT>(from + j * static_cast<int>(sizeof(GT)) * kWarpElems, lane, x);       // beyond K: not used
+        if (KI == 1) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[0][i] = x[i];
+        } else {
+            const Pair w = s.lambda[k < K ? k : 0];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const Pair y = k < K ? mul(w, x[i]) : both(-0.0f);
+                sum[j % SUMS][i] = !MANY && j < SUMS ? y : add(y, sum[j % SUMS][i], s.one);
+            }
+        }
+    }
+}
 // One kernel for each number KI of gradients in an item (1, 2, 4 or 8; MANY: more workers than that).  In flight
 // for each SM, with two CTAs on it: (stages - 1) * 16 items, 70 to 100 KB.
 __host__ __device__ constexpr int ring_stages(int workers, int grad_size) {
@@ -664,30 +715,11 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
                 read_words(from + kStageCodes + kWarpElems + 8 * lane, cu);
                 read_floats(from + kStageScales, scales);
             }
-#pragma unroll
-            for (int j = 0; j < KI; ++j) {
-                const int k = MANY ? chunk * KI + j : j;
-                Pair x[4];
-                read_grads<GT>(from + kStageGrads + j * kGrad * kWarpElems, lane, x);        // beyond K: not used
-                if (KI == 1) {               // the only weight is 1
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[0][i] = x[i];
-                } else {
-                    const Pair w = both(k < K ? a.src.lambda[k] : 0.0f);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const Pair y = k < K ? mul(w, x[i]) : both(-0.0f);
-                        sum[j % kSums][i] = !MANY && j < kSums ? y : add(y, sum[j % kSums][i], a.src.one);
-                    }
-                }
-            }
+            add_item<GT, KI, MANY>(a.src, from + kStageGrads, chunk, K, lane, sum);
             __syncwarp();                    // everybody has read the slot before anybody's copy overwrites it
             from = from == ring + (kStages - 1) * kStage ? ring : from + kStage;
         }
-#pragma unroll
-        for (int j = 1; j < kSums; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[0][i] = add(sum[0][i], sum[j][i], a.src.one);
+        join_sums<kSums>(sum, a.src.one);
         if (NORM) sq += sum_squares(sum[0]);
         Pair m[4], u[4];
         decode(cm, scales[0], m);
@@ -709,45 +741,79 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
 }
 
 // ---- the norm of the weighted gradient ------------------------------------------------------------------
-// CTAs take records blockIdx.x, blockIdx.x + gridDim.x, ...; with a staging buffer they also leave the aggregates
-// there, for the step that follows.  The CTA that arrives last adds the partials, in their order, and writes the
-// norm and the clipping factor max_norm / norm where the norm is larger than max_norm, else 1 (NaN does not clip).
+// A CTA takes a record of norm_batch CTA steps, all of whose loads are in flight at once (32 to 64 KB of gradients);
+// with a staging buffer it also leaves the aggregates there, for the step that follows.
+// LAST: the CTA that arrives last adds all partials, in order, which saves a launch; on grids of many waves the
+// fence and the atomic at every CTA's end cost more than it (110M bf16 elements of 16 workers: 1669 us against XXX),
+// and a fold kernel follows instead.
+
+// Blocks of a warp whose loads are in flight at once, by the registers that they take (32 to 64).
+template <typename GT>
+__host__ __device__ constexpr int norm_batch(int workers) {
+    return sizeof(GT) == 4 ? (workers <= 1 ? 4 : workers <= 2 ? 2 : 1) : (workers <= 1 ? 8 : workers <= 2 ? 4 : workers <= 4 ? 2 : 1);
+}
+
 template <typename GT>
 __device__ __noinline__ double norm_block_slow(const Source& s, const long long* grads, int offset, int lane, int n, float* staged) {
     Pair g[4];
-    aggregate<GT, 4, false>(s, grads, offset, lane, n, g);
+    aggregate<GT, 4, true, false>(s, grads, offset, lane, n, g);
     if (staged) store_f32<false>(staged, lane, n, g);
     return sum_squares(g);
 }
 
-template <typename GT, int KU>
-__global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 3) grad_norm_kernel(const __grid_constant__ NormArgs a) {
+// Norm and clipping factor from the sum of squares: max_norm / norm where the norm is larger than max_norm, else 1
+// (a NaN norm does not clip).
+__device__ __forceinline__ void write_norm(double total, float* norm, float* factor, float max_norm) {
+    const double root = sqrt(total);
+    if (norm) *norm = static_cast<float>(root);
+    if (factor) *factor = root > static_cast<double>(max_norm) ? static_cast<float>(max_norm / root) : 1.0f;
+}
+
+template <typename GT, int KU, bool MANY, bool LAST>
+__global__ void __launch_bounds__(kThreads, KU * sizeof(GT) > 16 || MANY ? 2 : 3) grad_norm_kernel(const __grid_constant__ NormArgs a) {
+    constexpr int kBatch = norm_batch<GT>(KU);
     __shared__ double smem[kWarps];
     __shared__ bool last;
     agg::griddep_launch_dependents();
     agg::griddep_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, base = (threadIdx.x >> 5) * kWarpElems;
+    const long long* rec = a.src.recs + blockIdx.x * static_cast<long long>(a.src.stride);
+    const long long cf = __ldg(rec + kNormCount);
+    const int count = static_cast<int>(cf & 0xffffffffLL);
+    float* staged = a.src.staged ? a.src.staged + __ldg(rec + kNormPosition) : nullptr;
     double sq = 0.0;
-    for (long long r = blockIdx.x; r < a.src.records; r += gridDim.x) {
-        const long long* rec = a.src.recs + r * a.src.stride;
-        const long long cf = __ldg(rec + kNormCount), position = __ldg(rec + kNormPosition);
-        const int count = static_cast<int>(cf & 0xffffffffLL);
-        const bool aligned = cf >> 32 & kGradsAligned;
-#pragma unroll 1
-        for (int offset = warp * kWarpElems; offset < count; offset += kSpan) {
-            const int n = min(count - offset, kWarpElems);
-            float* staged = a.src.staged ? a.src.staged + position + offset : nullptr;
-            if (aligned && n == kWarpElems) {
+    if (cf >> 32 & kGradsAligned && base + (kBatch - 1) * kSpan + kWarpElems <= count) {
+        if constexpr (MANY) {
+            Pair g[4];
+            aggregate<GT, KU, true, true>(a.src, rec + kNormGrads, base, lane, kWarpElems, g);
+            if (staged) store_f32<true>(staged + base, lane, kWarpElems, g);
+            sq = sum_squares(g);
+        } else {
+            GradRaw<GT> raw[kBatch][KU];
+#pragma unroll
+            for (int e = 0; e < kBatch; ++e)
+                load_round<GT, KU, true>(a.src, rec + kNormGrads, 0, base + e * kSpan, lane, kWarpElems, raw[e]);
+#pragma unroll
+            for (int e = 0; e < kBatch; ++e) {
                 Pair g[4];
-                aggregate<GT, KU, true>(a.src, rec + kNormGrads, offset, lane, n, g);
-                if (staged) store_f32<true>(staged, lane, n, g);
+                weigh_round<GT, KU>(a.src, raw[e], g);
+                if (staged) store_f32<true>(staged + base + e * kSpan, lane, kWarpElems, g);
                 sq += sum_squares(g);
-            } else {
-                sq += norm_block_slow<GT>(a.src, rec + kNormGrads, offset, lane, n, staged);
             }
         }
+    } else {
+        // a tensor's end, and tensors off the grid
+#pragma unroll 1
+        for (int offset = base; offset < count; offset += kSpan)
+            sq += norm_block_slow<GT>(a.src, rec + kNormGrads, offset, lane, min(count - offset, kWarpElems),
+                                      staged ? staged + offset : nullptr);
     }
+
     const double mine = agg::block_sum(sq, smem);
+    if (!LAST) {
+        if (threadIdx.x == 0) a.partials[blockIdx.x] = mine;
+        return;
+    }
     if (threadIdx.x == 0) {
         a.partials[blockIdx.x] = mine;
         __threadfence();
@@ -757,19 +823,17 @@ __global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 3) grad_norm_kernel(co
     if (!last) return;
     __threadfence();
     double acc = 0.0;
-    for (int i = threadIdx.x; i < static_cast<int>(gridDim.x); i += kThreads) acc += __ldcg(a.partials + i);
+    for (unsigned int i = threadIdx.x; i < gridDim.x; i += kThreads) acc += __ldcg(a.partials + i);
     const double total = agg::block_sum(acc, smem);
     if (threadIdx.x != 0) return;
     *a.ticket = 0u;
-    const double root = sqrt(total);
-    if (a.norm) *a.norm = static_cast<float>(root);
-    if (a.factor) *a.factor = root > static_cast<double>(a.max_norm) ? static_cast<float>(a.max_norm / root) : 1.0f;
+    write_norm(total, a.norm, a.factor, a.max_norm);
 }
 
-// Norm as the by-product of a step: folds its CTAs' partials, CTA c sums [c per, (c + 1) per); the last stage (one
-// CTA) writes the norm.
+// Folds partials: CTA c sums [c per, (c + 1) per); the last stage (one CTA, sums == NULL) writes the norm.
 static __global__ void __launch_bounds__(1024) fold_kernel(const double* __restrict__ partials, long long n, int per,
-                                                           double* __restrict__ sums, float* __restrict__ norm) {
+                                                           double* __restrict__ sums, float* __restrict__ norm,
+                                                           float* __restrict__ factor, float max_norm) {
     __shared__ double smem[32];
     agg::griddep_launch_dependents();
     agg::griddep_wait();
@@ -780,7 +844,7 @@ static __global__ void __launch_bounds__(1024) fold_kernel(const double* __restr
     const double total = agg::block_sum(acc, smem);
     if (threadIdx.x != 0) return;
     if (sums) sums[blockIdx.x] = total;
-    else *norm = static_cast<float>(sqrt(total));
+    else write_norm(total, norm, factor, max_norm);
 }
 
 }  // namespace adamw

@@ -66,6 +66,10 @@ struct Layout {
     size_t partials, sums, scalars, staged, end;                    // scalars: ticket, clipping factor
 };
 
+// Elements of a norm record: as much as the kernel for all K workers has in flight at once.
+template <typename GT>
+int norm_run(int K) { return kSpan * norm_batch<GT>(K <= 1 ? 1 : K <= 2 ? 2 : K <= 4 ? 4 : 8); }     // as in pick_norm
+
 // step: records of the optimizer step (state8: several CTA steps each); norm: records of the norm kernel.
 bool make_layout(int32_t K, db_dtype dt, bool state8, const int64_t* sizes, int32_t T, bool step, bool norm, Layout* L) {
     long long spans;
@@ -73,7 +77,7 @@ bool make_layout(int32_t K, db_dtype dt, bool state8, const int64_t* sizes, int3
     L->end = 0;
     L->step = L->norm = Records{};
     if (step) L->step = records_of(sizes, T, state8 ? run_of(spans) : kSpan, kRecGrads + K, &L->end);
-    if (norm) L->norm = records_of(sizes, T, run_of(spans), kNormGrads + K, &L->end);
+    if (norm) L->norm = records_of(sizes, T, dt == DB_F32 ? norm_run<float>(K) : norm_run<__nv_bfloat16>(K), kNormGrads + K, &L->end);
     const size_t n = static_cast<size_t>(std::max<long long>(1, std::max(L->step.count, L->norm.count)));
     L->partials = L->end;
     L->sums = L->partials + round256(8 * n);
@@ -150,7 +154,7 @@ db_status set_workers(const int32_t* b, int K, Source* s) {
     s->K = 0;
     for (int k = 0; k < K; ++k) {
         if (b[k] == 0) continue;
-        s->lambda[s->K] = static_cast<float>(static_cast<double>(b[k]) / static_cast<double>(total));
+        s->lambda[s->K] = pair_of(static_cast<float>(static_cast<double>(b[k]) / static_cast<double>(total)));
         s->worker[s->K++] = static_cast<unsigned char>(k);
     }
     return DB_OK;
@@ -172,55 +176,63 @@ cudaError_t launch(void (*fn)(Params...), long long grid, int block, size_t shar
     return cudaLaunchKernelEx(&cfg, fn, args...);
 }
 
-db_status launch_fold(double* partials, long long n, double* sums, float* norm, cudaStream_t stream) {
+db_status launch_fold(const Layout& L, char* table, long long n, float* norm, float* factor, float max_norm, cudaStream_t stream) {
+    const double* partials = reinterpret_cast<const double*>(table + L.partials);
+    double* sums = reinterpret_cast<double*>(table + L.sums);
     if (n > kFoldPer) {
         const long long stage = (n + kFoldPer - 1) / kFoldPer;
-        DB_CUDA_TRY(launch(fold_kernel, stage, 1024, 0, stream, static_cast<const double*>(partials), n, kFoldPer, sums,
-                           static_cast<float*>(nullptr)));
+        DB_CUDA_TRY(launch(fold_kernel, stage, 1024, 0, stream, partials, n, kFoldPer, sums, static_cast<float*>(nullptr),
+                           static_cast<float*>(nullptr), 0.0f));
         partials = sums;
         n = stage;
     }
-    DB_CUDA_TRY(launch(fold_kernel, 1, n > 256 ? 1024 : 256, 0, stream, static_cast<const double*>(partials), n,
-                       static_cast<int>(n), static_cast<double*>(nullptr), norm));
+    DB_CUDA_TRY(launch(fold_kernel, 1, n > 256 ? 1024 : 256, 0, stream, partials, n, static_cast<int>(n),
+                       static_cast<double*>(nullptr), norm, factor, max_norm));
     return DB_OK;
 }
 
 using NormFn = void (*)(const NormArgs);
-template <typename GT>
+template <typename GT, bool LAST>
 NormFn pick_norm(int K) {
-    if (K <= 1) return grad_norm_kernel<GT, 1>;
-    if (K <= 2) return grad_norm_kernel<GT, 2>;
-    if constexpr (sizeof(GT) == 4) return grad_norm_kernel<GT, 4>;
-    if (K <= 4) return grad_norm_kernel<GT, 4>;
-    return grad_norm_kernel<GT, 8>;
+    if (K <= 1) return grad_norm_kernel<GT, 1, false, LAST>;
+    if (K <= 2) return grad_norm_kernel<GT, 2, false, LAST>;
+    if (K <= 4) return grad_norm_kernel<GT, 4, false, LAST>;
+    if (K <= 8) return grad_norm_kernel<GT, 8, false, LAST>;
+    if constexpr (sizeof(GT) == 2)
+        if (K <= 16) return grad_norm_kernel<GT, 16, false, LAST>;
+    return grad_norm_kernel<GT, 8, true, LAST>;
 }
 
-// Norm (and aggregate, and clipping factor) of a plan's gradients: CTAs stay and take every grid-th record.
-db_status launch_norm(const Layout& L, char* table, db_dtype dt, Source src, float* norm, float* factor, float max_norm,
+// Norm (and aggregate, and clipping factor) of a plan's gradients.
+db_status launch_norm(const Layout& L, char* table, db_dtype dt, int workers, Source src, float* norm, float* factor, float max_norm,
                       cudaStream_t stream) {
     NormArgs a{};
     a.src = src;
     a.src.recs = reinterpret_cast<const long long*>(table + L.norm.at);
-    a.src.records = L.norm.count;
     a.src.stride = L.norm.stride;
     a.partials = reinterpret_cast<double*>(table + L.partials);
     a.ticket = reinterpret_cast<unsigned int*>(table + L.scalars);
     a.norm = norm;
     a.factor = factor;
     a.max_norm = max_norm;
-    const NormFn fn = dt == DB_F32 ? pick_norm<float>(src.K) : pick_norm<__nv_bfloat16>(src.K);
-    const long long resident = static_cast<long long>(sm_count()) * 8;
-    DB_CUDA_TRY(launch(fn, std::min(L.norm.count, resident), kThreads, 0, stream, a));
-    return DB_OK;
+    const bool last = L.norm.count <= 4 * sm_count();
+    // by the plan's workers, not the call's: the records are made for that kernel
+    const NormFn fn = dt == DB_F32 ? (last ? pick_norm<float, true>(workers) : pick_norm<float, false>(workers))
+                                   : (last ? pick_norm<__nv_bfloat16, true>(workers) : pick_norm<__nv_bfloat16, false>(workers));
+    DB_CUDA_TRY(launch(fn, L.norm.count, kThreads, 0, stream, a));
+    return last ? DB_OK : launch_fold(L, table, L.norm.count, norm, factor, max_norm, stream);
 }
 
 using StepFn = void (*)(const StepArgs);
 template <typename GT, bool CLIP, bool NORM>
 StepFn pick_workers(int K) {
-    if (K <= 1) return adamw_kernel<GT, 1, CLIP, NORM>;
-    if (K <= 2) return adamw_kernel<GT, 2, CLIP, NORM>;
-    if (K <= 4) return adamw_kernel<GT, 4, CLIP, NORM>;
-    return adamw_kernel<GT, 8, CLIP, NORM>;
+    if (K <= 1) return adamw_kernel<GT, 1, false, CLIP, NORM>;
+    if (K <= 2) return adamw_kernel<GT, 2, false, CLIP, NORM>;
+    if (K <= 4) return adamw_kernel<GT, 4, false, CLIP, NORM>;
+    if (K <= 8) return adamw_kernel<GT, 8, false, CLIP, NORM>;
+    if constexpr (sizeof(GT) == 2)
+        if (K <= 16) return adamw_kernel<GT, 16, false, CLIP, NORM>;
+    return adamw_kernel<GT, sizeof(GT) == 2 ? 8 : 4, true, CLIP, NORM>;
 }
 template <typename GT>
 StepFn pick_step(int K, bool clip, bool norm) {
@@ -228,11 +240,17 @@ StepFn pick_step(int K, bool clip, bool norm) {
     return norm ? pick_workers<GT, false, true>(K) : pick_workers<GT, false, false>(K);
 }
 
-// 8-bit moments: the kernel for K workers and the shared memory of its ring.  An item holds up to 4 KB of gradients.
+// Gradients of an item that goes through shared memory: up to 4 KB.
+template <typename GT>
+constexpr int most_workers() { return 16 / static_cast<int>(sizeof(GT)); }
+template <typename GT>
+int item_workers(int K) { return K <= 1 ? 1 : K <= 2 ? 2 : K <= 4 ? 4 : most_workers<GT>(); }
+
+// 8-bit moments: the kernel for K workers and the shared memory of its ring.
 template <typename GT, bool CLIP, bool NORM>
 StepFn pick_workers8(int K, size_t* shared) {
-    constexpr int kSize = static_cast<int>(sizeof(GT)), kMost = 16 / kSize;
-    *shared = ring_bytes(K <= 1 ? 1 : K <= 2 ? 2 : K <= 4 ? 4 : kMost, kSize);
+    constexpr int kMost = most_workers<GT>();
+    *shared = ring_bytes(item_workers<GT>(K), sizeof(GT));
     if (K <= 1) return adamw8_kernel<GT, 1, false, CLIP, NORM>;
     if (K <= 2) return adamw8_kernel<GT, 2, false, CLIP, NORM>;
     if (K <= 4) return adamw8_kernel<GT, 4, false, CLIP, NORM>;
@@ -245,18 +263,23 @@ StepFn pick_step8(int K, bool clip, bool norm, size_t* shared) {
     return norm ? pick_workers8<GT, false, true>(K, shared) : pick_workers8<GT, false, false>(K, shared);
 }
 
-// Every 8-bit kernel of a gradient type may use as much shared memory as its ring takes (per device: at plan creation).
+// The 8-bit kernels that a plan may launch may use as much shared memory as their rings take (per device: at creation).
 template <typename GT>
 cudaError_t allow_shared() {
+    cudaError_t err = cudaSuccess;
     for (int K : {1, 2, 4, 8, 9})
-        for (int mode = 0; mode < 3; ++mode) {
+        for (int mode = 0; err == cudaSuccess && mode < 3; ++mode) {
             size_t shared;
             const StepFn fn = pick_step8<GT>(K, mode == 1, mode == 2, &shared);
-            const cudaError_t err = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn),
-                                                         cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
-            if (err != cudaSuccess) return err;
+            err = cudaFuncSetAttribute(reinterpret_cast<const void*>(fn), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(shared));
         }
-    return cudaSuccess;
+    return err;
+}
+db_status allow_shared(db_dtype dt) {
+    cudaError_t err = allow_shared<float>();                  // a staged aggregate is fp32, whatever the gradients are
+    if (err == cudaSuccess && dt == DB_BF16) err = allow_shared<__nv_bfloat16>();
+    return err == cudaSuccess ? DB_OK : record_cuda_error(err, "db_adamw_plan_create");
 }
 
 }  // namespace
@@ -404,11 +427,7 @@ extern "C" db_status db_adamw_plan_create(db_adamw_plan** out, const void* const
         plan->K = K;
         plan->clip = clip;
         db_status st = upload(L, step, norm, plan->table, static_cast<cudaStream_t>(cuda_stream), "db_adamw_plan_create");
-        if (st == DB_OK && state8) {
-            cudaError_t err = allow_shared<float>();
-            if (err == cudaSuccess && grad_dtype == DB_BF16) err = allow_shared<__nv_bfloat16>();
-            if (err != cudaSuccess) st = record_cuda_error(err, "db_adamw_plan_create");
-        }
+        if (st == DB_OK && state8) st = allow_shared(grad_dtype);
         if (st != DB_OK) {
             delete plan;
             return st;
@@ -469,7 +488,7 @@ extern "C" db_status db_aggregate_adamw_multi(db_adamw_plan* plan, const int32_t
 
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (clip) {
-        const db_status s = launch_norm(L, plan->table, plan->grad_dtype, a.src, grad_norm, factor, max_norm, stream);
+        const db_status s = launch_norm(L, plan->table, plan->grad_dtype, plan->K, a.src, grad_norm, factor, max_norm, stream);
         if (s != DB_OK) return s;
     }
     const int K = staged ? 1 : a.src.K;
@@ -483,7 +502,7 @@ extern "C" db_status db_aggregate_adamw_multi(db_adamw_plan* plan, const int32_t
         fn = plan->grad_dtype == DB_F32 ? pick_step<float>(K, clip, norm) : pick_step<__nv_bfloat16>(K, clip, norm);
     }
     DB_CUDA_TRY(launch(fn, L.step.count, kThreads, shared, stream, a));
-    return norm ? launch_fold(a.partials, L.step.count, reinterpret_cast<double*>(plan->table + L.sums), grad_norm, stream) : DB_OK;
+    return norm ? launch_fold(L, plan->table, L.step.count, grad_norm, nullptr, 0.0f, stream) : DB_OK;
 }
 
 extern "C" size_t db_grad_norm_plan_device_bytes(int32_t K, db_dtype grad_dtype, const int64_t* sizes, int32_t T) {
@@ -550,6 +569,6 @@ extern "C" db_status db_grad_norm_multi(db_grad_norm_plan* plan, const int32_t* 
     const db_status st = set_workers(b, plan->K, &src);
     if (st != DB_OK) return st;
     if (plan->layout.norm.count == 0) return DB_OK;
-    return launch_norm(plan->layout, plan->table, plan->grad_dtype, src, grad_norm, nullptr, 0.0f,
+    return launch_norm(plan->layout, plan->table, plan->grad_dtype, plan->K, src, grad_norm, nullptr, 0.0f,
                        static_cast<cudaStream_t>(cuda_stream));
 }
