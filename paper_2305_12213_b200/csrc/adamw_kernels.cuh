@@ -24,6 +24,7 @@ constexpr int kLaneElems = 8;
 constexpr int kWarpElems = DB_ADAMW_BLOCK;                       // 32 lanes x 8 elements
 constexpr int kSpan = kThreads * kLaneElems;                       // elements of a CTA's step
 constexpr int kWarps = kThreads / 32;
+constexpr int kNormThreads = kThreads / 2;                         // the norm kernel: two CTAs for a record
 static_assert(kWarpElems == 32 * kLaneElems, "one warp per block of elements");
 
 // Words of 8 bytes of a run's record; the K gradient pointers follow at kRecGrads.
@@ -182,13 +183,17 @@ __device__ __forceinline__ void join_sums(Pair (&sum)[SUMS][4], Pair one) {
 // g = sum over the active workers of lambda_k g_k: products rounded to fp32, added in four partial sums (k mod 4,
 // k ascending) that are joined in order.  Shorter chains than one sum, and a pair's product and sum cost what two
 // FMAs do.  KU workers' loads at once; MANY: more than KU workers, in rounds.
+template <int KU>
+__device__ __forceinline__ void pointers_of(const Source& s, const long long* grads, int k0, long long (&from)[KU]) {
+#pragma unroll
+    for (int j = 0; j < KU; ++j) from[j] = k0 + j < s.K ? __ldg(grads + s.worker[k0 + j]) : 0;
+}
 template <typename GT, int KU, bool ALIGNED>
-__device__ __forceinline__ void load_round(const Source& s, const long long* grads, int k0, int offset, int lane, int n,
+__device__ __forceinline__ void load_round(const Source& s, const long long (&from)[KU], int k0, int offset, int lane, int n,
                                            GradRaw<GT> (&raw)[KU]) {
 #pragma unroll
     for (int j = 0; j < KU; ++j)
-        if (k0 + j < s.K)
-            raw[j].template load<ALIGNED>(reinterpret_cast<const GT*>(__ldg(grads + s.worker[k0 + j])) + offset, lane, n);
+        if (k0 + j < s.K) raw[j].template load<ALIGNED>(reinterpret_cast<const GT*>(from[j]) + offset, lane, n);
 }
 // All workers of a sum that fits one round: partial sum by partial sum.
 template <typename GT, int KU>
@@ -209,8 +214,10 @@ template <typename GT, int KU, bool MANY, bool ALIGNED>
 __device__ __forceinline__ void aggregate(const Source& s, const long long* grads, int offset, int lane, int n,
                                           Pair (&g)[4]) {
     GradRaw<GT> raw[KU];
+    long long from[KU];
     if constexpr (!MANY) {
-        load_round<GT, KU, ALIGNED>(s, grads, 0, offset, lane, n, raw);
+        pointers_of<KU>(s, grads, 0, from);
+        load_round<GT, KU, ALIGNED>(s, from, 0, offset, lane, n, raw);
         weigh_round<GT, KU>(s, raw, g);
     } else {
         static_assert(KU % 4 == 0, "worker k belongs to sum k mod 4");
@@ -221,7 +228,8 @@ __device__ __forceinline__ void aggregate(const Source& s, const long long* grad
             for (int i = 0; i < 4; ++i) sum[j][i] = both(-0.0f);
 #pragma unroll 1
         for (int k0 = 0; k0 < s.K; k0 += KU) {
-            load_round<GT, KU, ALIGNED>(s, grads, k0, offset, lane, n, raw);
+            pointers_of<KU>(s, grads, k0, from);
+            load_round<GT, KU, ALIGNED>(s, from, k0, offset, lane, n, raw);
 #pragma unroll
             for (int j = 0; j < KU; ++j)
                 if (k0 + j < s.K) {
@@ -761,6 +769,8 @@ __device__ __noinline__ double norm_block_slow(const Source& s, const long long*
     return sum_squares(g);
 }
 
+constexpr long long kAhead = 512;            // records
+
 // Norm and clipping factor from the sum of squares: max_norm / norm where the norm is larger than max_norm, else 1
 // (a NaN norm does not clip).
 __device__ __forceinline__ void write_norm(double total, float* norm, float* factor, float max_norm) {
@@ -770,17 +780,24 @@ __device__ __forceinline__ void write_norm(double total, float* norm, float* fac
 }
 
 template <typename GT, int KU, bool MANY, bool LAST>
-__global__ void __launch_bounds__(kThreads, KU * sizeof(GT) > 16 || MANY ? 2 : 3) grad_norm_kernel(const __grid_constant__ NormArgs a) {
+__global__ void __launch_bounds__(kNormThreads, KU * sizeof(GT) > 16 || MANY ? 4 : 6) grad_norm_kernel(const __grid_constant__ NormArgs a) {
     constexpr int kBatch = norm_batch<GT>(KU);
     __shared__ double smem[kWarps];
     __shared__ bool last;
     agg::griddep_launch_dependents();
     agg::griddep_wait();
-    const int lane = threadIdx.x & 31, base = (threadIdx.x >> 5) * kWarpElems;
-    const long long* rec = a.src.recs + blockIdx.x * static_cast<long long>(a.src.stride);
+    const int lane = threadIdx.x & 31;
+    const int base = ((threadIdx.x + (blockIdx.x & 1) * kNormThreads) >> 5) * kWarpElems;
+    const long long* rec = a.src.recs + (blockIdx.x >> 1) * static_cast<long long>(a.src.stride);
     const long long cf = __ldg(rec + kNormCount);
     const int count = static_cast<int>(cf & 0xffffffffLL);
     float* staged = a.src.staged ? a.src.staged + __ldg(rec + kNormPosition) : nullptr;
+    // the pointers with the count, not behind the branch on it: one trip to memory before the gradients' own
+    long long from[KU];
+    if constexpr (!MANY) pointers_of<KU>(a.src, rec + kNormGrads, 0, from);
+    // and the record of a CTA of the next wave to the L2, out of which the gradients have streamed it
+    if ((blockIdx.x >> 1) + kAhead < a.src.records && threadIdx.x < a.src.stride / 4)
+        agg::prefetch_l2(rec + kAhead * a.src.stride + 4 * threadIdx.x);
     double sq = 0.0;
     if (cf >> 32 & kGradsAligned && base + (kBatch - 1) * kSpan + kWarpElems <= count) {
         if constexpr (MANY) {
@@ -792,7 +809,7 @@ __global__ void __launch_bounds__(kThreads, KU * sizeof(GT) > 16 || MANY ? 2 : 3
             GradRaw<GT> raw[kBatch][KU];
 #pragma unroll
             for (int e = 0; e < kBatch; ++e)
-                load_round<GT, KU, true>(a.src, rec + kNormGrads, 0, base + e * kSpan, lane, kWarpElems, raw[e]);
+                load_round<GT, KU, true>(a.src, from, 0, base + e * kSpan, lane, kWarpElems, raw[e]);
 #pragma unroll
             for (int e = 0; e < kBatch; ++e) {
                 Pair g[4];
@@ -823,7 +840,7 @@ __global__ void __launch_bounds__(kThreads, KU * sizeof(GT) > 16 || MANY ? 2 : 3
     if (!last) return;
     __threadfence();
     double acc = 0.0;
-    for (unsigned int i = threadIdx.x; i < gridDim.x; i += kThreads) acc += __ldcg(a.partials + i);
+    for (unsigned int i = threadIdx.x; i < gridDim.x; i += kNormThreads) acc += __ldcg(a.partials + i);
     const double total = agg::block_sum(acc, smem);
     if (threadIdx.x != 0) return;
     *a.ticket = 0u;

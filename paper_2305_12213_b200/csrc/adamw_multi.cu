@@ -30,7 +30,7 @@ bool count_spans(const int64_t* sizes, int32_t T, long long* spans) {
     for (int32_t t = 0; t < T; ++t) {
         if (sizes[t] < 0) return false;
         sum += sizes[t] / kSpan + (sizes[t] % kSpan != 0);
-        if (sum > 0x7fffffffLL) return false;
+        if (sum > 0x3fffffffLL) return false;
     }
     *spans = sum;
     return true;
@@ -78,7 +78,7 @@ bool make_layout(int32_t K, db_dtype dt, bool state8, const int64_t* sizes, int3
     L->step = L->norm = Records{};
     if (step) L->step = records_of(sizes, T, state8 ? run_of(spans) : kSpan, kRecGrads + K, &L->end);
     if (norm) L->norm = records_of(sizes, T, dt == DB_F32 ? norm_run<float>(K) : norm_run<__nv_bfloat16>(K), kNormGrads + K, &L->end);
-    const size_t n = static_cast<size_t>(std::max<long long>(1, std::max(L->step.count, L->norm.count)));
+    const size_t n = static_cast<size_t>(std::max<long long>(1, std::max(L->step.count, 2 * L->norm.count)));
     L->partials = L->end;
     L->sums = L->partials + round256(8 * n);
     L->scalars = L->sums + round256(8 * (n / kFoldPer + 1));
@@ -209,18 +209,20 @@ db_status launch_norm(const Layout& L, char* table, db_dtype dt, int workers, So
     NormArgs a{};
     a.src = src;
     a.src.recs = reinterpret_cast<const long long*>(table + L.norm.at);
+    a.src.records = L.norm.count;
     a.src.stride = L.norm.stride;
     a.partials = reinterpret_cast<double*>(table + L.partials);
     a.ticket = reinterpret_cast<unsigned int*>(table + L.scalars);
     a.norm = norm;
     a.factor = factor;
     a.max_norm = max_norm;
-    const bool last = L.norm.count <= 4 * sm_count();
+    const long long grid = 2 * L.norm.count;
+    const bool last = grid <= 8 * sm_count();
     // by the plan's workers, not the call's: the records are made for that kernel
     const NormFn fn = dt == DB_F32 ? (last ? pick_norm<float, true>(workers) : pick_norm<float, false>(workers))
                                    : (last ? pick_norm<__nv_bfloat16, true>(workers) : pick_norm<__nv_bfloat16, false>(workers));
-    DB_CUDA_TRY(launch(fn, L.norm.count, kThreads, 0, stream, a));
-    return last ? DB_OK : launch_fold(L, table, L.norm.count, norm, factor, max_norm, stream);
+    DB_CUDA_TRY(launch(fn, grid, kNormThreads, 0, stream, a));
+    return last ? DB_OK : launch_fold(L, table, grid, norm, factor, max_norm, stream);
 }
 
 using StepFn = void (*)(const StepArgs);
