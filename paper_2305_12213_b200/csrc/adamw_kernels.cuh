@@ -555,16 +555,18 @@ __host__ __device__ constexpr int stage_bytes(int workers, int grad_size) {
     return kStageGrads + workers * grad_size * kWarpElems;
 }
 
-// One worker's 256 gradients to shared memory, in order, by the widest copy that the address allows.
+// One worker's 256 gradients to shared memory, in order; off the 16-byte grid by the widest copy that the address allows.
 template <typename GT>
-__device__ __forceinline__ void copy_block(bool aligned, uint32_t to, const GT* from, int lane) {
+__device__ __forceinline__ void copy_block(uint32_t to, const GT* from, int lane) {
+    constexpr int kBytes = static_cast<int>(sizeof(GT)) * kWarpElems;
+#pragma unroll
+    for (int i = 0; i < kBytes; i += 512) copy_async<16>(to + i + 16 * lane, reinterpret_cast<const char*>(from) + i + 16 * lane);
+}
+template <typename GT>
+__device__ __forceinline__ void copy_block_unaligned(uint32_t to, const GT* from, int lane) {
     constexpr int kBytes = static_cast<int>(sizeof(GT)) * kWarpElems;
     const char* src = reinterpret_cast<const char*>(from);
-    const uint32_t low = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(src));
-    if (aligned) {
-#pragma unroll
-        for (int i = 0; i < kBytes; i += 512) copy_async<16>(to + i + 16 * lane, src + i + 16 * lane);
-    } else if ((low & 3u) == 0u) {
+    if ((reinterpret_cast<uintptr_t>(src) & 3u) == 0u) {
 #pragma unroll
         for (int i = 0; i < kBytes; i += 128) copy_async<4>(to + i + 4 * lane, src + i + 4 * lane);
     } else {                                  // bf16 at an odd element
@@ -576,48 +578,52 @@ __device__ __forceinline__ void copy_block(bool aligned, uint32_t to, const GT* 
     }
 }
 
-__device__ __forceinline__ void read_pairs(uint32_t from, Pair (&x)[4]) {
-    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(x[0]), "=l"(x[1]) : "r"(from) : "memory");
-    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(x[2]), "=l"(x[3]) : "r"(from + 16) : "memory");
+// A lane's elements of a stage.
+__device__ __forceinline__ void read_pairs(const unsigned char* from, int lane, Pair (&x)[4]) {
+    const ulonglong2* q = reinterpret_cast<const ulonglong2*>(from) + 2 * lane;
+    const ulonglong2 a = q[0], b = q[1];
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
 }
-__device__ __forceinline__ void read_words(uint32_t from, uint32_t (&x)[2]) {
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(from) : "memory");
+__device__ __forceinline__ void read_codes(const unsigned char* from, int lane, uint32_t (&x)[2]) {
+    const uint2 r = reinterpret_cast<const uint2*>(from)[lane];
+    x[0] = r.x; x[1] = r.y;
 }
-__device__ __forceinline__ void read_floats(uint32_t from, float (&x)[2]) {
-    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(x[0]), "=f"(x[1]) : "r"(from) : "memory");
-}
-template <typename GT> __device__ __forceinline__ void read_grads(uint32_t from, int lane, Pair (&x)[4]);
-template <> __device__ __forceinline__ void read_grads<float>(uint32_t from, int lane, Pair (&x)[4]) { read_pairs(from + 32 * lane, x); }
-template <> __device__ __forceinline__ void read_grads<__nv_bfloat16>(uint32_t from, int lane, Pair (&x)[4]) {
-    uint32_t r[4];
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(from + 16 * lane) : "memory");
+template <typename GT> __device__ __forceinline__ void read_grads(const unsigned char* from, int lane, Pair (&x)[4]);
+template <> __device__ __forceinline__ void read_grads<float>(const unsigned char* from, int lane, Pair (&x)[4]) { read_pairs(from, lane, x); }
+template <> __device__ __forceinline__ void read_grads<__nv_bfloat16>(const unsigned char* from, int lane, Pair (&x)[4]) {
+    const uint4 r = reinterpret_cast<const uint4*>(from)[lane];
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = pack(__uint_as_float(r[i] << 16), __uint_as_float(r[i] & 0xffff0000u));
+    for (int i = 0; i < 4; ++i) x[i] = pack(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
+
+// Whether an item has a gradient at place j: the kernel for KI workers is taken for K in (KI / 2, KI].
+template <int KI, bool MANY>
+__device__ __forceinline__ bool has(int j, int chunk, int K) { return MANY ? chunk * KI + j < K : j <= KI / 2 || j < K; }
 
 // The aggregate's partial sums (worker k in sum k mod 4) with an item's gradients added; KI == 1: one worker, whose
 // weight is 1.
 template <typename GT, int KI, bool MANY, int SUMS>
-__device__ __forceinline__ void add_item(const Source& s, uint32_t from, int chunk, int K, int lane, Pair (&sum)[SUMS][4]) {
+__device__ __forceinline__ void add_item(const Source& s, const unsigned char* from, int chunk, int K, int lane, Pair (&sum)[SUMS][4]) {
 #pragma unroll
     for (int j = 0; j < KI; ++j) {
-        const int k = MANY ? chunk * KI + j : j;
-        Pair x[4];
-        read_grads<GT>(from + j * static_cast<int>(sizeof(GT)) * kWarpElems, lane, x);       // beyond K: not used
-        if (KI == 1) {
+        if (!MANY && j < SUMS) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[0][i] = x[i];
-        } else {
-            const Pair w = s.lambda[k < K ? k : 0];
+            for (int i = 0; i < 4; ++i) sum[j][i] = both(-0.0f);                             // adds nothing to anything
+        }
+        if (has<KI, MANY>(j, chunk, K)) {
+            Pair x[4];
+            read_grads<GT>(from + j * static_cast<int>(sizeof(GT)) * kWarpElems, lane, x);
+            const Pair w = KI == 1 ? 0ull : s.lambda[MANY ? chunk * KI + j : j];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const Pair y = k < K ? mul(w, x[i]) : both(-0.0f);
+                const Pair y = KI == 1 ? x[i] : mul(w, x[i]);
                 sum[j % SUMS][i] = !MANY && j < SUMS ? y : add(y, sum[j % SUMS][i], s.one);
             }
         }
     }
 }
+
 // One kernel for each number KI of gradients in an item (1, 2, 4 or 8; MANY: more workers than that).  In flight
 // for each SM, with two CTAs on it: (stages - 1) * 16 items, 70 to 100 KB.
 __host__ __device__ constexpr int ring_stages(int workers, int grad_size) {
@@ -648,7 +654,8 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
     const int mine = (count - warp * kWarpElems + kSpan - 1) / kSpan;                        // blocks that begin in the run
     int whole = cf >> 32 & kStateAligned ? (count - (warp + 1) * kWarpElems + kSpan) / kSpan : 0;
     if (whole < 0) whole = 0;
-    const uint32_t ring = shared_address(smem) + warp * (kStages * kStage);
+    const unsigned char* slots = smem + warp * (kStages * kStage);
+    const uint32_t ring = shared_address(slots);
     const char* params = reinterpret_cast<const char*>(__ldg(rec + kRecParam));
     const char* first = reinterpret_cast<const char*>(__ldg(rec + kRecFirst));
     const char* second = reinterpret_cast<const char*>(__ldg(rec + kRecSecond));
@@ -659,9 +666,12 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
     const char* my_params = params + 16 * lane;
     const char* my_codes = (lane < 16 ? first : second) + 16 * (lane & 15);
     const char* my_scale = lane == 0 ? first_scale : second_scale;
-    const char* only = KI == 1 ? (CLIP && a.src.staged ? reinterpret_cast<const char*>(a.src.staged + position)
-                                                        : reinterpret_cast<const char*>(__ldg(rec + kRecGrads + a.src.worker[0])))
-                               : nullptr;
+    // The gradients' pointers, worker by worker in the lanes: a shuffle fetches one, where a load for each copy would
+    // put its latency into every item.
+    const int other = lane + 32;
+    long long from_low = lane < K ? __ldg(rec + kRecGrads + a.src.worker[lane]) : 0;
+    const long long from_high = MANY && other < K ? __ldg(rec + kRecGrads + a.src.worker[other]) : 0;
+    if (CLIP && a.src.staged) from_low = reinterpret_cast<long long>(a.src.staged + position);
 
     auto copy_item = [&](int offset, int chunk, uint32_t to) {
         if (!MANY || chunk == 0) {
@@ -670,19 +680,25 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
             copy_async<16>(to + kStageCodes + 16 * lane, my_codes + offset);
             if (lane < 2) copy_async<4>(to + kStageScales + 4 * lane, my_scale + offset / (kWarpElems / 4));
         }
-#pragma unroll
-        for (int j = 0; j < KI; ++j) {
+        const uint32_t grads_to = to + kStageGrads;
+        auto pointer = [&](int j) {
             const int k = MANY ? chunk * KI + j : j;
-            if (KI == 1 || k < K) {
-                const char* g = KI == 1 ? only : reinterpret_cast<const char*>(__ldg(rec + kRecGrads + a.src.worker[k]));
-                copy_block<GT>(grads_aligned, to + kStageGrads + j * kGrad * kWarpElems,
-                               reinterpret_cast<const GT*>(g) + offset, lane);
-            }
+            return reinterpret_cast<const GT*>(__shfl_sync(0xffffffffu, MANY && k >= 32 ? from_high : from_low, k & 31)) + offset;
+        };
+        if (grads_aligned) {
+#pragma unroll
+            for (int j = 0; j < KI; ++j)
+                if (has<KI, MANY>(j, chunk, K)) copy_block(grads_to + j * kGrad * kWarpElems, pointer(j), lane);
+        } else {
+#pragma unroll 1
+            for (int j = 0; j < KI && (MANY ? chunk * KI + j : j) < K; ++j)
+                copy_block_unaligned(grads_to + j * kGrad * kWarpElems, pointer(j), lane);
         }
     };
 
     int next_offset = warp * kWarpElems, next_chunk = 0, left = whole * chunks;              // the item to copy
-    uint32_t to = ring, from = ring;
+    uint32_t to = ring;
+    const unsigned char* from = slots;
     auto issue = [&]() {
         if (left > 0) {
             copy_item(next_offset, next_chunk, to);
@@ -705,7 +721,7 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
     for (int block = 0; block < whole; ++block, offset += kSpan) {
         Pair sum[kSums][4], p[4];
         uint32_t cm[2], cu[2];
-        float scales[2];
+        float2 scales;
         if (MANY) {
 #pragma unroll
             for (int j = 0; j < kSums; ++j)
@@ -718,20 +734,20 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
             copy_wait<kStages - 1>();
             __syncwarp();
             if (!MANY || chunk == 0) {
-                read_pairs(from + 32 * lane, p);
-                read_words(from + kStageCodes + 8 * lane, cm);
-                read_words(from + kStageCodes + kWarpElems + 8 * lane, cu);
-                read_floats(from + kStageScales, scales);
+                read_pairs(from, lane, p);
+                read_codes(from + kStageCodes, lane, cm);
+                read_codes(from + kStageCodes + kWarpElems, lane, cu);
+                scales = *reinterpret_cast<const float2*>(from + kStageScales);
             }
             add_item<GT, KI, MANY>(a.src, from + kStageGrads, chunk, K, lane, sum);
             __syncwarp();                    // everybody has read the slot before anybody's copy overwrites it
-            from = from == ring + (kStages - 1) * kStage ? ring : from + kStage;
+            from = from == slots + (kStages - 1) * kStage ? slots : from + kStage;
         }
         join_sums<kSums>(sum, a.src.one);
         if (NORM) sq += sum_squares(sum[0]);
         Pair m[4], u[4];
-        decode(cm, scales[0], m);
-        decode(cu, scales[1], u);
+        decode(cm, scales.x, m);
+        decode(cu, scales.y, u);
         update<CLIP>(a, factor, decay, sum[0], p, m, u);
         store_f32<true>(reinterpret_cast<float*>(const_cast<char*>(params)) + offset, lane, kWarpElems, p);
         if (copy) store_copy<true>(copy, offset, lane, kWarpElems, p);
