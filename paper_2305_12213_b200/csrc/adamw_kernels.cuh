@@ -36,6 +36,8 @@ enum RecordWord {
 enum NormRecordWord { kNormCount = 0, kNormPosition, kNormGrads };
 constexpr int kStateAligned = 1, kGradsAligned = 2;              // flags: buffers aligned to a lane's vector
 
+constexpr long long kAhead = 512;            // records
+
 struct Source {                  // where the weighted gradient comes from
     const long long* recs;       // records, `stride` words apart
     long long records;
@@ -510,13 +512,26 @@ __device__ __noinline__ double step_block_slow(const StepArgs& a, const long lon
     return sq;
 }
 
+// A step's CTAs take the records in order, after a norm kernel in the opposite one: what that read or left last is
+// still in the L2.
+template <bool CLIP>
+__device__ __forceinline__ const long long* record_of(const Source& s) {
+    return s.recs + (CLIP ? s.records - 1 - blockIdx.x : blockIdx.x) * static_cast<long long>(s.stride);
+}
+// Asks the L2 for the record of a CTA of the next wave; the moments and gradients have streamed it out.
+template <bool CLIP>
+__device__ __forceinline__ void prefetch_record(const Source& s, const long long* rec) {
+    if (blockIdx.x + kAhead < s.records && threadIdx.x < s.stride / 4)
+        agg::prefetch_l2(rec + (CLIP ? -kAhead : kAhead) * s.stride + 4 * threadIdx.x);
+}
+
 // 32-bit moments: one CTA per record, one block per warp.
 template <typename GT, int KU, bool MANY, bool CLIP, bool NORM>
 __global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 4) adamw_kernel(const __grid_constant__ StepArgs a) {
     agg::griddep_launch_dependents();
     agg::griddep_wait();
     const int lane = threadIdx.x & 31, offset = (threadIdx.x >> 5) * kWarpElems;
-    const long long* rec = a.src.recs + blockIdx.x * static_cast<long long>(a.src.stride);
+    const long long* rec = record_of<CLIP>(a.src);
     const long long cf = __ldg(rec + kRecCount);
     const int n = static_cast<int>(cf & 0xffffffffLL) - offset, flags = static_cast<int>(cf >> 32);
     const float factor = CLIP ? __ldcg(a.factor) : 1.0f;
@@ -642,12 +657,13 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
     agg::griddep_launch_dependents();
     agg::griddep_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long* rec = a.src.recs + blockIdx.x * static_cast<long long>(a.src.stride);
+    const long long* rec = record_of<CLIP>(a.src);
     const long long cf = __ldg(rec + kRecCount);
     const int count = static_cast<int>(cf & 0xffffffffLL);
     const bool grads_aligned = cf >> 32 & kGradsAligned || (CLIP && a.src.staged);
     const float factor = CLIP ? __ldcg(a.factor) : 1.0f;
     const int K = a.src.K, chunks = MANY ? (K + KI - 1) / KI : 1;
+    prefetch_record<CLIP>(a.src, rec);
     double sq = 0.0;
 
     // blocks warp, warp + 8, ... of the run; whole ones of aligned tensors take the staged path
@@ -784,8 +800,6 @@ __device__ __noinline__ double norm_block_slow(const Source& s, const long long*
     if (staged) store_f32<false>(staged, lane, n, g);
     return sum_squares(g);
 }
-
-constexpr long long kAhead = 512;            // records
 
 // Norm and clipping factor from the sum of squares: max_norm / norm where the norm is larger than max_norm, else 1
 // (a NaN norm does not clip).
