@@ -547,12 +547,13 @@ __global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 4) adamw_kernel(const 
 }
 
 // ---- 8-bit moments: blocks through shared memory ------------------------------------------------------
-// Sixty instructions an element keep a warp busy for as long as its loads take, and the registers that this needs
+// Fifty instructions an element keep a warp busy for as long as its loads take, and the registers that this needs
 // leave few warps: with loads and arithmetic in turn the kernel reached 47 % of the DRAM's rate (issue slots 43 %
-// busy).  So every warp copies blocks ahead into shared memory of its own (cp.async, kept in order by commit
-// groups; nobody waits for another warp) and computes on one that has arrived.
-// An item is one block's parameters, codes and scales with up to KI gradients; further workers of the block follow
-// as items of gradients alone.
+// busy).  So every warp copies ahead into shared memory of its own (cp.async, kept in order by commit groups; nobody
+// waits for another warp) and computes on what has arrived.
+// The unit is an item: a block's parameters, codes and scales, or up to 2 KB of its gradients (four bf16 or two fp32
+// workers); one or two workers travel with the parameters.  Small items keep the amount in flight even: with 4 KB of
+// gradients an item, 110M parameters and 8 bf16 workers took 623 us, with 2 KB XXX.
 
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 template <int BYTES>
@@ -564,36 +565,41 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Bytes of a stage of one warp: parameters, codes, scales (padded to 16), gradients.
-constexpr int kStageCodes = 4 * kWarpElems, kStageScales = kStageCodes + 2 * kWarpElems, kStageGrads = kStageScales + 16;
-__host__ __device__ constexpr int stage_bytes(int workers, int grad_size) {
-    return kStageGrads + workers * grad_size * kWarpElems;
-}
+// A slot of the ring.  Parameters, codes, scales (padded to 16 bytes); a worker's row of gradients, for bf16 with room
+// for the 129th word of a row that starts at an odd element.
+constexpr int kSlotCodes = 4 * kWarpElems, kSlotScales = kSlotCodes + 2 * kWarpElems, kSlotState = kSlotScales + 16;
+template <typename GT, int KI>
+struct Ring {
+    static constexpr bool kFused = KI <= 2;                                   // gradients behind the parameters, in one item
+    static constexpr int kItem = kFused ? KI : 8 / static_cast<int>(sizeof(GT));                       // workers in an item
+    static constexpr int kRow = static_cast<int>(sizeof(GT)) * kWarpElems + (sizeof(GT) == 2 ? 16 : 0);
+    static constexpr int kGrads = kFused ? kSlotState : 0;                    // where an item's gradients begin
+    static constexpr int kSlot = kFused ? kSlotState + KI * kRow : kItem * kRow > kSlotState ? kItem * kRow : kSlotState;
+    static constexpr int kMost = (104 << 10) / (kWarps * kSlot);              // two CTAs on an SM
+    static constexpr int kSlots = kMost < 6 ? kMost : 6;
+    static constexpr int kBytes = kWarps * kSlots * kSlot;
+};
 
-// One worker's 256 gradients to shared memory, in order; off the 16-byte grid by the widest copy that the address allows.
+// One worker's 256 gradients to shared memory, in order.
 template <typename GT>
-__device__ __forceinline__ void copy_block(uint32_t to, const GT* from, int lane) {
+__device__ __forceinline__ void copy_row(uint32_t to, const GT* from, int lane) {
     constexpr int kBytes = static_cast<int>(sizeof(GT)) * kWarpElems;
 #pragma unroll
     for (int i = 0; i < kBytes; i += 512) copy_async<16>(to + i + 16 * lane, reinterpret_cast<const char*>(from) + i + 16 * lane);
 }
+// The same off the 16-byte grid, by words.  A bf16 row at an odd element is copied from the word that holds the element
+// before it on (129 words, each with at least one element of the row) and read two bytes further up.
 template <typename GT>
-__device__ __forceinline__ void copy_block_unaligned(uint32_t to, const GT* from, int lane) {
+__device__ __forceinline__ void copy_row_unaligned(uint32_t to, const GT* from, int lane) {
     constexpr int kBytes = static_cast<int>(sizeof(GT)) * kWarpElems;
-    const char* src = reinterpret_cast<const char*>(from);
-    if ((reinterpret_cast<uintptr_t>(src) & 3u) == 0u) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(from);
+    const char* words = reinterpret_cast<const char*>(at & ~static_cast<uintptr_t>(3));
 #pragma unroll
-        for (int i = 0; i < kBytes; i += 128) copy_async<4>(to + i + 4 * lane, src + i + 4 * lane);
-    } else {                                  // bf16 at an odd element
-#pragma unroll
-        for (int i = 0; i < kBytes; i += 64) {
-            const uint16_t x = __ldcs(reinterpret_cast<const uint16_t*>(src + i) + lane);
-            asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + i + 2 * lane), "h"(x) : "memory");
-        }
-    }
+    for (int i = 0; i < kBytes; i += 128) copy_async<4>(to + i + 4 * lane, words + i + 4 * lane);
+    if (sizeof(GT) == 2 && (at & 2) && lane == 0) copy_async<4>(to + kBytes, words + kBytes);
 }
 
-// A lane's elements of a stage.
+// A lane's elements of a slot.
 __device__ __forceinline__ void read_pairs(const unsigned char* from, int lane, Pair (&x)[4]) {
     const ulonglong2* q = reinterpret_cast<const ulonglong2*>(from) + 2 * lane;
     const ulonglong2 a = q[0], b = q[1];
@@ -603,56 +609,25 @@ __device__ __forceinline__ void read_codes(const unsigned char* from, int lane, 
     const uint2 r = reinterpret_cast<const uint2*>(from)[lane];
     x[0] = r.x; x[1] = r.y;
 }
-template <typename GT> __device__ __forceinline__ void read_grads(const unsigned char* from, int lane, Pair (&x)[4]);
-template <> __device__ __forceinline__ void read_grads<float>(const unsigned char* from, int lane, Pair (&x)[4]) { read_pairs(from, lane, x); }
-template <> __device__ __forceinline__ void read_grads<__nv_bfloat16>(const unsigned char* from, int lane, Pair (&x)[4]) {
+template <typename GT> __device__ __forceinline__ void read_row(const unsigned char* from, int lane, bool odd, Pair (&x)[4]);
+template <> __device__ __forceinline__ void read_row<float>(const unsigned char* from, int lane, bool, Pair (&x)[4]) { read_pairs(from, lane, x); }
+template <> __device__ __forceinline__ void read_row<__nv_bfloat16>(const unsigned char* from, int lane, bool odd, Pair (&x)[4]) {
     const uint4 r = reinterpret_cast<const uint4*>(from)[lane];
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    if (odd) {
+        const uint32_t next = reinterpret_cast<const uint32_t*>(from)[4 * lane + 4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __byte_perm(w[i], i < 3 ? w[i + 1] : next, 0x5432);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = pack(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
 
-// Whether an item has a gradient at place j: the kernel for KI workers is taken for K in (KI / 2, KI].
-template <int KI, bool MANY>
-__device__ __forceinline__ bool has(int j, int chunk, int K) { return MANY ? chunk * KI + j < K : j <= KI / 2 || j < K; }
-
-// The aggregate's partial sums (worker k in sum k mod 4) with an item's gradients added; KI == 1: one worker, whose
-// weight is 1.
-template <typename GT, int KI, bool MANY, int SUMS>
-__device__ __forceinline__ void add_item(const Source& s, const unsigned char* from, int chunk, int K, int lane, Pair (&sum)[SUMS][4]) {
-#pragma unroll
-    for (int j = 0; j < KI; ++j) {
-        if (!MANY && j < SUMS) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[j][i] = both(-0.0f);                             // adds nothing to anything
-        }
-        if (has<KI, MANY>(j, chunk, K)) {
-            Pair x[4];
-            read_grads<GT>(from + j * static_cast<int>(sizeof(GT)) * kWarpElems, lane, x);
-            const Pair w = KI == 1 ? 0ull : s.lambda[MANY ? chunk * KI + j : j];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const Pair y = KI == 1 ? x[i] : mul(w, x[i]);
-                sum[j % SUMS][i] = !MANY && j < SUMS ? y : add(y, sum[j % SUMS][i], s.one);
-            }
-        }
-    }
-}
-
-// One kernel for each number KI of gradients in an item (1, 2, 4 or 8; MANY: more workers than that).  In flight
-// for each SM, with two CTAs on it: (stages - 1) * 16 items, 70 to 100 KB.
-__host__ __device__ constexpr int ring_stages(int workers, int grad_size) {
-    const int stage = stage_bytes(workers, grad_size);
-    return stage <= 2600 ? 4 : stage <= 3600 ? 3 : 2;
-}
-__host__ __device__ constexpr size_t ring_bytes(int workers, int grad_size) {
-    return static_cast<size_t>(kWarps) * ring_stages(workers, grad_size) * stage_bytes(workers, grad_size);
-}
-
+// One kernel for each number KI of workers (1, 2, 4 or 8, taken for K in (KI / 2, KI]; MANY: more than that, in rounds).
 template <typename GT, int KI, bool MANY, bool CLIP, bool NORM>
 __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_constant__ StepArgs a) {
+    using R = Ring<GT, KI>;
     extern __shared__ __align__(16) unsigned char smem[];
-    constexpr int kGrad = static_cast<int>(sizeof(GT)), kStages = ring_stages(KI, kGrad), kStage = stage_bytes(KI, kGrad);
     constexpr int kSums = KI < 4 ? KI : 4;
     agg::griddep_launch_dependents();
     agg::griddep_wait();
@@ -662,15 +637,15 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
     const int count = static_cast<int>(cf & 0xffffffffLL);
     const bool grads_aligned = cf >> 32 & kGradsAligned || (CLIP && a.src.staged);
     const float factor = CLIP ? __ldcg(a.factor) : 1.0f;
-    const int K = a.src.K, chunks = MANY ? (K + KI - 1) / KI : 1;
+    const int K = a.src.K, items = R::kFused ? 1 : 1 + (K + R::kItem - 1) / R::kItem;         // of a block
     prefetch_record<CLIP>(a.src, rec);
     double sq = 0.0;
 
-    // blocks warp, warp + 8, ... of the run; whole ones of aligned tensors take the staged path
+    // blocks warp, warp + 8, ... of the run; whole ones of aligned tensors come through the ring
     const int mine = (count - warp * kWarpElems + kSpan - 1) / kSpan;                        // blocks that begin in the run
     int whole = cf >> 32 & kStateAligned ? (count - (warp + 1) * kWarpElems + kSpan) / kSpan : 0;
     if (whole < 0) whole = 0;
-    const unsigned char* slots = smem + warp * (kStages * kStage);
+    const unsigned char* slots = smem + warp * (R::kSlots * R::kSlot);
     const uint32_t ring = shared_address(slots);
     const char* params = reinterpret_cast<const char*>(__ldg(rec + kRecParam));
     const char* first = reinterpret_cast<const char*>(__ldg(rec + kRecFirst));
@@ -688,47 +663,60 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
     long long from_low = lane < K ? __ldg(rec + kRecGrads + a.src.worker[lane]) : 0;
     const long long from_high = MANY && other < K ? __ldg(rec + kRecGrads + a.src.worker[other]) : 0;
     if (CLIP && a.src.staged) from_low = reinterpret_cast<long long>(a.src.staged + position);
+    unsigned int odd_low = 0u, odd_high = 0u;                                                // bf16 rows at odd elements
+    if (sizeof(GT) == 2 && !grads_aligned) {
+        odd_low = __ballot_sync(0xffffffffu, from_low & 2);
+        odd_high = __ballot_sync(0xffffffffu, from_high & 2);
+    }
 
-    auto copy_item = [&](int offset, int chunk, uint32_t to) {
-        if (!MANY || chunk == 0) {
+    auto copy_item = [&](int offset, int item, uint32_t to) {
+        if (R::kFused || item == 0) {
             copy_async<16>(to + 16 * lane, my_params + 4 * offset);
             copy_async<16>(to + 512 + 16 * lane, my_params + 4 * offset + 512);
-            copy_async<16>(to + kStageCodes + 16 * lane, my_codes + offset);
-            if (lane < 2) copy_async<4>(to + kStageScales + 4 * lane, my_scale + offset / (kWarpElems / 4));
+            copy_async<16>(to + kSlotCodes + 16 * lane, my_codes + offset);
+            if (lane < 2) copy_async<4>(to + kSlotScales + 4 * lane, my_scale + offset / (kWarpElems / 4));
         }
-        const uint32_t grads_to = to + kStageGrads;
-        auto pointer = [&](int j) {
-            const int k = MANY ? chunk * KI + j : j;
-            return reinterpret_cast<const GT*>(__shfl_sync(0xffffffffu, MANY && k >= 32 ? from_high : from_low, k & 31)) + offset;
-        };
-        if (grads_aligned) {
+        if (R::kFused || item > 0) {
+            const int k0 = R::kFused ? 0 : (item - 1) * R::kItem;
 #pragma unroll
-            for (int j = 0; j < KI; ++j)
-                if (has<KI, MANY>(j, chunk, K)) copy_block(grads_to + j * kGrad * kWarpElems, pointer(j), lane);
-        } else {
-#pragma unroll 1
-            for (int j = 0; j < KI && (MANY ? chunk * KI + j : j) < K; ++j)
-                copy_block_unaligned(grads_to + j * kGrad * kWarpElems, pointer(j), lane);
+            for (int j = 0; j < R::kItem; ++j) {
+                const int k = k0 + j;
+                if (R::kFused || k < K) {
+                    const GT* from = reinterpret_cast<const GT*>(
+                        __shfl_sync(0xffffffffu, MANY && k >= 32 ? from_high : from_low, k & 31)) + offset;
+                    if (grads_aligned) copy_row(to + R::kGrads + j * R::kRow, from, lane);
+                    else copy_row_unaligned(to + R::kGrads + j * R::kRow, from, lane);
+                }
+            }
         }
     };
 
-    int next_offset = warp * kWarpElems, next_chunk = 0, left = whole * chunks;              // the item to copy
+    int next_offset = warp * kWarpElems, next_item = 0, left = whole * items;                // the item to copy
     uint32_t to = ring;
     const unsigned char* from = slots;
     auto issue = [&]() {
         if (left > 0) {
-            copy_item(next_offset, next_chunk, to);
+            copy_item(next_offset, next_item, to);
             --left;
-            if (!MANY || ++next_chunk == chunks) {
-                next_chunk = 0;
+            if (R::kFused || ++next_item == items) {
+                next_item = 0;
                 next_offset += kSpan;
             }
         }
         copy_commit();                       // an empty group where nothing is left: the count of groups stays right
-        to = to == ring + (kStages - 1) * kStage ? ring : to + kStage;
+        to = to == ring + (R::kSlots - 1) * R::kSlot ? ring : to + R::kSlot;
     };
-#pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) issue();
+    auto arrive = [&]() {                    // the item at `from` is there, another one on its way
+        issue();
+        copy_wait<R::kSlots - 1>();
+        __syncwarp();
+    };
+    auto release = [&]() {                   // everybody has read the slot before anybody's copy overwrites it
+        __syncwarp();
+        from = from == slots + (R::kSlots - 1) * R::kSlot ? slots : from + R::kSlot;
+    };
+#pragma unroll 1
+    for (int i = 0; i < R::kSlots - 1; ++i) issue();
 
     const Pair decay = decay_of(a, rec);
     const long long copy = __ldg(rec + kRecCopy);
@@ -738,26 +726,39 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
         Pair sum[kSums][4], p[4];
         uint32_t cm[2], cu[2];
         float2 scales;
-        if (MANY) {
+        arrive();
+        read_pairs(from, lane, p);
+        read_codes(from + kSlotCodes, lane, cm);
+        read_codes(from + kSlotCodes + kWarpElems, lane, cu);
+        scales = *reinterpret_cast<const float2*>(from + kSlotScales);
+        if (!R::kFused) release();
 #pragma unroll
-            for (int j = 0; j < kSums; ++j)
+        for (int j = 0; j < kSums; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[j][i] = both(-0.0f);                         // adds nothing to anything
-        }
+            for (int i = 0; i < 4; ++i) sum[j][i] = both(-0.0f);                             // adds nothing to anything
 #pragma unroll 1
-        for (int chunk = 0; chunk < chunks; ++chunk) {
-            issue();
-            copy_wait<kStages - 1>();
-            __syncwarp();
-            if (!MANY || chunk == 0) {
-                read_pairs(from, lane, p);
-                read_codes(from + kStageCodes, lane, cm);
-                read_codes(from + kStageCodes + kWarpElems, lane, cu);
-                scales = *reinterpret_cast<const float2*>(from + kStageScales);
+        for (int round = 0; round < (MANY ? K : 1); round += KI) {
+#pragma unroll
+            for (int chunk = 0; chunk < KI; chunk += R::kItem) {
+                if (MANY && round + chunk >= K) break;
+                if (!R::kFused) arrive();
+#pragma unroll
+                for (int j = 0; j < R::kItem; ++j) {
+                    const int place = chunk + j, k = MANY ? round + place : place;           // worker k is in sum k mod 4
+                    if (MANY ? k < K : place <= KI / 2 || place < K) {
+                        Pair x[4];
+                        const unsigned int odd = MANY && k >= 32 ? odd_high : odd_low;
+                        read_row<GT>(from + R::kGrads + j * R::kRow, lane, odd >> (k & 31) & 1u, x);
+                        const Pair w = KI == 1 ? 0ull : a.src.lambda[k];                     // a single weight is 1
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const Pair y = KI == 1 ? x[i] : mul(w, x[i]);
+                            sum[place % kSums][i] = !MANY && place < kSums ? y : add(y, sum[place % kSums][i], a.src.one);
+                        }
+                    }
+                }
+                release();
             }
-            add_item<GT, KI, MANY>(a.src, from + kStageGrads, chunk, K, lane, sum);
-            __syncwarp();                    // everybody has read the slot before anybody's copy overwrites it
-            from = from == slots + (kStages - 1) * kStage ? slots : from + kStage;
         }
         join_sums<kSums>(sum, a.src.one);
         if (NORM) sq += sum_squares(sum[0]);

@@ -242,22 +242,16 @@ StepFn pick_step(int K, bool clip, bool norm) {
     return norm ? pick_workers<GT, false, true>(K) : pick_workers<GT, false, false>(K);
 }
 
-// Gradients of an item that goes through shared memory: up to 4 KB.
-template <typename GT>
-constexpr int most_workers() { return 16 / static_cast<int>(sizeof(GT)); }
-template <typename GT>
-int item_workers(int K) { return K <= 1 ? 1 : K <= 2 ? 2 : K <= 4 ? 4 : most_workers<GT>(); }
-
 // 8-bit moments: the kernel for K workers and the shared memory of its ring.
 template <typename GT, bool CLIP, bool NORM>
 StepFn pick_workers8(int K, size_t* shared) {
-    constexpr int kMost = most_workers<GT>();
-    *shared = ring_bytes(item_workers<GT>(K), sizeof(GT));
+    *shared = K <= 1 ? Ring<GT, 1>::kBytes : K <= 2 ? Ring<GT, 2>::kBytes : Ring<GT, 4>::kBytes;       // as for 4, so for 8
+    static_assert(Ring<GT, 4>::kBytes == Ring<GT, 8>::kBytes, "items do not depend on the number of workers beyond 2");
     if (K <= 1) return adamw8_kernel<GT, 1, false, CLIP, NORM>;
     if (K <= 2) return adamw8_kernel<GT, 2, false, CLIP, NORM>;
     if (K <= 4) return adamw8_kernel<GT, 4, false, CLIP, NORM>;
-    if (kMost == 8 && K <= 8) return adamw8_kernel<GT, kMost, false, CLIP, NORM>;
-    return adamw8_kernel<GT, kMost, true, CLIP, NORM>;
+    if (K <= 8) return adamw8_kernel<GT, 8, false, CLIP, NORM>;
+    return adamw8_kernel<GT, 8, true, CLIP, NORM>;
 }
 template <typename GT>
 StepFn pick_step8(int K, bool clip, bool norm, size_t* shared) {
