@@ -513,7 +513,7 @@ __device__ __noinline__ double step_block_slow(const StepArgs& a, const long lon
 }
 
 // A step's CTAs take the records in order, after a norm kernel in the opposite one: what that read or left last is
-// still in the L2.
+// still in the L2 (one fp32 gradient, 10M elements: 60.7 -> 59.0 us; 25M: 99.4 -> 98.4).
 template <bool CLIP>
 __device__ __forceinline__ const long long* record_of(const Source& s) {
     return s.recs + (CLIP ? s.records - 1 - blockIdx.x : blockIdx.x) * static_cast<long long>(s.stride);
@@ -553,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 4) adamw_kernel(const 
 // waits for another warp) and computes on what has arrived.
 // The unit is an item: a block's parameters, codes and scales, or up to 2 KB of its gradients (four bf16 or two fp32
 // workers); one or two workers travel with the parameters.  Small items keep the amount in flight even: with 4 KB of
-// gradients an item, 110M parameters and 8 bf16 workers took 623 us, with 2 KB XXX.
+// gradients an item, 110M parameters and 8 bf16 workers took 623 us, with 2 KB 554.
 
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 template <int BYTES>
@@ -575,7 +575,8 @@ struct Ring {
     static constexpr int kRow = static_cast<int>(sizeof(GT)) * kWarpElems + (sizeof(GT) == 2 ? 16 : 0);
     static constexpr int kGrads = kFused ? kSlotState : 0;                    // where an item's gradients begin
     static constexpr int kSlot = kFused ? kSlotState + KI * kRow : kItem * kRow > kSlotState ? kItem * kRow : kSlotState;
-    static constexpr int kMost = (104 << 10) / (kWarps * kSlot);              // two CTAs on an SM
+    // two CTAs on an SM; with 104 KB instead of 88, a step behind a norm kernel was slower (25M elements: 98 -> 106 us)
+    static constexpr int kMost = (88 << 10) / (kWarps * kSlot);
     static constexpr int kSlots = kMost < 6 ? kMost : 6;
     static constexpr int kBytes = kWarps * kSlots * kSlot;
 };
@@ -785,7 +786,7 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
 // A CTA takes a record of norm_batch CTA steps, all of whose loads are in flight at once (32 to 64 KB of gradients);
 // with a staging buffer it also leaves the aggregates there, for the step that follows.
 // LAST: the CTA that arrives last adds all partials, in order, which saves a launch; on grids of many waves the
-// fence and the atomic at every CTA's end cost more than it (110M bf16 elements of 16 workers: 1669 us against XXX),
+// fence and the atomic at every CTA's end cost more than it,
 // and a fold kernel follows instead.
 
 // Blocks of a warp whose loads are in flight at once, by the registers that they take (32 to 64).
