@@ -37,6 +37,7 @@ enum NormRecordWord { kNormCount = 0, kNormPosition, kNormGrads };
 constexpr int kStateAligned = 1, kGradsAligned = 2;              // flags: buffers aligned to a lane's vector
 
 constexpr long long kAhead = 512;            // records
+constexpr int kFoldInStep = 512;             // partials that a clipped step adds itself
 
 struct Source {                  // where the weighted gradient comes from
     const long long* recs;       // records, `stride` words apart
@@ -61,7 +62,12 @@ struct NormArgs {
 struct StepArgs {
     Source src;
     double* partials;            // norm partials (NORM only)
-    const float* factor;         // clipping factor in device memory (CLIP only)
+    // CLIP: the clipping factor in device memory; or, where partial_count > 0, the norm's partials, which every warp
+    // adds for itself (CTA 0 then writes the norm)
+    const float* factor;
+    int partial_count;
+    float max_norm;
+    float* norm;
     // pairs of fp32, both halves alike, as the packed arithmetic takes them
     unsigned long long beta1, one_minus_beta1, beta2, one_minus_beta2;
     unsigned long long minus_step_size;   // -lr / (1 - beta1^t)
@@ -142,24 +148,38 @@ __device__ __forceinline__ void store_f32(float* p, int lane, int n, const Pair 
     }
 }
 
-// Raw gradient vectors, widened only when they are used, so that several workers' loads are in flight at once.
+// How a lane reads its eight gradients of a block: a vector of consecutive ones (kVector); a whole block off the
+// vector grid, coalesced by words (kRows); element by element below n (kMasked).  kRows' and kMasked's fp32 lanes
+// have elements lane + 32 i; kRows' bf16 lanes have the pairs 64 i + 2 lane.
+enum Access { kVector, kRows, kMasked };
+
+// Raw gradients, widened only when they are used, so that several workers' loads are in flight at once.
 template <typename GT> struct GradRaw;
 template <> struct GradRaw<float> {
     Pair x[4];
-    template <bool ALIGNED>
-    __device__ __forceinline__ void load(const void* base, int lane, int n) {
-        load_f32<ALIGNED>(static_cast<const float*>(base), lane, n, x);
+    template <Access A>
+    __device__ __forceinline__ void load(const float* p, int lane, int n) {
+        load_f32<A == kVector>(p, lane, A == kMasked ? n : kWarpElems, x);
     }
+    template <Access A>
+    __device__ __forceinline__ void arrange(long long, int) {}
     __device__ __forceinline__ Pair get(int i) const { return x[i]; }
 };
 template <> struct GradRaw<__nv_bfloat16> {
-    uint32_t x[4];               // bf16 is the high half of a binary32: widening is a shift, exact
-    template <bool ALIGNED>
-    __device__ __forceinline__ void load(const void* base, int lane, int n) {
-        const uint16_t* p = static_cast<const uint16_t*>(base);
-        if (ALIGNED) {
+    uint32_t x[4], after;        // bf16 is the high half of a binary32: widening is a shift, exact
+    template <Access A>
+    __device__ __forceinline__ void load(const __nv_bfloat16* from, int lane, int n) {
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(from);
+        if (A == kVector) {
             const uint4 r = __ldcs(reinterpret_cast<const uint4*>(p + 8 * lane));
             x[0] = r.x; x[1] = r.y; x[2] = r.z; x[3] = r.w;
+        } else if (A == kRows) {
+            // words of two; a row at an odd element begins in the word of the element before it and has 129 words
+            const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+            const uint32_t* words = reinterpret_cast<const uint32_t*>(at & ~static_cast<uintptr_t>(3));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = __ldcs(words + lane + 32 * i);
+            after = __ldcs(words + (at & 2 ? 128 : 0));          // without a branch, which would part the loads
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -169,10 +189,49 @@ template <> struct GradRaw<__nv_bfloat16> {
             }
         }
     }
+    // kRows, an odd row: a pair's second element is in the next lane's word.
+    template <Access A>
+    __device__ __forceinline__ void arrange(long long at, int lane) {
+        if (A != kRows || (at & 2) == 0) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t up = __shfl_down_sync(0xffffffffu, x[i], 1);
+            const uint32_t row = __shfl_sync(0xffffffffu, i < 3 ? x[i + 1] : after, 0);
+            x[i] = __byte_perm(x[i], lane == 31 ? row : up, 0x5432);
+        }
+    }
     __device__ __forceinline__ Pair get(int i) const {
         return pack(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u));
     }
 };
+
+// kRows' elements to memory (a multiple of eight elements from an aligned address), or to consecutive ones by way of 256
+// floats of shared memory.
+template <typename GT>
+__device__ __forceinline__ void store_rows(float* p, int lane, const Pair (&x)[4]) {
+    if (sizeof(GT) == 4) {
+        store_f32<false>(p, lane, kWarpElems, x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) reinterpret_cast<Pair*>(p)[lane + 32 * i] = x[i];
+    }
+}
+template <typename GT>
+__device__ __forceinline__ void to_vector(float* buffer, int lane, Pair (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (sizeof(GT) == 4) {
+            buffer[lane + 64 * i] = lo(x[i]);
+            buffer[lane + 64 * i + 32] = hi(x[i]);
+        } else {
+            reinterpret_cast<Pair*>(buffer)[lane + 32 * i] = x[i];
+        }
+    }
+    __syncwarp();
+    const ulonglong2* q = reinterpret_cast<const ulonglong2*>(buffer) + 2 * lane;
+    const ulonglong2 a = q[0], b = q[1];
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
+}
 
 template <int SUMS>
 __device__ __forceinline__ void join_sums(Pair (&sum)[SUMS][4], Pair one) {
@@ -190,12 +249,19 @@ __device__ __forceinline__ void pointers_of(const Source& s, const long long* gr
 #pragma unroll
     for (int j = 0; j < KU; ++j) from[j] = k0 + j < s.K ? __ldg(grads + s.worker[k0 + j]) : 0;
 }
-template <typename GT, int KU, bool ALIGNED>
+template <typename GT, int KU, Access A>
 __device__ __forceinline__ void load_round(const Source& s, const long long (&from)[KU], int k0, int offset, int lane, int n,
                                            GradRaw<GT> (&raw)[KU]) {
 #pragma unroll
     for (int j = 0; j < KU; ++j)
-        if (k0 + j < s.K) raw[j].template load<ALIGNED>(reinterpret_cast<const GT*>(from[j]) + offset, lane, n);
+        if (k0 + j < s.K) raw[j].template load<A>(reinterpret_cast<const GT*>(from[j]) + offset, lane, n);
+}
+// offset is a multiple of 256: a row is odd where its tensor is
+template <typename GT, int KU, Access A>
+__device__ __forceinline__ void arrange_round(const Source& s, const long long (&from)[KU], int k0, int lane, GradRaw<GT> (&raw)[KU]) {
+#pragma unroll
+    for (int j = 0; j < KU; ++j)
+        if (A == kRows && k0 + j < s.K) raw[j].template arrange<A>(from[j], lane);
 }
 // All workers of a sum that fits one round: partial sum by partial sum.
 template <typename GT, int KU>
@@ -212,14 +278,15 @@ __device__ __forceinline__ void weigh_round(const Source& s, const GradRaw<GT> (
         }
     }
 }
-template <typename GT, int KU, bool MANY, bool ALIGNED>
+template <typename GT, int KU, bool MANY, Access A>
 __device__ __forceinline__ void aggregate(const Source& s, const long long* grads, int offset, int lane, int n,
                                           Pair (&g)[4]) {
     GradRaw<GT> raw[KU];
     long long from[KU];
     if constexpr (!MANY) {
         pointers_of<KU>(s, grads, 0, from);
-        load_round<GT, KU, ALIGNED>(s, from, 0, offset, lane, n, raw);
+        load_round<GT, KU, A>(s, from, 0, offset, lane, n, raw);
+        arrange_round<GT, KU, A>(s, from, 0, lane, raw);
         weigh_round<GT, KU>(s, raw, g);
     } else {
         static_assert(KU % 4 == 0, "worker k belongs to sum k mod 4");
@@ -231,7 +298,8 @@ __device__ __forceinline__ void aggregate(const Source& s, const long long* grad
 #pragma unroll 1
         for (int k0 = 0; k0 < s.K; k0 += KU) {
             pointers_of<KU>(s, grads, k0, from);
-            load_round<GT, KU, ALIGNED>(s, from, k0, offset, lane, n, raw);
+            load_round<GT, KU, A>(s, from, k0, offset, lane, n, raw);
+            arrange_round<GT, KU, A>(s, from, k0, lane, raw);
 #pragma unroll
             for (int j = 0; j < KU; ++j)
                 if (k0 + j < s.K) {
@@ -465,12 +533,16 @@ __device__ __forceinline__ void store_moments(const StepArgs& a, uint8_t* first,
     }
 }
 
-// A block straight from global memory to registers and back.
-template <typename GT, int KU, bool MANY, bool STATE8, bool CLIP, bool NORM, bool ALIGNED>
+// A block straight from global memory to registers and back.  A: kVector; kRows (vectors but for the gradients, which
+// go through `buffer`, 256 floats of shared memory); kMasked.
+template <typename GT, int KU, bool MANY, bool STATE8, bool CLIP, bool NORM, Access A>
 __device__ __forceinline__ void step_block(const StepArgs& a, const long long* rec, int offset, int lane, int n, float factor,
-                                           double& sq) {
+                                           float* buffer, double& sq) {
+    constexpr bool ALIGNED = A != kMasked;
     float* param = reinterpret_cast<float*>(__ldg(rec + kRecParam)) + offset;
     Pair p[4], m[4], u[4], g[4];
+    // rows take more registers: their sum first, then the states
+    if (A == kRows) aggregate<GT, KU, MANY, A>(a.src, rec + kRecGrads, offset, lane, n, g);
     load_f32<ALIGNED>(param, lane, n, p);
     const long long first = __ldg(rec + kRecFirst), second = __ldg(rec + kRecSecond);
     float *first_scale = nullptr, *second_scale = nullptr;
@@ -489,8 +561,9 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const long long* r
     const long long position = __ldg(rec + kRecPosition) + offset;
     if (CLIP && a.src.staged)
         load_f32<ALIGNED>(a.src.staged + position, lane, n, g);
-    else
-        aggregate<GT, KU, MANY, ALIGNED>(a.src, rec + kRecGrads, offset, lane, n, g);
+    else if (A != kRows)
+        aggregate<GT, KU, MANY, A>(a.src, rec + kRecGrads, offset, lane, n, g);
+    if (A == kRows) to_vector<GT>(buffer, lane, g);
     if (NORM) sq += sum_squares(g);
     update<CLIP>(a, factor, decay_of(a, rec), g, p, m, u);
     store_f32<ALIGNED>(param, lane, n, p);
@@ -508,8 +581,36 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const long long* r
 template <typename GT, bool STATE8, bool CLIP, bool NORM>
 __device__ __noinline__ double step_block_slow(const StepArgs& a, const long long* rec, int offset, int lane, int n, float factor) {
     double sq = 0.0;
-    step_block<GT, 4, true, STATE8, CLIP, NORM, false>(a, rec, offset, lane, n, factor, sq);
+    step_block<GT, 4, true, STATE8, CLIP, NORM, kMasked>(a, rec, offset, lane, n, factor, nullptr, sq);
     return sq;
+}
+
+// Norm and clipping factor from the sum of squares: max_norm / norm where the norm is larger than max_norm, else 1
+// (a NaN norm does not clip).
+__device__ __forceinline__ void write_norm(double total, float* norm, float* factor, float max_norm) {
+    const double root = sqrt(total);
+    if (norm) *norm = static_cast<float>(root);
+    if (factor) *factor = root > static_cast<double>(max_norm) ? static_cast<float>(max_norm / root) : 1.0f;
+}
+
+template <bool CLIP>
+__device__ __forceinline__ float clip_factor(const StepArgs& a, int lane) {
+    if (!CLIP) return 1.0f;
+    if (a.partial_count == 0) return __ldcg(a.factor);
+    double total = 0.0;
+#pragma unroll 1
+    for (int i = lane; i < a.partial_count; i += 256) {              // eight loads at once
+        double x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = i + 32 * j < a.partial_count ? __ldcg(a.partials + i + 32 * j) : 0.0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) total += x[j];
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
+    float factor;
+    write_norm(total, blockIdx.x == 0 && threadIdx.x == 0 ? a.norm : nullptr, &factor, a.max_norm);
+    return factor;
 }
 
 // A step's CTAs take the records in order, after a norm kernel in the opposite one: what that read or left last is
@@ -534,13 +635,16 @@ __global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 4) adamw_kernel(const 
     const long long* rec = record_of<CLIP>(a.src);
     const long long cf = __ldg(rec + kRecCount);
     const int n = static_cast<int>(cf & 0xffffffffLL) - offset, flags = static_cast<int>(cf >> 32);
-    const float factor = CLIP ? __ldcg(a.factor) : 1.0f;
+    const float factor = clip_factor<CLIP>(a, lane);
     double sq = 0.0;
+    __shared__ __align__(16) float buffer[kSpan];
     if (n > 0) {
-        const bool aligned = flags & kStateAligned && (flags & kGradsAligned || (CLIP && a.src.staged));
-        if (aligned && n >= kWarpElems)
-            step_block<GT, KU, MANY, false, CLIP, NORM, true>(a, rec, offset, lane, kWarpElems, factor, sq);
-        else
+        if (flags & kStateAligned && n >= kWarpElems) {
+            if (flags & kGradsAligned || (CLIP && a.src.staged))
+                step_block<GT, KU, MANY, false, CLIP, NORM, kVector>(a, rec, offset, lane, kWarpElems, factor, nullptr, sq);
+            else
+                step_block<GT, KU, MANY, false, CLIP, NORM, kRows>(a, rec, offset, lane, kWarpElems, factor, buffer + offset, sq);
+        } else
             sq = step_block_slow<GT, false, CLIP, NORM>(a, rec, offset, lane, min(n, kWarpElems), factor);
     }
     if (NORM) agg::store_norm_partial(a.partials, sq);
@@ -637,7 +741,6 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
     const long long cf = __ldg(rec + kRecCount);
     const int count = static_cast<int>(cf & 0xffffffffLL);
     const bool grads_aligned = cf >> 32 & kGradsAligned || (CLIP && a.src.staged);
-    const float factor = CLIP ? __ldcg(a.factor) : 1.0f;
     const int K = a.src.K, items = R::kFused ? 1 : 1 + (K + R::kItem - 1) / R::kItem;         // of a block
     prefetch_record<CLIP>(a.src, rec);
     double sq = 0.0;
@@ -719,6 +822,7 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
 #pragma unroll 1
     for (int i = 0; i < R::kSlots - 1; ++i) issue();
 
+    const float factor = clip_factor<CLIP>(a, lane);
     const Pair decay = decay_of(a, rec);
     const long long copy = __ldg(rec + kRecCopy);
     int offset = warp * kWarpElems;
@@ -798,17 +902,59 @@ __host__ __device__ constexpr int norm_batch(int workers) {
 template <typename GT>
 __device__ __noinline__ double norm_block_slow(const Source& s, const long long* grads, int offset, int lane, int n, float* staged) {
     Pair g[4];
-    aggregate<GT, 4, true, false>(s, grads, offset, lane, n, g);
+    aggregate<GT, 4, true, kMasked>(s, grads, offset, lane, n, g);
     if (staged) store_f32<false>(staged, lane, n, g);
     return sum_squares(g);
 }
 
-// Norm and clipping factor from the sum of squares: max_norm / norm where the norm is larger than max_norm, else 1
-// (a NaN norm does not clip).
-__device__ __forceinline__ void write_norm(double total, float* norm, float* factor, float max_norm) {
-    const double root = sqrt(total);
-    if (norm) *norm = static_cast<float>(root);
-    if (factor) *factor = root > static_cast<double>(max_norm) ? static_cast<float>(max_norm / root) : 1.0f;
+// A warp's `whole` >= 1 blocks of a batch.  Where they may be fewer than a batch (FULL == false), the last one is loaded
+// again in place of the missing and not counted: no branch parts the loads.
+template <typename GT, int KU, bool MANY, Access A, bool FULL>
+__device__ __forceinline__ double norm_blocks(const Source& s, const long long* rec, const long long (&from)[KU], int base,
+                                              int whole, int lane, float* staged) {
+    constexpr int kBatch = norm_batch<GT>(KU);
+    double sq = 0.0;
+    GradRaw<GT> raw[kBatch][KU];
+    if (!MANY) {
+#pragma unroll
+        for (int e = 0; e < kBatch; ++e)
+            load_round<GT, KU, A>(s, from, 0, base + (FULL ? e : min(e, whole - 1)) * kSpan, lane, kWarpElems, raw[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < kBatch; ++e) {
+        const int offset = base + e * kSpan;
+        if (!FULL && e >= whole) break;
+        Pair g[4];
+        if constexpr (MANY) {
+            aggregate<GT, KU, true, A>(s, rec + kNormGrads, offset, lane, kWarpElems, g);
+        } else {
+            arrange_round<GT, KU, A>(s, from, 0, lane, raw[e]);
+            weigh_round<GT, KU>(s, raw[e], g);
+        }
+        if (staged) {
+            if (A == kVector) store_f32<true>(staged + offset, lane, kWarpElems, g);
+            else store_rows<GT>(staged + offset, lane, g);
+        }
+        sq += sum_squares(g);
+    }
+    return sq;
+}
+
+// The end of a tensor: fewer blocks than a batch, the last one shorter than 256.  Kept out of the kernel's registers.
+template <typename GT, int KU, bool MANY>
+__device__ __noinline__ double norm_end(const Source& s, const long long* rec, int base, int whole, int lane, int count, bool aligned,
+                                        float* staged) {
+    double sq = 0.0;
+    long long from[KU];
+    if (!MANY) pointers_of<KU>(s, rec + kNormGrads, 0, from);
+    if (whole > 0) {
+        if (aligned) sq = norm_blocks<GT, KU, MANY, kVector, false>(s, rec, from, base, whole, lane, staged);
+        else sq = norm_blocks<GT, KU, MANY, kRows, false>(s, rec, from, base, whole, lane, staged);
+    }
+    const int end = base + whole * kSpan;
+    if (end < count)
+        sq += norm_block_slow<GT>(s, rec + kNormGrads, end, lane, count - end, staged ? staged + end : nullptr);
+    return sq;
 }
 
 template <typename GT, int KU, bool MANY, bool LAST>
@@ -831,31 +977,13 @@ __global__ void __launch_bounds__(kNormThreads, KU * sizeof(GT) > 16 || MANY ? 4
     if ((blockIdx.x >> 1) + kAhead < a.src.records && threadIdx.x < a.src.stride / 4)
         agg::prefetch_l2(rec + kAhead * a.src.stride + 4 * threadIdx.x);
     double sq = 0.0;
-    if (cf >> 32 & kGradsAligned && base + (kBatch - 1) * kSpan + kWarpElems <= count) {
-        if constexpr (MANY) {
-            Pair g[4];
-            aggregate<GT, KU, true, true>(a.src, rec + kNormGrads, base, lane, kWarpElems, g);
-            if (staged) store_f32<true>(staged + base, lane, kWarpElems, g);
-            sq = sum_squares(g);
-        } else {
-            GradRaw<GT> raw[kBatch][KU];
-#pragma unroll
-            for (int e = 0; e < kBatch; ++e)
-                load_round<GT, KU, true>(a.src, from, 0, base + e * kSpan, lane, kWarpElems, raw[e]);
-#pragma unroll
-            for (int e = 0; e < kBatch; ++e) {
-                Pair g[4];
-                weigh_round<GT, KU>(a.src, raw[e], g);
-                if (staged) store_f32<true>(staged + base + e * kSpan, lane, kWarpElems, g);
-                sq += sum_squares(g);
-            }
-        }
-    } else {
-        // a tensor's end, and tensors off the grid
-#pragma unroll 1
-        for (int offset = base; offset < count; offset += kSpan)
-            sq += norm_block_slow<GT>(a.src, rec + kNormGrads, offset, lane, min(count - offset, kWarpElems),
-                                      staged ? staged + offset : nullptr);
+    const int whole = (count - base - kWarpElems + kSpan) / kSpan;           // of 256
+    const bool aligned = cf >> 32 & kGradsAligned;
+    if (whole >= kBatch) {
+        if (aligned) sq = norm_blocks<GT, KU, MANY, kVector, true>(a.src, rec, from, base, kBatch, lane, staged);
+        else sq = norm_blocks<GT, KU, MANY, kRows, true>(a.src, rec, from, base, kBatch, lane, staged);
+    } else if (base < count) {
+        sq = norm_end<GT, KU, MANY>(a.src, rec, base, max(whole, 0), lane, count, aligned, staged);
     }
 
     const double mine = agg::block_sum(sq, smem);

@@ -203,9 +203,10 @@ NormFn pick_norm(int K) {
     return grad_norm_kernel<GT, 8, true, LAST>;
 }
 
-// Norm (and aggregate, and clipping factor) of a plan's gradients.
+// Norm (and aggregate, and clipping factor) of a plan's gradients.  left: where the caller adds the partials itself if
+// they are few, their number (0: done here).
 db_status launch_norm(const Layout& L, char* table, db_dtype dt, int workers, Source src, float* norm, float* factor, float max_norm,
-                      cudaStream_t stream) {
+                      int* left, cudaStream_t stream) {
     NormArgs a{};
     a.src = src;
     a.src.recs = reinterpret_cast<const long long*>(table + L.norm.at);
@@ -217,12 +218,13 @@ db_status launch_norm(const Layout& L, char* table, db_dtype dt, int workers, So
     a.factor = factor;
     a.max_norm = max_norm;
     const long long grid = 2 * L.norm.count;
-    const bool last = grid <= 8 * sm_count();
+    const bool leave = left && grid <= kFoldInStep, last = !leave && grid <= 8 * sm_count();
+    if (left) *left = leave ? static_cast<int>(grid) : 0;
     // by the plan's workers, not the call's: the records are made for that kernel
     const NormFn fn = dt == DB_F32 ? (last ? pick_norm<float, true>(workers) : pick_norm<float, false>(workers))
                                    : (last ? pick_norm<__nv_bfloat16, true>(workers) : pick_norm<__nv_bfloat16, false>(workers));
     DB_CUDA_TRY(launch(fn, grid, kNormThreads, 0, stream, a));
-    return last ? DB_OK : launch_fold(L, table, grid, norm, factor, max_norm, stream);
+    return leave || last ? DB_OK : launch_fold(L, table, grid, norm, factor, max_norm, stream);
 }
 
 using StepFn = void (*)(const StepArgs);
@@ -484,7 +486,10 @@ extern "C" db_status db_aggregate_adamw_multi(db_adamw_plan* plan, const int32_t
 
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (clip) {
-        const db_status s = launch_norm(L, plan->table, plan->grad_dtype, plan->K, a.src, grad_norm, factor, max_norm, stream);
+        a.norm = grad_norm;
+        a.max_norm = max_norm;
+        const db_status s = launch_norm(L, plan->table, plan->grad_dtype, plan->K, a.src, grad_norm, factor, max_norm,
+                                        &a.partial_count, stream);
         if (s != DB_OK) return s;
     }
     const int K = staged ? 1 : a.src.K;
@@ -565,6 +570,6 @@ extern "C" db_status db_grad_norm_multi(db_grad_norm_plan* plan, const int32_t* 
     const db_status st = set_workers(b, plan->K, &src);
     if (st != DB_OK) return st;
     if (plan->layout.norm.count == 0) return DB_OK;
-    return launch_norm(plan->layout, plan->table, plan->grad_dtype, plan->K, src, grad_norm, nullptr, 0.0f,
+    return launch_norm(plan->layout, plan->table, plan->grad_dtype, plan->K, src, grad_norm, nullptr, 0.0f, nullptr,
                        static_cast<cudaStream_t>(cuda_stream));
 }
