@@ -12,6 +12,7 @@
 #include <cuda_fp8.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "agg_device.cuh"
 #include "dynbatch.h"
@@ -479,12 +480,12 @@ __device__ __forceinline__ void store_copy(long long to, int offset, int lane, i
     }
 }
 
-// Both moments of a block to 8 bits: codes at `first`, `second`, scales by lane 0.
+// Both moments of a block to 8 bits; scales by lane 0.  Elements beyond the block's end have zero moments and leave the
+// maximum alone.
 template <bool ALIGNED>
-__device__ __forceinline__ void store_moments(const StepArgs& a, uint8_t* first, uint8_t* second, float* first_scale,
-                                              float* second_scale, long long position, int lane, int n,
-                                              const Pair (&m)[4], const Pair (&u)[4]) {
-    // elements beyond n have zero moments: they leave the maximum alone
+__device__ __forceinline__ void encode_moments(const StepArgs& a, float* first_scale, float* second_scale, long long position,
+                                               int lane, const Pair (&m)[4], const Pair (&u)[4], uint32_t (&cm)[2],
+                                               uint32_t (&cu)[2]) {
     const BlockScale sm = block_scale(top_of(m)), su = block_scale(top_of(u));
     Pair ym[4], yu[4];
     scale_down(m, sm.top, ym);
@@ -511,8 +512,10 @@ __device__ __forceinline__ void store_moments(const StepArgs& a, uint8_t* first,
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) wm[j] |= __float_as_uint(j & 1 ? hi(m[j >> 1]) : lo(m[j >> 1])) & 0x80000000u;
-    const uint32_t cm[2] = {top_bytes(wm[0], wm[1], wm[2], wm[3]) & sm.keep, top_bytes(wm[4], wm[5], wm[6], wm[7]) & sm.keep};
-    uint32_t cu[2] = {top_bytes(wu[0], wu[1], wu[2], wu[3]), top_bytes(wu[4], wu[5], wu[6], wu[7])};
+    cm[0] = top_bytes(wm[0], wm[1], wm[2], wm[3]) & sm.keep;
+    cm[1] = top_bytes(wm[4], wm[5], wm[6], wm[7]) & sm.keep;
+    cu[0] = top_bytes(wu[0], wu[1], wu[2], wu[3]);
+    cu[1] = top_bytes(wu[4], wu[5], wu[6], wu[7]);
     // A second moment that is not zero is never held as zero: the next step divides by its root.  Codes are below
     // 128, so a byte is zero where subtracting one borrows into its top bit.
     if (((cu[0] - 0x01010101u) | (cu[1] - 0x01010101u)) & 0x80808080u) {
@@ -525,8 +528,6 @@ __device__ __forceinline__ void store_moments(const StepArgs& a, uint8_t* first,
     }
     cu[0] &= su.keep;
     cu[1] &= su.keep;
-    store_codes<ALIGNED>(first, lane, n, cm);
-    store_codes<ALIGNED>(second, lane, n, cu);
     if (lane == 0) {
         *first_scale = sm.scale;
         *second_scale = su.scale;
@@ -569,8 +570,10 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const long long* r
     store_f32<ALIGNED>(param, lane, n, p);
     if (const long long copy = __ldg(rec + kRecCopy)) store_copy<ALIGNED>(copy, offset, lane, n, p);
     if (STATE8) {
-        store_moments<ALIGNED>(a, reinterpret_cast<uint8_t*>(first) + offset, reinterpret_cast<uint8_t*>(second) + offset,
-                               first_scale, second_scale, position, lane, n, m, u);
+        uint32_t cm[2], cu[2];
+        encode_moments<ALIGNED>(a, first_scale, second_scale, position, lane, m, u, cm, cu);
+        store_codes<ALIGNED>(reinterpret_cast<uint8_t*>(first) + offset, lane, n, cm);
+        store_codes<ALIGNED>(reinterpret_cast<uint8_t*>(second) + offset, lane, n, cu);
     } else {
         store_f32<ALIGNED>(reinterpret_cast<float*>(first) + offset, lane, n, m);
         store_f32<ALIGNED>(reinterpret_cast<float*>(second) + offset, lane, n, u);
@@ -685,23 +688,41 @@ struct Ring {
     static constexpr int kBytes = kWarps * kSlots * kSlot;
 };
 
-// One worker's 256 gradients to shared memory, in order.
-template <typename GT>
-__device__ __forceinline__ void copy_row(uint32_t to, const GT* from, int lane) {
-    constexpr int kBytes = static_cast<int>(sizeof(GT)) * kWarpElems;
+// The first `have` bytes (none if it is negative) of BYTES, and zeros: the end of a buffer.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from, int have) {
+    const int bytes = have < 0 ? 0 : have > BYTES ? BYTES : have;
+    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(BYTES), "r"(bytes) : "memory");
+}
+
+// One worker's 256 gradients to shared memory, in order; n < 256: and zeros behind the n-th.
+template <bool FULL, typename GT>
+__device__ __forceinline__ void copy_row(uint32_t to, const GT* from, int lane, int n) {
+    constexpr int kSize = static_cast<int>(sizeof(GT)), kBytes = kSize * kWarpElems;
+    const char* src = reinterpret_cast<const char*>(from);
 #pragma unroll
-    for (int i = 0; i < kBytes; i += 512) copy_async<16>(to + i + 16 * lane, reinterpret_cast<const char*>(from) + i + 16 * lane);
+    for (int i = 0; i < kBytes; i += 512) {
+        const int at = i + 16 * lane;
+        if (FULL) copy_async<16>(to + at, src + at);
+        else copy_async<16>(to + at, src + at, kSize * n - at);
+    }
 }
 // The same off the 16-byte grid, by words.  A bf16 row at an odd element is copied from the word that holds the element
-// before it on (129 words, each with at least one element of the row) and read two bytes further up.
-template <typename GT>
-__device__ __forceinline__ void copy_row_unaligned(uint32_t to, const GT* from, int lane) {
-    constexpr int kBytes = static_cast<int>(sizeof(GT)) * kWarpElems;
-    const uintptr_t at = reinterpret_cast<uintptr_t>(from);
-    const char* words = reinterpret_cast<const char*>(at & ~static_cast<uintptr_t>(3));
+// before it on and read two bytes further up (129 words; every word has at least one element of the row).
+template <bool FULL, typename GT>
+__device__ __forceinline__ void copy_row_unaligned(uint32_t to, const GT* from, int lane, int n) {
+    constexpr int kSize = static_cast<int>(sizeof(GT)), kBytes = kSize * kWarpElems;
+    const uintptr_t address = reinterpret_cast<uintptr_t>(from);
+    const char* words = reinterpret_cast<const char*>(address & ~static_cast<uintptr_t>(3));
+    const int have = kSize * n + static_cast<int>(address & 3);
 #pragma unroll
-    for (int i = 0; i < kBytes; i += 128) copy_async<4>(to + i + 4 * lane, words + i + 4 * lane);
-    if (sizeof(GT) == 2 && (at & 2) && lane == 0) copy_async<4>(to + kBytes, words + kBytes);
+    for (int i = 0; i < kBytes; i += 128) {
+        const int at = i + 4 * lane;
+        if (FULL) copy_async<4>(to + at, words + at);
+        else copy_async<4>(to + at, words + at, have - at);
+    }
+    if (kSize == 2 && (address & 2) && lane == 0) copy_async<4>(to + kBytes, words + kBytes, have - kBytes);
 }
 
 // A lane's elements of a slot.
@@ -745,10 +766,10 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
     prefetch_record<CLIP>(a.src, rec);
     double sq = 0.0;
 
-    // blocks warp, warp + 8, ... of the run; whole ones of aligned tensors come through the ring
+    // blocks warp, warp + 8, ... of the run; those of aligned tensors come through the ring
     const int mine = (count - warp * kWarpElems + kSpan - 1) / kSpan;                        // blocks that begin in the run
-    int whole = cf >> 32 & kStateAligned ? (count - (warp + 1) * kWarpElems + kSpan) / kSpan : 0;
-    if (whole < 0) whole = 0;
+    const int blocks = cf >> 32 & kStateAligned ? mine : 0;
+    const int whole = blocks - (blocks > 0 && warp * kWarpElems + (blocks - 1) * kSpan + kWarpElems > count);
     const unsigned char* slots = smem + warp * (R::kSlots * R::kSlot);
     const uint32_t ring = shared_address(slots);
     const char* params = reinterpret_cast<const char*>(__ldg(rec + kRecParam));
@@ -773,39 +794,56 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
         odd_high = __ballot_sync(0xffffffffu, from_high & 2);
     }
 
-    auto copy_item = [&](int offset, int item, uint32_t to) {
+    auto copy_item = [&](auto full, int offset, int item, uint32_t to) {
+        constexpr bool kFull = decltype(full)::value;
+        const int n = kFull ? kWarpElems : count - offset;
         if (R::kFused || item == 0) {
-            copy_async<16>(to + 16 * lane, my_params + 4 * offset);
-            copy_async<16>(to + 512 + 16 * lane, my_params + 4 * offset + 512);
-            copy_async<16>(to + kSlotCodes + 16 * lane, my_codes + offset);
+            if (kFull) {
+                copy_async<16>(to + 16 * lane, my_params + 4 * offset);
+                copy_async<16>(to + 512 + 16 * lane, my_params + 4 * offset + 512);
+                copy_async<16>(to + kSlotCodes + 16 * lane, my_codes + offset);
+            } else {
+                copy_async<16>(to + 16 * lane, my_params + 4 * offset, 4 * n - 16 * lane);
+                copy_async<16>(to + 512 + 16 * lane, my_params + 4 * offset + 512, 4 * n - 512 - 16 * lane);
+                copy_async<16>(to + kSlotCodes + 16 * lane, my_codes + offset, n - 16 * (lane & 15));
+            }
             if (lane < 2) copy_async<4>(to + kSlotScales + 4 * lane, my_scale + offset / (kWarpElems / 4));
         }
         if (R::kFused || item > 0) {
             const int k0 = R::kFused ? 0 : (item - 1) * R::kItem;
-#pragma unroll
-            for (int j = 0; j < R::kItem; ++j) {
+            auto row = [&](int j) {
                 const int k = k0 + j;
-                if (R::kFused || k < K) {
-                    const GT* from = reinterpret_cast<const GT*>(
-                        __shfl_sync(0xffffffffu, MANY && k >= 32 ? from_high : from_low, k & 31)) + offset;
-                    if (grads_aligned) copy_row(to + R::kGrads + j * R::kRow, from, lane);
-                    else copy_row_unaligned(to + R::kGrads + j * R::kRow, from, lane);
+                return reinterpret_cast<const GT*>(__shfl_sync(0xffffffffu, MANY && k >= 32 ? from_high : from_low, k & 31)) + offset;
+            };
+            if (kFull && grads_aligned) {
+#pragma unroll
+                for (int j = 0; j < R::kItem; ++j)
+                    if (R::kFused || k0 + j < K) copy_row<true>(to + R::kGrads + j * R::kRow, row(j), lane, n);
+            } else {
+#pragma unroll 1
+                for (int j = 0; j < R::kItem && (R::kFused || k0 + j < K); ++j) {
+                    if (grads_aligned) copy_row<false>(to + R::kGrads + j * R::kRow, row(j), lane, n);
+                    else copy_row_unaligned<kFull>(to + R::kGrads + j * R::kRow, row(j), lane, n);
                 }
             }
         }
     };
 
-    int next_offset = warp * kWarpElems, next_item = 0, left = whole * items;                // the item to copy
+    int next_offset = warp * kWarpElems, next_item = 0;                                       // the item to copy
+    int left = whole * items, rest = (blocks - whole) * items;                               // of whole blocks, of a shorter one
     uint32_t to = ring;
     const unsigned char* from = slots;
     auto issue = [&]() {
         if (left > 0) {
-            copy_item(next_offset, next_item, to);
+            copy_item(std::true_type(), next_offset, next_item, to);
             --left;
             if (R::kFused || ++next_item == items) {
                 next_item = 0;
                 next_offset += kSpan;
             }
+        } else if (rest > 0) {
+            copy_item(std::false_type(), next_offset, next_item++, to);
+            --rest;
         }
         copy_commit();                       // an empty group where nothing is left: the count of groups stays right
         to = to == ring + (R::kSlots - 1) * R::kSlot ? ring : to + R::kSlot;
@@ -826,8 +864,10 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
     const Pair decay = decay_of(a, rec);
     const long long copy = __ldg(rec + kRecCopy);
     int offset = warp * kWarpElems;
-#pragma unroll 1
-    for (int block = 0; block < whole; ++block, offset += kSpan) {
+    // A block.  The common one, whole and with its rows at even elements, is a loop of its own: tests for the others
+    // in it cost 3 to 6 %.
+    auto do_block = [&](auto common) {
+        constexpr bool kCommon = decltype(common)::value;
         Pair sum[kSums][4], p[4];
         uint32_t cm[2], cu[2];
         float2 scales;
@@ -853,7 +893,7 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
                     if (MANY ? k < K : place <= KI / 2 || place < K) {
                         Pair x[4];
                         const unsigned int odd = MANY && k >= 32 ? odd_high : odd_low;
-                        read_row<GT>(from + R::kGrads + j * R::kRow, lane, odd >> (k & 31) & 1u, x);
+                        read_row<GT>(from + R::kGrads + j * R::kRow, lane, !kCommon && odd >> (k & 31) & 1u, x);
                         const Pair w = KI == 1 ? 0ull : a.src.lambda[k];                     // a single weight is 1
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
@@ -871,17 +911,41 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
         decode(cm, scales.x, m);
         decode(cu, scales.y, u);
         update<CLIP>(a, factor, decay, sum[0], p, m, u);
-        store_f32<true>(reinterpret_cast<float*>(const_cast<char*>(params)) + offset, lane, kWarpElems, p);
-        if (copy) store_copy<true>(copy, offset, lane, kWarpElems, p);
-        store_moments<true>(a, reinterpret_cast<uint8_t*>(const_cast<char*>(first)) + offset,
-                            reinterpret_cast<uint8_t*>(const_cast<char*>(second)) + offset,
-                            reinterpret_cast<float*>(const_cast<char*>(first_scale)) + offset / kWarpElems,
-                            reinterpret_cast<float*>(const_cast<char*>(second_scale)) + offset / kWarpElems, position + offset,
-                            lane, kWarpElems, m, u);
-    }
-    // a tensor's last, shorter block, and tensors off the grid
+        float* param = reinterpret_cast<float*>(const_cast<char*>(params)) + offset;
+        uint8_t* codes_m = reinterpret_cast<uint8_t*>(const_cast<char*>(first)) + offset;
+        uint8_t* codes_u = reinterpret_cast<uint8_t*>(const_cast<char*>(second)) + offset;
+        const bool full = kCommon || offset + kWarpElems <= count;
+        if (full) {
+            store_f32<true>(param, lane, kWarpElems, p);
+            if (copy) store_copy<true>(copy, offset, lane, kWarpElems, p);
+        }
+        encode_moments<true>(a, reinterpret_cast<float*>(const_cast<char*>(first_scale)) + offset / kWarpElems,
+                             reinterpret_cast<float*>(const_cast<char*>(second_scale)) + offset / kWarpElems, position + offset,
+                             lane, m, u, cm, cu);
+        if (full) {
+            store_codes<true>(codes_m, lane, kWarpElems, cm);
+            store_codes<true>(codes_u, lane, kWarpElems, cu);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int j = 8 * lane + i;
+                if (j >= count - offset) break;
+                const float x = i & 1 ? hi(p[i >> 1]) : lo(p[i >> 1]);
+                param[j] = x;
+                if (copy) reinterpret_cast<__nv_bfloat16*>(copy)[offset + j] = __float2bfloat16_rn(x);
+                codes_m[j] = static_cast<uint8_t>(cm[i >> 2] >> (8 * (i & 3)));
+                codes_u[j] = static_cast<uint8_t>(cu[i >> 2] >> (8 * (i & 3)));
+            }
+        }
+    };
+    const int common = odd_low | odd_high ? 0 : whole;
 #pragma unroll 1
-    for (int block = whole; block < mine; ++block, offset += kSpan)
+    for (int block = 0; block < common; ++block, offset += kSpan) do_block(std::true_type());
+#pragma unroll 1
+    for (int block = common; block < blocks; ++block, offset += kSpan) do_block(std::false_type());
+    // tensors off the grid
+#pragma unroll 1
+    for (int block = blocks; block < mine; ++block, offset += kSpan)
         sq += step_block_slow<GT, true, CLIP, NORM>(a, rec, offset, lane, min(count - offset, kWarpElems), factor);
     if (NORM) agg::store_norm_partial(a.partials, sq);
 }
