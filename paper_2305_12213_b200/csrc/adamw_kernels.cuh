@@ -885,7 +885,7 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
         for (int round = 0; round < (MANY ? K : 1); round += KI) {
 #pragma unroll
             for (int chunk = 0; chunk < KI; chunk += R::kItem) {
-                if (MANY && round + chunk >= K) break;
+                if (MANY ? round + chunk >= K : chunk > KI / 2 && chunk >= K) break;         // no such item
                 if (!R::kFused) arrive();
 #pragma unroll
                 for (int j = 0; j < R::kItem; ++j) {

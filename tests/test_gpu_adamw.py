@@ -555,3 +555,47 @@ def test_codes_are_the_definitions_exactly(K, grad):
             assert np.array_equal(got, np.where(x < 0, -want, want))
             assert np.array_equal(f64(scales), (top.astype(np.float32) * np.float32(1 / 448)).astype(np.float64))
         position += -(-size // 256) * 256
+
+
+@pytest.mark.parametrize("grad", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("K", [1, 2, 3, 4, 5, 6, 7, 8, 9, 12, 13, 17, 35])
+@pytest.mark.parametrize("state8", [False, True])
+def test_a_long_run_of_blocks_is_its_pieces(state8, K, grad):
+    """A tensor of 10.2M elements, of which every warp takes several blocks in turn, against the same memory as a list of
+    tensors of 2048 and 4096 elements, of which it takes one: the same bits, clipped and not, also with gradients at odd
+    elements and a last block that is shorter."""
+    sizes = [2048, 4096] * 1666 + [2048 + 77]
+    n = sum(sizes)
+    starts = np.concatenate([[0], np.cumsum(sizes)[:-1]]).tolist()
+    g = [torch.empty(n + 1, dtype=grad, device=DEV).normal_(0, 1e-2) for _ in range(K)]
+    dt = E4M3 if state8 else torch.float32
+    blocks = binding.adamw_scale_elems(n)
+
+    def fresh():
+        p = inputs.normal(n, 0.02, 5, DEV)
+        m, u = (torch.zeros(n, device=DEV).to(dt) for _ in range(2))
+        s = [torch.zeros(blocks, device=DEV) for _ in range(2)] if state8 else None
+        return p, torch.zeros(n, dtype=torch.bfloat16, device=DEV), m, u, s
+
+    def cut(t, unit=1):
+        return [t[a // unit:a // unit + -(-k // unit)] for a, k in zip(starts, sizes)]
+
+    for shift in (0, 1):
+        rows = [x[shift:shift + n] for x in g]
+        whole, parts = fresh(), fresh()
+        p, w, m, u, s = whole
+        one = binding.AdamWPlan([[x] for x in rows], [p], [m], [u], *([[s[0]], [s[1]]] if state8 else [None, None]), [w], clip=True)
+        p, w, m, u, s = parts
+        many = binding.AdamWPlan([cut(x) for x in rows], cut(p), cut(m), cut(u),
+                                 *([cut(s[0], 256), cut(s[1], 256)] if state8 else [None, None]), cut(w), clip=True)
+        b, norms = batches(K), torch.zeros(2, device=DEV)
+        for t, limit in ((1, 0.0), (2, 1e9), (3, 3.0)):
+            one.step(b, LR, B1, B2, EPS, t, limit, 7, norms[:1] if limit else None)
+            many.step(b, LR, B1, B2, EPS, t, limit, 7, norms[1:] if limit else None)
+        torch.cuda.synchronize()
+        # both sums are fp64, so the norms are the same float (but for one pair in 10^8) and the third step's factor, too
+        assert norms[0].item() == norms[1].item() > 3.0
+        for x, y in zip(whole[:4], parts[:4]):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+        if state8:
+            assert torch.equal(whole[4][0], parts[4][0]) and torch.equal(whole[4][1], parts[4][1])
