@@ -231,7 +231,8 @@ db_status db_multi_plan_destroy(db_multi_plan* plan);
  * otherwise element-wise.  Results do not depend on it.  No
  * buffer that a step writes may overlap another one of the plan (DB_ERR_ARG).  Steps
  * on one plan must not overlap on the device (two captured graphs of steps on one plan
- * neither); a captured step replays its b, lr, step and seed.
+ * neither); a captured step replays its b, lr, step and seed.  The device that is
+ * current at the plan's creation has to be current at its steps.
  * A clipped step is two launches (norm, update), one without clipping is one, or two or
  * three with grad_norm.
  * ------------------------------------------------------------------------ */

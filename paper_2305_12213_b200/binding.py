@@ -561,6 +561,24 @@ class _ListPlan:
             *[p for g in grads for p in self._pointers(g, self.grad_dtype, "grads[k]")])
         self._b = (c_int32 * self.K)()
         self._h = c_void_p()
+        self._streams = set()                            # raw handles of the streams that the table is known to be used on
+
+    def _make_table(self, nbytes: int, stream: Optional[torch.cuda.Stream]) -> None:
+        # the allocator may hand out memory that work queued on the current stream still uses
+        self.table = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+        self._streams.add(torch._C._cuda_getCurrentRawStream(self.device.index))
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream(self.device))
+
+    def _used_on(self, handle: int, stream: Optional[torch.cuda.Stream]) -> None:
+        """First use of the table on a stream other than its own: the allocator must not give the memory away before that
+        stream is done with it.  (Not while the stream is captured: a graph needs the plan to stay alive anyway.)"""
+        s = torch.cuda.current_stream(self.device) if stream is None else stream
+        with torch.cuda.stream(s):
+            if torch.cuda.is_current_stream_capturing():
+                return
+        self.table.record_stream(s)
+        self._streams.add(handle)
 
     def _pointers(self, tensors, dtype, name, sizes=None):
         tensors = list(tensors)
@@ -585,6 +603,8 @@ class _ListPlan:
             handle = stream.cuda_stream
         else:
             handle = torch._C._cuda_getCurrentRawStream(self.device.index)
+        if handle not in self._streams:
+            self._used_on(handle, stream)
         if torch.cuda.current_device() == self.device.index:
             _check(fn(*args, handle))
         else:
@@ -651,7 +671,7 @@ class AdamWPlan(_ListPlan):
         flags = DB_ADAMW_CLIP if clip else 0
         state_code = DB_F32 if state == torch.float32 else DB_E4M3
         nbytes = int(lib().db_adamw_plan_device_bytes(self.K, self._code, state_code, self._sizes, self.T, flags))
-        self.table = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+        self._make_table(nbytes, stream)
         self._call(lib().db_adamw_plan_create, ctypes.byref(self._h), self._grads, self._code, self.K, self._sizes, self.T,
                    p, w, m, u, state_code, ms, us, wd, flags, self.table.data_ptr(), self.table.numel(), stream=stream)
         self._fn = lib().db_aggregate_adamw_multi
@@ -672,7 +692,7 @@ class GradNormPlan(_ListPlan):
     def __init__(self, grads: Sequence[Sequence[torch.Tensor]], stream: Optional[torch.cuda.Stream] = None):
         super().__init__(grads, None)
         nbytes = int(lib().db_grad_norm_plan_device_bytes(self.K, self._code, self._sizes, self.T))
-        self.table = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+        self._make_table(nbytes, stream)
         self._call(lib().db_grad_norm_plan_create, ctypes.byref(self._h), self._grads, self._code, self.K, self._sizes,
                    self.T, self.table.data_ptr(), self.table.numel(), stream=stream)
         self._fn = lib().db_grad_norm_multi

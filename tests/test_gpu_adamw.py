@@ -599,3 +599,23 @@ def test_a_long_run_of_blocks_is_its_pieces(state8, K, grad):
             assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
         if state8:
             assert torch.equal(whole[4][0], parts[4][0]) and torch.equal(whole[4][1], parts[4][1])
+
+
+def test_a_plan_that_is_dropped_behind_a_step_on_another_stream():
+    """The records' memory is not handed out again while the step's kernels may still read it.  (Addresses are compared;
+    nothing is written there.)"""
+    n = 1_000_000
+    a = Problem([n], 1, torch.float32, False, 8)
+    s = torch.cuda.Stream()
+    plan = a.plan()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)                      # the step starts some milliseconds later
+    plan.step([1], LR, B1, B2, EPS, 1, stream=s)
+    begin, size = plan.table.data_ptr(), plan.table.numel()
+    plan.close()
+    del plan
+    others = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(4)]
+    assert not s.query()
+    assert all(x.data_ptr() + size <= begin or begin + size <= x.data_ptr() for x in others)
+    torch.cuda.synchronize()
