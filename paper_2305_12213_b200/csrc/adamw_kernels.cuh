@@ -4,9 +4,18 @@
 // Work is laid out in blocks of 256 consecutive elements of one tensor, one warp each: the unit that shares a
 // scale when the moments are held in 8 bits.  A record in device memory holds the pointers of a run of up to
 // `run` elements (a multiple of 2048, one step of a CTA's eight warps) of one tensor; a CTA takes a record.
-// Lanes own eight elements: consecutive ones when every buffer of the tensor is aligned (one 32-byte access for
-// fp32, 16 for bf16, 8 for e4m3), otherwise every 32nd one, element by element.  What is computed for an element
-// does not depend on which lane has it.
+// Lanes own eight consecutive elements (one 32-byte access for fp32, 16 for bf16, 8 for e4m3) where a tensor's states
+// are aligned; its gradients, where they are not, are read by words and handed to their lanes through shared memory.
+// Off that grid, and at a tensor's end, blocks go element by element.  What is computed for an element does not depend
+// on which lane has it.
+//
+// All three kernels are bound by the memory (a parameter costs K gradients + 24 bytes with 32-bit moments, + 12 with
+// 8-bit ones, and 50 to 60 instructions).  Measured on B200, bytes counted once, against its copy rate of 6.56 TB/s:
+//   32-bit, 470M parameters, one bf16 gradient, bf16 copy   1951 us   6.72 TB/s   1.03
+//   32-bit, 25.6M, eight fp32 gradients                      213 us   6.72 TB/s   1.02
+//    8-bit, 116M, one bf16 gradient, bf16 copy               289 us   6.44 TB/s   0.98
+//    8-bit, 110M, eight bf16 gradients, bf16 copy             534 us   6.15 TB/s   0.94
+//   norm, 110M, sixteen bf16 gradients                       589 us   5.93 TB/s   0.90
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
@@ -32,13 +41,17 @@ static_assert(kWarpElems == 32 * kLaneElems, "one warp per block of elements");
 enum RecordWord {
     kRecParam = 0, kRecFirst, kRecSecond, kRecCount,             // count | flags << 32
     kRecFirstScale, kRecSecondScale, kRecCopy, kRecDecay,        // bits of the fp32 weight decay
-    kRecPosition, kRecSpare, kRecGrads
+    kRecPosition, kRecGrads
 };
 enum NormRecordWord { kNormCount = 0, kNormPosition, kNormGrads };
 constexpr int kStateAligned = 1, kGradsAligned = 2;              // flags: buffers aligned to a lane's vector
 
-constexpr long long kAhead = 512;            // records
-constexpr int kFoldInStep = 512;             // partials that a clipped step adds itself
+// Records ahead of a CTA's own that it asks the L2 for (a wave is some hundred): the data that streams through has
+// evicted them, and a CTA that meets its record in DRAM starts 0.5 us later (norm of 110M, 16 workers: 692 -> 611 us).
+constexpr long long kAhead = 512;
+// Partials that a clipped step adds itself, every warp for itself, which takes the fold off the chain norm - fold - step
+// (20,000 parameters: 8.9 -> 6.6 us); with more of them the reads cost more than the launch.
+constexpr int kFoldInStep = 512;
 
 struct Source {                  // where the weighted gradient comes from
     const long long* recs;       // records, `stride` words apart
@@ -402,17 +415,12 @@ __device__ __forceinline__ void scale_down(const Pair (&x)[4], float s, Pair (&y
     }
 }
 
-template <bool ALIGNED>
+// Codes element by element (lane + 32 i, those below n); aligned ones come through shared memory.
 __device__ __forceinline__ void load_codes(const uint8_t* p, int lane, int n, uint32_t (&c)[2]) {
     c[0] = c[1] = 0u;
-    if (ALIGNED) {
-        const uint2 r = __ldcs(reinterpret_cast<const uint2*>(p + 8 * lane));
-        c[0] = r.x; c[1] = r.y;
-    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (lane + 32 * i < n) c[i >> 2] |= static_cast<uint32_t>(__ldcs(p + lane + 32 * i)) << (8 * (i & 3));
-    }
+    for (int i = 0; i < 8; ++i)
+        if (lane + 32 * i < n) c[i >> 2] |= static_cast<uint32_t>(__ldcs(p + lane + 32 * i)) << (8 * (i & 3));
 }
 __device__ __forceinline__ void decode(const uint32_t (&c)[2], float scale, Pair (&x)[4]) {
 #pragma unroll
@@ -553,9 +561,9 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const long long* r
         first_scale = reinterpret_cast<float*>(__ldg(rec + kRecFirstScale)) + offset / kWarpElems;
         second_scale = reinterpret_cast<float*>(__ldg(rec + kRecSecondScale)) + offset / kWarpElems;
         uint32_t c[2];
-        load_codes<ALIGNED>(reinterpret_cast<const uint8_t*>(first) + offset, lane, n, c);
+        load_codes(reinterpret_cast<const uint8_t*>(first) + offset, lane, n, c);
         decode(c, *first_scale, m);
-        load_codes<ALIGNED>(reinterpret_cast<const uint8_t*>(second) + offset, lane, n, c);
+        load_codes(reinterpret_cast<const uint8_t*>(second) + offset, lane, n, c);
         decode(c, *second_scale, u);
     } else {
         load_f32<ALIGNED>(reinterpret_cast<const float*>(first) + offset, lane, n, m);
@@ -631,7 +639,8 @@ __device__ __forceinline__ void prefetch_record(const Source& s, const long long
         agg::prefetch_l2(rec + (CLIP ? -kAhead : kAhead) * s.stride + 4 * threadIdx.x);
 }
 
-// 32-bit moments: one CTA per record, one block per warp.
+// 32-bit moments: one CTA per record, one block per warp, all its loads in flight at once; sixteen warps (up to two
+// workers 32) on an SM keep 64 KB and more on the way.
 template <typename GT, int KU, bool MANY, bool CLIP, bool NORM>
 __global__ void __launch_bounds__(kThreads, KU >= 4 ? 2 : 4) adamw_kernel(const __grid_constant__ StepArgs a) {
     agg::griddep_launch_dependents();

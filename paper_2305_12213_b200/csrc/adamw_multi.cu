@@ -40,8 +40,9 @@ bool count_spans(const int64_t* sizes, int32_t T, long long* spans) {
 // instead of reading the K gradients a second time.
 bool stages(int K, db_dtype dt) { return static_cast<size_t>(K) * grad_bytes(dt) > 8; }
 
-// Elements of a record: as many CTA steps, up to eight, as leave 2400 records (16 for each of 148 SMs) where the
-// list has so many.
+// Elements of an 8-bit step's record: as many CTA steps, up to eight, as leave 2400 records (16 for each of 148 SMs)
+// where the list has so many.  A longer run fills its ring less often, but spreads the CTAs' streams (470M
+// parameters, 4, 8, 16, 32 steps: 1536, 1487, 1521, 1577 us; 5M, 1 to 4: 33.6, 31.7, 34.5, 37.7).
 int run_of(long long spans) {
     const long long steps = spans / 2400;
     return kSpan * static_cast<int>(steps < 1 ? 1 : steps > 8 ? 8 : steps);
