@@ -40,12 +40,14 @@ bool count_spans(const int64_t* sizes, int32_t T, long long* spans) {
 // instead of reading the K gradients a second time.
 bool stages(int K, db_dtype dt) { return static_cast<size_t>(K) * grad_bytes(dt) > 8; }
 
-// Elements of an 8-bit step's record: as many CTA steps, up to eight, as leave 2400 records (16 for each of 148 SMs)
-// where the list has so many.  A longer run fills its ring less often, but spreads the CTAs' streams (470M
-// parameters, 4, 8, 16, 32 steps: 1536, 1487, 1521, 1577 us; 5M, 1 to 4: 33.6, 31.7, 34.5, 37.7).
+// Elements of an 8-bit step's record, in CTA steps: one for short lists, two from 2000 steps on (a ring is filled once
+// for both), and up to eight as long as 2400 records are left (16 for each of 148 SMs).  A longer run fills its ring
+// less often, but spreads the CTAs' streams and fills the last wave less evenly (us; 5M parameters, one bf16 gradient,
+// 1, 2, 3 steps: 22.9, 18.5, 17.7; 10M, four fp32, 2, 4, 6: 48.2, 52.3, 50.0; 25M, four fp32, 5, 8: 112.9, 120.3; 470M,
+// one bf16, clipped, 4, 8, 16: 1536, 1487, 1521).
 int run_of(long long spans) {
-    const long long steps = spans / 2400;
-    return kSpan * static_cast<int>(steps < 1 ? 1 : steps > 8 ? 8 : steps);
+    const long long least = spans < 2000 ? 1 : 2;
+    return kSpan * static_cast<int>(std::min<long long>(8, std::max(least, spans / 2400)));
 }
 
 // One kind of records: `run` elements each, `stride` words apart.
