@@ -233,8 +233,8 @@ db_status db_multi_plan_destroy(db_multi_plan* plan);
  * on one plan must not overlap on the device (two captured graphs of steps on one plan
  * neither); a captured step replays its b, lr, step and seed.  The device that is
  * current at the plan's creation has to be current at its steps.
- * A clipped step is two launches (norm, update), one without clipping is one, or two or
- * three with grad_norm.
+ * A step without clipping is one launch (with grad_norm two or three), a clipped one two
+ * on short lists and up to four on long ones (norm, one or two folds, update).
  * ------------------------------------------------------------------------ */
 #define DB_ADAMW_BLOCK 256
 #define DB_ADAMW_CLIP 1u
@@ -271,7 +271,8 @@ db_status db_adamw_plan_destroy(db_adamw_plan* plan);
  * it or use another optimizer.  The aggregate is formed in fp32 as above, squares
  * and their sum in fp64; the sum's order depends on the device and the list alone.
  * Arguments are those of the AdamW plan; grad_norm: device, one float.  Calls on
- * one plan must not overlap on the device.  One launch.
+ * one plan must not overlap on the device.  One launch on short lists, two or three
+ * on long ones.
  * ------------------------------------------------------------------------ */
 typedef struct db_grad_norm_plan db_grad_norm_plan;
 
