@@ -181,11 +181,11 @@ db_status db_multi_plan_destroy(db_multi_plan* plan);
  *     m <- beta1 m + (1 - beta1) h        u <- beta2 u + (1 - beta2) h^2
  *     p <- p (1 - lr wd) - lr (m / (1 - beta1^t)) / (sqrt(u / (1 - beta2^t)) + eps)
  * wd is the tensor's weight decay; p takes m and u before they are rounded to
- * 8 bits; a u below 2^-126 counts as 0 under the root.  All arithmetic is fp32, squares and sum of the norm are fp64.  g adds
- * the rounded products of the workers with b[k] > 0 in four partial sums (every
- * fourth of them, k ascending), joined in order; in m and u every product and sum
- * is rounded on its own, as written.  So they, and with them the 8-bit codes, are
- * the same bits on any device and at any alignment.
+ * 8 bits; a u below 2^-126 counts as 0 under the root.  All arithmetic is fp32,
+ * squares and sum of the norm are fp64.  g adds the rounded products of the workers
+ * with b[k] > 0, k ascending, in order within groups of four, and the groups' sums in
+ * order; in m and u every product and sum is rounded on its own, as written.  So they,
+ * and with them the 8-bit codes, are the same bits on any device and at any alignment.
  *
  *   grads        host array of K*T device pointers, grads[k*T + t] = worker k's
  *                gradient of tensor t (sizes[t] elements of grad_dtype, fp32 or bf16)

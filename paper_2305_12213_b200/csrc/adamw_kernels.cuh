@@ -247,17 +247,9 @@ __device__ __forceinline__ void to_vector(float* buffer, int lane, Pair (&x)[4])
     x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
 }
 
-template <int SUMS>
-__device__ __forceinline__ void join_sums(Pair (&sum)[SUMS][4], Pair one) {
-#pragma unroll
-    for (int j = 1; j < SUMS; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum[0][i] = add(sum[0][i], sum[j][i], one);
-}
-
-// g = sum over the active workers of lambda_k g_k: products rounded to fp32, added in four partial sums (k mod 4,
-// k ascending) that are joined in order.  Shorter chains than one sum, and a pair's product and sum cost what two
-// FMAs do.  KU workers' loads at once; MANY: more than KU workers, in rounds.
+// g = sum over the active workers of lambda_k g_k: products rounded to fp32, added in order within groups of four
+// workers, the groups' sums added in order.  Chains stay short, two sums are all that is held, and a pair's product and
+// sum cost what two FMAs do.  KU workers' loads at once; MANY: more than KU workers, in rounds.
 template <int KU>
 __device__ __forceinline__ void pointers_of(const Source& s, const long long* grads, int k0, long long (&from)[KU]) {
 #pragma unroll
@@ -277,18 +269,19 @@ __device__ __forceinline__ void arrange_round(const Source& s, const long long (
     for (int j = 0; j < KU; ++j)
         if (A == kRows && k0 + j < s.K) raw[j].template arrange<A>(from[j], lane);
 }
-// All workers of a sum that fits one round: partial sum by partial sum.
-template <typename GT, int KU>
-__device__ __forceinline__ void weigh_round(const Source& s, const GradRaw<GT> (&raw)[KU], Pair (&g)[4]) {
+// Adds the round's groups to g; FIRST: g begins with them.
+template <typename GT, int KU, bool FIRST>
+__device__ __forceinline__ void weigh_round(const Source& s, const GradRaw<GT> (&raw)[KU], int k0, Pair (&g)[4]) {
 #pragma unroll
-    for (int j = 0; j < (KU < 4 ? KU : 4); ++j) {
+    for (int j = 0; j < KU; j += 4) {
+        if (j > 0 && k0 + j >= s.K) break;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            Pair x = j < s.K ? mul(s.lambda[j], raw[j].get(i)) : both(-0.0f);                // -0 adds nothing to anything
+            Pair x = mul(s.lambda[k0 + j], raw[j].get(i));
 #pragma unroll
-            for (int l = j + 4; l < KU; l += 4)
-                if (l < s.K) x = add(mul(s.lambda[l], raw[l].get(i)), x, s.one);
-            g[i] = j == 0 ? x : add(x, g[i], s.one);
+            for (int l = j + 1; l < j + 4 && l < KU; ++l)
+                if (k0 + l < s.K) x = add(mul(s.lambda[k0 + l], raw[l].get(i)), x, s.one);
+            g[i] = FIRST && j == 0 ? x : add(x, g[i], s.one);
         }
     }
 }
@@ -301,29 +294,18 @@ __device__ __forceinline__ void aggregate(const Source& s, const long long* grad
         pointers_of<KU>(s, grads, 0, from);
         load_round<GT, KU, A>(s, from, 0, offset, lane, n, raw);
         arrange_round<GT, KU, A>(s, from, 0, lane, raw);
-        weigh_round<GT, KU>(s, raw, g);
+        weigh_round<GT, KU, true>(s, raw, 0, g);
     } else {
-        static_assert(KU % 4 == 0, "worker k belongs to sum k mod 4");
-        Pair sum[4][4];
+        static_assert(KU % 4 == 0, "groups of four workers");
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[j][i] = both(-0.0f);
+        for (int i = 0; i < 4; ++i) g[i] = both(-0.0f);                  // adds nothing to anything
 #pragma unroll 1
         for (int k0 = 0; k0 < s.K; k0 += KU) {
             pointers_of<KU>(s, grads, k0, from);
             load_round<GT, KU, A>(s, from, k0, offset, lane, n, raw);
             arrange_round<GT, KU, A>(s, from, k0, lane, raw);
-#pragma unroll
-            for (int j = 0; j < KU; ++j)
-                if (k0 + j < s.K) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[j & 3][i] = add(mul(s.lambda[k0 + j], raw[j].get(i)), sum[j & 3][i], s.one);
-                }
+            weigh_round<GT, KU, false>(s, raw, k0, g);
         }
-        join_sums<4>(sum, s.one);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) g[i] = sum[0][i];
     }
 }
 
@@ -765,7 +747,6 @@ template <typename GT, int KI, bool MANY, bool CLIP, bool NORM>
 __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_constant__ StepArgs a) {
     using R = Ring<GT, KI>;
     extern __shared__ __align__(16) unsigned char smem[];
-    constexpr int kSums = KI < 4 ? KI : 4;
     agg::griddep_launch_dependents();
     agg::griddep_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -879,7 +860,7 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
     // in it cost 3 to 6 %.
     auto do_block = [&](auto common) {
         constexpr bool kCommon = decltype(common)::value;
-        Pair sum[kSums][4], p[4];
+        Pair sum[4], part[4], p[4];
         uint32_t cm[2], cu[2];
         float2 scales;
         arrive();
@@ -888,10 +869,10 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
         read_codes(from + kSlotCodes + kWarpElems, lane, cu);
         scales = *reinterpret_cast<const float2*>(from + kSlotScales);
         if (!R::kFused) release();
+        if (MANY) {
 #pragma unroll
-        for (int j = 0; j < kSums; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[j][i] = both(-0.0f);                             // adds nothing to anything
+            for (int i = 0; i < 4; ++i) sum[i] = both(-0.0f);                                // adds nothing to anything
+        }
 #pragma unroll 1
         for (int round = 0; round < (MANY ? K : 1); round += KI) {
 #pragma unroll
@@ -900,7 +881,7 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
                 if (!R::kFused) arrive();
 #pragma unroll
                 for (int j = 0; j < R::kItem; ++j) {
-                    const int place = chunk + j, k = MANY ? round + place : place;           // worker k is in sum k mod 4
+                    const int place = chunk + j, k = MANY ? round + place : place;
                     if (MANY ? k < K : place <= KI / 2 || place < K) {
                         Pair x[4];
                         const unsigned int odd = MANY && k >= 32 ? odd_high : odd_low;
@@ -909,19 +890,24 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const Pair y = KI == 1 ? x[i] : mul(w, x[i]);
-                            sum[place % kSums][i] = !MANY && place < kSums ? y : add(y, sum[place % kSums][i], a.src.one);
+                            part[i] = place % 4 == 0 ? y : add(y, part[i], a.src.one);
                         }
                     }
                 }
                 release();
+                // the group of four is complete, or its last workers are missing and so is the item after this one
+                const int next = chunk + R::kItem;
+                if (next % 4 == 0 || next >= KI || (MANY ? round + next : next) >= K) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[i] = !MANY && chunk < 4 ? part[i] : add(part[i], sum[i], a.src.one);
+                }
             }
         }
-        join_sums<kSums>(sum, a.src.one);
-        if (NORM) sq += sum_squares(sum[0]);
+        if (NORM) sq += sum_squares(sum);
         Pair m[4], u[4];
         decode(cm, scales.x, m);
         decode(cu, scales.y, u);
-        update<CLIP>(a, factor, decay, sum[0], p, m, u);
+        update<CLIP>(a, factor, decay, sum, p, m, u);
         float* param = reinterpret_cast<float*>(const_cast<char*>(params)) + offset;
         uint8_t* codes_m = reinterpret_cast<uint8_t*>(const_cast<char*>(first)) + offset;
         uint8_t* codes_u = reinterpret_cast<uint8_t*>(const_cast<char*>(second)) + offset;
@@ -1004,7 +990,7 @@ __device__ __forceinline__ double norm_blocks(const Source& s, const long long* 
             aggregate<GT, KU, true, A>(s, rec + kNormGrads, offset, lane, kWarpElems, g);
         } else {
             arrange_round<GT, KU, A>(s, from, 0, lane, raw[e]);
-            weigh_round<GT, KU>(s, raw[e], g);
+            weigh_round<GT, KU, true>(s, raw[e], 0, g);
         }
         if (staged) {
             if (A == kVector) store_f32<true>(staged + offset, lane, kWarpElems, g);
