@@ -665,16 +665,19 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// A slot of the ring.  Parameters, codes, scales (padded to 16 bytes); a worker's row of gradients, for bf16 with room
-// for the 129th word of a row that starts at an odd element.
+// A slot of the ring.  Parameters, codes, scales (padded to 16 bytes); a worker's row of gradients, with room for the
+// piece by which a row off the 16-byte grid is longer.
 constexpr int kSlotCodes = 4 * kWarpElems, kSlotScales = kSlotCodes + 2 * kWarpElems, kSlotState = kSlotScales + 16;
 template <typename GT, int KI>
 struct Ring {
     static constexpr bool kFused = KI <= 2;                                   // gradients behind the parameters, in one item
     static constexpr int kItem = kFused ? KI : 8 / static_cast<int>(sizeof(GT));                       // workers in an item
-    static constexpr int kRow = static_cast<int>(sizeof(GT)) * kWarpElems + (sizeof(GT) == 2 ? 16 : 0);
+    static constexpr int kRow = static_cast<int>(sizeof(GT)) * kWarpElems, kLongRow = kRow + 16;     // off the grid
     static constexpr int kGrads = kFused ? kSlotState : 0;                    // where an item's gradients begin
-    static constexpr int kSlot = kFused ? kSlotState + KI * kRow : kItem * kRow > kSlotState ? kItem * kRow : kSlotState;
+    // whole lines of 128 bytes: with rows of fp32 16 bytes longer and slots as they came, 110M parameters and 4 workers
+    // took 117 us instead of 113
+    static constexpr int kUsed = kFused ? kSlotState + KI * kLongRow : kItem * kLongRow > kSlotState ? kItem * kLongRow : kSlotState;
+    static constexpr int kSlot = (kUsed + 127) / 128 * 128;
     // two CTAs on an SM; with 104 KB instead of 88, a step behind a norm kernel was slower (25M elements: 98 -> 106 us)
     static constexpr int kMost = (88 << 10) / (kWarps * kSlot);
     static constexpr int kSlots = kMost < 6 ? kMost : 6;
@@ -701,21 +704,23 @@ __device__ __forceinline__ void copy_row(uint32_t to, const GT* from, int lane, 
         else copy_async<16>(to + at, src + at, kSize * n - at);
     }
 }
-// The same off the 16-byte grid, by words.  A bf16 row at an odd element is copied from the word that holds the element
-// before it on and read two bytes further up (129 words; every word has at least one element of the row).
+// The same off the 16-byte grid: shared memory holds the row as far off it as global memory does, so that all but its
+// first piece can be copied 16 bytes at a time.  The first goes by words, the last is cut behind the row; a bf16 row at
+// an odd word half begins with the word that holds the element before it.  Rows copied by words to the grid: ragged 5M,
+// three fp32 gradients, 30.0 us instead of 29.1; 25M, sixteen fp32 365 instead of 314, eight bf16 163 instead of 145.
 template <bool FULL, typename GT>
 __device__ __forceinline__ void copy_row_unaligned(uint32_t to, const GT* from, int lane, int n) {
     constexpr int kSize = static_cast<int>(sizeof(GT)), kBytes = kSize * kWarpElems;
     const uintptr_t address = reinterpret_cast<uintptr_t>(from);
-    const char* words = reinterpret_cast<const char*>(address & ~static_cast<uintptr_t>(3));
-    const int have = kSize * n + static_cast<int>(address & 3);
+    const int off = static_cast<int>(address & 15), have = kSize * n + off;
+    const char* src = reinterpret_cast<const char*>(address - off);
+    if (lane < 4 && 4 * lane + 4 > off) copy_async<4>(to + 4 * lane, src + 4 * lane, have - 4 * lane);
 #pragma unroll
-    for (int i = 0; i < kBytes; i += 128) {
-        const int at = i + 4 * lane;
-        if (FULL) copy_async<4>(to + at, words + at);
-        else copy_async<4>(to + at, words + at, have - at);
+    for (int i = 16; i <= kBytes; i += 512) {
+        const int at = i + 16 * lane;
+        if (FULL && i + 512 < kBytes) copy_async<16>(to + at, src + at);
+        else copy_async<16>(to + at, src + at, have - at);
     }
-    if (kSize == 2 && (address & 2) && lane == 0) copy_async<4>(to + kBytes, words + kBytes, have - kBytes);
 }
 
 // A lane's elements of a slot.
@@ -728,18 +733,48 @@ __device__ __forceinline__ void read_codes(const unsigned char* from, int lane, 
     const uint2 r = reinterpret_cast<const uint2*>(from)[lane];
     x[0] = r.x; x[1] = r.y;
 }
-template <typename GT> __device__ __forceinline__ void read_row(const unsigned char* from, int lane, bool odd, Pair (&x)[4]);
-template <> __device__ __forceinline__ void read_row<float>(const unsigned char* from, int lane, bool, Pair (&x)[4]) { read_pairs(from, lane, x); }
-template <> __device__ __forceinline__ void read_row<__nv_bfloat16>(const unsigned char* from, int lane, bool odd, Pair (&x)[4]) {
-    const uint4 r = reinterpret_cast<const uint4*>(from)[lane];
-    uint32_t w[4] = {r.x, r.y, r.z, r.w};
-    if (odd) {
-        const uint32_t next = reinterpret_cast<const uint32_t*>(from)[4 * lane + 4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __byte_perm(w[i], i < 3 ? w[i + 1] : next, 0x5432);
-    }
+__device__ __forceinline__ void widen(const uint32_t* w, Pair (&x)[4]) {                      // bf16
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = pack(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+}
+template <typename GT>
+__device__ __forceinline__ void read_row(const unsigned char* from, int lane, Pair (&x)[4]) {
+    if constexpr (sizeof(GT) == 4) {
+        read_pairs(from, lane, x);
+    } else {
+        const uint4 r = reinterpret_cast<const uint4*>(from)[lane];
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+        widen(w, x);
+    }
+}
+// A row that begins `off` bytes into its slot (the same for the whole warp).
+template <typename GT>
+__device__ __forceinline__ void read_row_at(const unsigned char* from, int lane, int off, Pair (&x)[4]) {
+    constexpr int kWords = 2 * sizeof(GT);                                                   // of a lane
+    uint32_t w[kWords + 4];
+#pragma unroll
+    for (int i = 0; i < kWords + 4; i += 4) {
+        const uint4 r = reinterpret_cast<const uint4*>(from + 4 * kWords * lane)[i / 4];
+        w[i] = r.x; w[i + 1] = r.y; w[i + 2] = r.z; w[i + 3] = r.w;
+    }
+    if (off & 8) {
+#pragma unroll
+        for (int i = 0; i < kWords + 2; ++i) w[i] = w[i + 2];
+    }
+    if (off & 4) {
+#pragma unroll
+        for (int i = 0; i < kWords + 1; ++i) w[i] = w[i + 1];
+    }
+    if constexpr (sizeof(GT) == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = pack(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    } else {
+        if (off & 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __byte_perm(w[i], w[i + 1], 0x5432);
+        }
+        widen(w, x);
+    }
 }
 
 // One kernel for each number KI of workers (1, 2, 4 or 8, taken for K in (KI / 2, KI]; MANY: more than that, in rounds).
@@ -780,12 +815,6 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
     long long from_low = lane < K ? __ldg(rec + kRecGrads + a.src.worker[lane]) : 0;
     const long long from_high = MANY && other < K ? __ldg(rec + kRecGrads + a.src.worker[other]) : 0;
     if (CLIP && a.src.staged) from_low = reinterpret_cast<long long>(a.src.staged + position);
-    unsigned int odd_low = 0u, odd_high = 0u;                                                // bf16 rows at odd elements
-    if (sizeof(GT) == 2 && !grads_aligned) {
-        odd_low = __ballot_sync(0xffffffffu, from_low & 2);
-        odd_high = __ballot_sync(0xffffffffu, from_high & 2);
-    }
-
     auto copy_item = [&](auto full, int offset, int item, uint32_t to) {
         constexpr bool kFull = decltype(full)::value;
         const int n = kFull ? kWarpElems : count - offset;
@@ -815,7 +844,7 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
 #pragma unroll 1
                 for (int j = 0; j < R::kItem && (R::kFused || k0 + j < K); ++j) {
                     if (grads_aligned) copy_row<false>(to + R::kGrads + j * R::kRow, row(j), lane, n);
-                    else copy_row_unaligned<kFull>(to + R::kGrads + j * R::kRow, row(j), lane, n);
+                    else copy_row_unaligned<kFull>(to + R::kGrads + j * R::kLongRow, row(j), lane, n);
                 }
             }
         }
@@ -856,10 +885,10 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
     const Pair decay = decay_of(a, rec);
     const long long copy = __ldg(rec + kRecCopy);
     int offset = warp * kWarpElems;
-    // A block.  The common one, whole and with its rows at even elements, is a loop of its own: tests for the others
-    // in it cost 3 to 6 %.
-    auto do_block = [&](auto common) {
-        constexpr bool kCommon = decltype(common)::value;
+    // A block.  Whole ones with their rows on the grid, and off it, are loops of their own: tests for the others in the
+    // first cost 3 to 6 %.
+    auto do_block = [&](auto whole_block, auto on_grid) {
+        constexpr bool kWhole = decltype(whole_block)::value, kOnGrid = decltype(on_grid)::value;
         Pair sum[4], part[4], p[4];
         uint32_t cm[2], cu[2];
         float2 scales;
@@ -884,8 +913,12 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
                     const int place = chunk + j, k = MANY ? round + place : place;
                     if (MANY ? k < K : place <= KI / 2 || place < K) {
                         Pair x[4];
-                        const unsigned int odd = MANY && k >= 32 ? odd_high : odd_low;
-                        read_row<GT>(from + R::kGrads + j * R::kRow, lane, !kCommon && odd >> (k & 31) & 1u, x);
+                        if (kOnGrid || (!kWhole && grads_aligned)) {
+                            read_row<GT>(from + R::kGrads + j * R::kRow, lane, x);
+                        } else {
+                            const long long at = __shfl_sync(0xffffffffu, MANY && k >= 32 ? from_high : from_low, k & 31);
+                            read_row_at<GT>(from + R::kGrads + j * R::kLongRow, lane, static_cast<int>(at & 15), x);
+                        }
                         const Pair w = KI == 1 ? 0ull : a.src.lambda[k];                     // a single weight is 1
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
@@ -911,15 +944,14 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
         float* param = reinterpret_cast<float*>(const_cast<char*>(params)) + offset;
         uint8_t* codes_m = reinterpret_cast<uint8_t*>(const_cast<char*>(first)) + offset;
         uint8_t* codes_u = reinterpret_cast<uint8_t*>(const_cast<char*>(second)) + offset;
-        const bool full = kCommon || offset + kWarpElems <= count;
-        if (full) {
+                if (kWhole) {
             store_f32<true>(param, lane, kWarpElems, p);
             if (copy) store_copy<true>(copy, offset, lane, kWarpElems, p);
         }
         encode_moments<true>(a, reinterpret_cast<float*>(const_cast<char*>(first_scale)) + offset / kWarpElems,
                              reinterpret_cast<float*>(const_cast<char*>(second_scale)) + offset / kWarpElems, position + offset,
                              lane, m, u, cm, cu);
-        if (full) {
+        if (kWhole) {
             store_codes<true>(codes_m, lane, kWarpElems, cm);
             store_codes<true>(codes_u, lane, kWarpElems, cu);
         } else {
@@ -935,14 +967,18 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
             }
         }
     };
-    const int common = odd_low | odd_high ? 0 : whole;
+    int block = 0;
+    if (grads_aligned) {
 #pragma unroll 1
-    for (int block = 0; block < common; ++block, offset += kSpan) do_block(std::true_type());
+        for (; block < whole; ++block, offset += kSpan) do_block(std::true_type(), std::true_type());
+    } else {
 #pragma unroll 1
-    for (int block = common; block < blocks; ++block, offset += kSpan) do_block(std::false_type());
+        for (; block < whole; ++block, offset += kSpan) do_block(std::true_type(), std::false_type());
+    }
+    for (; block < blocks; ++block, offset += kSpan) do_block(std::false_type(), std::false_type());
     // tensors off the grid
 #pragma unroll 1
-    for (int block = blocks; block < mine; ++block, offset += kSpan)
+    for (; block < mine; ++block, offset += kSpan)
         sq += step_block_slow<GT, true, CLIP, NORM>(a, rec, offset, lane, min(count - offset, kWarpElems), factor);
     if (NORM) agg::store_norm_partial(a.partials, sq);
 }

@@ -156,6 +156,32 @@ def test_any_alignment_gives_the_same_bits(shift, grad_shift, grad, state8):
     assert abs(n[0].item() - n[1].item()) <= 2 * ref.EPS32 * n[0].item()     # other lanes, other fp32 partial sums of eight
 
 
+@pytest.mark.parametrize("state8", [False, True])
+@pytest.mark.parametrize("grad", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("K", [1, 2, 3, 5, 8, 13, 40])
+def test_every_worker_at_its_own_offset(K, grad, state8):
+    """Worker k's gradients lie k % 9 elements behind an aligned address, between NaNs: the same bits as with all of them
+    aligned, for whole and for shorter blocks."""
+    sizes = SIZES + [7001]
+    a = Problem(sizes, K, grad, state8, 44, copy=True, fresh=False)
+    c = a.clone()
+    c.grads = []
+    for k, rows in enumerate(a.grads):
+        at = 16 + (k + 1) % 9                                        # K = 1: an odd element
+        backs = [torch.full((x.numel() + 48,), math.nan, dtype=grad, device=DEV) for x in rows]
+        c.grads.append([back[at:at + x.numel()].copy_(x) for back, x in zip(backs, rows)])
+    b, n = batches(K), torch.zeros(2, device=DEV)
+    for prob, out in ((a, n[:1]), (c, n[1:])):
+        plan = prob.plan(clip=True)
+        plan.step(b, LR, B1, B2, EPS, 3, seed=8)
+        plan.step(b, LR, B1, B2, EPS, 4, max_norm=1e9, seed=8, grad_norm=out)
+    torch.cuda.synchronize()
+    assert n[0].item() > 0 and abs(n[0].item() - n[1].item()) <= 2 * ref.EPS32 * n[0].item()     # other lanes' fp32 squares
+    for x, y in zip(a.all_tensors(), c.all_tensors()):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)) if x.dtype == E4M3 else torch.equal(x, y)
+    assert all(untouched(x) for x in c.all_tensors())
+
+
 def norm_tolerance(K):
     """Relative bound of the fp32 norm: the aggregate's K roundings act on single elements (at most K 2^-24 (sum of
     magnitudes / magnitude), here about sqrt(K) larger at most), a lane's eight squares 8 2^-24 / 2, the result 2^-24."""
