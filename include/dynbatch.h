@@ -212,8 +212,9 @@ db_status db_multi_plan_destroy(db_multi_plan* plan);
  *                k's buffers are not read
  *   max_norm     0 (no clipping) or the finite bound > 0
  *   seed         DB_E4M3: seed of the stochastic rounding; ignored for DB_F32
- *   grad_norm    device, one float that receives norm (before clipping), or NULL
- *                (no elements in the whole list: nothing is enqueued, it stays)
+ *   grad_norm    device, one float outside the plan's buffers that receives norm
+ *                (before clipping), or NULL (no elements in the whole list: nothing is
+ *                enqueued, it stays)
  *
  * 8-bit moments.  For a block with a = max |x|, s = max(a, 2^-100): scale = s (1/448),
  * y = |x| 448 / s, q = 2^(max(floor(log2 y), -6) - 3), and the code's magnitude is

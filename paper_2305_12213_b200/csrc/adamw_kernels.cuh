@@ -5,7 +5,7 @@
 // scale when the moments are held in 8 bits.  A record in device memory holds the pointers of a run of up to
 // `run` elements (a multiple of 2048, one step of a CTA's eight warps) of one tensor; a CTA takes a record.
 // Lanes own eight consecutive elements (one 32-byte access for fp32, 16 for bf16, 8 for e4m3) where a tensor's states
-// are aligned; its gradients, where they are not, are read by words and handed to their lanes through shared memory.
+// are aligned; its gradients, where they are not, reach their lanes through shared memory.
 // Off that grid, and at a tensor's end, blocks go element by element.  What is computed for an element does not depend
 // on which lane has it.
 //
