@@ -559,7 +559,7 @@ class _ListPlan:
                 raise ValueError("gradient and parameter sizes differ")
         self._grads = (c_void_p * (self.K * self.T))(
             *[p for g in grads for p in self._pointers(g, self.grad_dtype, "grads[k]")])
-        self._b = (c_int32 * self.K)()
+        self._batches = c_int32 * self.K
         self._h = c_void_p()
         self._streams = set()                            # raw handles of the streams that the table is known to be used on
 
@@ -614,8 +614,7 @@ class _ListPlan:
     def _workers(self, b: Sequence[int]):
         if len(b) != self.K:
             raise ValueError("len(b) != K")
-        self._b[:] = b
-        return self._b
+        return self._batches(*b)                         # each call its own: another thread's may be under way
 
     def _scalar(self, t: Optional[torch.Tensor]) -> Optional[int]:
         if t is not None and (t.device != self.device or t.numel() < 1):
