@@ -3,6 +3,7 @@ import ctypes
 import threading
 from types import SimpleNamespace
 
+import numpy as np
 import pytest
 import torch
 
@@ -64,3 +65,19 @@ def test_a_call_keeps_its_batch_sizes_while_another_thread_calls(plans, which):
     b_done.set()
     a.join(10)
     assert seen == {"A": [1, 2, 3], "B": [70, 0, 5]}
+
+@pytest.mark.parametrize("which", [0, 1])
+def test_batch_sizes_of_any_integer_type_and_none_that_does_not_fit(plans, which):
+    got = []
+    plan = plans(2, lambda read: got.append(read()))[which]
+    for b in ([3, 4], (3, 4), np.array([3, 4]), [np.int64(3), np.int32(4)]):
+        _step(plan, b)
+    assert got == [[3, 4]] * 4
+    for bad in ([2**31, 1], [2**32 + 3, 4], [-(2**31) - 1, 1]):         # none is cut to 32 bits and taken
+        with pytest.raises(ValueError):
+            _step(plan, bad)
+    with pytest.raises(TypeError):
+        _step(plan, [1.5, 2])
+    with pytest.raises(ValueError):
+        _step(plan, [1])
+    assert len(got) == 4
