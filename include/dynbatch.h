@@ -233,7 +233,8 @@ db_status db_multi_plan_destroy(db_multi_plan* plan);
  * buffer that a step writes may overlap another one of the plan (DB_ERR_ARG).  Steps
  * on one plan must not overlap on the device (two captured graphs of steps on one plan
  * neither); a captured step replays its b, lr, step and seed.  The device that is
- * current at the plan's creation has to be current at its steps.
+ * current at the plan's creation has to be current at its steps.  Several host threads
+ * may call on one plan at once: each call's launches stay together on its stream.
  * A step without clipping is one launch (with grad_norm two or three), a clipped one two
  * on short lists and up to four on long ones (norm, one or two folds, update).
  * ------------------------------------------------------------------------ */
@@ -272,8 +273,8 @@ db_status db_adamw_plan_destroy(db_adamw_plan* plan);
  * it or use another optimizer.  The aggregate is formed in fp32 as above, squares
  * and their sum in fp64; the sum's order depends on the device and the list alone.
  * Arguments are those of the AdamW plan; grad_norm: device, one float.  Calls on
- * one plan must not overlap on the device.  One launch on short lists, two or three
- * on long ones.
+ * one plan must not overlap on the device; several host threads may make them, as
+ * above.  One launch on short lists, two or three on long ones.
  * ------------------------------------------------------------------------ */
 typedef struct db_grad_norm_plan db_grad_norm_plan;
 

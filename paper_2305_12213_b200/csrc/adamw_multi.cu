@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstdint>
 #include <exception>
+#include <mutex>
 #include <new>
 #include <utility>
 #include <vector>
@@ -292,6 +293,7 @@ struct db_adamw_plan {
     db_dtype grad_dtype = DB_F32, state_dtype = DB_F32;
     int32_t K = 0;
     bool clip = false;
+    std::mutex launches;         // held while a call enqueues, so that no other thread's kernels come between its own
 };
 
 struct db_grad_norm_plan {
@@ -299,6 +301,7 @@ struct db_grad_norm_plan {
     char* table = nullptr;
     db_dtype grad_dtype = DB_F32;
     int32_t K = 0;
+    std::mutex launches;
 };
 
 namespace dynbatch {
@@ -488,6 +491,7 @@ extern "C" db_status db_aggregate_adamw_multi(db_adamw_plan* plan, const int32_t
     a.key1 = static_cast<uint32_t>(z >> 32);
 
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const std::lock_guard<std::mutex> together(plan->launches);
     if (clip) {
         a.norm = grad_norm;
         a.max_norm = max_norm;
@@ -573,6 +577,7 @@ extern "C" db_status db_grad_norm_multi(db_grad_norm_plan* plan, const int32_t* 
     const db_status st = set_workers(b, plan->K, &src);
     if (st != DB_OK) return st;
     if (plan->layout.norm.count == 0) return DB_OK;
+    const std::lock_guard<std::mutex> together(plan->launches);
     return launch_norm(plan->layout, plan->table, plan->grad_dtype, plan->K, src, grad_norm, nullptr, 0.0f, nullptr,
                        static_cast<cudaStream_t>(cuda_stream));
 }
