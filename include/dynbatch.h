@@ -185,7 +185,10 @@ db_status db_multi_plan_destroy(db_multi_plan* plan);
  * squares and sum of the norm are fp64.  g adds the rounded products of the workers
  * with b[k] > 0, k ascending, in order within groups of four, and the groups' sums in
  * order; in m and u every product and sum is rounded on its own, as written.  So they,
- * and with them the 8-bit codes, are the same bits on any device and at any alignment.
+ * and with them the 8-bit codes, are the same bits on any device, at any alignment and
+ * in any cut of a tensor at a multiple of DB_ADAMW_BLOCK: without clipping always, with
+ * it for the same c.  c comes from norm, whose sum has an order of its own (below), and
+ * may differ by one unit in its last place where that order does.
  *
  *   grads        host array of K*T device pointers, grads[k*T + t] = worker k's
  *                gradient of tensor t (sizes[t] elements of grad_dtype, fp32 or bf16)
@@ -222,17 +225,22 @@ db_status db_multi_plan_destroy(db_multi_plan* plan);
  * distance, so that a moving average whose change is far below a code's step still
  * moves, on the average, as it should.  r has 16 random bits: the low (first moment)
  * or high (second moment) half of hash(256 * blocks of the tensors before + index in
- * the tensor), keyed by seed and step; the same seed and step give the same bits
+ * the tensor), keyed by seed and step; the same seed and step give the same r
  * whatever the alignment or the launch.  A second moment > 0 is never stored as
  * code 0 (it gets 2^-9).  A block with a value that is not finite gets a NaN scale
  * and codes 0: NaN and Inf spread to their block of 256.
  *
- * Any alignment down to the element size is accepted; a tensor's accesses are 256-bit
- * wide when its fp32 buffers are 32-byte, its bf16 and 8-bit buffers 16-byte aligned,
- * otherwise element-wise.  Results do not depend on it.  No
+ * Any alignment down to the element size is accepted.  A tensor takes wide accesses
+ * when its fp32 buffers are 32-byte, its bf16 and 8-bit buffers 16-byte aligned.  Where
+ * gradients alone are not, they are read by words or 16-byte pieces (0.7 to 1.0 of the
+ * rate); where a parameter, moment or copy is not, the whole tensor goes element by
+ * element (0.3 to 0.7 of it).  An unaligned bf16 gradient may be read by 4-byte words, of
+ * which the first and the last can hold the element before and behind the buffer: it is
+ * read and dropped, so it may be written meanwhile.  No
  * buffer that a step writes may overlap another one of the plan (DB_ERR_ARG).  Steps
  * on one plan must not overlap on the device (two captured graphs of steps on one plan
- * neither); a captured step replays its b, lr, step and seed.  The device that is
+ * neither); a captured step replays its b, lr, step and seed, and reads the plan's table
+ * at each replay, so table and buffers have to outlive the graph.  The device that is
  * current at the plan's creation has to be current at its steps.  Several host threads
  * may call on one plan at once: each call's launches stay together on its stream.
  * A step without clipping is one launch (with grad_norm two or three), a clipped one two
@@ -271,7 +279,8 @@ db_status db_adamw_plan_destroy(db_adamw_plan* plan);
  *     *grad_norm = sqrt(sum over all tensors and elements of (sum_k lambda_k g_k)^2)
  * What a clipped AdamW step computes first, for callers that log it, decide by
  * it or use another optimizer.  The aggregate is formed in fp32 as above, squares
- * and their sum in fp64; the sum's order depends on the device and the list alone.
+ * and their sum in fp64; the sum's order depends on the device, the list, K, grad_dtype
+ * and the gradients' alignment, so the same call on the same plan gives the same bits.
  * Arguments are those of the AdamW plan; grad_norm: device, one float.  Calls on
  * one plan must not overlap on the device; several host threads may make them, as
  * above.  One launch on short lists, two or three on long ones.

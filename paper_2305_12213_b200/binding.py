@@ -647,6 +647,7 @@ class AdamWPlan(_ListPlan):
     first_moment[t], second_moment[t] all float32, or all float8_e4m3fn with first_scale[t], second_scale[t] of
     adamw_scale_elems(numel) float32 elements; params_bf16[t] optional bfloat16 working copies, weight_decay
     one coefficient for each tensor.  clip: whether steps may pass max_norm > 0.
+    A CUDA graph that holds a step reads the plan's table at each replay: keep the plan as long as the graph.
     """
 
     _destroy = "db_adamw_plan_destroy"
@@ -691,7 +692,8 @@ class AdamWPlan(_ListPlan):
 
 
 class GradNormPlan(_ListPlan):
-    """db_grad_norm_plan: the global norm of the workers' weighted gradient over a fixed list of tensors."""
+    """db_grad_norm_plan: the global norm of the workers' weighted gradient over a fixed list of tensors.  A CUDA graph that
+    holds a call reads the plan's table at each replay: keep the plan as long as the graph."""
 
     _destroy = "db_grad_norm_plan_destroy"
 

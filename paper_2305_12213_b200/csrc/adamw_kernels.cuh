@@ -6,11 +6,13 @@
 // `run` elements (a multiple of 2048, one step of a CTA's eight warps) of one tensor; a CTA takes a record.
 // Lanes own eight consecutive elements (one 32-byte access for fp32, 16 for bf16, 8 for e4m3) where a tensor's states
 // are aligned; its gradients, where they are not, reach their lanes through shared memory.
-// Off that grid, and at a tensor's end, blocks go element by element.  What is computed for an element does not depend
-// on which lane has it.
+// A tensor whose states are off that grid goes element by element, and so does its last, shorter block (with 8-bit
+// moments and aligned states that block comes through the ring like the others).  What is computed for an element does
+// not depend on which lane has it.
 //
-// All three kernels are bound by the memory (a parameter costs K gradients + 24 bytes with 32-bit moments, + 12 with
-// 8-bit ones, and 50 to 60 instructions).  Measured on B200, bytes counted once, against its copy rate of 6.56 TB/s:
+// All three kernels are bound by the memory: a parameter costs K gradients + 24 bytes with 32-bit moments (19 instructions
+// for one worker, 37 for eight), + 12 with 8-bit ones (55 and 97); the norm K gradients alone (101 for sixteen workers).
+// Measured on B200, bytes counted once, against its copy rate of 6.56 TB/s:
 //   32-bit, 470M parameters, one bf16 gradient, bf16 copy   1951 us   6.72 TB/s   1.03
 //   32-bit, 25.6M, eight fp32 gradients                      213 us   6.72 TB/s   1.02
 //    8-bit, 116M, one bf16 gradient, bf16 copy               289 us   6.44 TB/s   0.98
@@ -50,7 +52,9 @@ constexpr int kStateAligned = 1, kGradsAligned = 2;              // flags: buffe
 // evicted them, and a CTA that meets its record in DRAM starts 0.5 us later (norm of 110M, 16 workers: 692 -> 611 us).
 constexpr long long kAhead = 512;
 // Partials that a clipped step adds itself, every warp for itself, which takes the fold off the chain norm - fold - step
-// (20,000 parameters: 8.9 -> 6.6 us); with more of them the reads cost more than the launch.
+// (replayed, us, against the fold in the norm kernel's last CTA or behind it: 20,000 parameters 6.4 and 7.5; 246 partials
+// 11.4 and 12.1; 490 from one fp32 gradient 18.7 and 16.7, from four 10.7 and 11.8 with 8-bit moments, 12.2 and 12.4 with
+// 32-bit ones; 734 26.5 and 20.8); with more of them the reads cost more than the launch.
 constexpr int kFoldInStep = 512;
 
 struct Source {                  // where the weighted gradient comes from
@@ -324,7 +328,9 @@ __device__ __forceinline__ double sum_squares(const Pair (&g)[4]) {
 
 // ---- 8-bit moments --------------------------------------------------------------------------------
 // 32 random bits for an element: two rounds of a 32 x 32 -> 64-bit multiply whose halves are folded together,
-// keyed by the call's seed and step.
+// keyed by the call's seed and step.  The multipliers are odd constants; 0xAC4C1B51 is one of Wellons' triple32 mixer,
+// 0x85EBCA6B (the position's high word) one of Appleby's MurmurHash3 finalizer.  Bias and evenness of both halves are
+// tested, not taken from them.
 __device__ __forceinline__ uint32_t fold_multiply(uint32_t x, uint32_t m) {
     const uint64_t z = static_cast<uint64_t>(x) * m;
     return static_cast<uint32_t>(z >> 32) ^ static_cast<uint32_t>(z);
@@ -674,7 +680,7 @@ struct Ring {
     static constexpr int kItem = kFused ? KI : 8 / static_cast<int>(sizeof(GT));                       // workers in an item
     static constexpr int kRow = static_cast<int>(sizeof(GT)) * kWarpElems, kLongRow = kRow + 16;     // off the grid
     static constexpr int kGrads = kFused ? kSlotState : 0;                    // where an item's gradients begin
-    // whole lines of 128 bytes: with rows of fp32 16 bytes longer and slots as they came, 110M parameters and 4 workers
+    // whole lines of 128 bytes: with rows of fp32 16 bytes longer and slots as they came, 25M parameters and 4 workers
     // took 117 us instead of 113
     static constexpr int kUsed = kFused ? kSlotState + KI * kLongRow : kItem * kLongRow > kSlotState ? kItem * kLongRow : kSlotState;
     static constexpr int kSlot = (kUsed + 127) / 128 * 128;
@@ -944,7 +950,7 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
         float* param = reinterpret_cast<float*>(const_cast<char*>(params)) + offset;
         uint8_t* codes_m = reinterpret_cast<uint8_t*>(const_cast<char*>(first)) + offset;
         uint8_t* codes_u = reinterpret_cast<uint8_t*>(const_cast<char*>(second)) + offset;
-                if (kWhole) {
+        if (kWhole) {
             store_f32<true>(param, lane, kWarpElems, p);
             if (copy) store_copy<true>(copy, offset, lane, kWarpElems, p);
         }
@@ -984,11 +990,10 @@ __global__ void __launch_bounds__(kThreads, 2) adamw8_kernel(const __grid_consta
 }
 
 // ---- the norm of the weighted gradient ------------------------------------------------------------------
-// A CTA takes a record of norm_batch CTA steps, all of whose loads are in flight at once (32 to 64 KB of gradients);
-// with a staging buffer it also leaves the aggregates there, for the step that follows.
+// Two CTAs of 128 threads share a record of norm_batch CTA steps of 256; all loads of a CTA are in flight at once (16 to
+// 32 KB of gradients); with a staging buffer it also leaves the aggregates there, for the step that follows.
 // LAST: the CTA that arrives last adds all partials, in order, which saves a launch; on grids of many waves the
-// fence and the atomic at every CTA's end cost more than it,
-// and a fold kernel follows instead.
+// fence and the atomic at every CTA's end cost more than it, and a fold kernel follows instead.
 
 // Blocks of a warp whose loads are in flight at once, by the registers that they take (32 to 64).
 template <typename GT>

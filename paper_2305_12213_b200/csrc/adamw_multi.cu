@@ -1,6 +1,7 @@
 // AdamW over a list of parameter tensors for K workers' batch-weighted gradients, moments in 32 or 8 bits, with
 // optional clipping by the global norm; and that norm alone.  A plan holds records in device memory, as for the
-// momentum step over a list; each step is one launch, two when it clips (norm of the aggregate, update).
+// momentum step over a list; a step is one launch (and one or two folds where it leaves the norm), two to four when it
+// clips: norm of the aggregate, on long lists one or two folds, update.
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
@@ -45,7 +46,9 @@ bool stages(int K, db_dtype dt) { return static_cast<size_t>(K) * grad_bytes(dt)
 // for both), and up to eight as long as 2400 records are left (16 for each of 148 SMs).  A longer run fills its ring
 // less often, but spreads the CTAs' streams and fills the last wave less evenly (us; 5M parameters, one bf16 gradient,
 // 1, 2, 3 steps: 22.9, 18.5, 17.7; 10M, four fp32, 2, 4, 6: 48.2, 52.3, 50.0; 25M, four fp32, 5, 8: 112.9, 120.3; 470M,
-// one bf16, clipped, 4, 8, 16: 1536, 1487, 1521).
+// one bf16, clipped, 4, 8, 16: 1536, 1487, 1521).  One step against two about 2000 of them (replayed, over buffers beyond
+// the L2): at 600 steps one bf16 gradient 7.3 and 7.0, three fp32 9.3 and 10.0, eight bf16 10.7 and 11.4; at 1000 10.8 and
+// 9.5, 13.8 and 12.7, 15.8 and 14.6; at 2000 18.6 and 15.5, 23.5 and 22.2, 27.1 and 25.7: two would do from 1000 on.
 int run_of(long long spans) {
     const long long least = spans < 2000 ? 1 : 2;
     return kSpan * static_cast<int>(std::min<long long>(8, std::max(least, spans / 2400)));
@@ -222,6 +225,11 @@ db_status launch_norm(const Layout& L, char* table, db_dtype dt, int workers, So
     a.factor = factor;
     a.max_norm = max_norm;
     const long long grid = 2 * L.norm.count;
+    // The norm kernel's last CTA adds the partials on grids of about a wave, which saves a launch where the host bounds the
+    // call: norms of 20k and 1M elements, one fp32 gradient, 5.1 and 5.4 us a call against 7.0 and 7.1 with a fold kernel;
+    // 1M, three gradients, 6.3 against 7.0; at the limit (4.5M, one; 1.1M, four) 7.5 against 7.3 and 8.2 against 7.6.  On the
+    // device alone (replayed) the fold kernel takes 0.4 to 1.1 us less at all of these; beyond the limit the last CTA costs
+    // another 2 to 5.
     const bool leave = left && grid <= kFoldInStep, last = !leave && grid <= 8 * sm_count();
     if (left) *left = leave ? static_cast<int>(grid) : 0;
     // by the plan's workers, not the call's: the records are made for that kernel

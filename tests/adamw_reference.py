@@ -22,8 +22,9 @@ def weights(b):
 
 
 def aggregate(grads, b):
-    """(g, bound): the weighted sum of the workers that have samples, and what a chain of fp32 FMAs may be off:
-    one rounding of a partial sum, at most the sum of magnitudes, for each worker."""
+    """(g, bound): the weighted sum of the workers that have samples, and what fp32 may be off: a product is rounded, then
+    the sums of its group of four (three at most), then the groups' sums (one for each four workers), so that n workers'
+    products are rounded n times at most (a single worker's weight is 1), each time by 2^-24 of the sum of magnitudes."""
     act = [(w, widen(g)) for w, g, n in zip(weights(b), grads, b) if n > 0]
     g = sum(w * x for w, x in act)
     size = sum(w * np.abs(x) for w, x in act)
