@@ -48,7 +48,7 @@ typedef enum {
 typedef enum {
     DB_F32 = 0,  /* IEEE binary32 */
     DB_BF16 = 1, /* bfloat16 (upper half of a binary32) */
-    DB_E4M3 = 2  /* 8-bit float, 4 exponent and 3 mantissa bits, largest value 448 (moments of AdamW only) */
+    DB_E4M3 = 2  /* 8-bit float, 4 exponent and 3 mantissa bits, largest value 448 (moments of AdamW, activations kept for a backward pass) */
 } db_dtype;
 
 /* Largest number of workers one call combines. */
@@ -525,6 +525,126 @@ db_status db_contract_f32(const float* A, int64_t a_row, int64_t a_k,
                           float* out, int64_t o_m, int64_t o_n, int32_t M,
                           int32_t N, int32_t K, int32_t* status,
                           void* cuda_stream);
+
+/* ------------------------------------------------------------------------
+ * Layers: a linear layer, a gated feed-forward block      (Section 3.1: the
+ * gradients that Eq. 2 weighs; the paper's workers get them from a framework)
+ *
+ * A worker's forward and backward pass through the layers that a language
+ * model consists of, for any number of rows (tokens of the worker's batch,
+ * which the controller changes).  Operands are bf16 (e.g. the working copy
+ * params_bf16 of an AdamW plan), products run on the tensor cores with fp32
+ * accumulation, everything up to the one rounding of an output is fp32; the
+ * gradients, bf16 or fp32, are what the aggregation takes.
+ *
+ * db_linear:            z = x w + bias,   y = act(z) + residual
+ * db_linear_grad:       dz = dy act'(z);  dx = dz w^T + dx_addend;
+ *                       dw = x^T dz;  dbias = column sums of dz
+ * db_gated_ffn:         gate = x w_gate,  up = x w_up,
+ *                       h = act(gate) up,  y = h w_down + residual
+ * db_gated_ffn_grad:    dh = dy w_down^T;  d_gate = dh up act'(gate),
+ *                       d_up = dh act(gate);
+ *                       dx = d_gate w_gate^T + d_up w_up^T + dx_addend;
+ *                       dw_gate = x^T d_gate;  dw_up = x^T d_up;  dw_down = h^T dy
+ *
+ * act is one of db_activation: none, max(z, 0) with slope 0 at 0, z P(z) with P the
+ * normal distribution function, z / (1 + e^-z).
+ *
+ * What is kept for the backward pass (z; gate and up) is written by the forward
+ * call, where wanted, as bf16 or as 8-bit checkpoints (below): rounded from the
+ * fp32 values, while y is computed from the values before that rounding.  The
+ * backward pass takes z, gate and up as they were kept; h is formed again from
+ * them.  dz, h, d_gate and d_up are rounded to bf16 on their way into the next
+ * product, since bf16 operands are what the tensor cores take at this rate.
+ *
+ *   x, dy, residual, dx_addend, y, dx   device, [rows, features] bf16, consecutive
+ *                elements in a row, *_pitch >= features elements from row to row
+ *   w            device, [n_in, n_out] row-major bf16 (w_gate, w_up: [width, hidden],
+ *                w_down: [hidden, width])
+ *   bias         device, n_out bf16, or NULL
+ *   residual     NULL: none; may be y itself with y's pitch (then updated in place)
+ *   z, gate, up  device, [rows, n_out] ([rows, hidden]) contiguous, DB_BF16 or DB_E4M3.
+ *                Forward: NULL keeps nothing (gate and up: both or neither).
+ *                Backward: required (z only if act is not DB_ACT_NONE)
+ *   z_scale, gate_scale, up_scale   device, [rows, ceil(n_out / 32)] bytes; DB_E4M3 only
+ *   dx, dw, dbias, dw_*   NULL: not wanted (one at least is); dw, dbias contiguous of
+ *                grad_dtype (DB_F32, DB_BF16); dx is bf16
+ *   dx_addend    added to dx, e.g. dy where the layer's input was also its residual;
+ *                NULL: none; may be dx itself with dx's pitch
+ *   rows         0 .. 2^30; 0: outputs of no rows, weight gradients zero
+ *   n_in, n_out, width, hidden   1 .. 2^24; a matrix has at most 2^40 elements
+ *   workspace    device scratch of >= the *_workspace_bytes of the same sizes (0 for
+ *                invalid ones), 256-byte aligned, uninitialised.  aligned != 0: every
+ *                operand (x, dy, weights) starts at a multiple of 16 bytes and has a pitch
+ *                of a multiple of 8; otherwise, and for feature counts that are not
+ *                multiples of 8, room for copies on that grid is included and made use
+ *                of.  Its first 32-bit word is a status word, as for db_worker_grad_ex.
+ *                The query depends on the current device's number of SMs.
+ *
+ * Buffers that a call writes must not overlap any other it touches, but as said above
+ * (DB_ERR_ARG).  Any alignment down to the element size is accepted; outputs with
+ * 16-byte aligned rows take wide stores.  NaN and Inf in a row of x stay in that row of
+ * y; in a weight gradient they spread to their feature.  The order of every sum depends
+ * on sizes and device alone: the same call gives the same bits.  fp32 weight gradients:
+ * adding into the accumulator truncates (up to about 4e-9 * rows, relative, towards
+ * zero).  Calls on one stream may share a workspace, calls that may overlap on the device
+ * (captured graphs of such calls too) need distinct ones.  Launches: forward 1 (linear), 2
+ * (block), backward 2 to 4 (linear), 3 (block), one more for each product whose reduction is
+ * split and for each operand off the grid; rows = 0: memsets.
+ * ------------------------------------------------------------------------ */
+typedef enum {
+    DB_ACT_NONE = 0,
+    DB_ACT_RELU = 1,
+    DB_ACT_GELU = 2,
+    DB_ACT_SILU = 3
+} db_activation;
+
+size_t db_linear_workspace_bytes(int64_t rows, int32_t n_in, int32_t n_out,
+                                 int32_t aligned);
+db_status db_linear(const void* x, int64_t x_pitch, const void* w,
+                    const void* bias, const void* residual,
+                    int64_t residual_pitch, db_activation act, int64_t rows,
+                    int32_t n_in, int32_t n_out, void* y, int64_t y_pitch,
+                    void* z, void* z_scale, db_dtype z_dtype, void* workspace,
+                    size_t workspace_bytes, void* cuda_stream);
+
+size_t db_linear_grad_workspace_bytes(int64_t rows, int32_t n_in,
+                                      int32_t n_out, int32_t aligned);
+db_status db_linear_grad(const void* dy, int64_t dy_pitch, const void* x,
+                         int64_t x_pitch, const void* w, const void* z,
+                         const void* z_scale, db_dtype z_dtype,
+                         db_activation act, int64_t rows, int32_t n_in,
+                         int32_t n_out, void* dx, int64_t dx_pitch,
+                         const void* dx_addend, int64_t dx_addend_pitch,
+                         void* dw, void* dbias, db_dtype grad_dtype,
+                         void* workspace, size_t workspace_bytes,
+                         void* cuda_stream);
+
+size_t db_gated_ffn_workspace_bytes(int64_t rows, int32_t width,
+                                    int32_t hidden, int32_t aligned);
+db_status db_gated_ffn(const void* x, int64_t x_pitch, const void* w_gate,
+                       const void* w_up, const void* w_down,
+                       const void* residual, int64_t residual_pitch,
+                       db_activation act, int64_t rows, int32_t width,
+                       int32_t hidden, void* y, int64_t y_pitch, void* gate,
+                       void* up, void* gate_scale, void* up_scale,
+                       db_dtype kept_dtype, void* workspace,
+                       size_t workspace_bytes, void* cuda_stream);
+
+size_t db_gated_ffn_grad_workspace_bytes(int64_t rows, int32_t width,
+                                         int32_t hidden, int32_t aligned);
+db_status db_gated_ffn_grad(const void* dy, int64_t dy_pitch, const void* x,
+                            int64_t x_pitch, const void* w_gate,
+                            const void* w_up, const void* w_down,
+                            const void* gate, const void* up,
+                            const void* gate_scale, const void* up_scale,
+                            db_dtype kept_dtype, db_activation act,
+                            int64_t rows, int32_t width, int32_t hidden,
+                            void* dx, int64_t dx_pitch, const void* dx_addend,
+                            int64_t dx_addend_pitch, void* dw_gate,
+                            void* dw_up, void* dw_down, db_dtype grad_dtype,
+                            void* workspace, size_t workspace_bytes,
+                            void* cuda_stream);
 
 /* ------------------------------------------------------------------------
  * Proportional batch-size controller, host side   (Section 3.3, Eq. 4-5)

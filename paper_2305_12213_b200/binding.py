@@ -23,6 +23,8 @@ DB_MAX_K = 64
 DB_STATIC_SCRATCH_BYTES = 1 << 20     # the built-in scratch of aggregate_update_static
 DB_ADAMW_BLOCK = 256                  # elements that share a scale of an 8-bit moment
 DB_ADAMW_CLIP = 1
+DB_ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+DB_CHECKPOINT_GROUP = 32              # values of a row that share a scale of an 8-bit checkpoint
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "csrc", "libdynbatch.so")
 
@@ -95,6 +97,22 @@ _SIGNATURES = {
                                        c_void_p, c_int32]),
     "db_controller_observe": (c_int32, [c_void_p, c_void_p, c_void_p, c_void_p]),
     "db_controller_destroy": (c_int32, [c_void_p]),
+    "db_linear_workspace_bytes": (c_size_t, [c_int64, c_int32, c_int32, c_int32]),
+    "db_linear": (c_int32, [c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_int32, c_int64, c_int32, c_int32,
+                            c_void_p, c_int64, c_void_p, c_void_p, c_int32, c_void_p, c_size_t, c_void_p]),
+    "db_linear_grad_workspace_bytes": (c_size_t, [c_int64, c_int32, c_int32, c_int32]),
+    "db_linear_grad": (c_int32, [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int32, c_int32,
+                                 c_int64, c_int32, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p,
+                                 c_int32, c_void_p, c_size_t, c_void_p]),
+    "db_gated_ffn_workspace_bytes": (c_size_t, [c_int64, c_int32, c_int32, c_int32]),
+    "db_gated_ffn": (c_int32, [c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_int32, c_int64,
+                               c_int32, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int32,
+                               c_void_p, c_size_t, c_void_p]),
+    "db_gated_ffn_grad_workspace_bytes": (c_size_t, [c_int64, c_int32, c_int32, c_int32]),
+    "db_gated_ffn_grad": (c_int32, [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                    c_void_p, c_void_p, c_int32, c_int32, c_int64, c_int32, c_int32, c_void_p, c_int64,
+                                    c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_size_t,
+                                    c_void_p]),
     "db_status_string": (c_char_p, [c_int32]),
     "db_last_cuda_error": (c_char_p, []),
 }
@@ -713,3 +731,208 @@ class GradNormPlan(_ListPlan):
 def adamw_scale_elems(n: int) -> int:
     """Scales of an 8-bit moment of n elements: one for each DB_ADAMW_BLOCK."""
     return -(-int(n) // DB_ADAMW_BLOCK)
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# layers: a call's tensors share one device, which is made current for it
+# ---------------------------------------------------------------------------------------------------------------
+class _Call:
+    """Collects the arguments of a layer call: every tensor is on the device of the first one."""
+
+    def __init__(self, first: torch.Tensor):
+        if not first.is_cuda:
+            raise TypeError("the tensors of a layer must be CUDA tensors")
+        self.device = first.device
+
+    def _here(self, t: torch.Tensor, name: str) -> None:
+        if t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, the call's first tensor on {self.device}")
+
+    def rows(self, t: Optional[torch.Tensor], rows: int, cols: int, name: str, dtype: torch.dtype = torch.bfloat16):
+        """Pointer and pitch of a [rows, cols] tensor whose rows are contiguous."""
+        if t is None:
+            return None, 0
+        self._here(t, name)
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}")
+        if tuple(t.shape) != (rows, cols):
+            raise ValueError(f"{name} must be [{rows}, {cols}]")
+        pitch = t.stride(0) if rows > 1 else cols
+        if (cols > 1 and t.stride(1) != 1) or pitch < cols:
+            raise ValueError(f"the rows of {name} must be contiguous and may not overlap")
+        return t.data_ptr(), pitch
+
+    def whole(self, t: Optional[torch.Tensor], shape, dtype: torch.dtype, name: str):
+        """Pointer of a contiguous tensor."""
+        if t is None:
+            return None
+        self._here(t, name)
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} must be {list(shape)}")
+        return _dev_ptr(t, dtype, name)
+
+    def kept(self, t: Optional[torch.Tensor], scale: Optional[torch.Tensor], rows: int, cols: int, name: str):
+        """Pointers and type of a tensor kept for the backward pass."""
+        if t is None:
+            return None, None, DB_BF16
+        if t.dtype == torch.float8_e4m3fn:
+            if scale is None:
+                raise ValueError(f"{name} in 8 bits needs {name}_scale")
+            return (self.whole(t, (rows, cols), t.dtype, name),
+                    self.whole(scale, (rows, checkpoint_scales(cols)), torch.float8_e8m0fnu, name + "_scale"), DB_E4M3)
+        return self.whole(t, (rows, cols), torch.bfloat16, name), None, DB_BF16
+
+    def grads(self, named, dtype=None):
+        """Pointers and common type of the wanted weight gradients: named = [(tensor, shape, name), ...]."""
+        for t, _, name in named:
+            if t is not None:
+                if dtype is not None and t.dtype != dtype:
+                    raise TypeError("weight gradients must have one type")
+                dtype = t.dtype
+        code = DB_BF16 if dtype is None else _dtype_code(dtype)
+        return [self.whole(t, shape, dtype, name) for t, shape, name in named], code
+
+    def workspace(self, t: torch.Tensor):
+        self._here(t, "workspace")
+        return t.data_ptr(), t.numel() * t.element_size()
+
+    def __call__(self, fn, *args, stream: Optional[torch.cuda.Stream] = None) -> None:
+        index = self.device.index
+        handle = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+        if torch.cuda.current_device() == index:
+            _check(fn(*args, handle))
+        else:
+            with torch.cuda.device(self.device):
+                _check(fn(*args, handle))
+
+
+def _activation(name: str) -> int:
+    try:
+        return DB_ACTIVATIONS[name]
+    except KeyError:
+        raise ValueError(f"activation must be one of {sorted(DB_ACTIVATIONS)}") from None
+
+
+def checkpoint_scales(n: int) -> int:
+    """Scales of a row of n values of an 8-bit checkpoint."""
+    return -(-int(n) // DB_CHECKPOINT_GROUP)
+
+
+def linear_workspace_bytes(rows: int, n_in: int, n_out: int, aligned: bool = True) -> int:
+    return int(lib().db_linear_workspace_bytes(int(rows), int(n_in), int(n_out), int(aligned)))
+
+
+def linear_grad_workspace_bytes(rows: int, n_in: int, n_out: int, aligned: bool = True) -> int:
+    return int(lib().db_linear_grad_workspace_bytes(int(rows), int(n_in), int(n_out), int(aligned)))
+
+
+def gated_ffn_workspace_bytes(rows: int, width: int, hidden: int, aligned: bool = True) -> int:
+    return int(lib().db_gated_ffn_workspace_bytes(int(rows), int(width), int(hidden), int(aligned)))
+
+
+def gated_ffn_grad_workspace_bytes(rows: int, width: int, hidden: int, aligned: bool = True) -> int:
+    return int(lib().db_gated_ffn_grad_workspace_bytes(int(rows), int(width), int(hidden), int(aligned)))
+
+
+def linear(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, workspace: torch.Tensor, bias: Optional[torch.Tensor] = None,
+           residual: Optional[torch.Tensor] = None, activation: str = "none", z: Optional[torch.Tensor] = None,
+           z_scale: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """db_linear: y = activation(x w + bias) + residual, bfloat16.
+
+    x [rows, n_in], y and residual [rows, n_out] may be slices of wider tensors (contiguous rows); w [n_in, n_out].
+    z receives x w + bias for the backward pass: bfloat16, or float8_e4m3fn with z_scale [rows, checkpoint_scales(n_out)]
+    (float8_e8m0fnu).  workspace: uint8, linear_workspace_bytes(...) bytes.
+    """
+    call = _Call(x)
+    rows, n_in = x.shape
+    n_out = w.shape[-1]
+    xp, x_pitch = call.rows(x, rows, n_in, "x")
+    rp, r_pitch = call.rows(residual, rows, n_out, "residual")
+    yp, y_pitch = call.rows(y, rows, n_out, "y")
+    zp, sp, zt = call.kept(z, z_scale, rows, n_out, "z")
+    call(lib().db_linear, xp, x_pitch, call.whole(w, (n_in, n_out), torch.bfloat16, "w"),
+         call.whole(bias, (n_out,), torch.bfloat16, "bias"), rp, r_pitch, _activation(activation), rows, n_in, n_out, yp,
+         y_pitch, zp, sp, zt, *call.workspace(workspace), stream=stream)
+
+
+def linear_grad(dy: torch.Tensor, x: Optional[torch.Tensor], w: torch.Tensor, workspace: torch.Tensor,
+                z: Optional[torch.Tensor] = None, z_scale: Optional[torch.Tensor] = None, activation: str = "none",
+                dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
+                dx_addend: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """db_linear_grad: the wanted ones of dx (+ dx_addend), dw and dbias; z as db_linear kept it (needed with an
+    activation).  dw and dbias are both float32 or both bfloat16; x is needed for dw.
+    workspace: linear_grad_workspace_bytes(...) bytes."""
+    call = _Call(dy)
+    n_in, n_out = w.shape
+    rows = dy.shape[0]
+    dyp, dy_pitch = call.rows(dy, rows, n_out, "dy")
+    xp, x_pitch = call.rows(x, rows, n_in, "x")
+    dxp, dx_pitch = call.rows(dx, rows, n_in, "dx")
+    ap, a_pitch = call.rows(dx_addend, rows, n_in, "dx_addend")
+    zp, sp, zt = call.kept(z, z_scale, rows, n_out, "z")
+    (dwp, dbp), code = call.grads([(dw, (n_in, n_out), "dw"), (dbias, (n_out,), "dbias")])
+    call(lib().db_linear_grad, dyp, dy_pitch, xp, x_pitch, call.whole(w, (n_in, n_out), torch.bfloat16, "w"), zp, sp, zt,
+         _activation(activation), rows, n_in, n_out, dxp, dx_pitch, ap, a_pitch, dwp, dbp, code,
+         *call.workspace(workspace), stream=stream)
+
+
+def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, y: torch.Tensor,
+              workspace: torch.Tensor, residual: Optional[torch.Tensor] = None, activation: str = "silu",
+              gate: Optional[torch.Tensor] = None, up: Optional[torch.Tensor] = None,
+              gate_scale: Optional[torch.Tensor] = None, up_scale: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> None:
+    """db_gated_ffn: y = (activation(x w_gate) * (x w_up)) w_down + residual, bfloat16.
+
+    x, y, residual [rows, width] may be slices of wider tensors; w_gate, w_up [width, hidden], w_down [hidden, width].
+    gate and up receive x w_gate and x w_up for the backward pass, both bfloat16 or both float8_e4m3fn with their scales
+    [rows, checkpoint_scales(hidden)].  workspace: gated_ffn_workspace_bytes(...) bytes.
+    """
+    call = _Call(x)
+    rows, width = x.shape
+    hidden = w_gate.shape[-1]
+    bf16 = torch.bfloat16
+    xp, x_pitch = call.rows(x, rows, width, "x")
+    rp, r_pitch = call.rows(residual, rows, width, "residual")
+    yp, y_pitch = call.rows(y, rows, width, "y")
+    gp, gs, gt = call.kept(gate, gate_scale, rows, hidden, "gate")
+    upp, us, ut = call.kept(up, up_scale, rows, hidden, "up")
+    if gate is not None and up is not None and gt != ut:
+        raise TypeError("gate and up must have one type")
+    call(lib().db_gated_ffn, xp, x_pitch, call.whole(w_gate, (width, hidden), bf16, "w_gate"),
+         call.whole(w_up, (width, hidden), bf16, "w_up"), call.whole(w_down, (hidden, width), bf16, "w_down"), rp, r_pitch,
+         _activation(activation), rows, width, hidden, yp, y_pitch, gp, upp, gs, us, gt, *call.workspace(workspace),
+         stream=stream)
+
+
+def gated_ffn_grad(dy: torch.Tensor, x: Optional[torch.Tensor], w_gate: torch.Tensor, w_up: torch.Tensor,
+                   w_down: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, workspace: torch.Tensor,
+                   gate_scale: Optional[torch.Tensor] = None, up_scale: Optional[torch.Tensor] = None,
+                   activation: str = "silu", dx: Optional[torch.Tensor] = None, dw_gate: Optional[torch.Tensor] = None,
+                   dw_up: Optional[torch.Tensor] = None, dw_down: Optional[torch.Tensor] = None,
+                   dx_addend: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """db_gated_ffn_grad: the wanted ones of dx (+ dx_addend), dw_gate, dw_up and dw_down; gate and up as db_gated_ffn kept
+    them.  The weight gradients have one type, float32 or bfloat16; x is needed for dw_gate and dw_up.
+    workspace: gated_ffn_grad_workspace_bytes(...) bytes."""
+    call = _Call(dy)
+    width, hidden = w_gate.shape
+    rows = dy.shape[0]
+    bf16 = torch.bfloat16
+    dyp, dy_pitch = call.rows(dy, rows, width, "dy")
+    xp, x_pitch = call.rows(x, rows, width, "x")
+    dxp, dx_pitch = call.rows(dx, rows, width, "dx")
+    ap, a_pitch = call.rows(dx_addend, rows, width, "dx_addend")
+    gp, gs, gt = call.kept(gate, gate_scale, rows, hidden, "gate")
+    upp, us, ut = call.kept(up, up_scale, rows, hidden, "up")
+    if gt != ut:
+        raise TypeError("gate and up must have one type")
+    (dgp, dup, ddp), code = call.grads([(dw_gate, (width, hidden), "dw_gate"), (dw_up, (width, hidden), "dw_up"),
+                                        (dw_down, (hidden, width), "dw_down")])
+    call(lib().db_gated_ffn_grad, dyp, dy_pitch, xp, x_pitch, call.whole(w_gate, (width, hidden), bf16, "w_gate"),
+         call.whole(w_up, (width, hidden), bf16, "w_up"), call.whole(w_down, (hidden, width), bf16, "w_down"), gp, upp, gs, us,
+         gt, _activation(activation), rows, width, hidden, dxp, dx_pitch, ap, a_pitch, dgp, dup, ddp, code,
+         *call.workspace(workspace), stream=stream)
+
+
+def layer_status(workspace: torch.Tensor) -> int:
+    """The status word at the start of a layer call's workspace (0 = every internal wait completed)."""
+    return int(workspace[:4].view(torch.int32).item())

@@ -1,0 +1,901 @@
+// The layers whose gradients the workers send: linear layer and gated feed-forward block, forward and backward
+// (entry points, planning, and the small kernels around the products of layer_gemm.cuh).
+#include <algorithm>
+#include <cstring>
+
+#include "common.h"
+#include "layer_gemm.cuh"
+
+namespace dynbatch {
+namespace {
+
+using bf16 = __nv_bfloat16;
+
+constexpr size_t kStatusBytes = 256;
+constexpr long long kMaxRows = 1LL << 30, kMaxFeatures = 1LL << 24, kMaxElements = 1LL << 40, kMaxPitch = 1LL << 31;
+
+size_t round256(size_t x) { return (x + 255) / 256 * 256; }
+__host__ __device__ constexpr long long cdiv(long long a, long long b) { return (a + b - 1) / b; }
+
+// ---------------------------------------------------------------------------------------------- small kernels
+// Copy of a bf16 matrix to rows of `to_pitch`: what brings operands to the 16-byte grid that TMA needs.
+__global__ void __launch_bounds__(256)
+repitch_kernel(const bf16* from, long long from_pitch, bf16* to, long long to_pitch, long long rows, int cols, int* clear_status) {
+    tc::griddep_wait();
+    tc::griddep_launch_dependents();
+    if (clear_status && blockIdx.x == 0 && threadIdx.x == 0) *clear_status = 0;
+    const long long per_row = cdiv(cols, 8), total = rows * per_row;
+    for (long long i = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x; i < total; i += static_cast<long long>(gridDim.x) * blockDim.x) {
+        const long long r = i / per_row;
+        const int c = static_cast<int>(i - r * per_row) * 8;
+        const bf16* p = from + r * from_pitch + c;
+        union { uint4 q; bf16 v[8]; } x;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x.v[j] = c + j < cols ? p[j] : __float2bfloat16_rn(0.f);
+        *reinterpret_cast<uint4*>(to + r * to_pitch + c) = x.q;
+    }
+}
+
+struct ActGradArgs {
+    const bf16* dy; long long dy_pitch;
+    lg::Kept z;
+    int z_e4m3, act;
+    bf16* dz; long long dz_pitch;        // nullptr: not written
+    float* sums; long long sums_pitch;   // [row slabs][sums_pitch] sums over the slab's rows, or nullptr
+    long long rows;
+    int cols, slab_rows;
+    int* clear_status;
+};
+
+// dz = dy act'(z) and the sums of its columns.  HBM-bound.  A warp takes 256 columns of a row, eight per lane; a CTA's
+// eight warps take every eighth row of a slab and add their sums in warp order, so the result does not depend on timing.
+__global__ void __launch_bounds__(256)
+act_grad_kernel(const __grid_constant__ ActGradArgs a) {
+    __shared__ float part[8][256];
+    tc::griddep_wait();
+    tc::griddep_launch_dependents();
+    if (a.clear_status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.clear_status = 0;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int col = (blockIdx.x * 32 + lane) * 8, n = min(8, a.cols - col);
+    const long long first = static_cast<long long>(blockIdx.y) * a.slab_rows, last = min(a.rows, first + a.slab_rows);
+    float sum[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+    if (n > 0) {
+        for (long long r = first + warp; r < last; r += 8) {
+            float d[8], z[8];
+            const bf16* p = a.dy + r * a.dy_pitch + col;
+            if (n == 8 && lg::aligned_to(p, 16)) {
+                const uint4 q = *reinterpret_cast<const uint4*>(p);
+                lg::unpack2(q.x, d[0], d[1]); lg::unpack2(q.y, d[2], d[3]);
+                lg::unpack2(q.z, d[4], d[5]); lg::unpack2(q.w, d[6], d[7]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[j] = j < n ? __bfloat162float(p[j]) : 0.f;
+            }
+            if (a.act != DB_ACT_NONE) {
+                if (a.z_e4m3) {
+                    const uint8_t* c = static_cast<const uint8_t*>(a.z.data) + r * a.cols + col;
+                    const float scale = ck8::scale_value(a.z.scale[r * ((a.cols + 31) / 32) + col / 32]);
+                    uint32_t w[2] = {0, 0};
+                    if (n == 8 && lg::aligned_to(c, 8)) {
+                        const uint2 q = *reinterpret_cast<const uint2*>(c);
+                        w[0] = q.x; w[1] = q.y;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (j < n) w[j / 4] |= static_cast<uint32_t>(c[j]) << (8 * (j % 4));
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) {
+                        const float2 t = ck8::values2(w[j / 4] >> (8 * (j % 4)));
+                        z[j] = t.x * scale; z[j + 1] = t.y * scale;
+                    }
+                } else {
+                    const bf16* c = static_cast<const bf16*>(a.z.data) + r * a.cols + col;
+                    if (n == 8 && lg::aligned_to(c, 16)) {
+                        const uint4 q = *reinterpret_cast<const uint4*>(c);
+                        lg::unpack2(q.x, z[0], z[1]); lg::unpack2(q.y, z[2], z[3]);
+                        lg::unpack2(q.z, z[4], z[5]); lg::unpack2(q.w, z[6], z[7]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) z[j] = j < n ? __bfloat162float(c[j]) : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float value, slope;
+                    lg::act_value_slope(z[j], a.act, value, slope);
+                    d[j] *= slope;
+                }
+            }
+            if (a.dz) {
+                bf16* q = a.dz + r * a.dz_pitch + col;   // workspace rows: aligned, pitch a multiple of 32
+                if (n == 8) {
+                    *reinterpret_cast<uint4*>(q) = make_uint4(lg::pack2(d[0], d[1]), lg::pack2(d[2], d[3]), lg::pack2(d[4], d[5]), lg::pack2(d[6], d[7]));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j < n) q[j] = __float2bfloat16_rn(d[j]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += d[j];
+        }
+    }
+    if (!a.sums) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) part[warp][lane * 8 + j] = sum[j];
+    __syncthreads();
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c < a.cols) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) s += part[w][threadIdx.x];
+        a.sums[blockIdx.y * a.sums_pitch + c] = s;
+    }
+}
+
+// Column sums: the slabs' sums added in slab order.
+__global__ void __launch_bounds__(128)
+bias_fold_kernel(const float* sums, long long pitch, int slabs, int cols, void* out, int out_f32) {
+    tc::griddep_wait();
+    tc::griddep_launch_dependents();
+    const int c = blockIdx.x * blockDim.x + threadIdx.x;
+    if (c >= cols) return;
+    float s = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < slabs; ++i) s += sums[i * pitch + c];
+    if (out_f32) static_cast<float*>(out)[c] = s;
+    else static_cast<bf16*>(out)[c] = __float2bfloat16_rn(s);
+}
+
+// ---------------------------------------------------------------------------------------------- launches
+// Every kernel of a call may be scheduled while its predecessor still runs and waits for it on the device.
+struct Launch {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    Launch(dim3 grid, dim3 block, size_t smem, cudaStream_t stream, int cluster = 1) {
+        std::memset(&cfg, 0, sizeof cfg);
+        cfg.gridDim = grid;
+        cfg.blockDim = block;
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = stream;
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = cluster > 1 ? 2 : 1;
+    }
+    Launch(const Launch&) = delete;
+    Launch& operator=(const Launch&) = delete;
+};
+
+using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled() {
+    static EncodeTiledFn fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeTiledFn>(p);
+    }();
+    return fn;
+}
+
+struct Matrix {              // bf16, row-major
+    const bf16* p = nullptr;
+    long long rows = 0, cols = 0, pitch = 0;
+};
+
+bool on_grid(const void* p, long long pitch) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && pitch % 8 == 0; }
+
+// Boxes of box_rows rows x 64 columns with the 128-byte swizzle; what lies outside the matrix reads as zero.
+db_status make_map(CUtensorMap* map, const Matrix& m, int box_rows) {
+    EncodeTiledFn enc = encode_tiled();
+    if (!enc) {
+        record_message("cuTensorMapEncodeTiled is not available from this driver");
+        return DB_ERR_CUDA;
+    }
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(m.cols), static_cast<cuuint64_t>(m.rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(m.pitch) * 2};
+    const cuuint32_t box[2] = {lg::kBlockK, static_cast<cuuint32_t>(box_rows)};
+    const cuuint32_t elem[2] = {1, 1};
+    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<bf16*>(m.p), dims, strides, box, elem,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        record_message("cuTensorMapEncodeTiled rejected an operand of a layer");
+        return DB_ERR_CUDA;
+    }
+    return DB_OK;
+}
+
+// ---------------------------------------------------------------------------------------------- the products' plan
+enum Kind { kForward, kGated, kInputGrad, kGatedGrad, kWeightGrad };   // which operands lie how, and the epilogue
+enum TileShape { kPair256, kSingle128, kSingle64, kTileShapes };
+
+using GemmFn = void (*)(const lg::GemmArgs);
+struct ShapeInfo { int cg, bn, smem; };
+template <int CG, int BN> constexpr ShapeInfo info() { return {CG, BN, lg::Shape<CG, BN>::kSmemBytes}; }
+constexpr ShapeInfo kShapes[kTileShapes] = {info<2, 256>(), info<1, 128>(), info<1, 64>()};
+
+template <int CG, int BN>
+GemmFn gemm_fn(Kind kind) {
+    switch (kind) {
+        case kForward: return lg::layer_gemm_kernel<CG, BN, false, true, lg::kEpiStore>;
+        case kInputGrad: return lg::layer_gemm_kernel<CG, BN, false, false, lg::kEpiStore>;
+        case kGatedGrad: return lg::layer_gemm_kernel<CG, BN, false, false, lg::kEpiGatedGrad>;
+        case kWeightGrad: return lg::layer_gemm_kernel<CG, BN, true, true, lg::kEpiStore>;
+        case kGated:
+            if constexpr (BN >= 128) return lg::layer_gemm_kernel<CG, BN, false, true, lg::kEpiGated>;
+            else return nullptr;
+    }
+    return nullptr;
+}
+GemmFn gemm_fn(Kind kind, TileShape shape) {
+    switch (shape) {
+        case kPair256: return gemm_fn<2, 256>(kind);
+        case kSingle128: return gemm_fn<1, 128>(kind);
+        default: return gemm_fn<1, 64>(kind);
+    }
+}
+
+struct Size { long long M, N; };
+struct Plan {
+    TileShape shape = kPair256;
+    int splits = 1, blocks_per_split = 1;
+    long long partial_floats = 0;
+};
+
+long long tiles_of(Kind kind, TileShape shape, const Size& s) {
+    const int tile_n = kind == kGated ? kShapes[shape].bn / 2 : kShapes[shape].bn;
+    return cdiv(s.M, lg::kRows * kShapes[shape].cg) * cdiv(s.N, tile_n);
+}
+
+// The tile shape and the number of pieces of the reduction with the least estimated time, in SM cycles.
+// A 64-deep block of a tile costs its products or its copies, whichever is longer, a tile something for its start and
+// end, and a split reduction a second kernel and the traffic of its partial sums.
+Plan make_plan(Kind kind, const Size* sizes, int n, long long blocks) {
+    constexpr double kBlock[kTileShapes] = {560, 420, 330}, kTile[kTileShapes] = {2600, 1700, 1300}, kCombine = 5000;
+    Plan best;
+    double least = 0;
+    if (n == 0) return best;
+    for (int i = 0; i < kTileShapes; ++i) {
+        const TileShape shape = static_cast<TileShape>(i);
+        if (!gemm_fn(kind, shape)) continue;
+        const long long workers = std::max(1, sm_count() / kShapes[i].cg);
+        long long tiles = 0, outputs = 0;
+        for (int j = 0; j < n; ++j) {
+            tiles += tiles_of(kind, shape, sizes[j]);
+            outputs += sizes[j].M * lg::partial_pitch(sizes[j].N) * (kind == kGated ? 2 : 1);
+        }
+        const long long most = std::min(blocks, std::max(1LL, workers / tiles));
+        for (long long want = 1; want <= most; ++want) {
+            const long long per = cdiv(blocks, want), splits = cdiv(blocks, per);
+            if (splits != want) continue;
+            const double time = static_cast<double>(cdiv(tiles * splits, workers)) * (per * kBlock[i]) + kTile[i] +
+                                (splits > 1 ? kCombine + outputs * (splits + 1) * 4 / 2500.0 : 0);
+            if (least == 0 || time < least) {
+                least = time;
+                best.shape = shape;
+                best.splits = static_cast<int>(splits);
+                best.blocks_per_split = static_cast<int>(per);
+                best.partial_floats = splits > 1 ? splits * outputs : 0;
+            }
+        }
+    }
+    return best;
+}
+
+// One product, or several with the same reduction, in one launch (two with a split reduction).
+struct Product {
+    Matrix a[2], b[2];           // sources of the reduction; kGated: b[0], b[1] the two weights
+    int sources = 1;
+    Size size;
+    lg::EpilogueArgs e;
+};
+
+long long depth(Kind kind, const Matrix& a) { return kind == kWeightGrad ? a.rows : a.cols; }
+
+db_status run_products(Kind kind, const Product* products, int n, float* partials, int* status, bool& clear, cudaStream_t stream) {
+    const bool a_mn = kind == kWeightGrad, b_mn = kind != kInputGrad && kind != kGatedGrad;
+    lg::GemmArgs g;
+    std::memset(static_cast<void*>(&g), 0, sizeof g);
+    Size sizes[lg::kMaxProblems];
+    long long blocks = 0;
+    for (int i = 0; i < n; ++i) {
+        sizes[i] = products[i].size;
+        lg::Problem& p = g.p[i];
+        p.M = static_cast<int>(sizes[i].M);
+        p.N = static_cast<int>(sizes[i].N);
+        p.blocks0 = static_cast<int>(cdiv(depth(kind, products[i].a[0]), lg::kBlockK));
+        p.blocks = p.blocks0 + (products[i].sources > 1 ? static_cast<int>(cdiv(depth(kind, products[i].a[1]), lg::kBlockK)) : 0);
+        blocks = std::max<long long>(blocks, p.blocks);
+        p.e = products[i].e;
+    }
+    const Plan plan = make_plan(kind, sizes, n, blocks);
+    const ShapeInfo& shape = kShapes[plan.shape];
+    const int tile_n = kind == kGated ? shape.bn / 2 : shape.bn;
+    long long tiles = 0, floats = 0;
+    for (int i = 0; i < n; ++i) {
+        lg::Problem& p = g.p[i];
+        p.m_tiles = static_cast<int>(cdiv(p.M, lg::kRows * shape.cg));
+        p.n_tiles = static_cast<int>(cdiv(p.N, tile_n));
+        p.partial = floats;
+        floats += plan.splits * static_cast<long long>(p.M) * lg::partial_pitch(p.N) * (kind == kGated ? 2 : 1);
+        g.tile_start[i] = static_cast<int>(tiles);
+        tiles += static_cast<long long>(p.m_tiles) * p.n_tiles * plan.splits;
+        const int sources = kind == kGated ? 2 : products[i].sources;
+        db_status st;
+        for (int s = 0; s < sources; ++s) {
+            if (s < products[i].sources && (st = make_map(&p.a[s], products[i].a[s], a_mn ? lg::kBlockK : lg::kRows)) != DB_OK) return st;
+            if ((st = make_map(&p.b[s], products[i].b[s], b_mn ? lg::kBlockK : shape.bn / shape.cg)) != DB_OK) return st;
+        }
+    }
+    g.tile_start[n] = static_cast<int>(tiles);
+    g.problems = n;
+    g.splits = plan.splits;
+    g.blocks_per_split = plan.blocks_per_split;
+    g.partials = partials;
+    g.status = status;
+    g.clear_status = clear;
+    clear = false;
+    const GemmFn fn = gemm_fn(kind, plan.shape);
+    DB_CUDA_TRY(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, shape.smem));
+    const long long workers = std::min<long long>(std::max(1, sm_count() / shape.cg), tiles);
+    Launch L(dim3(static_cast<unsigned>(workers * shape.cg)), dim3(lg::kThreads), shape.smem, stream, shape.cg);
+    DB_CUDA_TRY(cudaLaunchKernelEx(&L.cfg, fn, g));
+    if (plan.splits > 1) {
+        long long most = 0;
+        for (int i = 0; i < n; ++i) most = std::max(most, static_cast<long long>(g.p[i].M) * (lg::partial_pitch(g.p[i].N) / lg::kChunk));
+        Launch C(dim3(static_cast<unsigned>(cdiv(most, 128)), n), dim3(128), 0, stream);
+        GemmFn fold = kind == kGated ? lg::combine_kernel<lg::kEpiGated> : kind == kGatedGrad ? lg::combine_kernel<lg::kEpiGatedGrad>
+                                                                                            : lg::combine_kernel<lg::kEpiStore>;
+        DB_CUDA_TRY(cudaLaunchKernelEx(&C.cfg, fold, g));
+    }
+    return DB_OK;
+}
+
+// ---------------------------------------------------------------------------------------------- workspace, arguments
+struct Arena {               // hands out the workspace in pieces of whole 256 bytes; base may be null to count only
+    char* base;
+    size_t used = kStatusBytes;
+    explicit Arena(void* p) : base(static_cast<char*>(p)) {}
+    char* take(size_t bytes) {
+        char* p = base ? base + used : nullptr;
+        used += round256(bytes);
+        return p;
+    }
+};
+
+// An operand for TMA: the matrix itself where it lies on the 16-byte grid, else a copy in the workspace.
+struct Operands {
+    Arena& arena;
+    cudaStream_t stream;
+    int* status;
+    bool& clear;
+    db_status st = DB_OK;
+    Matrix of(const void* p, long long rows, long long cols, long long pitch) {
+        Matrix m{static_cast<const bf16*>(p), rows, cols, pitch};
+        if (on_grid(p, pitch)) return m;
+        m.pitch = (cols + 7) / 8 * 8;
+        bf16* to = reinterpret_cast<bf16*>(arena.take(static_cast<size_t>(rows * m.pitch) * 2));
+        if (arena.base && st == DB_OK) {
+            const long long pieces = rows * (m.pitch / 8);
+            Launch L(dim3(static_cast<unsigned>(std::min<long long>(cdiv(pieces, 256), 8LL * sm_count()))), dim3(256), 0, stream);
+            const cudaError_t err = cudaLaunchKernelEx(&L.cfg, repitch_kernel, m.p, pitch, to, m.pitch, rows, static_cast<int>(cols),
+                                                       clear ? status : static_cast<int*>(nullptr));
+            clear = false;
+            if (err != cudaSuccess) st = record_cuda_error(err, "repitch_kernel");
+        }
+        m.p = to;
+        return m;
+    }
+};
+
+struct Extent { const void* p; long long bytes; bool written; };
+long long extent_bytes(long long rows, long long cols, long long pitch, int size) { return rows > 0 ? ((rows - 1) * pitch + cols) * size : 0; }
+
+// Whether something that a call writes overlaps anything else it touches.
+bool overlaps(const Extent* x, int n) {
+    for (int i = 0; i < n; ++i)
+        for (int j = i + 1; j < n; ++j) {
+            if (!x[i].p || !x[j].p || !(x[i].written || x[j].written) || x[i].bytes <= 0 || x[j].bytes <= 0) continue;
+            const uintptr_t a = reinterpret_cast<uintptr_t>(x[i].p), b = reinterpret_cast<uintptr_t>(x[j].p);
+            if (a < b + static_cast<uintptr_t>(x[j].bytes) && b < a + static_cast<uintptr_t>(x[i].bytes)) return true;
+        }
+    return false;
+}
+
+bool valid_size(long long rows, long long n_in, long long n_out) {
+    return rows >= 0 && rows <= kMaxRows && n_in >= 1 && n_in <= kMaxFeatures && n_out >= 1 && n_out <= kMaxFeatures &&
+           rows * n_in <= kMaxElements && rows * n_out <= kMaxElements && n_in * n_out <= kMaxElements;
+}
+bool valid_pitch(const void* p, long long cols, long long pitch) { return !p || (pitch >= cols && pitch <= kMaxPitch); }
+bool odd_address(const void* p, int size) { return reinterpret_cast<uintptr_t>(p) % size != 0; }
+bool valid_act(int act) { return act >= DB_ACT_NONE && act <= DB_ACT_SILU; }
+long long scales_of(long long n) { return (n + ck8::kGroup - 1) / ck8::kGroup; }
+int kept_size(db_dtype t) { return t == DB_E4M3 ? 1 : 2; }
+
+db_status zero(void* p, long long bytes, cudaStream_t stream) {
+    if (p && bytes > 0) DB_CUDA_TRY(cudaMemsetAsync(p, 0, static_cast<size_t>(bytes), stream));
+    return DB_OK;
+}
+
+// ---------------------------------------------------------------------------------------------- linear layer
+struct LinearArgs {
+    const void *x, *w, *bias, *residual;
+    long long x_pitch, residual_pitch, rows;
+    int n_in, n_out, act;
+    void* y;
+    long long y_pitch;
+    void *z, *z_scale;
+    db_dtype z_dtype;
+};
+
+// Lays out the workspace and, with a base, launches; without one it only counts.
+db_status linear_forward(const LinearArgs& v, Arena& arena, cudaStream_t stream, bool aligned) {
+    int* status = reinterpret_cast<int*>(arena.base);
+    bool clear = true;
+    Operands ops{arena, stream, status, clear};
+    Product p;
+    const void* off = aligned ? nullptr : reinterpret_cast<const void*>(2);   // when counting: a pointer off the grid
+    const bool count = !arena.base;
+    const long long px = count ? (aligned ? (v.n_in + 7) / 8 * 8 : v.n_in) : v.x_pitch;
+    p.a[0] = ops.of(count ? off : v.x, v.rows, v.n_in, px);
+    p.b[0] = ops.of(count ? off : v.w, v.n_in, v.n_out, v.n_out);
+    p.size = {v.rows, v.n_out};
+    p.e.out = v.y; p.e.out_pitch = v.y_pitch;
+    p.e.bias = static_cast<const bf16*>(v.bias);
+    p.e.addend = static_cast<const bf16*>(v.residual); p.e.addend_pitch = v.residual_pitch;
+    p.e.kept[0] = {v.z, static_cast<uint8_t*>(v.z_scale)};
+    p.e.kept_e4m3 = v.z_dtype == DB_E4M3;
+    p.e.act = v.act;
+    const Plan plan = make_plan(kForward, &p.size, 1, cdiv(v.n_in, lg::kBlockK));
+    float* partials = reinterpret_cast<float*>(arena.take(static_cast<size_t>(plan.partial_floats) * 4));
+    if (count || ops.st != DB_OK) return ops.st;
+    return run_products(kForward, &p, 1, partials, status, clear, stream);
+}
+
+struct LinearGradArgs {
+    const void *dy, *x, *w, *z, *z_scale, *addend;
+    long long dy_pitch, x_pitch, addend_pitch, rows;
+    db_dtype z_dtype, grad_dtype;
+    int n_in, n_out, act;
+    void *dx, *dw, *dbias;
+    long long dx_pitch;
+};
+
+int slab_count(long long rows, long long cols) {   // about four CTAs per SM, at least 32 rows each
+    const long long across = cdiv(cols, 256);
+    return static_cast<int>(std::max(1LL, std::min(cdiv(rows, 32), cdiv(4LL * sm_count(), across))));
+}
+
+db_status linear_backward(const LinearGradArgs& v, Arena& arena, cudaStream_t stream, bool aligned) {
+    const bool count = !arena.base;
+    int* status = reinterpret_cast<int*>(arena.base);
+    bool clear = true;
+    const void* off = aligned ? nullptr : reinterpret_cast<const void*>(2);
+    const bool has_act = count || v.act != DB_ACT_NONE, want_bias = count || v.dbias, want_dw = count || v.dw, want_dx = count || v.dx;
+    Matrix dz{static_cast<const bf16*>(v.dy), v.rows, v.n_out, v.dy_pitch};
+    Operands ops{arena, stream, status, clear};
+    if (has_act || want_bias) {
+        ActGradArgs a{};
+        a.dy = static_cast<const bf16*>(v.dy); a.dy_pitch = v.dy_pitch;
+        a.z = {const_cast<void*>(v.z), static_cast<uint8_t*>(const_cast<void*>(v.z_scale))};
+        a.z_e4m3 = v.z_dtype == DB_E4M3;
+        a.act = v.act;
+        a.rows = v.rows; a.cols = v.n_out;
+        if (has_act) {
+            dz.pitch = (v.n_out + 31LL) / 32 * 32;
+            a.dz = reinterpret_cast<bf16*>(arena.take(static_cast<size_t>(v.rows * dz.pitch) * 2));
+            a.dz_pitch = dz.pitch;
+            dz.p = a.dz;
+        }
+        const int slabs = slab_count(v.rows, v.n_out);
+        a.slab_rows = static_cast<int>(cdiv(v.rows, slabs));
+        const int used = a.slab_rows ? static_cast<int>(cdiv(v.rows, a.slab_rows)) : 1;
+        if (want_bias) {
+            a.sums_pitch = (v.n_out + 31LL) / 32 * 32;
+            a.sums = reinterpret_cast<float*>(arena.take(static_cast<size_t>(slabs * a.sums_pitch) * 4));
+        }
+        if (!count) {
+            a.clear_status = status;
+            clear = false;
+            Launch L(dim3(static_cast<unsigned>(cdiv(v.n_out, 256)), used), dim3(256), 0, stream);
+            DB_CUDA_TRY(cudaLaunchKernelEx(&L.cfg, act_grad_kernel, a));
+            if (want_bias) {
+                Launch F(dim3(static_cast<unsigned>(cdiv(v.n_out, 128))), dim3(128), 0, stream);
+                DB_CUDA_TRY(cudaLaunchKernelEx(&F.cfg, bias_fold_kernel, static_cast<const float*>(a.sums), a.sums_pitch, used, v.n_out,
+                                               v.dbias, v.grad_dtype == DB_F32 ? 1 : 0));
+            }
+        }
+    }
+    if (count ? !aligned : !has_act && (want_dx || want_dw)) dz = ops.of(count ? off : v.dy, v.rows, v.n_out, count ? v.n_out : v.dy_pitch);
+    Plan plan_x, plan_w;
+    const Size size_x{v.rows, v.n_in}, size_w{v.n_in, v.n_out};
+    plan_x = make_plan(kInputGrad, &size_x, 1, cdiv(v.n_out, lg::kBlockK));
+    plan_w = make_plan(kWeightGrad, &size_w, 1, cdiv(v.rows, lg::kBlockK));
+    float* partials = reinterpret_cast<float*>(arena.take(static_cast<size_t>(std::max(plan_x.partial_floats, plan_w.partial_floats)) * 4));
+    if (want_dx) {
+        Product p;
+        p.a[0] = dz;
+        p.b[0] = ops.of(count ? off : v.w, v.n_in, v.n_out, count && aligned ? (v.n_out + 7) / 8 * 8 : v.n_out);
+        p.size = size_x;
+        p.e.out = v.dx; p.e.out_pitch = v.dx_pitch;
+        p.e.addend = static_cast<const bf16*>(v.addend); p.e.addend_pitch = v.addend_pitch;
+        if (ops.st != DB_OK) return ops.st;
+        if (!count) {
+            const db_status st = run_products(kInputGrad, &p, 1, partials, status, clear, stream);
+            if (st != DB_OK) return st;
+        }
+    }
+    if (want_dw) {
+        Product p;
+        p.a[0] = ops.of(count ? off : v.x, v.rows, v.n_in, count ? (aligned ? (v.n_in + 7) / 8 * 8 : v.n_in) : v.x_pitch);
+        p.b[0] = dz;
+        p.size = size_w;
+        p.e.out = v.dw; p.e.out_pitch = v.n_out;
+        p.e.out_f32 = v.grad_dtype == DB_F32;
+        if (ops.st != DB_OK) return ops.st;
+        if (!count) return run_products(kWeightGrad, &p, 1, partials, status, clear, stream);
+    }
+    return DB_OK;
+}
+
+// ---------------------------------------------------------------------------------------------- gated block
+struct GatedArgs {
+    const void *dy, *x, *w_gate, *w_up, *w_down, *residual;
+    long long dy_pitch, x_pitch, residual_pitch, rows;
+    int width, hidden, act;
+    void* y;                       // forward: y; backward: dx
+    long long y_pitch;
+    void *gate, *up, *gate_scale, *up_scale;
+    db_dtype kept_dtype, grad_dtype;
+    void *dw_gate, *dw_up, *dw_down;
+};
+
+db_status gated_forward(const GatedArgs& v, Arena& arena, cudaStream_t stream, bool aligned) {
+    const bool count = !arena.base;
+    int* status = reinterpret_cast<int*>(arena.base);
+    bool clear = true;
+    const void* off = aligned ? nullptr : reinterpret_cast<const void*>(2);
+    Operands ops{arena, stream, status, clear};
+    const long long h_pitch = (v.hidden + 31LL) / 32 * 32;
+    bf16* h = reinterpret_cast<bf16*>(arena.take(static_cast<size_t>(v.rows * h_pitch) * 2));
+    const auto pitch = [&](long long given, long long cols) { return !count ? given : aligned ? (cols + 7) / 8 * 8 : cols; };
+    Product p, q;
+    p.a[0] = ops.of(count ? off : v.x, v.rows, v.width, pitch(v.x_pitch, v.width));
+    p.b[0] = ops.of(count ? off : v.w_gate, v.width, v.hidden, pitch(v.hidden, v.hidden));
+    p.b[1] = ops.of(count ? off : v.w_up, v.width, v.hidden, pitch(v.hidden, v.hidden));
+    p.size = {v.rows, v.hidden};
+    p.e.out = h; p.e.out_pitch = h_pitch;
+    p.e.kept[0] = {v.gate, static_cast<uint8_t*>(v.gate_scale)};
+    p.e.kept[1] = {v.up, static_cast<uint8_t*>(v.up_scale)};
+    p.e.kept_e4m3 = v.kept_dtype == DB_E4M3;
+    p.e.act = v.act;
+    q.a[0] = Matrix{h, v.rows, v.hidden, h_pitch};
+    q.b[0] = ops.of(count ? off : v.w_down, v.hidden, v.width, pitch(v.width, v.width));
+    q.size = {v.rows, v.width};
+    q.e.out = v.y; q.e.out_pitch = v.y_pitch;
+    q.e.addend = static_cast<const bf16*>(v.residual); q.e.addend_pitch = v.residual_pitch;
+    const Plan a = make_plan(kGated, &p.size, 1, cdiv(v.width, lg::kBlockK)), b = make_plan(kForward, &q.size, 1, cdiv(v.hidden, lg::kBlockK));
+    float* partials = reinterpret_cast<float*>(arena.take(static_cast<size_t>(std::max(a.partial_floats, b.partial_floats)) * 4));
+    if (count || ops.st != DB_OK) return ops.st;
+    const db_status st = run_products(kGated, &p, 1, partials, status, clear, stream);
+    return st != DB_OK ? st : run_products(kForward, &q, 1, partials, status, clear, stream);
+}
+
+db_status gated_backward(const GatedArgs& v, Arena& arena, cudaStream_t stream, bool aligned) {
+    const bool count = !arena.base;
+    int* status = reinterpret_cast<int*>(arena.base);
+    bool clear = true;
+    const void* off = aligned ? nullptr : reinterpret_cast<const void*>(2);
+    Operands ops{arena, stream, status, clear};
+    const long long h_pitch = (v.hidden + 31LL) / 32 * 32;
+    const size_t h_bytes = static_cast<size_t>(v.rows * h_pitch) * 2;
+    bf16* h = reinterpret_cast<bf16*>(arena.take(h_bytes));
+    bf16* d_gate = reinterpret_cast<bf16*>(arena.take(h_bytes));
+    bf16* d_up = reinterpret_cast<bf16*>(arena.take(h_bytes));
+    const auto pitch = [&](long long given, long long cols) { return !count ? given : aligned ? (cols + 7) / 8 * 8 : cols; };
+    const bool want_dx = count || v.y, want_dw = count || v.dw_gate || v.dw_up || v.dw_down;
+    const Matrix dy = ops.of(count ? off : v.dy, v.rows, v.width, pitch(v.dy_pitch, v.width));
+    const Matrix mg{d_gate, v.rows, v.hidden, h_pitch}, mu{d_up, v.rows, v.hidden, h_pitch}, mh{h, v.rows, v.hidden, h_pitch};
+
+    Product p, q, w[3];
+    p.a[0] = dy;
+    p.b[0] = ops.of(count ? off : v.w_down, v.hidden, v.width, pitch(v.width, v.width));
+    p.size = {v.rows, v.hidden};
+    p.e.out = h; p.e.out_pitch = h_pitch;
+    p.e.d_gate = d_gate; p.e.d_up = d_up; p.e.d_pitch = h_pitch;
+    p.e.kept[0] = {v.gate, static_cast<uint8_t*>(v.gate_scale)};
+    p.e.kept[1] = {v.up, static_cast<uint8_t*>(v.up_scale)};
+    p.e.kept_e4m3 = v.kept_dtype == DB_E4M3;
+    p.e.act = v.act;
+    const Plan plan_p = make_plan(kGatedGrad, &p.size, 1, cdiv(v.width, lg::kBlockK));
+
+    if (want_dx) {
+        q.a[0] = mg; q.a[1] = mu;
+        q.b[0] = ops.of(count ? off : v.w_gate, v.width, v.hidden, pitch(v.hidden, v.hidden));
+        q.b[1] = ops.of(count ? off : v.w_up, v.width, v.hidden, pitch(v.hidden, v.hidden));
+        q.sources = 2;
+        q.size = {v.rows, v.width};
+        q.e.out = v.y; q.e.out_pitch = v.y_pitch;
+        q.e.addend = static_cast<const bf16*>(v.residual); q.e.addend_pitch = v.residual_pitch;
+    }
+    const Plan plan_q = make_plan(kInputGrad, &q.size, want_dx ? 1 : 0, 2 * cdiv(v.hidden, lg::kBlockK));
+
+    int n = 0;
+    Size sizes[3];
+    if (want_dw) {
+        const bool x_used = count || v.dw_gate || v.dw_up;
+        const Matrix x = x_used ? ops.of(count ? off : v.x, v.rows, v.width, pitch(v.x_pitch, v.width)) : Matrix{};
+        const auto add = [&](const Matrix& a, const Matrix& b, void* out) {
+            if (!count && !out) return;
+            w[n].a[0] = a; w[n].b[0] = b;
+            w[n].size = {a.cols, b.cols};
+            w[n].e.out = out; w[n].e.out_pitch = b.cols;
+            w[n].e.out_f32 = v.grad_dtype == DB_F32;
+            sizes[n] = w[n].size;
+            ++n;
+        };
+        add(x, mg, v.dw_gate);
+        add(x, mu, v.dw_up);
+        add(mh, dy, v.dw_down);
+    }
+    long long floats = std::max(plan_p.partial_floats, plan_q.partial_floats);
+    // which weight gradients a call wants decides how its reduction is split: room for any choice
+    if (count) {
+        const Size up{v.width, v.hidden}, down{v.hidden, v.width};
+        const Size choices[6][3] = {{up}, {down}, {up, up}, {up, down}, {up, up, down}, {up}};
+        const int counts[6] = {1, 1, 2, 2, 3, 1};
+        for (int i = 0; i < 6; ++i)
+            floats = std::max(floats, make_plan(kWeightGrad, choices[i], counts[i], cdiv(v.rows, lg::kBlockK)).partial_floats);
+    } else if (n) {
+        floats = std::max(floats, make_plan(kWeightGrad, sizes, n, cdiv(v.rows, lg::kBlockK)).partial_floats);
+    }
+    float* partials = reinterpret_cast<float*>(arena.take(static_cast<size_t>(floats) * 4));
+    if (count || ops.st != DB_OK) return ops.st;
+    db_status st = run_products(kGatedGrad, &p, 1, partials, status, clear, stream);
+    if (st == DB_OK && want_dx) st = run_products(kInputGrad, &q, 1, partials, status, clear, stream);
+    if (st == DB_OK && n) st = run_products(kWeightGrad, w, n, partials, status, clear, stream);
+    return st;
+}
+
+}  // namespace
+}  // namespace dynbatch
+
+// ---------------------------------------------------------------------------------------------- entry points
+extern "C" size_t db_linear_workspace_bytes(int64_t rows, int32_t n_in, int32_t n_out, int32_t aligned) {
+    using namespace dynbatch;
+    if (!valid_size(rows, n_in, n_out)) return 0;
+    LinearArgs v{};
+    v.rows = rows; v.n_in = n_in; v.n_out = n_out;
+    Arena arena(nullptr);
+    linear_forward(v, arena, nullptr, aligned && n_in % 8 == 0 && n_out % 8 == 0);
+    return arena.used;
+}
+
+extern "C" db_status db_linear(const void* x, int64_t x_pitch, const void* w, const void* bias, const void* residual,
+                               int64_t residual_pitch, db_activation act, int64_t rows, int32_t n_in, int32_t n_out, void* y,
+                               int64_t y_pitch, void* z, void* z_scale, db_dtype z_dtype, void* workspace,
+                               size_t workspace_bytes, void* cuda_stream) {
+    using namespace dynbatch;
+    if (!w || !workspace) return DB_ERR_NULL;
+    if (!valid_size(rows, n_in, n_out)) return DB_ERR_ARG;
+    if (rows > 0 && (!x || !y)) return DB_ERR_NULL;
+    if (!valid_act(act)) return DB_ERR_UNSUPPORTED;
+    if (z && z_dtype != DB_BF16 && z_dtype != DB_E4M3) return DB_ERR_UNSUPPORTED;
+    if (z && z_dtype == DB_E4M3 && !z_scale) return DB_ERR_NULL;
+    if (!valid_pitch(x, n_in, x_pitch) || !valid_pitch(y, n_out, y_pitch) || !valid_pitch(residual, n_out, residual_pitch)) return DB_ERR_ARG;
+    if (odd_address(x, 2) || odd_address(w, 2) || odd_address(bias, 2) || odd_address(residual, 2) || odd_address(y, 2) ||
+        (z && z_dtype == DB_BF16 && odd_address(z, 2)) || odd_address(workspace, 256))
+        return DB_ERR_ARG;
+    const bool e4m3 = z && z_dtype == DB_E4M3;
+    const bool in_place = residual == y && residual_pitch == y_pitch;
+    const Extent touched[] = {
+        {x, extent_bytes(rows, n_in, x_pitch, 2), false}, {w, extent_bytes(n_in, n_out, n_out, 2), false},
+        {bias, 2LL * n_out, false}, {in_place ? nullptr : residual, extent_bytes(rows, n_out, residual_pitch, 2), false},
+        {y, extent_bytes(rows, n_out, y_pitch, 2), true}, {z, z ? rows * n_out * kept_size(z_dtype) : 0, true},
+        {e4m3 ? z_scale : nullptr, rows * scales_of(n_out), true}, {workspace, static_cast<long long>(workspace_bytes), true}};
+    if (overlaps(touched, static_cast<int>(sizeof touched / sizeof touched[0]))) return DB_ERR_ARG;
+    const bool aligned = on_grid(x, x_pitch) && on_grid(w, n_out);
+    LinearArgs v{x, w, bias, residual, x_pitch, residual_pitch, rows, n_in, n_out, act, y, y_pitch, z, z_scale, z_dtype};
+    Arena need(nullptr);
+    linear_forward(v, need, nullptr, aligned);
+    if (workspace_bytes < need.used) return DB_ERR_ARG;
+    if (rows == 0) return zero(workspace, 4, static_cast<cudaStream_t>(cuda_stream));
+    Arena arena(workspace);
+    return linear_forward(v, arena, static_cast<cudaStream_t>(cuda_stream), aligned);
+}
+
+extern "C" size_t db_linear_grad_workspace_bytes(int64_t rows, int32_t n_in, int32_t n_out, int32_t aligned) {
+    using namespace dynbatch;
+    if (!valid_size(rows, n_in, n_out)) return 0;
+    LinearGradArgs v{};
+    v.rows = rows; v.n_in = n_in; v.n_out = n_out;
+    Arena arena(nullptr);
+    linear_backward(v, arena, nullptr, aligned && n_in % 8 == 0 && n_out % 8 == 0);
+    return arena.used;
+}
+
+extern "C" db_status db_linear_grad(const void* dy, int64_t dy_pitch, const void* x, int64_t x_pitch, const void* w,
+                                    const void* z, const void* z_scale, db_dtype z_dtype, db_activation act, int64_t rows,
+                                    int32_t n_in, int32_t n_out, void* dx, int64_t dx_pitch, const void* dx_addend,
+                                    int64_t dx_addend_pitch, void* dw, void* dbias, db_dtype grad_dtype, void* workspace,
+                                    size_t workspace_bytes, void* cuda_stream) {
+    using namespace dynbatch;
+    if (!workspace || (!dx && !dw && !dbias)) return DB_ERR_NULL;
+    if (!valid_size(rows, n_in, n_out)) return DB_ERR_ARG;
+    if (!valid_act(act)) return DB_ERR_UNSUPPORTED;
+    if (grad_dtype != DB_F32 && grad_dtype != DB_BF16) return DB_ERR_UNSUPPORTED;
+    if (act != DB_ACT_NONE && z_dtype != DB_BF16 && z_dtype != DB_E4M3) return DB_ERR_UNSUPPORTED;
+    if (rows > 0) {
+        if (!dy || (dw && !x) || (dx && !w)) return DB_ERR_NULL;
+        if (act != DB_ACT_NONE && (!z || (z_dtype == DB_E4M3 && !z_scale))) return DB_ERR_NULL;
+    }
+    if (dx_addend && !dx) return DB_ERR_ARG;
+    if (!valid_pitch(dy, n_out, dy_pitch) || !valid_pitch(dw ? x : nullptr, n_in, x_pitch) || !valid_pitch(dx, n_in, dx_pitch) ||
+        !valid_pitch(dx_addend, n_in, dx_addend_pitch))
+        return DB_ERR_ARG;
+    const bool with_z = act != DB_ACT_NONE;
+    const int g = grad_dtype == DB_F32 ? 4 : 2;
+    if (odd_address(dy, 2) || odd_address(x, 2) || odd_address(w, 2) || (with_z && z_dtype == DB_BF16 && odd_address(z, 2)) ||
+        odd_address(dx, 2) || odd_address(dx_addend, 2) || odd_address(dw, g) || odd_address(dbias, g) || odd_address(workspace, 256))
+        return DB_ERR_ARG;
+    const bool in_place = dx_addend == dx && dx_addend_pitch == dx_pitch;
+    const Extent touched[] = {
+        {dy, extent_bytes(rows, n_out, dy_pitch, 2), false}, {dw ? x : nullptr, extent_bytes(rows, n_in, x_pitch, 2), false},
+        {dx ? w : nullptr, extent_bytes(n_in, n_out, n_out, 2), false},
+        {with_z ? z : nullptr, rows * n_out * kept_size(z_dtype), false},
+        {with_z && z_dtype == DB_E4M3 ? z_scale : nullptr, rows * scales_of(n_out), false},
+        {in_place ? nullptr : dx_addend, extent_bytes(rows, n_in, dx_addend_pitch, 2), false},
+        {dx, extent_bytes(rows, n_in, dx_pitch, 2), true}, {dw, static_cast<long long>(n_in) * n_out * g, true},
+        {dbias, static_cast<long long>(n_out) * g, true}, {workspace, static_cast<long long>(workspace_bytes), true}};
+    if (overlaps(touched, static_cast<int>(sizeof touched / sizeof touched[0]))) return DB_ERR_ARG;
+    const bool aligned = (with_z || on_grid(dy, dy_pitch)) && (!dw || on_grid(x, x_pitch)) && (!dx || on_grid(w, n_out));
+    LinearGradArgs v{dy, x, w, z, z_scale, dx_addend, dy_pitch, x_pitch, dx_addend_pitch, rows, z_dtype, grad_dtype,
+                     n_in, n_out, act, dx, dw, dbias, dx_pitch};
+    Arena need(nullptr);
+    linear_backward(v, need, nullptr, aligned);
+    if (workspace_bytes < need.used) return DB_ERR_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (rows == 0) {             // a batch without rows has zero gradients
+        db_status st = zero(workspace, 4, stream);
+        if (st == DB_OK) st = zero(dw, static_cast<long long>(n_in) * n_out * g, stream);
+        return st != DB_OK ? st : zero(dbias, static_cast<long long>(n_out) * g, stream);
+    }
+    Arena arena(workspace);
+    return linear_backward(v, arena, stream, aligned);
+}
+
+extern "C" size_t db_gated_ffn_workspace_bytes(int64_t rows, int32_t width, int32_t hidden, int32_t aligned) {
+    using namespace dynbatch;
+    if (!valid_size(rows, width, hidden)) return 0;
+    GatedArgs v{};
+    v.rows = rows; v.width = width; v.hidden = hidden;
+    Arena arena(nullptr);
+    gated_forward(v, arena, nullptr, aligned && width % 8 == 0 && hidden % 8 == 0);
+    return arena.used;
+}
+
+extern "C" db_status db_gated_ffn(const void* x, int64_t x_pitch, const void* w_gate, const void* w_up, const void* w_down,
+                                  const void* residual, int64_t residual_pitch, db_activation act, int64_t rows, int32_t width,
+                                  int32_t hidden, void* y, int64_t y_pitch, void* gate, void* up, void* gate_scale,
+                                  void* up_scale, db_dtype kept_dtype, void* workspace, size_t workspace_bytes,
+                                  void* cuda_stream) {
+    using namespace dynbatch;
+    if (!w_gate || !w_up || !w_down || !workspace) return DB_ERR_NULL;
+    if (!valid_size(rows, width, hidden)) return DB_ERR_ARG;
+    if (rows > 0 && (!x || !y)) return DB_ERR_NULL;
+    if (!valid_act(act)) return DB_ERR_UNSUPPORTED;
+    if (!gate != !up) return DB_ERR_NULL;                         // both or neither
+    if (gate && kept_dtype != DB_BF16 && kept_dtype != DB_E4M3) return DB_ERR_UNSUPPORTED;
+    const bool e4m3 = gate && kept_dtype == DB_E4M3;
+    if (e4m3 && (!gate_scale || !up_scale)) return DB_ERR_NULL;
+    if (!valid_pitch(x, width, x_pitch) || !valid_pitch(y, width, y_pitch) || !valid_pitch(residual, width, residual_pitch)) return DB_ERR_ARG;
+    const bool kept16 = gate && !e4m3;
+    if (odd_address(x, 2) || odd_address(w_gate, 2) || odd_address(w_up, 2) || odd_address(w_down, 2) || odd_address(residual, 2) ||
+        odd_address(y, 2) || (kept16 && (odd_address(gate, 2) || odd_address(up, 2))) || odd_address(workspace, 256))
+        return DB_ERR_ARG;
+    const long long weight = 2LL * width * hidden, kept = gate ? rows * hidden * kept_size(kept_dtype) : 0, scales = rows * scales_of(hidden);
+    const bool in_place = residual == y && residual_pitch == y_pitch;
+    const Extent touched[] = {
+        {x, extent_bytes(rows, width, x_pitch, 2), false}, {w_gate, weight, false}, {w_up, weight, false}, {w_down, weight, false},
+        {in_place ? nullptr : residual, extent_bytes(rows, width, residual_pitch, 2), false},
+        {y, extent_bytes(rows, width, y_pitch, 2), true}, {gate, kept, true}, {up, kept, true},
+        {e4m3 ? gate_scale : nullptr, scales, true}, {e4m3 ? up_scale : nullptr, scales, true},
+        {workspace, static_cast<long long>(workspace_bytes), true}};
+    if (overlaps(touched, static_cast<int>(sizeof touched / sizeof touched[0]))) return DB_ERR_ARG;
+    const bool aligned = on_grid(x, x_pitch) && on_grid(w_gate, hidden) && on_grid(w_up, hidden) && on_grid(w_down, width);
+    GatedArgs v{};
+    v.x = x; v.x_pitch = x_pitch; v.w_gate = w_gate; v.w_up = w_up; v.w_down = w_down;
+    v.residual = residual; v.residual_pitch = residual_pitch; v.act = act;
+    v.rows = rows; v.width = width; v.hidden = hidden; v.y = y; v.y_pitch = y_pitch;
+    v.gate = gate; v.up = up; v.gate_scale = gate_scale; v.up_scale = up_scale; v.kept_dtype = kept_dtype;
+    Arena need(nullptr);
+    gated_forward(v, need, nullptr, aligned);
+    if (workspace_bytes < need.used) return DB_ERR_ARG;
+    if (rows == 0) return zero(workspace, 4, static_cast<cudaStream_t>(cuda_stream));
+    Arena arena(workspace);
+    return gated_forward(v, arena, static_cast<cudaStream_t>(cuda_stream), aligned);
+}
+
+extern "C" size_t db_gated_ffn_grad_workspace_bytes(int64_t rows, int32_t width, int32_t hidden, int32_t aligned) {
+    using namespace dynbatch;
+    if (!valid_size(rows, width, hidden)) return 0;
+    GatedArgs v{};
+    v.rows = rows; v.width = width; v.hidden = hidden;
+    Arena arena(nullptr);
+    gated_backward(v, arena, nullptr, aligned && width % 8 == 0 && hidden % 8 == 0);
+    return arena.used;
+}
+
+extern "C" db_status db_gated_ffn_grad(const void* dy, int64_t dy_pitch, const void* x, int64_t x_pitch, const void* w_gate,
+                                       const void* w_up, const void* w_down, const void* gate, const void* up,
+                                       const void* gate_scale, const void* up_scale, db_dtype kept_dtype, db_activation act,
+                                       int64_t rows, int32_t width, int32_t hidden, void* dx, int64_t dx_pitch,
+                                       const void* dx_addend, int64_t dx_addend_pitch, void* dw_gate, void* dw_up,
+                                       void* dw_down, db_dtype grad_dtype, void* workspace, size_t workspace_bytes,
+                                       void* cuda_stream) {
+    using namespace dynbatch;
+    if (!workspace || !w_down || (!dx && !dw_gate && !dw_up && !dw_down)) return DB_ERR_NULL;
+    if (!valid_size(rows, width, hidden)) return DB_ERR_ARG;
+    if (!valid_act(act)) return DB_ERR_UNSUPPORTED;
+    if (grad_dtype != DB_F32 && grad_dtype != DB_BF16) return DB_ERR_UNSUPPORTED;
+    if (kept_dtype != DB_BF16 && kept_dtype != DB_E4M3) return DB_ERR_UNSUPPORTED;
+    const bool e4m3 = kept_dtype == DB_E4M3, needs_x = dw_gate || dw_up;
+    if (rows > 0) {
+        if (!dy || !gate || !up || (e4m3 && (!gate_scale || !up_scale))) return DB_ERR_NULL;
+        if ((needs_x && !x) || (dx && (!w_gate || !w_up))) return DB_ERR_NULL;
+    }
+    if (dx_addend && !dx) return DB_ERR_ARG;
+    if (!valid_pitch(dy, width, dy_pitch) || !valid_pitch(needs_x ? x : nullptr, width, x_pitch) || !valid_pitch(dx, width, dx_pitch) ||
+        !valid_pitch(dx_addend, width, dx_addend_pitch))
+        return DB_ERR_ARG;
+    const int g = grad_dtype == DB_F32 ? 4 : 2;
+    if (odd_address(dy, 2) || odd_address(x, 2) || odd_address(w_gate, 2) || odd_address(w_up, 2) || odd_address(w_down, 2) ||
+        (!e4m3 && (odd_address(gate, 2) || odd_address(up, 2))) || odd_address(dx, 2) || odd_address(dx_addend, 2) ||
+        odd_address(dw_gate, g) || odd_address(dw_up, g) || odd_address(dw_down, g) || odd_address(workspace, 256))
+        return DB_ERR_ARG;
+    const long long weight = 2LL * width * hidden, grad = static_cast<long long>(g) * width * hidden;
+    const long long kept = rows * hidden * kept_size(kept_dtype), scales = rows * scales_of(hidden);
+    const bool in_place = dx_addend == dx && dx_addend_pitch == dx_pitch;
+    const Extent touched[] = {
+        {dy, extent_bytes(rows, width, dy_pitch, 2), false}, {needs_x ? x : nullptr, extent_bytes(rows, width, x_pitch, 2), false},
+        {dx ? w_gate : nullptr, weight, false}, {dx ? w_up : nullptr, weight, false}, {w_down, weight, false},
+        {gate, kept, false}, {up, kept, false}, {e4m3 ? gate_scale : nullptr, scales, false}, {e4m3 ? up_scale : nullptr, scales, false},
+        {in_place ? nullptr : dx_addend, extent_bytes(rows, width, dx_addend_pitch, 2), false},
+        {dx, extent_bytes(rows, width, dx_pitch, 2), true}, {dw_gate, grad, true}, {dw_up, grad, true}, {dw_down, grad, true},
+        {workspace, static_cast<long long>(workspace_bytes), true}};
+    if (overlaps(touched, static_cast<int>(sizeof touched / sizeof touched[0]))) return DB_ERR_ARG;
+    const bool aligned = on_grid(dy, dy_pitch) && (!needs_x || on_grid(x, x_pitch)) && on_grid(w_down, width) &&
+                         (!dx || (on_grid(w_gate, hidden) && on_grid(w_up, hidden)));
+    GatedArgs v{};
+    v.dy = dy; v.dy_pitch = dy_pitch; v.x = x; v.x_pitch = x_pitch;
+    v.w_gate = w_gate; v.w_up = w_up; v.w_down = w_down;
+    v.residual = dx_addend; v.residual_pitch = dx_addend_pitch; v.act = act;
+    v.rows = rows; v.width = width; v.hidden = hidden; v.y = dx; v.y_pitch = dx_pitch;
+    v.gate = const_cast<void*>(gate); v.up = const_cast<void*>(up);
+    v.gate_scale = const_cast<void*>(gate_scale); v.up_scale = const_cast<void*>(up_scale);
+    v.kept_dtype = kept_dtype; v.grad_dtype = grad_dtype;
+    v.dw_gate = dw_gate; v.dw_up = dw_up; v.dw_down = dw_down;
+    Arena need(nullptr);
+    gated_backward(v, need, nullptr, aligned);
+    if (workspace_bytes < need.used) return DB_ERR_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (rows == 0) {
+        db_status st = zero(workspace, 4, stream);
+        for (void* p : {dw_gate, dw_up, dw_down})
+            if (st == DB_OK) st = zero(p, grad, stream);
+        return st;
+    }
+    Arena arena(workspace);
+    return gated_backward(v, arena, stream, aligned);
+}
