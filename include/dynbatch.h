@@ -647,6 +647,74 @@ db_status db_gated_ffn_grad(const void* dy, int64_t dy_pitch, const void* x,
                             void* cuda_stream);
 
 /* ------------------------------------------------------------------------
+ * Activation checkpoints in 8 bits        (Section 3.3.1 bounds a worker's batch
+ * by its memory: what is kept for the backward pass is most of that)
+ *
+ * Each 32 consecutive values of a row share a power of two (the last group of a
+ * row may be shorter): scale = 2^e with e the smallest integer, at least -127, that
+ * brings the largest finite magnitude of the group to at most 448; code = e4m3(x /
+ * scale), to nearest, ties to even (with the largest scale, 2^120, at most 240: what is
+ * finite stays finite).  A value is then code * scale, within 2^-4 of x
+ * relative, or 2^-10 scale where that is more.  A value that is not finite gets the
+ * code NaN and does not enter its group's scale.  This is also what db_linear and
+ * db_gated_ffn write as DB_E4M3.
+ *
+ *   x       device, [rows, cols] bf16, x_pitch >= cols elements from row to row;
+ *           unpacked values are rounded to bf16, which is exact but below 2^-126
+ *   codes   device, [rows, cols] contiguous e4m3
+ *   scale   device, [rows, ceil(cols / 32)] contiguous bytes e + 127 (255: NaN)
+ *   rows >= 0 (0: DB_OK, nothing enqueued), 1 <= cols <= 2^24, at most 2^40 values
+ * Any alignment down to the element size; 16-byte aligned rows of x and 8-byte aligned
+ * rows of codes take wide accesses.  The buffers must not overlap.
+ * ------------------------------------------------------------------------ */
+#define DB_CHECKPOINT_GROUP 32
+
+db_status db_checkpoint_pack(const void* x, int64_t x_pitch, int64_t rows,
+                             int32_t cols, void* codes, void* scale,
+                             void* cuda_stream);
+db_status db_checkpoint_unpack(const void* codes, const void* scale,
+                               int64_t rows, int32_t cols, void* x,
+                               int64_t x_pitch, void* cuda_stream);
+
+/* ------------------------------------------------------------------------
+ * Embedding table: lookup with scaling, and the table's gradient
+ *
+ *     out[t]    = scale * table[tokens[t]]
+ *     dtable[v] = scale * (sum of dy[t] over all t with tokens[t] = v)
+ *
+ * A token outside [0, vocab) (e.g. -1 for the padding of a batch) looks up a row of
+ * zeros and has no gradient, as a label outside the classes has none in the worker
+ * gradient.  Sums are fp32, in the order of a stable sort of the tokens cut into units
+ * whose length depends on rows alone; no atomics on values: the same call gives the
+ * same bits.  Rows of dtable whose token does not occur are written as zeros.
+ *
+ *   tokens  device, rows int32
+ *   table, dtable   device, [vocab, width] contiguous, fp32 or bf16
+ *   out, dy device, [rows, width] fp32 or bf16, *_pitch >= width elements from row to row
+ *   rows    0 .. 2^28 (0: the lookup enqueues nothing, the gradient is zero), vocab
+ *           1 .. 2^26, width 1 .. 2^20, at most 2^40 elements in a matrix
+ *   workspace  device scratch of >= db_embedding_grad_workspace_bytes(rows, vocab,
+ *           width) bytes (0 for invalid sizes), 256-byte aligned, uninitialised; shared
+ *           by calls on one stream, distinct for calls that may overlap
+ * Any alignment down to the element size; 16-byte aligned rows take wide accesses.
+ * Buffers that a call writes must not overlap others (DB_ERR_ARG).  Launches: lookup 1;
+ * gradient 3 up to 8192 rows, beyond that 2 for each 9 bits of vocab and 2 more.
+ * ------------------------------------------------------------------------ */
+db_status db_embedding(const int32_t* tokens, const void* table,
+                       db_dtype table_dtype, float scale, int64_t rows,
+                       int32_t vocab, int32_t width, void* out,
+                       int64_t out_pitch, db_dtype out_dtype,
+                       void* cuda_stream);
+
+size_t db_embedding_grad_workspace_bytes(int64_t rows, int32_t vocab,
+                                         int32_t width);
+db_status db_embedding_grad(const int32_t* tokens, const void* dy,
+                            int64_t dy_pitch, db_dtype dy_dtype, float scale,
+                            int64_t rows, int32_t vocab, int32_t width,
+                            void* dtable, db_dtype grad_dtype, void* workspace,
+                            size_t workspace_bytes, void* cuda_stream);
+
+/* ------------------------------------------------------------------------
  * Proportional batch-size controller, host side   (Section 3.3, Eq. 4-5)
  *
  * One adjustment from per-worker throughputs X_k (samples per unit time):

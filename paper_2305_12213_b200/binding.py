@@ -113,6 +113,13 @@ _SIGNATURES = {
                                     c_void_p, c_void_p, c_int32, c_int32, c_int64, c_int32, c_int32, c_void_p, c_int64,
                                     c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_size_t,
                                     c_void_p]),
+    "db_checkpoint_pack": (c_int32, [c_void_p, c_int64, c_int64, c_int32, c_void_p, c_void_p, c_void_p]),
+    "db_checkpoint_unpack": (c_int32, [c_void_p, c_void_p, c_int64, c_int32, c_void_p, c_int64, c_void_p]),
+    "db_embedding": (c_int32, [c_void_p, c_void_p, c_int32, c_float, c_int64, c_int32, c_int32, c_void_p, c_int64, c_int32,
+                               c_void_p]),
+    "db_embedding_grad_workspace_bytes": (c_size_t, [c_int64, c_int32, c_int32]),
+    "db_embedding_grad": (c_int32, [c_void_p, c_void_p, c_int64, c_int32, c_float, c_int64, c_int32, c_int32, c_void_p,
+                                    c_int32, c_void_p, c_size_t, c_void_p]),
     "db_status_string": (c_char_p, [c_int32]),
     "db_last_cuda_error": (c_char_p, []),
 }
@@ -936,3 +943,58 @@ def gated_ffn_grad(dy: torch.Tensor, x: Optional[torch.Tensor], w_gate: torch.Te
 def layer_status(workspace: torch.Tensor) -> int:
     """The status word at the start of a layer call's workspace (0 = every internal wait completed)."""
     return int(workspace[:4].view(torch.int32).item())
+
+
+def checkpoint_pack(x: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor,
+                    stream: Optional[torch.cuda.Stream] = None) -> None:
+    """db_checkpoint_pack: x [rows, cols] bfloat16 (rows contiguous) to codes [rows, cols] float8_e4m3fn and scale
+    [rows, checkpoint_scales(cols)] float8_e8m0fnu."""
+    call = _Call(x)
+    rows, cols = x.shape
+    xp, pitch = call.rows(x, rows, cols, "x")
+    cp, sp, _ = call.kept(codes, scale, rows, cols, "codes") if codes.dtype == torch.float8_e4m3fn else (None, None, None)
+    if cp is None and rows:
+        raise TypeError("codes must be float8_e4m3fn")
+    call(lib().db_checkpoint_pack, xp, pitch, rows, cols, cp, sp, stream=stream)
+
+
+def checkpoint_unpack(codes: torch.Tensor, scale: torch.Tensor, x: torch.Tensor,
+                      stream: Optional[torch.cuda.Stream] = None) -> None:
+    """db_checkpoint_unpack: the values that codes and scale stand for, rounded to bfloat16, into x."""
+    call = _Call(codes)
+    rows, cols = codes.shape
+    if codes.dtype != torch.float8_e4m3fn:
+        raise TypeError("codes must be float8_e4m3fn")
+    xp, pitch = call.rows(x, rows, cols, "x")
+    cp, sp, _ = call.kept(codes, scale, rows, cols, "codes")
+    call(lib().db_checkpoint_unpack, cp, sp, rows, cols, xp, pitch, stream=stream)
+
+
+def embedding(tokens: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
+              stream: Optional[torch.cuda.Stream] = None) -> None:
+    """db_embedding: out[t] = scale * table[tokens[t]]; tokens int32 (outside the table: zeros), table and out float32 or
+    bfloat16, out's rows contiguous."""
+    call = _Call(tokens)
+    vocab, width = table.shape
+    rows = tokens.numel()
+    op, pitch = call.rows(out, rows, width, "out", out.dtype)
+    call(lib().db_embedding, call.whole(tokens, tokens.shape, torch.int32, "tokens"),
+         call.whole(table, (vocab, width), table.dtype, "table"), _dtype_code(table.dtype), float(scale), rows, vocab, width,
+         op, pitch, _dtype_code(out.dtype), stream=stream)
+
+
+def embedding_grad_workspace_bytes(rows: int, vocab: int, width: int) -> int:
+    return int(lib().db_embedding_grad_workspace_bytes(int(rows), int(vocab), int(width)))
+
+
+def embedding_grad(tokens: torch.Tensor, dy: torch.Tensor, dtable: torch.Tensor, workspace: torch.Tensor,
+                   scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """db_embedding_grad: dtable[v] = scale * sum of dy[t] with tokens[t] == v, every row written.  dy and dtable float32 or
+    bfloat16; workspace: embedding_grad_workspace_bytes(rows, vocab, width) bytes."""
+    call = _Call(tokens)
+    vocab, width = dtable.shape
+    rows = tokens.numel()
+    dp, pitch = call.rows(dy, rows, width, "dy", dy.dtype)
+    call(lib().db_embedding_grad, call.whole(tokens, tokens.shape, torch.int32, "tokens"), dp, pitch, _dtype_code(dy.dtype),
+         float(scale), rows, vocab, width, call.whole(dtable, (vocab, width), dtable.dtype, "dtable"),
+         _dtype_code(dtable.dtype), *call.workspace(workspace), stream=stream)

@@ -35,7 +35,7 @@ __global__ void __launch_bounds__(kBlock) checkpoint_pack_kernel(const __grid_co
         float v[8];
         const bf16* p = a.x + row * a.x_pitch + col;
         if (n == 8 && lg::aligned_to(p, 16)) {
-            const uint4 q = __ldcs(reinterpret_cast<const uint4*>(p));
+            const uint4 q = *reinterpret_cast<const uint4*>(p);
             lg::unpack2(q.x, v[0], v[1]); lg::unpack2(q.y, v[2], v[3]);
             lg::unpack2(q.z, v[4], v[5]); lg::unpack2(q.w, v[6], v[7]);
         } else {
@@ -51,6 +51,10 @@ __global__ void __launch_bounds__(kBlock) checkpoint_pack_kernel(const __grid_co
         const uint32_t byte = ck8::scale_byte(top);
         const float inverse = ck8::scale_inverse(byte);
         if ((piece & 3) == 0) a.scale[row * a.groups + piece / 4] = static_cast<uint8_t>(byte);
+        if (byte >= ck8::kTopByte) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = ck8::hold_finite(v[j]);
+        }
         const uint32_t c0 = ck8::codes4(v[0], v[1], v[2], v[3], inverse), c1 = ck8::codes4(v[4], v[5], v[6], v[7], inverse);
         uint8_t* to = a.codes + row * a.cols + col;
         if (n == 8 && lg::aligned_to(to, 8)) {
@@ -82,7 +86,7 @@ __global__ void __launch_bounds__(kBlock) checkpoint_unpack_kernel(const __grid_
         const uint8_t* p = a.codes + row * a.cols + col;
         uint32_t c[2] = {0, 0};
         if (n == 8 && lg::aligned_to(p, 8)) {
-            const uint2 q = __ldcs(reinterpret_cast<const uint2*>(p));
+            const uint2 q = *reinterpret_cast<const uint2*>(p);
             c[0] = q.x; c[1] = q.y;
         } else {
 #pragma unroll

@@ -43,6 +43,12 @@ __device__ __forceinline__ float finite_magnitude(float x) {  // 0 for what is n
     const float m = fabsf(x);
     return m < __uint_as_float(0x7F800000u) ? m : 0.f;
 }
+// With the largest scale, 2^120, the codes from 256 on would stand for 2^128 and more: finite values stop at 240 there.
+constexpr uint32_t kTopByte = 247;
+__device__ __forceinline__ float hold_finite(float x) {
+    const float limit = 240.f * __uint_as_float(kTopByte << 23);
+    return finite_magnitude(x) > limit ? copysignf(limit, x) : x;
+}
 __device__ __forceinline__ float2 values2(uint32_t two_codes) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two_codes & 0xFFFFu), __NV_E4M3);
     return __half22float2(__half2(h));

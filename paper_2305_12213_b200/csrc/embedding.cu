@@ -1,0 +1,643 @@
+// Embedding table: lookup with scaling, and the table's gradient by sorted tokens.
+//     out[t] = scale * table[token[t]]          d_table[v] = scale * sum over t with token[t] = v of dy[t], t ascending
+// Both are HBM-bound.  The gradient reads every row of dy once and writes every row of the table once: positions are
+// sorted by token (stable, so that a row's sum has one order), the sorted list is cut into equal units whatever the
+// tokens' frequencies are, a unit adds the rows of its runs of equal tokens in registers, and runs that reach over
+// units are joined by a second small kernel from the units' partial sums.  No float atomics: the same call gives the
+// same bits.
+#include <algorithm>
+#include <cstring>
+
+#include "common.h"
+#include "layer_gemm.cuh"
+
+namespace dynbatch {
+namespace {
+
+using bf16 = __nv_bfloat16;
+
+constexpr int kBlock = 256;
+constexpr int kDigitBits = 9, kBins = 1 << kDigitBits;
+constexpr int kSortWarps = kBlock / 32, kSteps = 8;
+constexpr int kPart = kBlock * kSteps;           // entries a CTA sorts at a time: 2048
+constexpr int kMaxSortBlocks = 512;              // every CTA reads all CTAs' counts, so their number is bounded
+constexpr int kSmallWarps = 32, kSmallRows = 8192;   // up to here one CTA sorts alone, in one launch
+constexpr long long kMaxRows = 1LL << 28, kMaxVocab = 1LL << 26, kMaxWidth = 1LL << 20;
+
+long long cdiv(long long a, long long b) { return (a + b - 1) / b; }
+
+// ---------------------------------------------------------------------------------------------- eight values of a row
+__device__ __forceinline__ void load8(const bf16* p, int n, float (&v)[8]) {
+    if (n == 8 && lg::aligned_to(p, 16)) {
+        const uint4 q = *reinterpret_cast<const uint4*>(p);
+        lg::unpack2(q.x, v[0], v[1]); lg::unpack2(q.y, v[2], v[3]);
+        lg::unpack2(q.z, v[4], v[5]); lg::unpack2(q.w, v[6], v[7]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < n ? __bfloat162float(p[j]) : 0.f;
+    }
+}
+__device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
+    if (n == 8 && lg::aligned_to(p, 16)) {
+        const float4 a = *reinterpret_cast<const float4*>(p), b = *(reinterpret_cast<const float4*>(p) + 1);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : 0.f;
+    }
+}
+__device__ __forceinline__ void store8(bf16* p, int n, const float (&v)[8]) {
+    if (n == 8 && lg::aligned_to(p, 16)) {
+        __stcs(reinterpret_cast<uint4*>(p), make_uint4(lg::pack2(v[0], v[1]), lg::pack2(v[2], v[3]), lg::pack2(v[4], v[5]), lg::pack2(v[6], v[7])));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) p[j] = __float2bfloat16_rn(v[j]);
+    }
+}
+__device__ __forceinline__ void store8(float* p, int n, const float (&v)[8]) {
+    if (n == 8 && lg::aligned_to(p, 16)) {
+        __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
+        __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) p[j] = v[j];
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- lookup
+struct LookupArgs {
+    const int* tokens;
+    const void* table;
+    void* out;
+    long long out_pitch, rows;
+    int vocab, width;
+    float scale;
+};
+
+// A thread has 8 values of a row and takes four rows' pieces at a time, so that four loads are under way.
+template <class TT, class OT>
+__global__ void __launch_bounds__(kBlock) embedding_kernel(const __grid_constant__ LookupArgs a) {
+    constexpr int kDeep = 4;
+    tc::griddep_wait();
+    tc::griddep_launch_dependents();
+    const TT* table = static_cast<const TT*>(a.table);
+    OT* out = static_cast<OT*>(a.out);
+    const long long per_row = (a.width + 7) / 8, total = a.rows * per_row;
+    const long long stride = static_cast<long long>(gridDim.x) * kBlock;
+    for (long long i = static_cast<long long>(blockIdx.x) * kBlock + threadIdx.x; i < total; i += stride * kDeep) {
+        float v[kDeep][8];
+        long long row[kDeep];
+        int col[kDeep], n[kDeep];
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d) {
+            const long long k = i + d * stride;
+            row[d] = k / per_row;
+            col[d] = static_cast<int>(k - row[d] * per_row) * 8;
+            n[d] = k < total ? min(8, a.width - col[d]) : 0;
+            const int token = k < total ? a.tokens[row[d]] : -1;
+            const bool in = token >= 0 && token < a.vocab;
+            load8(table + static_cast<long long>(in ? token : 0) * a.width + col[d], in ? n[d] : 0, v[d]);
+        }
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d) {
+            if (n[d] == 0) break;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[d][j] *= a.scale;
+            store8(out + row[d] * a.out_pitch + col[d], n[d], v[d]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- sorting positions by token
+struct SortArgs {
+    const int* tokens;            // first pass; tokens outside the table sort behind it, as key `vocab`
+    const int* keys_in; const int* pos_in;
+    int* keys_out; int* pos_out;
+    int* counts;                  // [CTA][bin]
+    uint8_t* present;             // [vocab] 1 where a token occurs: zeroed by the first pass, set by the last
+    int* joins;                   // number of runs to join, zeroed by the first pass
+    int rows, vocab, per_block, shift, first, last;
+};
+
+__device__ __forceinline__ int key_of(const int* tokens, int vocab, int i) {
+    const int t = tokens[i];
+    return t >= 0 && t < vocab ? t : vocab;
+}
+__device__ __forceinline__ int digit_of(int key, int shift) { return (key >> shift) & (kBins - 1); }
+
+__global__ void __launch_bounds__(kBlock) sort_count_kernel(const __grid_constant__ SortArgs a) {
+    __shared__ int bins[kBins];
+    tc::griddep_wait();
+    tc::griddep_launch_dependents();
+    for (int b = threadIdx.x; b < kBins; b += kBlock) bins[b] = 0;
+    if (a.first) {
+        for (int v = blockIdx.x * kBlock + threadIdx.x; v < a.vocab; v += gridDim.x * kBlock) a.present[v] = 0;
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.joins = 0;
+    }
+    __syncthreads();
+    const int begin = blockIdx.x * a.per_block, end = min(a.rows, begin + a.per_block);
+    for (int i = begin + threadIdx.x; i < end; i += kBlock)
+        atomicAdd(&bins[digit_of(a.first ? key_of(a.tokens, a.vocab, i) : a.keys_in[i], a.shift)], 1);
+    __syncthreads();
+    for (int b = threadIdx.x; b < kBins; b += kBlock) a.counts[blockIdx.x * kBins + b] = bins[b];
+}
+
+// Exclusive sum over the bins, two per thread of the first eight warps; `total` holds kBins values and is replaced.
+__device__ __forceinline__ void scan_bins(int* total, int* warp_sum) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int x = 0, y = 0, s = 0;
+    if (tid < kBins / 2) {
+        x = total[2 * tid]; y = total[2 * tid + 1];
+        s = x + y;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(0xFFFFFFFFu, s, d);
+            if (lane >= d) s += o;
+        }
+        if (lane == 31) warp_sum[warp] = s;
+    }
+    __syncthreads();
+    if (tid < kBins / 2) {
+        int before = s - x - y;
+        for (int w = 0; w < warp; ++w) before += warp_sum[w];
+        total[2 * tid] = before;
+        total[2 * tid + 1] = before + x;
+    }
+    __syncthreads();
+}
+
+// Ranks of 32 * STEPS * WARPS consecutive entries by digit, stable: a warp's entries are consecutive, and within a step
+// equal digits are ranked by lane.  counters[WARPS][kBins] becomes the number of equal digits in earlier warps.
+template <int WARPS, int STEPS>
+__device__ __forceinline__ void rank_entries(const int (&key)[STEPS], int shift, int entries_left, unsigned short* counters,
+                                             int (&rank)[STEPS]) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    unsigned short* mine = counters + warp * kBins;
+    for (int b = lane; b < kBins; b += 32) mine[b] = 0;
+    __syncwarp();
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        const bool in = s * 32 + lane < entries_left;
+        const unsigned live = __ballot_sync(0xFFFFFFFFu, in);
+        rank[s] = 0;
+        if (in) {
+            const int d = digit_of(key[s], shift);
+            const unsigned same = __match_any_sync(live, d);
+            const int below = __popc(same & ((1u << lane) - 1));
+            const int before = mine[d];
+            __syncwarp(live);
+            if (below == 0) mine[d] = static_cast<unsigned short>(before + __popc(same));
+            rank[s] = before + below;
+        }
+        __syncwarp();
+    }
+}
+
+__global__ void __launch_bounds__(kBlock) sort_scatter_kernel(const __grid_constant__ SortArgs a) {
+    __shared__ unsigned short counters[kSortWarps * kBins];
+    __shared__ int base[kBins], total[kBins], warp_sum[kSortWarps];
+    tc::griddep_wait();
+    tc::griddep_launch_dependents();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    for (int b = tid; b < kBins; b += kBlock) {
+        int before = 0, all = 0;
+#pragma unroll 8
+        for (int j = 0; j < static_cast<int>(gridDim.x); ++j) {
+            const int c = a.counts[j * kBins + b];
+            all += c;
+            if (j < static_cast<int>(blockIdx.x)) before += c;
+        }
+        base[b] = before;
+        total[b] = all;
+    }
+    __syncthreads();
+    scan_bins(total, warp_sum);
+    for (int b = tid; b < kBins; b += kBlock) base[b] += total[b];
+    __syncthreads();
+    const int begin = blockIdx.x * a.per_block, end = min(a.rows, begin + a.per_block);
+    for (int part = begin; part < end; part += kPart) {
+        const int first = part + warp * 32 * kSteps;
+        const int left = max(0, min(32 * kSteps, end - first));
+        int key[kSteps], pos[kSteps], rank[kSteps];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int i = first + s * 32 + lane;
+            const bool in = s * 32 + lane < left;
+            key[s] = in ? (a.first ? key_of(a.tokens, a.vocab, i) : a.keys_in[i]) : 0;
+            pos[s] = in ? (a.first ? i : a.pos_in[i]) : 0;
+        }
+        rank_entries<kSortWarps, kSteps>(key, a.shift, left, counters, rank);
+        __syncthreads();
+        for (int b = tid; b < kBins; b += kBlock) {       // counts become the start of each warp's entries
+            int at = 0;
+#pragma unroll
+            for (int w = 0; w < kSortWarps; ++w) {
+                const int c = counters[w * kBins + b];
+                counters[w * kBins + b] = static_cast<unsigned short>(at);
+                at += c;
+            }
+            total[b] = at;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            if (s * 32 + lane < left) {
+                const int d = digit_of(key[s], a.shift);
+                const int to = base[d] + counters[warp * kBins + d] + rank[s];
+                a.keys_out[to] = key[s];
+                a.pos_out[to] = pos[s];
+                if (a.last && key[s] < a.vocab) a.present[key[s]] = 1;
+            }
+        }
+        __syncthreads();
+        for (int b = tid; b < kBins; b += kBlock) base[b] += total[b];
+        __syncthreads();
+    }
+}
+
+// All passes in one CTA, in shared memory: the whole sort costs one launch where a launch is what it costs.
+struct SmallSortArgs {
+    const int* tokens;
+    int* keys_out; int* pos_out;
+    uint8_t* present;
+    int* joins;
+    int rows, vocab, passes;
+};
+constexpr int kSmallSmem = kSmallRows * 8 + kSmallWarps * kBins * 2;
+
+__global__ void __launch_bounds__(kSmallWarps * 32) small_sort_kernel(const __grid_constant__ SmallSortArgs a) {
+    extern __shared__ int small_smem[];
+    int* keys = small_smem;
+    int* poss = small_smem + kSmallRows;
+    unsigned short* counters = reinterpret_cast<unsigned short*>(small_smem + 2 * kSmallRows);
+    __shared__ int total[kBins], warp_sum[kSmallWarps];
+    constexpr int kThreads = kSmallWarps * 32, kDepth = kSmallRows / kThreads;
+    tc::griddep_wait();
+    tc::griddep_launch_dependents();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    for (int v = tid; v < a.vocab; v += kThreads) a.present[v] = 0;
+    if (tid == 0) *a.joins = 0;
+    // entries dealt to the warps in equal consecutive parts of whole steps
+    const int steps = (a.rows + kThreads - 1) / kThreads, first = warp * 32 * steps, left = max(0, min(32 * steps, a.rows - first));
+    int key[kDepth], pos[kDepth], rank[kDepth];
+#pragma unroll
+    for (int s = 0; s < kDepth; ++s) {
+        const bool in = s * 32 + lane < left;
+        pos[s] = first + s * 32 + lane;
+        key[s] = in ? key_of(a.tokens, a.vocab, pos[s]) : 0;
+    }
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const int shift = pass * kDigitBits;
+        rank_entries<kSmallWarps, kDepth>(key, shift, left, counters, rank);
+        __syncthreads();
+        if (tid < kBins) {
+            int at = 0;
+#pragma unroll
+            for (int w = 0; w < kSmallWarps; ++w) {
+                const int c = counters[w * kBins + tid];
+                counters[w * kBins + tid] = static_cast<unsigned short>(at);
+                at += c;
+            }
+            total[tid] = at;
+        }
+        __syncthreads();
+        scan_bins(total, warp_sum);
+        const bool last = pass + 1 == a.passes;
+#pragma unroll
+        for (int s = 0; s < kDepth; ++s) {
+            if (s * 32 + lane < left) {
+                const int d = digit_of(key[s], shift);
+                const int to = total[d] + counters[warp * kBins + d] + rank[s];
+                if (last) {
+                    a.keys_out[to] = key[s];
+                    a.pos_out[to] = pos[s];
+                    if (key[s] < a.vocab) a.present[key[s]] = 1;
+                } else {
+                    keys[to] = key[s];
+                    poss[to] = pos[s];
+                }
+            }
+        }
+        __syncthreads();
+        if (!last) {
+#pragma unroll
+            for (int s = 0; s < kDepth; ++s) {
+                if (s * 32 + lane < left) {
+                    key[s] = keys[first + s * 32 + lane];
+                    pos[s] = poss[first + s * 32 + lane];
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- sums of runs
+struct SumArgs {
+    const int* keys; const int* pos;
+    const uint8_t* present;
+    const void* dy; long long dy_pitch;
+    void* out;
+    float* head; float* tail;     // [unit][width]: the part of a run that came from an earlier unit, that goes on in the next
+    int* joins; int* join_list;   // units in which a run begins that goes on
+    int rows, vocab, width;
+    int unit, units;              // sorted entries per unit
+    int threads_per_row;          // a power of two up to kBlock: 8 columns each
+    int sum_ctas;                 // the CTAs behind these write the rows of tokens that do not occur
+    float scale;
+};
+
+template <class DT, class OT>
+__global__ void __launch_bounds__(kBlock) embedding_sum_kernel(const __grid_constant__ SumArgs a) {
+    constexpr int kDeep = 4;
+    tc::griddep_wait();
+    tc::griddep_launch_dependents();
+    const int group = threadIdx.x / a.threads_per_row, groups = kBlock / a.threads_per_row;
+    const int col = (blockIdx.y * a.threads_per_row + threadIdx.x % a.threads_per_row) * 8, n = min(8, a.width - col);
+    if (n <= 0) return;
+    OT* out = static_cast<OT*>(a.out);
+    if (static_cast<int>(blockIdx.x) >= a.sum_ctas) {
+        const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        const int step = (gridDim.x - a.sum_ctas) * groups;
+        for (int v = (blockIdx.x - a.sum_ctas) * groups + group; v < a.vocab; v += step)
+            if (!a.present[v]) store8(out + static_cast<long long>(v) * a.width + col, n, zero);
+        return;
+    }
+    const int unit = blockIdx.x * groups + group;
+    if (unit >= a.units) return;
+    const int begin = unit * a.unit, end = min(a.rows, begin + a.unit);
+    const DT* dy = static_cast<const DT*>(a.dy);
+    int current = a.keys[begin];
+    bool from_before = begin > 0 && a.keys[begin - 1] == current;
+    const int next = end < a.rows ? a.keys[end] : -1;
+    float sum[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+    const auto flush = [&](bool goes_on) {
+        if (current >= a.vocab) return;
+        if (from_before) {
+            store8(a.head + static_cast<long long>(unit) * a.width + col, n, sum);
+        } else if (goes_on) {
+            store8(a.tail + static_cast<long long>(unit) * a.width + col, n, sum);
+            if (col == 0) a.join_list[atomicAdd(a.joins, 1)] = unit;
+        } else {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = sum[j] * a.scale;
+            store8(out + static_cast<long long>(current) * a.width + col, n, v);
+        }
+    };
+    for (int i = begin; i < end; i += kDeep) {
+        int key[kDeep];
+        float v[kDeep][8];
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d) {
+            const bool in = i + d < end;
+            key[d] = in ? a.keys[i + d] : -1;
+            const long long row = in ? a.pos[i + d] : 0;
+            load8(dy + row * a.dy_pitch + col, in && key[d] < a.vocab ? n : 0, v[d]);
+        }
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d) {
+            if (i + d >= end) break;
+            if (key[d] != current) {
+                flush(false);
+                current = key[d];
+                from_before = false;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += v[d][j];
+        }
+    }
+    flush(next == current);
+}
+
+// Runs over several units: the beginning's sum, then the units' in a fixed order (eight warps, each every eighth unit).
+template <class OT>
+__global__ void __launch_bounds__(kBlock) embedding_join_kernel(const __grid_constant__ SumArgs a) {
+    constexpr int kWarps = kBlock / 32, kDeep = 4;
+    __shared__ float part[kWarps][32 * 8 + 8];
+    tc::griddep_wait();
+    tc::griddep_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int slices = (a.width + 255) / 256, joins = *a.joins;
+    for (long long i = blockIdx.x; i < static_cast<long long>(joins) * slices; i += gridDim.x) {
+        const int unit = a.join_list[i / slices], col = static_cast<int>(i % slices) * 256 + lane * 8, n = max(0, min(8, a.width - col));
+        const int key = a.keys[min(a.rows, (unit + 1) * a.unit) - 1];
+        float sum[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+        if (warp == 0) load8(a.tail + static_cast<long long>(unit) * a.width + col, n, sum);
+        bool more = true;
+        for (int u = unit + 1 + warp; more; u += kWarps * kDeep) {
+            float v[kDeep][8];
+            bool in[kDeep];
+#pragma unroll
+            for (int d = 0; d < kDeep; ++d) {
+                const int w = u + d * kWarps;
+                in[d] = w < a.units && a.keys[static_cast<long long>(w) * a.unit] == key;
+                load8(a.head + static_cast<long long>(in[d] ? w : unit) * a.width + col, in[d] ? n : 0, v[d]);
+            }
+#pragma unroll
+            for (int d = 0; d < kDeep; ++d)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] += v[d][j];
+            more = in[kDeep - 1];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) part[warp][lane * 8 + j] = sum[j];
+        __syncthreads();
+        if (warp == 0) {
+#pragma unroll
+            for (int w = 1; w < kWarps; ++w)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] += part[w][lane * 8 + j];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] *= a.scale;
+            if (n > 0) store8(static_cast<OT*>(a.out) + static_cast<long long>(key) * a.width + col, n, sum);
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- host
+struct Launch {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr;
+    Launch(dim3 grid, int block, size_t smem, cudaStream_t stream) {
+        std::memset(&cfg, 0, sizeof cfg);
+        cfg.gridDim = grid;
+        cfg.blockDim = dim3(block);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = stream;
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+    }
+    Launch(const Launch&) = delete;
+    Launch& operator=(const Launch&) = delete;
+};
+
+bool valid_size(long long rows, long long vocab, long long width) {
+    return rows >= 0 && rows <= kMaxRows && vocab >= 1 && vocab <= kMaxVocab && width >= 1 && width <= kMaxWidth &&
+           rows * width <= (1LL << 40) && vocab * width <= (1LL << 40);
+}
+
+// Entries per unit: few enough that short batches fill the GPU, enough that partial sums stay rare in long ones.
+int unit_of(long long rows) { return rows <= 4096 ? 8 : rows <= 16384 ? 16 : 32; }
+
+struct GradLayout {
+    size_t keys[2], pos[2], counts, present, joins, join_list, head, tail, total;
+    int unit, units;
+};
+GradLayout grad_layout(long long rows, long long vocab, long long width) {
+    GradLayout L;
+    size_t at = 0;
+    const auto take = [&](long long bytes) {
+        const size_t p = at;
+        at += (static_cast<size_t>(bytes) + 255) / 256 * 256;
+        return p;
+    };
+    L.unit = unit_of(rows);
+    L.units = static_cast<int>(cdiv(rows, L.unit));
+    for (int i = 0; i < 2; ++i) {
+        L.keys[i] = take(4 * rows);
+        L.pos[i] = take(4 * rows);
+    }
+    L.counts = take(4LL * kBins * std::min<long long>(kMaxSortBlocks, cdiv(rows, kPart)));
+    L.present = take(vocab);
+    L.joins = take(4);
+    L.join_list = take(4LL * L.units);
+    L.head = take(4LL * L.units * width);
+    L.tail = take(4LL * L.units * width);
+    L.total = at + 256;
+    return L;
+}
+
+bool apart(const void* a, long long na, const void* b, long long nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return na <= 0 || nb <= 0 || x + static_cast<uintptr_t>(na) <= y || y + static_cast<uintptr_t>(nb) <= x;
+}
+int size_of(db_dtype t) { return t == DB_F32 ? 4 : 2; }
+bool valid_type(db_dtype t) { return t == DB_F32 || t == DB_BF16; }
+
+template <class DT, class OT>
+db_status launch_sum(const SumArgs& a, dim3 grid, cudaStream_t stream) {
+    Launch S(grid, kBlock, 0, stream);
+    DB_CUDA_TRY(cudaLaunchKernelEx(&S.cfg, embedding_sum_kernel<DT, OT>, a));
+    if (a.units > 1) {
+        Launch J(dim3(static_cast<unsigned>(std::min<long long>(4LL * sm_count(), static_cast<long long>(a.units) * cdiv(a.width, 256)))), kBlock, 0, stream);
+        DB_CUDA_TRY(cudaLaunchKernelEx(&J.cfg, embedding_join_kernel<OT>, a));
+    }
+    return DB_OK;
+}
+
+}  // namespace
+}  // namespace dynbatch
+
+extern "C" db_status db_embedding(const int32_t* tokens, const void* table, db_dtype table_dtype, float scale, int64_t rows,
+                                  int32_t vocab, int32_t width, void* out, int64_t out_pitch, db_dtype out_dtype,
+                                  void* cuda_stream) {
+    using namespace dynbatch;
+    if (!valid_size(rows, vocab, width)) return DB_ERR_ARG;
+    if (!valid_type(table_dtype) || !valid_type(out_dtype)) return DB_ERR_UNSUPPORTED;
+    if (!table || (rows > 0 && (!tokens || !out))) return DB_ERR_NULL;
+    const int ts = size_of(table_dtype), os = size_of(out_dtype);
+    if (rows > 0 && (out_pitch < width || out_pitch > (1LL << 31))) return DB_ERR_ARG;
+    if (reinterpret_cast<uintptr_t>(tokens) % 4 || reinterpret_cast<uintptr_t>(table) % ts || reinterpret_cast<uintptr_t>(out) % os) return DB_ERR_ARG;
+    if (rows == 0) return DB_OK;
+    const long long no = ((rows - 1) * out_pitch + width) * os;
+    if (!apart(out, no, tokens, 4 * rows) || !apart(out, no, table, static_cast<long long>(vocab) * width * ts)) return DB_ERR_ARG;
+    const LookupArgs a{tokens, table, out, out_pitch, rows, vocab, width, scale};
+    const long long pieces = rows * ((width + 7) / 8);
+    Launch L(dim3(static_cast<unsigned>(std::min<long long>(cdiv(pieces, kBlock), 8LL * sm_count()))), kBlock, 0, static_cast<cudaStream_t>(cuda_stream));
+    void (*fn)(const LookupArgs) = table_dtype == DB_F32 ? (out_dtype == DB_F32 ? embedding_kernel<float, float> : embedding_kernel<float, bf16>)
+                                                         : (out_dtype == DB_F32 ? embedding_kernel<bf16, float> : embedding_kernel<bf16, bf16>);
+    DB_CUDA_TRY(cudaLaunchKernelEx(&L.cfg, fn, a));
+    return DB_OK;
+}
+
+extern "C" size_t db_embedding_grad_workspace_bytes(int64_t rows, int32_t vocab, int32_t width) {
+    using namespace dynbatch;
+    return valid_size(rows, vocab, width) ? grad_layout(rows, vocab, width).total : 0;
+}
+
+extern "C" db_status db_embedding_grad(const int32_t* tokens, const void* dy, int64_t dy_pitch, db_dtype dy_dtype, float scale,
+                                       int64_t rows, int32_t vocab, int32_t width, void* dtable, db_dtype grad_dtype,
+                                       void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    using namespace dynbatch;
+    if (!valid_size(rows, vocab, width)) return DB_ERR_ARG;
+    if (!valid_type(dy_dtype) || !valid_type(grad_dtype)) return DB_ERR_UNSUPPORTED;
+    if (!dtable || !workspace || (rows > 0 && (!tokens || !dy))) return DB_ERR_NULL;
+    const int ds = size_of(dy_dtype), gs = size_of(grad_dtype);
+    if (rows > 0 && (dy_pitch < width || dy_pitch > (1LL << 31))) return DB_ERR_ARG;
+    if (reinterpret_cast<uintptr_t>(tokens) % 4 || reinterpret_cast<uintptr_t>(dy) % ds || reinterpret_cast<uintptr_t>(dtable) % gs ||
+        reinterpret_cast<uintptr_t>(workspace) % 256)
+        return DB_ERR_ARG;
+    const GradLayout L = grad_layout(rows, vocab, width);
+    if (workspace_bytes < L.total) return DB_ERR_ARG;
+    const long long nd = rows > 0 ? ((rows - 1) * dy_pitch + width) * ds : 0, ng = static_cast<long long>(vocab) * width * gs;
+    const long long nw = static_cast<long long>(workspace_bytes);
+    if (!apart(dtable, ng, dy, nd) || !apart(dtable, ng, tokens, 4 * rows) || !apart(dtable, ng, workspace, nw) ||
+        !apart(workspace, nw, dy, nd) || !apart(workspace, nw, tokens, 4 * rows))
+        return DB_ERR_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (rows == 0) {
+        DB_CUDA_TRY(cudaMemsetAsync(dtable, 0, static_cast<size_t>(ng), stream));
+        return DB_OK;
+    }
+    char* base = static_cast<char*>(workspace);
+    const auto ints = [&](size_t at) { return reinterpret_cast<int*>(base + at); };
+    // digits of 9 bits until the largest key, vocab (a token outside the table), is covered
+    int passes = 1;
+    while (vocab >> (passes * kDigitBits)) ++passes;
+    int sorted = 0;
+    if (rows <= kSmallRows) {
+        SmallSortArgs s{tokens, ints(L.keys[0]), ints(L.pos[0]), reinterpret_cast<uint8_t*>(base + L.present), ints(L.joins),
+                        static_cast<int>(rows), vocab, passes};
+        DB_CUDA_TRY(cudaFuncSetAttribute(small_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem));
+        Launch S(dim3(1), kSmallWarps * 32, kSmallSmem, stream);
+        DB_CUDA_TRY(cudaLaunchKernelEx(&S.cfg, small_sort_kernel, s));
+    } else {
+        SortArgs s{};
+        s.tokens = tokens; s.rows = static_cast<int>(rows); s.vocab = vocab;
+        s.counts = ints(L.counts);
+        s.present = reinterpret_cast<uint8_t*>(base + L.present);
+        s.joins = ints(L.joins);
+        const int blocks = static_cast<int>(std::min<long long>(kMaxSortBlocks, cdiv(rows, kPart)));
+        s.per_block = static_cast<int>(cdiv(cdiv(rows, blocks), kPart) * kPart);
+        const int used = static_cast<int>(cdiv(rows, s.per_block));
+        for (int p = 0; p < passes; ++p) {
+            s.first = p == 0; s.last = p + 1 == passes; s.shift = p * kDigitBits;
+            s.keys_in = ints(L.keys[(p + 1) & 1]); s.pos_in = ints(L.pos[(p + 1) & 1]);
+            s.keys_out = ints(L.keys[p & 1]); s.pos_out = ints(L.pos[p & 1]);
+            sorted = p & 1;
+            Launch C(dim3(used), kBlock, 0, stream), S(dim3(used), kBlock, 0, stream);
+            DB_CUDA_TRY(cudaLaunchKernelEx(&C.cfg, sort_count_kernel, s));
+            DB_CUDA_TRY(cudaLaunchKernelEx(&S.cfg, sort_scatter_kernel, s));
+        }
+    }
+    SumArgs a{};
+    a.keys = ints(L.keys[sorted]); a.pos = ints(L.pos[sorted]);
+    a.present = reinterpret_cast<uint8_t*>(base + L.present);
+    a.dy = dy; a.dy_pitch = dy_pitch; a.out = dtable;
+    a.head = reinterpret_cast<float*>(base + L.head); a.tail = reinterpret_cast<float*>(base + L.tail);
+    a.joins = ints(L.joins); a.join_list = ints(L.join_list);
+    a.rows = static_cast<int>(rows); a.vocab = vocab; a.width = width;
+    a.unit = L.unit; a.units = L.units; a.scale = scale;
+    int t = 1;
+    while (t < kBlock && t * 8 < width) t *= 2;
+    a.threads_per_row = t;
+    const int groups = kBlock / t;
+    a.sum_ctas = static_cast<int>(cdiv(L.units, groups));
+    const long long zero_ctas = std::min<long long>(cdiv(vocab, groups), 4LL * sm_count());
+    const dim3 grid(static_cast<unsigned>(a.sum_ctas + zero_ctas), static_cast<unsigned>(cdiv(width, 8LL * t)));
+    if (dy_dtype == DB_F32) return grad_dtype == DB_F32 ? launch_sum<float, float>(a, grid, stream) : launch_sum<float, bf16>(a, grid, stream);
+    return grad_dtype == DB_F32 ? launch_sum<bf16, float>(a, grid, stream) : launch_sum<bf16, bf16>(a, grid, stream);
+}

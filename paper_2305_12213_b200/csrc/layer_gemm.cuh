@@ -125,21 +125,28 @@ __device__ __forceinline__ void store_row(float* p, int n, const float (&v)[kChu
             if (i < n) p[i] = v[i];
     }
 }
-__device__ __forceinline__ void keep_row(const Kept& k, int e4m3, long long row, int col, int N, int n, const float (&v)[kChunk]) {
+__device__ __forceinline__ void keep_row(const Kept& k, int e4m3, long long row, int col, int N, int n, const float (&x)[kChunk]) {
     if (!e4m3) {
-        store_row(static_cast<__nv_bfloat16*>(k.data) + row * N + col, n, v);
+        store_row(static_cast<__nv_bfloat16*>(k.data) + row * N + col, n, x);
         return;
     }
     float top = 0.f;
 #pragma unroll
     for (int i = 0; i < kChunk; ++i)
-        if (i < n) top = fmaxf(top, ck8::finite_magnitude(v[i]));
+        if (i < n) top = fmaxf(top, ck8::finite_magnitude(x[i]));
     const uint32_t byte = ck8::scale_byte(top);
     const float inverse = ck8::scale_inverse(byte);
     k.scale[row * ((N + kChunk - 1) / kChunk) + col / kChunk] = static_cast<uint8_t>(byte);
     uint32_t c[8];
+    if (byte < ck8::kTopByte) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = ck8::codes4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inverse);
+        for (int i = 0; i < 8; ++i) c[i] = ck8::codes4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3], inverse);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            c[i] = ck8::codes4(ck8::hold_finite(x[4 * i]), ck8::hold_finite(x[4 * i + 1]), ck8::hold_finite(x[4 * i + 2]),
+                               ck8::hold_finite(x[4 * i + 3]), inverse);
+    }
     uint8_t* p = static_cast<uint8_t*>(k.data) + row * N + col;
     if (n == kChunk && aligned_to(p, 16)) {
         *reinterpret_cast<uint4*>(p) = make_uint4(c[0], c[1], c[2], c[3]);

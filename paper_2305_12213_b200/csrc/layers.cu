@@ -265,6 +265,9 @@ Plan make_plan(Kind kind, const Size* sizes, int n, long long blocks) {
     constexpr double kBlock[kTileShapes] = {560, 420, 330}, kTile[kTileShapes] = {2600, 1700, 1300}, kCombine = 5000;
     Plan best;
     double least = 0;
+    if (blocks == 0) return best;                            // no rows: nothing is launched
+    for (int j = 0; j < n; ++j)
+        if (sizes[j].M == 0) return best;
     if (n == 0) return best;
     for (int i = 0; i < kTileShapes; ++i) {
         const TileShape shape = static_cast<TileShape>(i);
