@@ -6,7 +6,7 @@
 // One persistent CTA (or pair of CTAs) per SM (pair) walks the output tiles:
 //   warp 0   (one lane) copies 64-deep operand blocks into a ring of shared-memory stages by TMA
 //   warp 1   owns the tensor memory; one lane issues four tcgen05.mma a stage (of the pair's first CTA alone)
-//   warps 2-9  take the finished accumulator out of tensor memory, 32 columns of a row per thread, apply the epilogue
+//   the others take the finished accumulator out of tensor memory, 32 columns of a row per thread, apply the epilogue
 //            and store; two accumulators, so that this runs under the next tile's products.
 // A pair (cta_group::2) computes 256 rows x BN columns: each CTA holds its own 128 rows of A and half of B's, and the
 // tensor cores of both read both halves, so an operand byte in shared memory serves twice as many products.
@@ -26,8 +26,6 @@ namespace lg {
 
 constexpr int kRows = 128;             // rows of A a CTA holds = its tensor-memory lanes
 constexpr int kBlockK = 64;            // bf16 in a 128-byte swizzled row
-constexpr int kEpilogueWarps = 8;      // two per tensor-memory lane quarter, half of the tile's columns each
-constexpr int kThreads = 64 + 32 * kEpilogueWarps;
 constexpr int kMaxProblems = 3;
 constexpr int kChunk = 32;             // columns of a row that a thread takes at once
 
@@ -70,7 +68,7 @@ struct GemmArgs {
     Problem p[kMaxProblems];
     int tile_start[kMaxProblems + 1];   // first tile of a problem, and their number; a tile for each split
     int problems;
-    int splits, blocks_per_split;       // splits > 1: tiles leave as fp32 partial sums, folded by combine_kernel
+    int splits, blocks_per_split;       // splits > 1: the reduction is cut into pieces, whose fp32 sums combine_kernel joins
     float* partials;                    // [problem][split][gate, up][M][columns rounded up to 32]
     int* status;
     int clear_status;                   // the first CTA zeroes *status
@@ -87,43 +85,88 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&t);
 }
-// n of the 32 values exist; the others come back as zero
-__device__ __forceinline__ void load_row(const __nv_bfloat16* p, int n, float (&v)[kChunk]) {
-    if (n == kChunk && aligned_to(p, 16)) {
+// Accesses of 32 bytes: a thread has a row of its own, so a warp's access touches 32 lines, and the fewer accesses the better.
+__device__ __forceinline__ void load32(const void* p, uint32_t* q) {
+    unsigned long long x[4];
+    asm volatile("ld.global.v4.b64 {%0,%1,%2,%3}, [%4];" : "=l"(x[0]), "=l"(x[1]), "=l"(x[2]), "=l"(x[3]) : "l"(p) : "memory");
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint4 q = *(reinterpret_cast<const uint4*>(p) + i);
-            unpack2(q.x, v[8 * i + 0], v[8 * i + 1]);
-            unpack2(q.y, v[8 * i + 2], v[8 * i + 3]);
-            unpack2(q.z, v[8 * i + 4], v[8 * i + 5]);
-            unpack2(q.w, v[8 * i + 6], v[8 * i + 7]);
+    for (int i = 0; i < 4; ++i) {
+        q[2 * i] = static_cast<uint32_t>(x[i]);
+        q[2 * i + 1] = static_cast<uint32_t>(x[i] >> 32);
+    }
+}
+__device__ __forceinline__ void store32(void* p, const uint32_t* q) {
+    unsigned long long x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = q[2 * i] | (static_cast<unsigned long long>(q[2 * i + 1]) << 32);
+    asm volatile("st.global.v4.b64 [%0], {%1,%2,%3,%4};" ::"l"(p), "l"(x[0]), "l"(x[1]), "l"(x[2]), "l"(x[3]) : "memory");
+}
+__device__ __forceinline__ void load16(const void* p, uint32_t* q) {
+    const uint4 x = *static_cast<const uint4*>(p);
+    q[0] = x.x; q[1] = x.y; q[2] = x.z; q[3] = x.w;
+}
+__device__ __forceinline__ void store16(void* p, const uint32_t* q) { *static_cast<uint4*>(p) = make_uint4(q[0], q[1], q[2], q[3]); }
+
+// BYTES bytes of a row, `valid` of them there (the rest zero), in units of `UNIT` bytes: the widest access that address
+// and length allow.
+template <int BYTES, class UNIT>
+__device__ __forceinline__ void load_bytes(const UNIT* p, int valid, uint32_t (&q)[BYTES / 4]) {
+    if (valid == BYTES / static_cast<int>(sizeof(UNIT)) && aligned_to(p, 16)) {
+        if (aligned_to(p, 32)) {
+#pragma unroll
+            for (int i = 0; i < BYTES / 32; ++i) load32(reinterpret_cast<const char*>(p) + 32 * i, q + 8 * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < BYTES / 16; ++i) load16(reinterpret_cast<const char*>(p) + 16 * i, q + 4 * i);
         }
     } else {
+        constexpr int kPer = 4 / sizeof(UNIT);
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i) v[i] = i < n ? __bfloat162float(p[i]) : 0.f;
+        for (int i = 0; i < BYTES / 4; ++i) {
+            q[i] = 0;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (i * kPer + j < valid) q[i] |= static_cast<uint32_t>(p[i * kPer + j]) << (8 * sizeof(UNIT) * j);
+        }
     }
+}
+template <int BYTES, class UNIT>
+__device__ __forceinline__ void store_bytes(UNIT* p, int valid, const uint32_t (&q)[BYTES / 4]) {
+    if (valid == BYTES / static_cast<int>(sizeof(UNIT)) && aligned_to(p, 16)) {
+        if (aligned_to(p, 32)) {
+#pragma unroll
+            for (int i = 0; i < BYTES / 32; ++i) store32(reinterpret_cast<char*>(p) + 32 * i, q + 8 * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < BYTES / 16; ++i) store16(reinterpret_cast<char*>(p) + 16 * i, q + 4 * i);
+        }
+    } else {
+        constexpr int kPer = 4 / sizeof(UNIT);
+#pragma unroll
+        for (int i = 0; i < BYTES / 4; ++i)
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (i * kPer + j < valid) p[i * kPer + j] = static_cast<UNIT>(q[i] >> (8 * sizeof(UNIT) * j));
+    }
+}
+__device__ __forceinline__ void load_raw(const __nv_bfloat16* p, int n, uint32_t (&q)[16]) {
+    load_bytes<64>(reinterpret_cast<const unsigned short*>(p), n, q);
+}
+__device__ __forceinline__ void unpack_row(const uint32_t (&q)[16], float (&v)[kChunk]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) unpack2(q[i], v[2 * i], v[2 * i + 1]);
 }
 __device__ __forceinline__ void store_row(__nv_bfloat16* p, int n, const float (&v)[kChunk]) {
-    if (n == kChunk && aligned_to(p, 16)) {
+    uint32_t q[16];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *(reinterpret_cast<uint4*>(p) + i) = make_uint4(pack2(v[8 * i], v[8 * i + 1]), pack2(v[8 * i + 2], v[8 * i + 3]),
-                                                            pack2(v[8 * i + 4], v[8 * i + 5]), pack2(v[8 * i + 6], v[8 * i + 7]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i)
-            if (i < n) p[i] = __float2bfloat16_rn(v[i]);
-    }
+    for (int i = 0; i < 16; ++i) q[i] = pack2(v[2 * i], v[2 * i + 1]);
+    store_bytes<64>(reinterpret_cast<unsigned short*>(p), n, q);
 }
 __device__ __forceinline__ void store_row(float* p, int n, const float (&v)[kChunk]) {
-    if (n == kChunk && aligned_to(p, 16)) {
+    uint32_t q[kChunk];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) *(reinterpret_cast<float4*>(p) + i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i)
-            if (i < n) p[i] = v[i];
-    }
+    for (int i = 0; i < kChunk; ++i) q[i] = __float_as_uint(v[i]);
+    store_bytes<4 * kChunk>(reinterpret_cast<uint32_t*>(p), n, q);
 }
 __device__ __forceinline__ void keep_row(const Kept& k, int e4m3, long long row, int col, int N, int n, const float (&x)[kChunk]) {
     if (!e4m3) {
@@ -147,63 +190,59 @@ __device__ __forceinline__ void keep_row(const Kept& k, int e4m3, long long row,
             c[i] = ck8::codes4(ck8::hold_finite(x[4 * i]), ck8::hold_finite(x[4 * i + 1]), ck8::hold_finite(x[4 * i + 2]),
                                ck8::hold_finite(x[4 * i + 3]), inverse);
     }
-    uint8_t* p = static_cast<uint8_t*>(k.data) + row * N + col;
-    if (n == kChunk && aligned_to(p, 16)) {
-        *reinterpret_cast<uint4*>(p) = make_uint4(c[0], c[1], c[2], c[3]);
-        *(reinterpret_cast<uint4*>(p) + 1) = make_uint4(c[4], c[5], c[6], c[7]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i)
-            if (i < n) p[i] = static_cast<uint8_t>(c[i / 4] >> (8 * (i % 4)));
-    }
+    store_bytes<32>(static_cast<uint8_t*>(k.data) + row * N + col, n, c);
 }
-__device__ __forceinline__ void kept_row(const Kept& k, int e4m3, long long row, int col, int N, int n, float (&v)[kChunk]) {
+// A kept row as it lies in memory (16 words of bf16, or 8 of codes and the scale), fetched before it is needed.
+struct RawRow {
+    uint32_t q[16];
+    uint32_t scale;
+};
+__device__ __forceinline__ void fetch_row(const Kept& k, int e4m3, long long row, int col, int N, int n, RawRow& r) {
     if (!e4m3) {
-        load_row(static_cast<const __nv_bfloat16*>(k.data) + row * N + col, n, v);
+        load_raw(static_cast<const __nv_bfloat16*>(k.data) + row * N + col, n, r.q);
         return;
     }
-    const uint8_t* p = static_cast<const uint8_t*>(k.data) + row * N + col;
-    const float scale = ck8::scale_value(k.scale[row * ((N + kChunk - 1) / kChunk) + col / kChunk]);
     uint32_t c[8];
-    if (n == kChunk && aligned_to(p, 16)) {
-        const uint4 q0 = *reinterpret_cast<const uint4*>(p), q1 = *(reinterpret_cast<const uint4*>(p) + 1);
-        c[0] = q0.x; c[1] = q0.y; c[2] = q0.z; c[3] = q0.w;
-        c[4] = q1.x; c[5] = q1.y; c[6] = q1.z; c[7] = q1.w;
-    } else {
+    load_bytes<32>(static_cast<const uint8_t*>(k.data) + row * N + col, n, c);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            c[i] = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (4 * i + j < n) c[i] |= static_cast<uint32_t>(p[4 * i + j]) << (8 * j);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float2 a = ck8::values2(c[i]), b = ck8::values2(c[i] >> 16);
-        v[4 * i + 0] = a.x * scale; v[4 * i + 1] = a.y * scale;
-        v[4 * i + 2] = b.x * scale; v[4 * i + 3] = b.y * scale;
-    }
+    for (int i = 0; i < 8; ++i) r.q[i] = c[i];
+    r.scale = k.scale[row * ((N + kChunk - 1) / kChunk) + col / kChunk];
 }
-
 // ------------------------------------------------------------------------------------------------ activations
 // silu(z) = z s, s = 1 / (1 + e^-z);  gelu(z) = z P(z), P the normal distribution function.  The fast exponential and
 // quotient are off by a few 2^-23 of a value that is rounded to 2^-9.
+// P by formula 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions: for x >= 0
+//     erfc(x) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) e^(-x^2),  t = 1 / (1 + 0.3275911 x),  off by at most 1.5e-7,
+// with x = |z| / sqrt(2): P is erfc / 2 below zero and 1 - erfc / 2 above.  Two special-function instructions, and the
+// e^(-z^2 / 2) is the one that the slope needs; with erff the epilogue, not the products, set the time of a 1024-deep
+// layer (8191 x 1024 to 4096: 92 us).
+__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+__device__ __forceinline__ float normal_cdf(float z, float& bell) {
+    const float t = __fdividef(1.f, fmaf(0.23164190f, fabsf(z), 1.f));       // 0.3275911 / sqrt(2)
+    bell = __expf(-0.5f * z * z);
+    const float poly = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
+    const float tail = 0.5f * t * poly * bell;
+    return z < 0.f ? tail : 1.f - tail;
+}
 __device__ __forceinline__ float act_value(float z, int act) {
-    if (act == DB_ACT_SILU) return z * __fdividef(1.f, 1.f + __expf(-z));
-    if (act == DB_ACT_GELU) return z * (0.5f + 0.5f * erff(z * 0.70710678f));
+    if (act == DB_ACT_SILU) return z * sigmoid(z);
+    if (act == DB_ACT_GELU) {
+        float bell;
+        return z * normal_cdf(z, bell);
+    }
     if (act == DB_ACT_RELU) return z < 0.f ? 0.f : z;
     return z;
 }
 __device__ __forceinline__ void act_value_slope(float z, int act, float& value, float& slope) {
     if (act == DB_ACT_SILU) {
-        const float s = __fdividef(1.f, 1.f + __expf(-z));
+        const float s = sigmoid(z);
         value = z * s;
-        slope = s * (1.f + z * (1.f - s));
+        slope = fmaf(value, 1.f - s, s);
     } else if (act == DB_ACT_GELU) {
-        const float p = 0.5f + 0.5f * erff(z * 0.70710678f);
+        float bell;
+        const float p = normal_cdf(z, bell);
         value = z * p;
-        slope = p + z * 0.39894228f * __expf(-0.5f * z * z);
+        slope = fmaf(z * 0.39894228f, bell, p);
     } else if (act == DB_ACT_RELU) {
         value = z < 0.f ? 0.f : z;
         slope = z <= 0.f ? 0.f : 1.f;
@@ -225,26 +264,64 @@ __device__ __forceinline__ void act_row(float (&v)[kChunk], int act) {
         for (int i = 0; i < kChunk; ++i) v[i] = act_value(v[i], DB_ACT_RELU);
     }
 }
+// Two values at a time, packed as they are done: 48 words of results instead of 96 floats.
 template <int ACT>
-__device__ __forceinline__ void gated_grad_row(const float (&dh)[kChunk], float (&gate)[kChunk], float (&up)[kChunk], float (&h)[kChunk]) {
+__device__ __forceinline__ void gated_grad_row(const float (&dh)[kChunk], const RawRow& gate, const RawRow& up, int e4m3,
+                                               uint32_t (&d_gate)[16], uint32_t (&d_up)[16], uint32_t (&h)[16]) {
+    const float gate_scale = e4m3 ? ck8::scale_value(gate.scale) : 0.f, up_scale = e4m3 ? ck8::scale_value(up.scale) : 0.f;
 #pragma unroll
-    for (int i = 0; i < kChunk; ++i) {
-        float a, slope;
-        act_value_slope(gate[i], ACT, a, slope);
-        h[i] = a * up[i];
-        gate[i] = dh[i] * up[i] * slope;
-        up[i] = dh[i] * a;
+    for (int i = 0; i < 16; ++i) {
+        float2 z, u;
+        if (e4m3) {
+            z = ck8::values2(gate.q[i / 2] >> (16 * (i % 2)));
+            u = ck8::values2(up.q[i / 2] >> (16 * (i % 2)));
+            z.x *= gate_scale; z.y *= gate_scale;
+            u.x *= up_scale; u.y *= up_scale;
+        } else {
+            unpack2(gate.q[i], z.x, z.y);
+            unpack2(up.q[i], u.x, u.y);
+        }
+        float2 a, s;
+        act_value_slope(z.x, ACT, a.x, s.x);
+        act_value_slope(z.y, ACT, a.y, s.y);
+        h[i] = pack2(a.x * u.x, a.y * u.y);
+        d_gate[i] = pack2(dh[2 * i] * u.x * s.x, dh[2 * i + 1] * u.y * s.y);
+        d_up[i] = pack2(dh[2 * i] * a.x, dh[2 * i + 1] * a.y);
     }
 }
 
-// n >= 1 columns of row `row` from column `col` (a multiple of 32): v the accumulator (kEpiGated: gate's), u up's.
+// What the epilogue of 32 columns reads: fetched ahead, while the accumulator of the columns before is worked on.
 template <int EPI>
-__device__ __forceinline__ void epilogue_row(const EpilogueArgs& e, long long row, int col, int N, int n, float (&v)[kChunk],
+struct Fetched {
+    uint32_t addend[16];
+};
+template <>
+struct Fetched<kEpiGated> {};
+template <>
+struct Fetched<kEpiGatedGrad> {
+    RawRow gate, up;
+};
+template <int EPI>
+__device__ __forceinline__ void epilogue_fetch(const EpilogueArgs& e, long long row, int col, int N, Fetched<EPI>& f) {
+    const int n = min(kChunk, N - col);
+    if constexpr (EPI == kEpiStore) {
+        if (e.addend) load_raw(e.addend + row * e.addend_pitch + col, n, f.addend);
+    } else if constexpr (EPI == kEpiGatedGrad) {
+        fetch_row(e.kept[0], e.kept_e4m3, row, col, N, n, f.gate);
+        fetch_row(e.kept[1], e.kept_e4m3, row, col, N, n, f.up);
+    }
+}
+// Columns col (a multiple of 32) to col + 32, but not past N: v the accumulator (kEpiGated: gate's), u up's.
+template <int EPI>
+__device__ __forceinline__ void epilogue_row(const EpilogueArgs& e, long long row, int col, int N, const Fetched<EPI>& f, float (&v)[kChunk],
                                              float (&u)[kChunk]) {
-    if (EPI == kEpiStore) {
+    const int n = min(kChunk, N - col);
+    if constexpr (EPI == kEpiStore) {
         if (e.bias) {
+            uint32_t q[16];
             float b[kChunk];
-            load_row(e.bias + col, n, b);
+            load_raw(e.bias + col, n, q);
+            unpack_row(q, b);
 #pragma unroll
             for (int i = 0; i < kChunk; ++i) v[i] += b[i];
         }
@@ -252,13 +329,13 @@ __device__ __forceinline__ void epilogue_row(const EpilogueArgs& e, long long ro
         act_row(v, e.act);
         if (e.addend) {
             float r[kChunk];
-            load_row(e.addend + row * e.addend_pitch + col, n, r);
+            unpack_row(f.addend, r);
 #pragma unroll
             for (int i = 0; i < kChunk; ++i) v[i] += r[i];
         }
         if (e.out_f32) store_row(static_cast<float*>(e.out) + row * e.out_pitch + col, n, v);
         else store_row(static_cast<__nv_bfloat16*>(e.out) + row * e.out_pitch + col, n, v);
-    } else if (EPI == kEpiGated) {
+    } else if constexpr (EPI == kEpiGated) {
         if (e.kept[0].data) {
             keep_row(e.kept[0], e.kept_e4m3, row, col, N, n, v);
             keep_row(e.kept[1], e.kept_e4m3, row, col, N, n, u);
@@ -268,17 +345,14 @@ __device__ __forceinline__ void epilogue_row(const EpilogueArgs& e, long long ro
         for (int i = 0; i < kChunk; ++i) v[i] *= u[i];
         store_row(static_cast<__nv_bfloat16*>(e.out) + row * e.out_pitch + col, n, v);
     } else {
-        float gate[kChunk];
-        kept_row(e.kept[0], e.kept_e4m3, row, col, N, n, gate);
-        kept_row(e.kept[1], e.kept_e4m3, row, col, N, n, u);
-        float h[kChunk];
-        if (e.act == DB_ACT_SILU) gated_grad_row<DB_ACT_SILU>(v, gate, u, h);
-        else if (e.act == DB_ACT_GELU) gated_grad_row<DB_ACT_GELU>(v, gate, u, h);
-        else if (e.act == DB_ACT_RELU) gated_grad_row<DB_ACT_RELU>(v, gate, u, h);
-        else gated_grad_row<DB_ACT_NONE>(v, gate, u, h);
-        store_row(e.d_gate + row * e.d_pitch + col, n, gate);
-        store_row(e.d_up + row * e.d_pitch + col, n, u);
-        store_row(static_cast<__nv_bfloat16*>(e.out) + row * e.out_pitch + col, n, h);
+        uint32_t d_gate[16], d_up[16], h[16];
+        if (e.act == DB_ACT_SILU) gated_grad_row<DB_ACT_SILU>(v, f.gate, f.up, e.kept_e4m3, d_gate, d_up, h);
+        else if (e.act == DB_ACT_GELU) gated_grad_row<DB_ACT_GELU>(v, f.gate, f.up, e.kept_e4m3, d_gate, d_up, h);
+        else if (e.act == DB_ACT_RELU) gated_grad_row<DB_ACT_RELU>(v, f.gate, f.up, e.kept_e4m3, d_gate, d_up, h);
+        else gated_grad_row<DB_ACT_NONE>(v, f.gate, f.up, e.kept_e4m3, d_gate, d_up, h);
+        store_bytes<64>(reinterpret_cast<unsigned short*>(e.d_gate + row * e.d_pitch + col), n, d_gate);
+        store_bytes<64>(reinterpret_cast<unsigned short*>(e.d_up + row * e.d_pitch + col), n, d_up);
+        store_bytes<64>(static_cast<unsigned short*>(e.out) + row * e.out_pitch + col, n, h);
     }
 }
 
@@ -319,6 +393,12 @@ __device__ __forceinline__ void mma_commit(uint64_t* bar) {
     else
         tc::mma_commit(bar);
 }
+// True in one lane of a converged warp, always the same one.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t mine;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(mine));
+    return mine != 0;
+}
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -338,6 +418,9 @@ __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
 }
 __device__ __forceinline__ void expect_tx(uint64_t* bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(tc::smem_u32(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map, bool used) {
+    if (used) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
 }
 // One box; x counts bf16 of the contiguous dimension and is a multiple of 64 here (128 bytes).
 template <int CG>
@@ -373,11 +456,17 @@ struct Shape {
     static constexpr int kABytes = kRows * 128;
     static constexpr int kBBytes = kBRows * 128;
     static constexpr int kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = 196608 / kStageBytes;     // 192 KB: six stages of 32 KB, eight of 24 KB
+    // A pair's CTA has an SM to itself and 192 KB of stages (6 of 32 KB, 8 of 24).  Two single CTAs share an SM, 96 KB each: one
+    // works on its accumulator or starts up while the other's products run, a successor's among them.
+    static constexpr int kCtas = CG == 2 ? 1 : 2;
+    static constexpr int kStages = 196608 / kCtas / kStageBytes;
     static constexpr int kSmemBytes = kStages * kStageBytes + 1024;
+    static constexpr int kEpilogueWarps = CG == 2 ? 8 : 4;   // two (one) per tensor-memory lane quarter, each its share of the columns
+    static constexpr int kThreads = 64 + 32 * kEpilogueWarps;
     static constexpr uint32_t kTmemColumns = 2 * BN;         // two accumulators
-    static_assert(kTmemColumns <= 512 && (kTmemColumns & (kTmemColumns - 1)) == 0 && kTmemColumns >= 32, "a power of two up to 512");
+    static_assert(kCtas * kTmemColumns <= 512 && (kTmemColumns & (kTmemColumns - 1)) == 0 && kTmemColumns >= 32, "a power of two up to 512");
     static_assert(kBRows >= 64 && BN % 64 == 0, "whole blocks of 64 output indices");
+    static_assert(kCtas * (kSmemBytes + 1536) <= 233472, "228 KB with the barriers and what the system takes for each CTA");
 };
 
 struct Tile { int problem, split, m, n; };
@@ -409,7 +498,7 @@ __device__ __forceinline__ void k_range(const GemmArgs& g, const Tile& t, int& b
 __host__ __device__ constexpr long long partial_pitch(long long N) { return (N + kChunk - 1) / kChunk * kChunk; }
 
 template <int CG, int BN, bool A_MN, bool B_MN, int EPI>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Shape<CG, BN>::kThreads, Shape<CG, BN>::kCtas)
 layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
     using S = Shape<CG, BN>;
     constexpr int kTileN = EPI == kEpiGated ? BN / 2 : BN;   // output columns of a tile
@@ -436,10 +525,15 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
         }
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(&ready_bar[i], 1);
-            tc::mbar_init(&taken_bar[i], CG * kEpilogueWarps);
+            tc::mbar_init(&taken_bar[i], CG * S::kEpilogueWarps);
         }
         tc::mbar_init(&drain_bar, 1);
         tc::fence_barrier_init();
+    }
+    if (warp == 0 && lane < 2) {
+        const bool second = EPI == kEpiGated || g.p[0].blocks > g.p[0].blocks0;
+        prefetch_map(lane == 0 ? &g.p[0].a[0] : &g.p[0].b[0], true);
+        prefetch_map(lane == 0 ? &g.p[0].a[1] : &g.p[0].b[1], lane == 0 ? g.p[0].blocks > g.p[0].blocks0 : second);
     }
     if (warp == 1) tmem_alloc<CG>(&tmem_slot, S::kTmemColumns);
     tc::tc_fence_before();
@@ -454,25 +548,27 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
     if (g.clear_status && blockIdx.x == 0 && tid == 0) *g.status = 0;
 
     if (warp == 0) {
-        if (lane == 0) {
-            int it = 0;                                       // stages filled so far
-            bool ok = true;
-            for (int t = worker; t < total && ok; t += workers) {
-                const Tile tile = decode(g, t);
-                const Problem& p = g.p[tile.problem];
-                int k, k_end;
-                k_range(g, tile, k, k_end);
-                const int m0 = tile.m * S::kTileM + static_cast<int>(rank) * kRows;
-                // what this CTA holds of B: gated, a pair's CTAs take one weight each, a single CTA half of both
-                const int n0 = tile.n * kTileN + (EPI == kEpiGated ? 0 : static_cast<int>(rank) * S::kBRows);
-                for (; k < k_end; ++k, ++it) {
-                    const int s = it % S::kStages;
-                    if (!(ok = tc::mbar_wait(&empty_bar[s], ((it / S::kStages) & 1) ^ 1, &abort_flag, g.status, 0x301))) break;
-                    const uint32_t bar = CG == 2 ? in_first_cta(&full_bar[s]) : tc::smem_u32(&full_bar[s]);
-                    if (rank == 0) expect_tx(&full_bar[s], CG * S::kStageBytes);
-                    const int source = k >= p.blocks0;
-                    const int k0 = (source ? k - p.blocks0 : k) * kBlockK;
-                    const uint32_t a = tc::smem_u32(tiles + s * S::kStageBytes), b = a + S::kABytes;
+        // The whole warp walks the loop and one elected lane issues: what is uniform stays in uniform registers.
+        int stage = 0, it = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int t = worker; t < total && ok; t += workers) {
+            const Tile tile = decode(g, t);
+            const Problem& p = g.p[tile.problem];
+            int k, k_end;
+            k_range(g, tile, k, k_end);
+            const int blocks0 = p.blocks0;
+            const int m0 = tile.m * S::kTileM + static_cast<int>(rank) * kRows;
+            // what this CTA holds of B: gated, a pair's CTAs take one weight each, a single CTA half of both
+            const int n0 = tile.n * kTileN + (EPI == kEpiGated ? 0 : static_cast<int>(rank) * S::kBRows);
+            for (; k < k_end; ++k, ++it) {
+                if (!(ok = tc::mbar_wait(&empty_bar[stage], phase ^ 1, &abort_flag, g.status, 0x301))) break;
+                if (elect_one()) {
+                    const uint32_t bar = CG == 2 ? in_first_cta(&full_bar[stage]) : tc::smem_u32(&full_bar[stage]);
+                    if (rank == 0) expect_tx(&full_bar[stage], CG * S::kStageBytes);
+                    const int source = k >= blocks0;
+                    const int k0 = (source ? k - blocks0 : k) * kBlockK;
+                    const uint32_t a = tc::smem_u32(tiles + stage * S::kStageBytes), b = a + S::kABytes;
                     if (A_MN) {
 #pragma unroll
                         for (int c = 0; c < kRows / 64; ++c) tma_load<CG>(a + c * 8192, &p.a[source], m0 + 64 * c, k0, bar);
@@ -491,24 +587,28 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
                         tma_load<CG>(b, &p.b[source], k0, n0, bar);
                     }
                 }
+                __syncwarp();
+                if (++stage == S::kStages) { stage = 0; phase ^= 1; }
             }
-            if (ok) {
-                // every product that reads this CTA's stages has finished, and its arrival has reached this CTA
-                for (int i = it > S::kStages ? it - S::kStages : 0; i < it && ok; ++i)
-                    ok = tc::mbar_wait(&empty_bar[i % S::kStages], (i / S::kStages) & 1, &abort_flag, g.status, 0x302);
-            }
-            if (!ok) {
-                // copies under way land within microseconds; their barrier may be the other CTA's
-                const unsigned long long t0 = tc::global_ns();
-                while (tc::global_ns() - t0 < 5000000ull) {}
-            }
+        }
+        // every product that reads this CTA's stages has finished, and its arrival has reached this CTA
+        for (int i = 0; i < S::kStages && ok && i < it; ++i) {
+            if (--stage < 0) { stage = S::kStages - 1; phase ^= 1; }
+            ok = tc::mbar_wait(&empty_bar[stage], phase, &abort_flag, g.status, 0x302);
+        }
+        if (!ok) {
+            // copies under way land within microseconds; their barrier may be the other CTA's
+            const unsigned long long t0 = tc::global_ns();
+            while (tc::global_ns() - t0 < 5000000ull) {}
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             constexpr uint32_t idesc = instr_desc_bf16(S::kTileM, BN, A_MN, B_MN);
             constexpr uint32_t kStepA = (A_MN ? 2048 : 32) >> 4, kStepB = (B_MN ? 2048 : 32) >> 4;   // 16 of the reduction
-            int it = 0, n = 0;
+            const uint32_t base = tc::smem_u32(tiles);
+            int stage = 0, n = 0;
+            uint32_t phase = 0;
             bool ok = true;
             for (int t = worker; t < total && ok; t += workers, ++n) {
                 const Tile tile = decode(g, t);
@@ -518,63 +618,76 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
                 if (!(ok = tc::mbar_wait(&taken_bar[buf], ((n >> 1) & 1) ^ 1, &abort_flag, g.status, 0x303))) break;
                 tc::tc_fence_after();
                 const uint32_t acc = tmem + buf * BN;
-                for (bool first = true; k < k_end; ++k, ++it, first = false) {
-                    const int s = it % S::kStages;
-                    if (!(ok = tc::mbar_wait(&full_bar[s], (it / S::kStages) & 1, &abort_flag, g.status, 0x304))) break;
+                uint32_t accumulate = 0;
+                for (; k < k_end; ++k) {
+                    if (!(ok = tc::mbar_wait(&full_bar[stage], phase, &abort_flag, g.status, 0x304))) break;
                     tc::tc_fence_after();
-                    const uint32_t a = tc::smem_u32(tiles + s * S::kStageBytes);
-                    const uint64_t da = smem_desc<A_MN>(a), db = smem_desc<B_MN>(a + S::kABytes);
+                    if (elect_one()) {
+                        const uint32_t a = base + stage * S::kStageBytes;
+                        const uint64_t da = smem_desc<A_MN>(a), db = smem_desc<B_MN>(a + S::kABytes);
+                        mma_bf16<CG>(acc, da, db, idesc, accumulate);
 #pragma unroll
-                    for (int i = 0; i < kBlockK / 16; ++i)
-                        mma_bf16<CG>(acc, da + i * kStepA, db + i * kStepB, idesc, !(first && i == 0));
-                    mma_commit<CG>(&empty_bar[s]);
+                        for (int i = 1; i < kBlockK / 16; ++i) mma_bf16<CG>(acc, da + i * kStepA, db + i * kStepB, idesc, 1);
+                        mma_commit<CG>(&empty_bar[stage]);
+                    }
+                    __syncwarp();
+                    accumulate = 1;
+                    if (++stage == S::kStages) { stage = 0; phase ^= 1; }
                 }
-                if (ok) mma_commit<CG>(&ready_bar[buf]);
+                if (ok && elect_one()) mma_commit<CG>(&ready_bar[buf]);
+                __syncwarp();
             }
             if (!ok) {
-                mma_commit<CG>(&drain_bar);
-                unsigned long long t0 = tc::global_ns();
+                if (elect_one()) mma_commit<CG>(&drain_bar);
+                __syncwarp();
+                const unsigned long long t0 = tc::global_ns();
                 while (!tc::mbar_try_wait(&drain_bar, 0) && tc::global_ns() - t0 < tc::kWaitLimitNs) {}
             }
         }
         __syncwarp();
     } else {
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const int quarter = warp & 3, part = (warp - 2) >> 2;
         int n = 0;
         for (int t = worker; t < total; t += workers, ++n) {
             const Tile tile = decode(g, t);
             const Problem& p = g.p[tile.problem];
-            const int buf = n & 1;
-            if (!__all_sync(0xFFFFFFFFu, tc::mbar_wait(&ready_bar[buf], (n >> 1) & 1, &abort_flag, g.status, 0x305))) break;
-            tc::tc_fence_after();
+            const int buf = n & 1, N = p.N;
+            constexpr int kPerWarp = kTileN * 4 / S::kEpilogueWarps;
             const long long row = static_cast<long long>(tile.m) * S::kTileM + rank * kRows + quarter * 32 + lane;
-            const uint32_t acc = tmem + buf * BN + (static_cast<uint32_t>(quarter * 32) << 16);
-            constexpr int kPerWarp = kTileN / 2;
-            const int N = p.N;
+            const int first = tile.n * kTileN + part * kPerWarp, columns = min(kPerWarp, N - first);   // may be none
+            const bool in = row < p.M && g.splits == 1;       // the epilogue is applied here, or to the joined sum
+            Fetched<EPI> now, next;
+            if (in && columns > 0) epilogue_fetch<EPI>(p.e, row, first, N, now);
+            // one lane asks: 256 threads asking at once slow the two that feed the tensor cores (0.32 us a block, not 0.2)
+            bool ready = false;
+            if (lane == 0) ready = tc::mbar_wait(&ready_bar[buf], (n >> 1) & 1, &abort_flag, g.status, 0x305);
+            if (!__shfl_sync(0xFFFFFFFFu, ready, 0)) break;
+            tc::tc_fence_after();
+            const uint32_t acc = tmem + buf * BN + (static_cast<uint32_t>(quarter * 32) << 16) + part * kPerWarp;
 #pragma unroll 1
-            for (int c = 0; c < kPerWarp; c += kChunk) {
+            for (int c = 0; c < columns; c += kChunk) {
                 __syncwarp();                                  // rows past the end rejoin for the next read
-                const int in_tile = half * kPerWarp + c, col = tile.n * kTileN + in_tile;
-                if (col >= N) break;                           // the same for the whole warp
+                const int col = first + c;
+                if (in && c + kChunk < columns) epilogue_fetch<EPI>(p.e, row, col + kChunk, N, next);
                 uint32_t raw[kChunk];
                 float v[kChunk], u[kChunk];
-                tc::tmem_load32(acc + in_tile, raw);
+                tc::tmem_load32(acc + c, raw);
 #pragma unroll
                 for (int i = 0; i < kChunk; ++i) v[i] = __uint_as_float(raw[i]);
                 if (EPI == kEpiGated) {
-                    tc::tmem_load32(acc + kTileN + in_tile, raw);
+                    tc::tmem_load32(acc + kTileN + c, raw);
 #pragma unroll
                     for (int i = 0; i < kChunk; ++i) u[i] = __uint_as_float(raw[i]);
                 }
-                if (row >= p.M) continue;
-                if (g.splits > 1) {
+                if (in) {
+                    epilogue_row<EPI>(p.e, row, col, N, now, v, u);
+                } else if (row < p.M) {
                     const long long pitch = partial_pitch(N), plane = p.M * pitch;
                     float* to = g.partials + p.partial + tile.split * plane * (EPI == kEpiGated ? 2 : 1) + row * pitch + col;
                     store_row(to, kChunk, v);
                     if (EPI == kEpiGated) store_row(to + plane, kChunk, u);
-                } else {
-                    epilogue_row<EPI>(p.e, row, col, N, min(kChunk, N - col), v, u);
                 }
+                now = next;
             }
             tc::tc_fence_before();
             __syncwarp();
@@ -593,35 +706,49 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
     }
 }
 
-// Folds the partial sums of a split reduction in split order and applies the epilogue; a thread has 32 columns of a row.
+// Joins the partial sums of a split reduction in the pieces' order and applies the epilogue.  A CTA has 32 chunks of 32
+// columns: its threads add four columns each, whole lines at a time and eight pieces under way, one warp does the epilogue.
 template <int EPI>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(256)
 combine_kernel(const __grid_constant__ GemmArgs g) {
+    constexpr int kParts = EPI == kEpiGated ? 2 : 1;
+    __shared__ float4 sums[kParts][32][kChunk / 4 + 1];
     tc::griddep_wait();
     tc::griddep_launch_dependents();
     const Problem& p = g.p[blockIdx.y];
-    const long long pitch = partial_pitch(p.N), plane = p.M * pitch, chunks = pitch / kChunk;
-    const long long i = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x;
-    if (i >= p.M * chunks) return;
-    const long long row = i / chunks;
-    const int col = static_cast<int>(i - row * chunks) * kChunk;
-    const long long step = plane * (EPI == kEpiGated ? 2 : 1);
-    const float* from = g.partials + p.partial + row * pitch + col;
-    float v[kChunk], u[kChunk];
+    const long long pitch = partial_pitch(p.N), plane = p.M * pitch, step = plane * kParts, chunks = p.M * (pitch / kChunk);
+    const long long first = static_cast<long long>(blockIdx.x) * 32;
+    const float* from = g.partials + p.partial + (first * kChunk + 4 * threadIdx.x);
+    if (first + threadIdx.x / 8 < chunks) {
 #pragma unroll
-    for (int j = 0; j < kChunk; ++j) v[j] = u[j] = 0.f;
-    for (int s = 0; s < g.splits; ++s) {
-#pragma unroll
-        for (int j = 0; j < kChunk; j += 4) {
-            const float4 q = *reinterpret_cast<const float4*>(from + s * step + j);
-            v[j] += q.x; v[j + 1] += q.y; v[j + 2] += q.z; v[j + 3] += q.w;
-            if (EPI == kEpiGated) {
-                const float4 r = *reinterpret_cast<const float4*>(from + s * step + plane + j);
-                u[j] += r.x; u[j + 1] += r.y; u[j + 2] += r.z; u[j + 3] += r.w;
+        for (int part = 0; part < kParts; ++part) {
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+            for (int s = 0; s < g.splits; ++s) {
+                const float4 q = *reinterpret_cast<const float4*>(from + s * step + part * plane);
+                sum.x += q.x; sum.y += q.y; sum.z += q.z; sum.w += q.w;
             }
+            sums[part][threadIdx.x / 8][threadIdx.x % 8] = sum;
         }
     }
-    epilogue_row<EPI>(p.e, row, col, p.N, static_cast<int>(min(static_cast<long long>(kChunk), static_cast<long long>(p.N) - col)), v, u);
+    __syncthreads();
+    const long long chunk = first + threadIdx.x;
+    if (threadIdx.x >= 32 || chunk >= chunks) return;
+    const long long row = chunk / (pitch / kChunk);
+    const int col = static_cast<int>(chunk - row * (pitch / kChunk)) * kChunk;
+    Fetched<EPI> f;
+    epilogue_fetch<EPI>(p.e, row, col, p.N, f);
+    float v[kChunk], u[kChunk];
+#pragma unroll
+    for (int j = 0; j < kChunk / 4; ++j) {
+        const float4 q = sums[0][threadIdx.x][j];
+        v[4 * j] = q.x; v[4 * j + 1] = q.y; v[4 * j + 2] = q.z; v[4 * j + 3] = q.w;
+        if (EPI == kEpiGated) {
+            const float4 w = sums[kParts - 1][threadIdx.x][j];
+            u[4 * j] = w.x; u[4 * j + 1] = w.y; u[4 * j + 2] = w.z; u[4 * j + 3] = w.w;
+        }
+    }
+    epilogue_row<EPI>(p.e, row, col, p.N, f, v, u);
 }
 
 }  // namespace lg

@@ -1,6 +1,7 @@
 // The layers whose gradients the workers send: linear layer and gated feed-forward block, forward and backward
 // (entry points, planning, and the small kernels around the products of layer_gemm.cuh).
 #include <algorithm>
+#include <atomic>
 #include <cstring>
 
 #include "common.h"
@@ -218,12 +219,15 @@ db_status make_map(CUtensorMap* map, const Matrix& m, int box_rows) {
 
 // ---------------------------------------------------------------------------------------------- the products' plan
 enum Kind { kForward, kGated, kInputGrad, kGatedGrad, kWeightGrad };   // which operands lie how, and the epilogue
-enum TileShape { kPair256, kSingle128, kSingle64, kTileShapes };
+enum TileShape { kPair256, kPair128, kSingle128, kSingle64, kTileShapes };
 
 using GemmFn = void (*)(const lg::GemmArgs);
-struct ShapeInfo { int cg, bn, smem; };
-template <int CG, int BN> constexpr ShapeInfo info() { return {CG, BN, lg::Shape<CG, BN>::kSmemBytes}; }
-constexpr ShapeInfo kShapes[kTileShapes] = {info<2, 256>(), info<1, 128>(), info<1, 64>()};
+struct ShapeInfo { int cg, bn, smem, ctas, threads; };
+template <int CG, int BN> constexpr ShapeInfo info() {
+    using S = lg::Shape<CG, BN>;
+    return {CG, BN, S::kSmemBytes, S::kCtas, S::kThreads};
+}
+constexpr ShapeInfo kShapes[kTileShapes] = {info<2, 256>(), info<2, 128>(), info<1, 128>(), info<1, 64>()};
 
 template <int CG, int BN>
 GemmFn gemm_fn(Kind kind) {
@@ -241,6 +245,7 @@ GemmFn gemm_fn(Kind kind) {
 GemmFn gemm_fn(Kind kind, TileShape shape) {
     switch (shape) {
         case kPair256: return gemm_fn<2, 256>(kind);
+        case kPair128: return gemm_fn<2, 128>(kind);
         case kSingle128: return gemm_fn<1, 128>(kind);
         default: return gemm_fn<1, 64>(kind);
     }
@@ -259,29 +264,27 @@ long long tiles_of(Kind kind, TileShape shape, const Size& s) {
 }
 
 // The tile shape and the number of pieces of the reduction with the least estimated time, in SM cycles.
-// A 64-deep block of a tile costs its products or its copies, whichever is longer, a tile something for its start and
-// end, and a split reduction a second kernel and the traffic of its partial sums.
+// A 64-deep block of a tile costs its products or its copies (about 57 bytes a cycle reach an SM), whichever is longer,
+// a tile something for its start and end, and a reduction in pieces a second kernel and the traffic of the partial sums.
 Plan make_plan(Kind kind, const Size* sizes, int n, long long blocks) {
-    constexpr double kBlock[kTileShapes] = {560, 420, 330}, kTile[kTileShapes] = {2600, 1700, 1300}, kCombine = 5000;
+    constexpr double kBlock[kTileShapes] = {560, 430, 560, 420}, kTile[kTileShapes] = {2600, 2000, 1700, 1300}, kCombine = 4000;
     Plan best;
-    double least = 0;
-    if (blocks == 0) return best;                            // no rows: nothing is launched
+    if (blocks == 0 || n == 0) return best;                  // no rows: nothing is launched
     for (int j = 0; j < n; ++j)
         if (sizes[j].M == 0) return best;
-    if (n == 0) return best;
+    const int sms = sm_count();
+    double least = 0;
     for (int i = 0; i < kTileShapes; ++i) {
         const TileShape shape = static_cast<TileShape>(i);
         if (!gemm_fn(kind, shape)) continue;
-        const long long workers = std::max(1, sm_count() / kShapes[i].cg);
+        const long long workers = std::max(1, sms / kShapes[i].cg);
         long long tiles = 0, outputs = 0;
         for (int j = 0; j < n; ++j) {
             tiles += tiles_of(kind, shape, sizes[j]);
             outputs += sizes[j].M * lg::partial_pitch(sizes[j].N) * (kind == kGated ? 2 : 1);
         }
-        const long long most = std::min(blocks, std::max(1LL, workers / tiles));
-        for (long long want = 1; want <= most; ++want) {
+        for (long long want = std::min(blocks, std::max(1LL, workers / tiles));; want = (want + 1) / 2) {
             const long long per = cdiv(blocks, want), splits = cdiv(blocks, per);
-            if (splits != want) continue;
             const double time = static_cast<double>(cdiv(tiles * splits, workers)) * (per * kBlock[i]) + kTile[i] +
                                 (splits > 1 ? kCombine + outputs * (splits + 1) * 4 / 2500.0 : 0);
             if (least == 0 || time < least) {
@@ -291,9 +294,23 @@ Plan make_plan(Kind kind, const Size* sizes, int n, long long blocks) {
                 best.blocks_per_split = static_cast<int>(per);
                 best.partial_floats = splits > 1 ? splits * outputs : 0;
             }
+            if (want == 1) break;
         }
     }
     return best;
+}
+
+// Once per kernel and device: the attribute call costs a microsecond.
+db_status allow_smem(Kind kind, TileShape shape, GemmFn fn, int bytes) {
+    constexpr int kDevices = 64;
+    static std::atomic<unsigned char> done[kDevices][kWeightGrad + 1][kTileShapes];
+    int device = 0;
+    DB_CUDA_TRY(cudaGetDevice(&device));
+    const bool known = device >= 0 && device < kDevices;
+    if (known && done[device][kind][shape].load(std::memory_order_relaxed)) return DB_OK;
+    DB_CUDA_TRY(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    if (known) done[device][kind][shape].store(1, std::memory_order_relaxed);
+    return DB_OK;
 }
 
 // One product, or several with the same reduction, in one launch (two with a split reduction).
@@ -350,14 +367,16 @@ db_status run_products(Kind kind, const Product* products, int n, float* partial
     g.clear_status = clear;
     clear = false;
     const GemmFn fn = gemm_fn(kind, plan.shape);
-    DB_CUDA_TRY(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, shape.smem));
-    const long long workers = std::min<long long>(std::max(1, sm_count() / shape.cg), tiles);
-    Launch L(dim3(static_cast<unsigned>(workers * shape.cg)), dim3(lg::kThreads), shape.smem, stream, shape.cg);
+    const db_status st = allow_smem(kind, plan.shape, fn, shape.smem);
+    if (st != DB_OK) return st;
+    // as many CTAs (pairs) as fit share the tiles out
+    const long long workers = std::min<long long>(std::max(1, sm_count() * shape.ctas / shape.cg), tiles);
+    Launch L(dim3(static_cast<unsigned>(workers * shape.cg)), dim3(shape.threads), shape.smem, stream, shape.cg);
     DB_CUDA_TRY(cudaLaunchKernelEx(&L.cfg, fn, g));
     if (plan.splits > 1) {
         long long most = 0;
         for (int i = 0; i < n; ++i) most = std::max(most, static_cast<long long>(g.p[i].M) * (lg::partial_pitch(g.p[i].N) / lg::kChunk));
-        Launch C(dim3(static_cast<unsigned>(cdiv(most, 128)), n), dim3(128), 0, stream);
+        Launch C(dim3(static_cast<unsigned>(cdiv(most, 32)), n), dim3(256), 0, stream);
         GemmFn fold = kind == kGated ? lg::combine_kernel<lg::kEpiGated> : kind == kGatedGrad ? lg::combine_kernel<lg::kEpiGatedGrad>
                                                                                             : lg::combine_kernel<lg::kEpiStore>;
         DB_CUDA_TRY(cudaLaunchKernelEx(&C.cfg, fold, g));
