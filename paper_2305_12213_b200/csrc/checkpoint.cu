@@ -51,11 +51,7 @@ __global__ void __launch_bounds__(kBlock) checkpoint_pack_kernel(const __grid_co
         const uint32_t byte = ck8::scale_byte(top);
         const float inverse = ck8::scale_inverse(byte);
         if ((piece & 3) == 0) a.scale[row * a.groups + piece / 4] = static_cast<uint8_t>(byte);
-        if (byte >= ck8::kTopByte) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = ck8::hold_finite(v[j]);
-        }
-        const uint32_t c0 = ck8::codes4(v[0], v[1], v[2], v[3], inverse), c1 = ck8::codes4(v[4], v[5], v[6], v[7], inverse);
+        const uint32_t c0 = ck8::codes4(v[0], v[1], v[2], v[3], inverse, byte), c1 = ck8::codes4(v[4], v[5], v[6], v[7], inverse, byte);
         uint8_t* to = a.codes + row * a.cols + col;
         if (n == 8 && lg::aligned_to(to, 8)) {
             __stcs(reinterpret_cast<uint2*>(to), make_uint2(c0, c1));

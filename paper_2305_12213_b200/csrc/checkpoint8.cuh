@@ -27,14 +27,8 @@ __device__ __forceinline__ float scale_value(uint32_t byte) {  // 2^(byte - 127)
 __device__ __forceinline__ float scale_inverse(uint32_t byte) {  // 2^(127 - byte), for byte <= 247
     return __uint_as_float((254u - byte) << 23);
 }
-// Codes of four values; what is not finite becomes the code NaN.
-__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inverse) {
-    const float nan = __uint_as_float(0x7FFFFFFFu);
-    const float inf = __uint_as_float(0x7F800000u);
-    a = fabsf(a) < inf ? a * inverse : nan;
-    b = fabsf(b) < inf ? b * inverse : nan;
-    c = fabsf(c) < inf ? c * inverse : nan;
-    d = fabsf(d) < inf ? d * inverse : nan;
+// Codes of four scaled values; a NaN gets the code NaN.
+__device__ __forceinline__ uint32_t codes_of_finite(float a, float b, float c, float d) {
     const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
     const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
     return lo | (hi << 16);
@@ -43,11 +37,16 @@ __device__ __forceinline__ float finite_magnitude(float x) {  // 0 for what is n
     const float m = fabsf(x);
     return m < __uint_as_float(0x7F800000u) ? m : 0.f;
 }
-// With the largest scale, 2^120, the codes from 256 on would stand for 2^128 and more: finite values stop at 240 there.
+// The same for any values, not yet scaled: infinities get the code NaN too, and with the largest scale, 2^120, the codes
+// from 256 on would stand for 2^128 and more, so finite values stop at 240 there.
 constexpr uint32_t kTopByte = 247;
-__device__ __forceinline__ float hold_finite(float x) {
-    const float limit = 240.f * __uint_as_float(kTopByte << 23);
-    return finite_magnitude(x) > limit ? copysignf(limit, x) : x;
+__device__ __forceinline__ float held(float x, float inverse, uint32_t byte) {
+    const float m = fabsf(x), y = x * inverse;
+    if (!(m < __uint_as_float(0x7F800000u))) return __uint_as_float(0x7FFFFFFFu);
+    return byte >= kTopByte && fabsf(y) > 240.f ? copysignf(240.f, y) : y;
+}
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inverse, uint32_t byte) {
+    return codes_of_finite(held(a, inverse, byte), held(b, inverse, byte), held(c, inverse, byte), held(d, inverse, byte));
 }
 __device__ __forceinline__ float2 values2(uint32_t two_codes) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two_codes & 0xFFFFu), __NV_E4M3);

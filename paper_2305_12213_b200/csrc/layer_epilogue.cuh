@@ -1,0 +1,425 @@
+// What follows a layer's product on the accumulator, 32 columns of a row per thread: bias, activation, residual, gating and
+// its gradient, and what is kept for the backward pass.  All in fp32, two values per instruction where there is one for two.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "checkpoint8.cuh"
+#include "dynbatch.h"
+
+namespace dynbatch {
+namespace lg {
+
+constexpr int kChunk = 32;             // columns of a row that a thread takes at once
+
+enum Epilogue {
+    kEpiStore = 0,      // out = act(acc + bias) + addend, acc + bias kept if wanted
+    kEpiGated = 1,      // two accumulators side by side: out = act(gate) * up, both kept if wanted
+    kEpiGatedGrad = 2   // acc = dh: with gate and up as kept, d_gate, d_up and h
+};
+
+struct Kept {                    // a tensor [M, N] as it is held for the backward pass
+    void* data = nullptr;        // bf16 or e4m3 codes, N per row; nullptr: not kept
+    uint8_t* scale = nullptr;    // e4m3: ceil(N / 32) bytes per row
+};
+
+struct EpilogueArgs {
+    void* out = nullptr;         // kEpiStore: [M, N]; kEpiGated: h; kEpiGatedGrad: h
+    long long out_pitch = 0;
+    const __nv_bfloat16* bias = nullptr;
+    const __nv_bfloat16* addend = nullptr;
+    long long addend_pitch = 0;
+    Kept kept[2];                // kEpiStore: [0]; the others: gate, up
+    __nv_bfloat16* d_gate = nullptr;   // kEpiGatedGrad
+    __nv_bfloat16* d_up = nullptr;
+    long long d_pitch = 0;
+    int kept_e4m3 = 0;
+    int out_f32 = 0;
+    int act = DB_ACT_NONE;
+};
+
+// ------------------------------------------------------------------------------------------------ two floats
+using Pair = unsigned long long;
+
+__device__ __forceinline__ Pair pair(float a, float b) {
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void halves(Pair p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ Pair both(float x) { return pair(x, x); }
+__device__ __forceinline__ Pair mul(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Pair add(Pair a, Pair b) {
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Pair mul_add(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+// ------------------------------------------------------------------------------------------------ 32 values of a row
+__device__ __forceinline__ bool aligned_to(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+__device__ __forceinline__ void unpack2(uint32_t two, float& a, float& b) {
+    a = __uint_as_float(two << 16);
+    b = __uint_as_float(two & 0xFFFF0000u);
+}
+__device__ __forceinline__ Pair unpack_pair(uint32_t two) { return pair(__uint_as_float(two << 16), __uint_as_float(two & 0xFFFF0000u)); }
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&t);
+}
+__device__ __forceinline__ uint32_t pack_pair(Pair p) {
+    float a, b;
+    halves(p, a, b);
+    return pack2(a, b);
+}
+// Accesses of 32 bytes: a thread has a row of its own, so a warp's access touches 32 lines, and the fewer accesses the better.
+__device__ __forceinline__ void load32(const void* p, uint32_t* q) {
+    unsigned long long x[4];
+    asm volatile("ld.global.v4.b64 {%0,%1,%2,%3}, [%4];" : "=l"(x[0]), "=l"(x[1]), "=l"(x[2]), "=l"(x[3]) : "l"(p) : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        q[2 * i] = static_cast<uint32_t>(x[i]);
+        q[2 * i + 1] = static_cast<uint32_t>(x[i] >> 32);
+    }
+}
+__device__ __forceinline__ void store32(void* p, const uint32_t* q) {
+    unsigned long long x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = q[2 * i] | (static_cast<unsigned long long>(q[2 * i + 1]) << 32);
+    asm volatile("st.global.v4.b64 [%0], {%1,%2,%3,%4};" ::"l"(p), "l"(x[0]), "l"(x[1]), "l"(x[2]), "l"(x[3]) : "memory");
+}
+__device__ __forceinline__ void load16(const void* p, uint32_t* q) {
+    const uint4 x = *static_cast<const uint4*>(p);
+    q[0] = x.x; q[1] = x.y; q[2] = x.z; q[3] = x.w;
+}
+__device__ __forceinline__ void store16(void* p, const uint32_t* q) { *static_cast<uint4*>(p) = make_uint4(q[0], q[1], q[2], q[3]); }
+
+// BYTES bytes of a row, `valid` of them there (the rest zero), in units of `UNIT` bytes: the widest access that address
+// and length allow.
+template <int BYTES, class UNIT>
+__device__ __forceinline__ void load_bytes(const UNIT* p, int valid, uint32_t (&q)[BYTES / 4]) {
+    if (valid == BYTES / static_cast<int>(sizeof(UNIT)) && aligned_to(p, 16)) {
+        if (aligned_to(p, 32)) {
+#pragma unroll
+            for (int i = 0; i < BYTES / 32; ++i) load32(reinterpret_cast<const char*>(p) + 32 * i, q + 8 * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < BYTES / 16; ++i) load16(reinterpret_cast<const char*>(p) + 16 * i, q + 4 * i);
+        }
+    } else {
+        constexpr int kPer = 4 / sizeof(UNIT);
+#pragma unroll
+        for (int i = 0; i < BYTES / 4; ++i) {
+            q[i] = 0;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (i * kPer + j < valid) q[i] |= static_cast<uint32_t>(p[i * kPer + j]) << (8 * sizeof(UNIT) * j);
+        }
+    }
+}
+template <int BYTES, class UNIT>
+__device__ __forceinline__ void store_bytes(UNIT* p, int valid, const uint32_t (&q)[BYTES / 4]) {
+    if (valid == BYTES / static_cast<int>(sizeof(UNIT)) && aligned_to(p, 16)) {
+        if (aligned_to(p, 32)) {
+#pragma unroll
+            for (int i = 0; i < BYTES / 32; ++i) store32(reinterpret_cast<char*>(p) + 32 * i, q + 8 * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < BYTES / 16; ++i) store16(reinterpret_cast<char*>(p) + 16 * i, q + 4 * i);
+        }
+    } else {
+        constexpr int kPer = 4 / sizeof(UNIT);
+#pragma unroll
+        for (int i = 0; i < BYTES / 4; ++i)
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (i * kPer + j < valid) p[i * kPer + j] = static_cast<UNIT>(q[i] >> (8 * sizeof(UNIT) * j));
+    }
+}
+__device__ __forceinline__ void load_raw(const __nv_bfloat16* p, int n, uint32_t (&q)[16]) {
+    load_bytes<64>(reinterpret_cast<const unsigned short*>(p), n, q);
+}
+__device__ __forceinline__ void store_row(__nv_bfloat16* p, int n, const Pair (&v)[16]) {
+    uint32_t q[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) q[i] = pack_pair(v[i]);
+    store_bytes<64>(reinterpret_cast<unsigned short*>(p), n, q);
+}
+__device__ __forceinline__ void store_row(float* p, int n, const Pair (&v)[16]) {
+    uint32_t q[kChunk];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        q[2 * i] = static_cast<uint32_t>(v[i]);
+        q[2 * i + 1] = static_cast<uint32_t>(v[i] >> 32);
+    }
+    store_bytes<4 * kChunk>(reinterpret_cast<uint32_t*>(p), n, q);
+}
+// Values past the row's end are zero or NaN here (a product with the zeros that TMA reads there) and do not enter the scale.
+__device__ __forceinline__ void keep_row(const Kept& k, int e4m3, long long row, int col, int N, int n, const Pair (&x)[16]) {
+    if (!e4m3) {
+        store_row(static_cast<__nv_bfloat16*>(k.data) + row * N + col, n, x);
+        return;
+    }
+    float top = 0.f;                                           // maxima pass NaN over
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float a, b;
+        halves(x[i], a, b);
+        top = fmaxf(top, fmaxf(fabsf(a), fabsf(b)));
+    }
+    uint32_t byte = ck8::scale_byte(top);
+    uint32_t c[8];
+    if (byte < ck8::kTopByte) {                                // and so top is finite
+        const Pair inverse = both(ck8::scale_inverse(byte));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float y[4];
+            halves(mul(x[2 * i], inverse), y[0], y[1]);
+            halves(mul(x[2 * i + 1], inverse), y[2], y[3]);
+            c[i] = ck8::codes_of_finite(y[0], y[1], y[2], y[3]);
+        }
+    } else {
+        top = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float a, b;
+            halves(x[i], a, b);
+            top = fmaxf(top, fmaxf(ck8::finite_magnitude(a), ck8::finite_magnitude(b)));
+        }
+        byte = ck8::scale_byte(top);
+        const float inverse = ck8::scale_inverse(byte);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float y[4];
+            halves(x[2 * i], y[0], y[1]);
+            halves(x[2 * i + 1], y[2], y[3]);
+            c[i] = ck8::codes4(y[0], y[1], y[2], y[3], inverse, byte);
+        }
+    }
+    k.scale[row * ((N + kChunk - 1) / kChunk) + col / kChunk] = static_cast<uint8_t>(byte);
+    store_bytes<32>(static_cast<uint8_t*>(k.data) + row * N + col, n, c);
+}
+// A kept row as it lies in memory (16 words of bf16, or 8 of codes and the scale), fetched before it is needed.
+struct RawRow {
+    uint32_t q[16];
+    uint32_t scale;
+};
+__device__ __forceinline__ void fetch_row(const Kept& k, int e4m3, long long row, int col, int N, int n, RawRow& r) {
+    if (!e4m3) {
+        load_raw(static_cast<const __nv_bfloat16*>(k.data) + row * N + col, n, r.q);
+        return;
+    }
+    uint32_t c[8];
+    load_bytes<32>(static_cast<const uint8_t*>(k.data) + row * N + col, n, c);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.q[i] = c[i];
+    r.scale = k.scale[row * ((N + kChunk - 1) / kChunk) + col / kChunk];
+}
+
+// ------------------------------------------------------------------------------------------------ activations
+// silu(z) = z s, s = 1 / (1 + e^-z);  gelu(z) = z P(z), P the normal distribution function.  The approximate exponential
+// and reciprocal are off by a few 2^-23 of a value that is rounded to 2^-9; arguments and results below 2^-126 count as 0.
+// P by formula 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions: for x >= 0
+//     erfc(x) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) e^(-x^2),  t = 1 / (1 + 0.3275911 x),  off by at most 1.5e-7,
+// with x = |z| / sqrt(2): P is erfc / 2 below zero and 1 - erfc / 2 above, so gelu = max(z, 0) - |z| erfc / 2.  Two
+// special-function instructions, and the e^(-z^2 / 2) is the one that the slope needs.  With erff the epilogue, not the
+// products, set the time of a 1024-deep layer (8191 x 1024 to 4096: 92 us).
+__device__ __forceinline__ float exp2_fast(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float reciprocal_fast(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ Pair exp2_pair(Pair x) {
+    float a, b;
+    halves(x, a, b);
+    return pair(exp2_fast(a), exp2_fast(b));
+}
+__device__ __forceinline__ Pair reciprocal_pair(Pair x) {
+    float a, b;
+    halves(x, a, b);
+    return pair(reciprocal_fast(a), reciprocal_fast(b));
+}
+constexpr float kLog2e = 1.44269504f;
+__device__ __forceinline__ Pair sigmoid(Pair z) { return reciprocal_pair(add(exp2_pair(mul(z, both(-kLog2e))), both(1.f))); }
+__device__ __forceinline__ Pair magnitude(Pair z) { return z & 0x7FFFFFFF7FFFFFFFull; }
+__device__ __forceinline__ Pair positive_part(Pair z) {       // a NaN stays one
+    float a, b;
+    halves(z, a, b);
+    return pair(a < 0.f ? 0.f : a, b < 0.f ? 0.f : b);
+}
+// bell = e^(-z^2 / 2); returns erfc(|z| / sqrt(2)) / 2
+__device__ __forceinline__ Pair normal_tail(Pair z, Pair& bell) {
+    const Pair t = reciprocal_pair(mul_add(magnitude(z), both(0.23164190f), both(1.f)));   // 0.3275911 / sqrt(2)
+    bell = exp2_pair(mul(mul(z, both(-0.5f * kLog2e)), z));
+    Pair poly = mul_add(both(0.5f * 1.061405429f), t, both(-0.5f * 1.453152027f));
+    poly = mul_add(poly, t, both(0.5f * 1.421413741f));
+    poly = mul_add(poly, t, both(-0.5f * 0.284496736f));
+    poly = mul_add(poly, t, both(0.5f * 0.254829592f));
+    return mul(mul(poly, t), bell);
+}
+template <int ACT>
+__device__ __forceinline__ Pair act_pair(Pair z) {
+    if (ACT == DB_ACT_SILU) return mul(z, sigmoid(z));
+    if (ACT == DB_ACT_GELU) {
+        Pair bell;
+        const Pair tail = normal_tail(z, bell);
+        return mul_add(magnitude(z) ^ 0x8000000080000000ull, tail, positive_part(z));
+    }
+    if (ACT == DB_ACT_RELU) return positive_part(z);
+    return z;
+}
+template <int ACT>
+__device__ __forceinline__ void act_pair_slope(Pair z, Pair& value, Pair& slope) {
+    if (ACT == DB_ACT_SILU) {
+        const Pair s = sigmoid(z);
+        value = mul(z, s);
+        slope = mul_add(value, mul_add(s, both(-1.f), both(1.f)), s);
+    } else if (ACT == DB_ACT_GELU) {
+        Pair bell;
+        const Pair tail = normal_tail(z, bell);
+        value = mul_add(magnitude(z) ^ 0x8000000080000000ull, tail, positive_part(z));
+        // P(z) - 1/2 has z's sign and the magnitude 1/2 - tail
+        const Pair centred = mul_add(tail, both(-1.f), both(0.5f)) ^ (z & 0x8000000080000000ull);
+        slope = mul_add(mul(z, both(0.39894228f)), bell, add(centred, both(0.5f)));
+    } else if (ACT == DB_ACT_RELU) {
+        value = positive_part(z);
+        float a, b;
+        halves(z, a, b);
+        slope = pair(a <= 0.f ? 0.f : 1.f, b <= 0.f ? 0.f : 1.f);
+    } else {
+        value = z;
+        slope = both(1.f);
+    }
+}
+// The branch on the activation is taken once for a row, not for each value.
+template <int ACT>
+__device__ __forceinline__ void act_row(Pair (&v)[16]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = act_pair<ACT>(v[i]);
+}
+__device__ __forceinline__ void act_row(Pair (&v)[16], int act) {
+    if (act == DB_ACT_SILU) act_row<DB_ACT_SILU>(v);
+    else if (act == DB_ACT_GELU) act_row<DB_ACT_GELU>(v);
+    else if (act == DB_ACT_RELU) act_row<DB_ACT_RELU>(v);
+}
+// d *= act'(z), four pairs
+__device__ __forceinline__ void times_slope(Pair (&d)[4], const Pair (&z)[4], int act) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        Pair value, slope;
+        if (act == DB_ACT_SILU) act_pair_slope<DB_ACT_SILU>(z[i], value, slope);
+        else if (act == DB_ACT_GELU) act_pair_slope<DB_ACT_GELU>(z[i], value, slope);
+        else act_pair_slope<DB_ACT_RELU>(z[i], value, slope);
+        d[i] = mul(d[i], slope);
+    }
+}
+// Two values at a time, packed as they are done: 48 words of results instead of 96 floats.
+template <int ACT, bool E4M3>
+__device__ __forceinline__ void gated_grad_row(const Pair (&dh)[16], const RawRow& gate, const RawRow& up, uint32_t (&d_gate)[16],
+                                               uint32_t (&d_up)[16], uint32_t (&h)[16]) {
+    const Pair gate_scale = both(E4M3 ? ck8::scale_value(gate.scale) : 1.f), up_scale = both(E4M3 ? ck8::scale_value(up.scale) : 1.f);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        Pair z, u, a, s;
+        if (E4M3) {
+            const float2 x = ck8::values2(gate.q[i / 2] >> (16 * (i % 2))), y = ck8::values2(up.q[i / 2] >> (16 * (i % 2)));
+            z = mul(pair(x.x, x.y), gate_scale);
+            u = mul(pair(y.x, y.y), up_scale);
+        } else {
+            z = unpack_pair(gate.q[i]);
+            u = unpack_pair(up.q[i]);
+        }
+        act_pair_slope<ACT>(z, a, s);
+        h[i] = pack_pair(mul(a, u));
+        d_gate[i] = pack_pair(mul(mul(dh[i], u), s));
+        d_up[i] = pack_pair(mul(dh[i], a));
+    }
+}
+template <bool E4M3>
+__device__ __forceinline__ void gated_grad_row(int act, const Pair (&dh)[16], const RawRow& gate, const RawRow& up, uint32_t (&d_gate)[16],
+                                               uint32_t (&d_up)[16], uint32_t (&h)[16]) {
+    if (act == DB_ACT_SILU) gated_grad_row<DB_ACT_SILU, E4M3>(dh, gate, up, d_gate, d_up, h);
+    else if (act == DB_ACT_GELU) gated_grad_row<DB_ACT_GELU, E4M3>(dh, gate, up, d_gate, d_up, h);
+    else if (act == DB_ACT_RELU) gated_grad_row<DB_ACT_RELU, E4M3>(dh, gate, up, d_gate, d_up, h);
+    else gated_grad_row<DB_ACT_NONE, E4M3>(dh, gate, up, d_gate, d_up, h);
+}
+
+// ------------------------------------------------------------------------------------------------ the epilogue of a row
+// What the epilogue of 32 columns reads: fetched ahead, while the accumulator of the columns before is worked on.
+template <int EPI>
+struct Fetched {
+    uint32_t addend[16];
+};
+template <>
+struct Fetched<kEpiGated> {};
+template <>
+struct Fetched<kEpiGatedGrad> {
+    RawRow gate, up;
+};
+template <int EPI>
+__device__ __forceinline__ void epilogue_fetch(const EpilogueArgs& e, long long row, int col, int N, Fetched<EPI>& f) {
+    const int n = min(kChunk, N - col);
+    if constexpr (EPI == kEpiStore) {
+        if (e.addend) load_raw(e.addend + row * e.addend_pitch + col, n, f.addend);
+    } else if constexpr (EPI == kEpiGatedGrad) {
+        fetch_row(e.kept[0], e.kept_e4m3, row, col, N, n, f.gate);
+        fetch_row(e.kept[1], e.kept_e4m3, row, col, N, n, f.up);
+    }
+}
+// Columns col (a multiple of 32) to col + 32, but not past N: v the accumulator (kEpiGated: gate's), u up's.
+template <int EPI>
+__device__ __forceinline__ void epilogue_row(const EpilogueArgs& e, long long row, int col, int N, const Fetched<EPI>& f, Pair (&v)[16],
+                                             Pair (&u)[16]) {
+    const int n = min(kChunk, N - col);
+    if constexpr (EPI == kEpiStore) {
+        if (e.bias) {
+            uint32_t q[16];
+            load_raw(e.bias + col, n, q);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = add(v[i], unpack_pair(q[i]));
+        }
+        if (e.kept[0].data) keep_row(e.kept[0], e.kept_e4m3, row, col, N, n, v);
+        act_row(v, e.act);
+        if (e.addend) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = add(v[i], unpack_pair(f.addend[i]));
+        }
+        if (e.out_f32) store_row(static_cast<float*>(e.out) + row * e.out_pitch + col, n, v);
+        else store_row(static_cast<__nv_bfloat16*>(e.out) + row * e.out_pitch + col, n, v);
+    } else if constexpr (EPI == kEpiGated) {
+        if (e.kept[0].data) {
+            keep_row(e.kept[0], e.kept_e4m3, row, col, N, n, v);
+            keep_row(e.kept[1], e.kept_e4m3, row, col, N, n, u);
+        }
+        act_row(v, e.act);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = mul(v[i], u[i]);
+        store_row(static_cast<__nv_bfloat16*>(e.out) + row * e.out_pitch + col, n, v);
+    } else {
+        uint32_t d_gate[16], d_up[16], h[16];
+        if (e.kept_e4m3) gated_grad_row<true>(e.act, v, f.gate, f.up, d_gate, d_up, h);
+        else gated_grad_row<false>(e.act, v, f.gate, f.up, d_gate, d_up, h);
+        store_bytes<64>(reinterpret_cast<unsigned short*>(e.d_gate + row * e.d_pitch + col), n, d_gate);
+        store_bytes<64>(reinterpret_cast<unsigned short*>(e.d_up + row * e.d_pitch + col), n, d_up);
+        store_bytes<64>(static_cast<unsigned short*>(e.out) + row * e.out_pitch + col, n, h);
+    }
+}
+
+}  // namespace lg
+}  // namespace dynbatch

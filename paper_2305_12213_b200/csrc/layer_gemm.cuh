@@ -18,7 +18,7 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 
-#include "checkpoint8.cuh"
+#include "layer_epilogue.cuh"
 #include "tc_gemm.cuh"
 
 namespace dynbatch {
@@ -27,33 +27,6 @@ namespace lg {
 constexpr int kRows = 128;             // rows of A a CTA holds = its tensor-memory lanes
 constexpr int kBlockK = 64;            // bf16 in a 128-byte swizzled row
 constexpr int kMaxProblems = 3;
-constexpr int kChunk = 32;             // columns of a row that a thread takes at once
-
-enum Epilogue {
-    kEpiStore = 0,      // out = act(acc + bias) + addend, acc + bias kept if wanted
-    kEpiGated = 1,      // two accumulators side by side: out = act(gate) * up, both kept if wanted
-    kEpiGatedGrad = 2   // acc = dh: with gate and up as kept, d_gate, d_up and h
-};
-
-struct Kept {                    // a tensor [M, N] as it is held for the backward pass
-    void* data = nullptr;        // bf16 or e4m3 codes, N per row; nullptr: not kept
-    uint8_t* scale = nullptr;    // e4m3: ceil(N / 32) bytes per row
-};
-
-struct EpilogueArgs {
-    void* out = nullptr;         // kEpiStore: [M, N]; kEpiGated: h; kEpiGatedGrad: h
-    long long out_pitch = 0;
-    const __nv_bfloat16* bias = nullptr;
-    const __nv_bfloat16* addend = nullptr;
-    long long addend_pitch = 0;
-    Kept kept[2];                // kEpiStore: [0]; the others: gate, up
-    __nv_bfloat16* d_gate = nullptr;   // kEpiGatedGrad
-    __nv_bfloat16* d_up = nullptr;
-    long long d_pitch = 0;
-    int kept_e4m3 = 0;
-    int out_f32 = 0;
-    int act = DB_ACT_NONE;
-};
 
 struct Problem {
     CUtensorMap a[2], b[2];      // the reduction's two sources; kEpiGated: b[0] gate's and b[1] up's weights
@@ -73,288 +46,6 @@ struct GemmArgs {
     int* status;
     int clear_status;                   // the first CTA zeroes *status
 };
-
-// ------------------------------------------------------------------------------------------------ 32 values of a row
-__device__ __forceinline__ bool aligned_to(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-__device__ __forceinline__ void unpack2(uint32_t two, float& a, float& b) {
-    a = __uint_as_float(two << 16);
-    b = __uint_as_float(two & 0xFFFF0000u);
-}
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-    const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&t);
-}
-// Accesses of 32 bytes: a thread has a row of its own, so a warp's access touches 32 lines, and the fewer accesses the better.
-__device__ __forceinline__ void load32(const void* p, uint32_t* q) {
-    unsigned long long x[4];
-    asm volatile("ld.global.v4.b64 {%0,%1,%2,%3}, [%4];" : "=l"(x[0]), "=l"(x[1]), "=l"(x[2]), "=l"(x[3]) : "l"(p) : "memory");
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        q[2 * i] = static_cast<uint32_t>(x[i]);
-        q[2 * i + 1] = static_cast<uint32_t>(x[i] >> 32);
-    }
-}
-__device__ __forceinline__ void store32(void* p, const uint32_t* q) {
-    unsigned long long x[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = q[2 * i] | (static_cast<unsigned long long>(q[2 * i + 1]) << 32);
-    asm volatile("st.global.v4.b64 [%0], {%1,%2,%3,%4};" ::"l"(p), "l"(x[0]), "l"(x[1]), "l"(x[2]), "l"(x[3]) : "memory");
-}
-__device__ __forceinline__ void load16(const void* p, uint32_t* q) {
-    const uint4 x = *static_cast<const uint4*>(p);
-    q[0] = x.x; q[1] = x.y; q[2] = x.z; q[3] = x.w;
-}
-__device__ __forceinline__ void store16(void* p, const uint32_t* q) { *static_cast<uint4*>(p) = make_uint4(q[0], q[1], q[2], q[3]); }
-
-// BYTES bytes of a row, `valid` of them there (the rest zero), in units of `UNIT` bytes: the widest access that address
-// and length allow.
-template <int BYTES, class UNIT>
-__device__ __forceinline__ void load_bytes(const UNIT* p, int valid, uint32_t (&q)[BYTES / 4]) {
-    if (valid == BYTES / static_cast<int>(sizeof(UNIT)) && aligned_to(p, 16)) {
-        if (aligned_to(p, 32)) {
-#pragma unroll
-            for (int i = 0; i < BYTES / 32; ++i) load32(reinterpret_cast<const char*>(p) + 32 * i, q + 8 * i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < BYTES / 16; ++i) load16(reinterpret_cast<const char*>(p) + 16 * i, q + 4 * i);
-        }
-    } else {
-        constexpr int kPer = 4 / sizeof(UNIT);
-#pragma unroll
-        for (int i = 0; i < BYTES / 4; ++i) {
-            q[i] = 0;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                if (i * kPer + j < valid) q[i] |= static_cast<uint32_t>(p[i * kPer + j]) << (8 * sizeof(UNIT) * j);
-        }
-    }
-}
-template <int BYTES, class UNIT>
-__device__ __forceinline__ void store_bytes(UNIT* p, int valid, const uint32_t (&q)[BYTES / 4]) {
-    if (valid == BYTES / static_cast<int>(sizeof(UNIT)) && aligned_to(p, 16)) {
-        if (aligned_to(p, 32)) {
-#pragma unroll
-            for (int i = 0; i < BYTES / 32; ++i) store32(reinterpret_cast<char*>(p) + 32 * i, q + 8 * i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < BYTES / 16; ++i) store16(reinterpret_cast<char*>(p) + 16 * i, q + 4 * i);
-        }
-    } else {
-        constexpr int kPer = 4 / sizeof(UNIT);
-#pragma unroll
-        for (int i = 0; i < BYTES / 4; ++i)
-#pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                if (i * kPer + j < valid) p[i * kPer + j] = static_cast<UNIT>(q[i] >> (8 * sizeof(UNIT) * j));
-    }
-}
-__device__ __forceinline__ void load_raw(const __nv_bfloat16* p, int n, uint32_t (&q)[16]) {
-    load_bytes<64>(reinterpret_cast<const unsigned short*>(p), n, q);
-}
-__device__ __forceinline__ void unpack_row(const uint32_t (&q)[16], float (&v)[kChunk]) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) unpack2(q[i], v[2 * i], v[2 * i + 1]);
-}
-__device__ __forceinline__ void store_row(__nv_bfloat16* p, int n, const float (&v)[kChunk]) {
-    uint32_t q[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) q[i] = pack2(v[2 * i], v[2 * i + 1]);
-    store_bytes<64>(reinterpret_cast<unsigned short*>(p), n, q);
-}
-__device__ __forceinline__ void store_row(float* p, int n, const float (&v)[kChunk]) {
-    uint32_t q[kChunk];
-#pragma unroll
-    for (int i = 0; i < kChunk; ++i) q[i] = __float_as_uint(v[i]);
-    store_bytes<4 * kChunk>(reinterpret_cast<uint32_t*>(p), n, q);
-}
-__device__ __forceinline__ void keep_row(const Kept& k, int e4m3, long long row, int col, int N, int n, const float (&x)[kChunk]) {
-    if (!e4m3) {
-        store_row(static_cast<__nv_bfloat16*>(k.data) + row * N + col, n, x);
-        return;
-    }
-    float top = 0.f;
-#pragma unroll
-    for (int i = 0; i < kChunk; ++i)
-        if (i < n) top = fmaxf(top, ck8::finite_magnitude(x[i]));
-    const uint32_t byte = ck8::scale_byte(top);
-    const float inverse = ck8::scale_inverse(byte);
-    k.scale[row * ((N + kChunk - 1) / kChunk) + col / kChunk] = static_cast<uint8_t>(byte);
-    uint32_t c[8];
-    if (byte < ck8::kTopByte) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = ck8::codes4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3], inverse);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            c[i] = ck8::codes4(ck8::hold_finite(x[4 * i]), ck8::hold_finite(x[4 * i + 1]), ck8::hold_finite(x[4 * i + 2]),
-                               ck8::hold_finite(x[4 * i + 3]), inverse);
-    }
-    store_bytes<32>(static_cast<uint8_t*>(k.data) + row * N + col, n, c);
-}
-// A kept row as it lies in memory (16 words of bf16, or 8 of codes and the scale), fetched before it is needed.
-struct RawRow {
-    uint32_t q[16];
-    uint32_t scale;
-};
-__device__ __forceinline__ void fetch_row(const Kept& k, int e4m3, long long row, int col, int N, int n, RawRow& r) {
-    if (!e4m3) {
-        load_raw(static_cast<const __nv_bfloat16*>(k.data) + row * N + col, n, r.q);
-        return;
-    }
-    uint32_t c[8];
-    load_bytes<32>(static_cast<const uint8_t*>(k.data) + row * N + col, n, c);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r.q[i] = c[i];
-    r.scale = k.scale[row * ((N + kChunk - 1) / kChunk) + col / kChunk];
-}
-// ------------------------------------------------------------------------------------------------ activations
-// silu(z) = z s, s = 1 / (1 + e^-z);  gelu(z) = z P(z), P the normal distribution function.  The fast exponential and
-// quotient are off by a few 2^-23 of a value that is rounded to 2^-9.
-// P by formula 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions: for x >= 0
-//     erfc(x) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) e^(-x^2),  t = 1 / (1 + 0.3275911 x),  off by at most 1.5e-7,
-// with x = |z| / sqrt(2): P is erfc / 2 below zero and 1 - erfc / 2 above.  Two special-function instructions, and the
-// e^(-z^2 / 2) is the one that the slope needs; with erff the epilogue, not the products, set the time of a 1024-deep
-// layer (8191 x 1024 to 4096: 92 us).
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
-__device__ __forceinline__ float normal_cdf(float z, float& bell) {
-    const float t = __fdividef(1.f, fmaf(0.23164190f, fabsf(z), 1.f));       // 0.3275911 / sqrt(2)
-    bell = __expf(-0.5f * z * z);
-    const float poly = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
-    const float tail = 0.5f * t * poly * bell;
-    return z < 0.f ? tail : 1.f - tail;
-}
-__device__ __forceinline__ float act_value(float z, int act) {
-    if (act == DB_ACT_SILU) return z * sigmoid(z);
-    if (act == DB_ACT_GELU) {
-        float bell;
-        return z * normal_cdf(z, bell);
-    }
-    if (act == DB_ACT_RELU) return z < 0.f ? 0.f : z;
-    return z;
-}
-__device__ __forceinline__ void act_value_slope(float z, int act, float& value, float& slope) {
-    if (act == DB_ACT_SILU) {
-        const float s = sigmoid(z);
-        value = z * s;
-        slope = fmaf(value, 1.f - s, s);
-    } else if (act == DB_ACT_GELU) {
-        float bell;
-        const float p = normal_cdf(z, bell);
-        value = z * p;
-        slope = fmaf(z * 0.39894228f, bell, p);
-    } else if (act == DB_ACT_RELU) {
-        value = z < 0.f ? 0.f : z;
-        slope = z <= 0.f ? 0.f : 1.f;
-    } else {
-        value = z;
-        slope = 1.f;
-    }
-}
-// The branch on the activation is taken once for a row, not for each value.
-__device__ __forceinline__ void act_row(float (&v)[kChunk], int act) {
-    if (act == DB_ACT_SILU) {
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i) v[i] = act_value(v[i], DB_ACT_SILU);
-    } else if (act == DB_ACT_GELU) {
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i) v[i] = act_value(v[i], DB_ACT_GELU);
-    } else if (act == DB_ACT_RELU) {
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i) v[i] = act_value(v[i], DB_ACT_RELU);
-    }
-}
-// Two values at a time, packed as they are done: 48 words of results instead of 96 floats.
-template <int ACT>
-__device__ __forceinline__ void gated_grad_row(const float (&dh)[kChunk], const RawRow& gate, const RawRow& up, int e4m3,
-                                               uint32_t (&d_gate)[16], uint32_t (&d_up)[16], uint32_t (&h)[16]) {
-    const float gate_scale = e4m3 ? ck8::scale_value(gate.scale) : 0.f, up_scale = e4m3 ? ck8::scale_value(up.scale) : 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        float2 z, u;
-        if (e4m3) {
-            z = ck8::values2(gate.q[i / 2] >> (16 * (i % 2)));
-            u = ck8::values2(up.q[i / 2] >> (16 * (i % 2)));
-            z.x *= gate_scale; z.y *= gate_scale;
-            u.x *= up_scale; u.y *= up_scale;
-        } else {
-            unpack2(gate.q[i], z.x, z.y);
-            unpack2(up.q[i], u.x, u.y);
-        }
-        float2 a, s;
-        act_value_slope(z.x, ACT, a.x, s.x);
-        act_value_slope(z.y, ACT, a.y, s.y);
-        h[i] = pack2(a.x * u.x, a.y * u.y);
-        d_gate[i] = pack2(dh[2 * i] * u.x * s.x, dh[2 * i + 1] * u.y * s.y);
-        d_up[i] = pack2(dh[2 * i] * a.x, dh[2 * i + 1] * a.y);
-    }
-}
-
-// What the epilogue of 32 columns reads: fetched ahead, while the accumulator of the columns before is worked on.
-template <int EPI>
-struct Fetched {
-    uint32_t addend[16];
-};
-template <>
-struct Fetched<kEpiGated> {};
-template <>
-struct Fetched<kEpiGatedGrad> {
-    RawRow gate, up;
-};
-template <int EPI>
-__device__ __forceinline__ void epilogue_fetch(const EpilogueArgs& e, long long row, int col, int N, Fetched<EPI>& f) {
-    const int n = min(kChunk, N - col);
-    if constexpr (EPI == kEpiStore) {
-        if (e.addend) load_raw(e.addend + row * e.addend_pitch + col, n, f.addend);
-    } else if constexpr (EPI == kEpiGatedGrad) {
-        fetch_row(e.kept[0], e.kept_e4m3, row, col, N, n, f.gate);
-        fetch_row(e.kept[1], e.kept_e4m3, row, col, N, n, f.up);
-    }
-}
-// Columns col (a multiple of 32) to col + 32, but not past N: v the accumulator (kEpiGated: gate's), u up's.
-template <int EPI>
-__device__ __forceinline__ void epilogue_row(const EpilogueArgs& e, long long row, int col, int N, const Fetched<EPI>& f, float (&v)[kChunk],
-                                             float (&u)[kChunk]) {
-    const int n = min(kChunk, N - col);
-    if constexpr (EPI == kEpiStore) {
-        if (e.bias) {
-            uint32_t q[16];
-            float b[kChunk];
-            load_raw(e.bias + col, n, q);
-            unpack_row(q, b);
-#pragma unroll
-            for (int i = 0; i < kChunk; ++i) v[i] += b[i];
-        }
-        if (e.kept[0].data) keep_row(e.kept[0], e.kept_e4m3, row, col, N, n, v);
-        act_row(v, e.act);
-        if (e.addend) {
-            float r[kChunk];
-            unpack_row(f.addend, r);
-#pragma unroll
-            for (int i = 0; i < kChunk; ++i) v[i] += r[i];
-        }
-        if (e.out_f32) store_row(static_cast<float*>(e.out) + row * e.out_pitch + col, n, v);
-        else store_row(static_cast<__nv_bfloat16*>(e.out) + row * e.out_pitch + col, n, v);
-    } else if constexpr (EPI == kEpiGated) {
-        if (e.kept[0].data) {
-            keep_row(e.kept[0], e.kept_e4m3, row, col, N, n, v);
-            keep_row(e.kept[1], e.kept_e4m3, row, col, N, n, u);
-        }
-        act_row(v, e.act);
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i) v[i] *= u[i];
-        store_row(static_cast<__nv_bfloat16*>(e.out) + row * e.out_pitch + col, n, v);
-    } else {
-        uint32_t d_gate[16], d_up[16], h[16];
-        if (e.act == DB_ACT_SILU) gated_grad_row<DB_ACT_SILU>(v, f.gate, f.up, e.kept_e4m3, d_gate, d_up, h);
-        else if (e.act == DB_ACT_GELU) gated_grad_row<DB_ACT_GELU>(v, f.gate, f.up, e.kept_e4m3, d_gate, d_up, h);
-        else if (e.act == DB_ACT_RELU) gated_grad_row<DB_ACT_RELU>(v, f.gate, f.up, e.kept_e4m3, d_gate, d_up, h);
-        else gated_grad_row<DB_ACT_NONE>(v, f.gate, f.up, e.kept_e4m3, d_gate, d_up, h);
-        store_bytes<64>(reinterpret_cast<unsigned short*>(e.d_gate + row * e.d_pitch + col), n, d_gate);
-        store_bytes<64>(reinterpret_cast<unsigned short*>(e.d_up + row * e.d_pitch + col), n, d_up);
-        store_bytes<64>(static_cast<unsigned short*>(e.out) + row * e.out_pitch + col, n, h);
-    }
-}
 
 // ------------------------------------------------------------------------------------------------ PTX wrappers
 template <int CG>
@@ -670,14 +361,14 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
                 const int col = first + c;
                 if (in && c + kChunk < columns) epilogue_fetch<EPI>(p.e, row, col + kChunk, N, next);
                 uint32_t raw[kChunk];
-                float v[kChunk], u[kChunk];
+                Pair v[kChunk / 2], u[kChunk / 2];
                 tc::tmem_load32(acc + c, raw);
 #pragma unroll
-                for (int i = 0; i < kChunk; ++i) v[i] = __uint_as_float(raw[i]);
+                for (int i = 0; i < kChunk / 2; ++i) v[i] = pair(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1]));
                 if (EPI == kEpiGated) {
                     tc::tmem_load32(acc + kTileN + c, raw);
 #pragma unroll
-                    for (int i = 0; i < kChunk; ++i) u[i] = __uint_as_float(raw[i]);
+                    for (int i = 0; i < kChunk / 2; ++i) u[i] = pair(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1]));
                 }
                 if (in) {
                     epilogue_row<EPI>(p.e, row, col, N, now, v, u);
@@ -738,14 +429,14 @@ combine_kernel(const __grid_constant__ GemmArgs g) {
     const int col = static_cast<int>(chunk - row * (pitch / kChunk)) * kChunk;
     Fetched<EPI> f;
     epilogue_fetch<EPI>(p.e, row, col, p.N, f);
-    float v[kChunk], u[kChunk];
+    Pair v[kChunk / 2], u[kChunk / 2];
 #pragma unroll
     for (int j = 0; j < kChunk / 4; ++j) {
         const float4 q = sums[0][threadIdx.x][j];
-        v[4 * j] = q.x; v[4 * j + 1] = q.y; v[4 * j + 2] = q.z; v[4 * j + 3] = q.w;
+        v[2 * j] = pair(q.x, q.y); v[2 * j + 1] = pair(q.z, q.w);
         if (EPI == kEpiGated) {
             const float4 w = sums[kParts - 1][threadIdx.x][j];
-            u[4 * j] = w.x; u[4 * j + 1] = w.y; u[4 * j + 2] = w.z; u[4 * j + 3] = w.w;
+            u[2 * j] = pair(w.x, w.y); u[2 * j + 1] = pair(w.z, w.w);
         }
     }
     epilogue_row<EPI>(p.e, row, col, p.N, f, v, u);

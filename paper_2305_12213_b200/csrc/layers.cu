@@ -11,6 +11,7 @@ namespace dynbatch {
 namespace {
 
 using bf16 = __nv_bfloat16;
+using lg::Pair;
 
 constexpr size_t kStatusBytes = 256;
 constexpr long long kMaxRows = 1LL << 30, kMaxFeatures = 1LL << 24, kMaxElements = 1LL << 40, kMaxPitch = 1LL << 31;
@@ -37,6 +38,19 @@ repitch_kernel(const bf16* from, long long from_pitch, bf16* to, long long to_pi
     }
 }
 
+// Eight values of a row as pairs, n of them there.
+__device__ __forceinline__ void load8(const bf16* p, int n, Pair (&v)[4]) {
+    if (n == 8 && lg::aligned_to(p, 16)) {
+        const uint4 q = *reinterpret_cast<const uint4*>(p);
+        v[0] = lg::unpack_pair(q.x); v[1] = lg::unpack_pair(q.y);
+        v[2] = lg::unpack_pair(q.z); v[3] = lg::unpack_pair(q.w);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            v[j] = lg::pair(2 * j < n ? __bfloat162float(p[2 * j]) : 0.f, 2 * j + 1 < n ? __bfloat162float(p[2 * j + 1]) : 0.f);
+    }
+}
+
 struct ActGradArgs {
     const bf16* dy; long long dy_pitch;
     lg::Kept z;
@@ -59,25 +73,17 @@ act_grad_kernel(const __grid_constant__ ActGradArgs a) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int col = (blockIdx.x * 32 + lane) * 8, n = min(8, a.cols - col);
     const long long first = static_cast<long long>(blockIdx.y) * a.slab_rows, last = min(a.rows, first + a.slab_rows);
-    float sum[8];
+    Pair sum[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+    for (int j = 0; j < 4; ++j) sum[j] = lg::both(0.f);
     if (n > 0) {
         for (long long r = first + warp; r < last; r += 8) {
-            float d[8], z[8];
-            const bf16* p = a.dy + r * a.dy_pitch + col;
-            if (n == 8 && lg::aligned_to(p, 16)) {
-                const uint4 q = *reinterpret_cast<const uint4*>(p);
-                lg::unpack2(q.x, d[0], d[1]); lg::unpack2(q.y, d[2], d[3]);
-                lg::unpack2(q.z, d[4], d[5]); lg::unpack2(q.w, d[6], d[7]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) d[j] = j < n ? __bfloat162float(p[j]) : 0.f;
-            }
+            Pair d[4], z[4];
+            load8(a.dy + r * a.dy_pitch + col, n, d);
             if (a.act != DB_ACT_NONE) {
                 if (a.z_e4m3) {
                     const uint8_t* c = static_cast<const uint8_t*>(a.z.data) + r * a.cols + col;
-                    const float scale = ck8::scale_value(a.z.scale[r * ((a.cols + 31) / 32) + col / 32]);
+                    const Pair scale = lg::both(ck8::scale_value(a.z.scale[r * ((a.cols + 31) / 32) + col / 32]));
                     uint32_t w[2] = {0, 0};
                     if (n == 8 && lg::aligned_to(c, 8)) {
                         const uint2 q = *reinterpret_cast<const uint2*>(c);
@@ -88,45 +94,36 @@ act_grad_kernel(const __grid_constant__ ActGradArgs a) {
                             if (j < n) w[j / 4] |= static_cast<uint32_t>(c[j]) << (8 * (j % 4));
                     }
 #pragma unroll
-                    for (int j = 0; j < 8; j += 2) {
-                        const float2 t = ck8::values2(w[j / 4] >> (8 * (j % 4)));
-                        z[j] = t.x * scale; z[j + 1] = t.y * scale;
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 t = ck8::values2(w[j / 2] >> (16 * (j % 2)));
+                        z[j] = lg::mul(lg::pair(t.x, t.y), scale);
                     }
                 } else {
-                    const bf16* c = static_cast<const bf16*>(a.z.data) + r * a.cols + col;
-                    if (n == 8 && lg::aligned_to(c, 16)) {
-                        const uint4 q = *reinterpret_cast<const uint4*>(c);
-                        lg::unpack2(q.x, z[0], z[1]); lg::unpack2(q.y, z[2], z[3]);
-                        lg::unpack2(q.z, z[4], z[5]); lg::unpack2(q.w, z[6], z[7]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) z[j] = j < n ? __bfloat162float(c[j]) : 0.f;
-                    }
+                    load8(static_cast<const bf16*>(a.z.data) + r * a.cols + col, n, z);
                 }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    float value, slope;
-                    lg::act_value_slope(z[j], a.act, value, slope);
-                    d[j] *= slope;
-                }
+                lg::times_slope(d, z, a.act);
             }
             if (a.dz) {
                 bf16* q = a.dz + r * a.dz_pitch + col;   // workspace rows: aligned, pitch a multiple of 32
                 if (n == 8) {
-                    *reinterpret_cast<uint4*>(q) = make_uint4(lg::pack2(d[0], d[1]), lg::pack2(d[2], d[3]), lg::pack2(d[4], d[5]), lg::pack2(d[6], d[7]));
+                    *reinterpret_cast<uint4*>(q) = make_uint4(lg::pack_pair(d[0]), lg::pack_pair(d[1]), lg::pack_pair(d[2]), lg::pack_pair(d[3]));
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (j < n) q[j] = __float2bfloat16_rn(d[j]);
+                    for (int j = 0; j < 4; ++j) {
+                        float x, y;
+                        lg::halves(d[j], x, y);
+                        if (2 * j < n) q[2 * j] = __float2bfloat16_rn(x);
+                        if (2 * j + 1 < n) q[2 * j + 1] = __float2bfloat16_rn(y);
+                    }
                 }
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[j] += d[j];
+            for (int j = 0; j < 4; ++j) sum[j] = lg::add(sum[j], d[j]);
         }
     }
     if (!a.sums) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) part[warp][lane * 8 + j] = sum[j];
+    for (int j = 0; j < 4; ++j) lg::halves(sum[j], part[warp][lane * 8 + 2 * j], part[warp][lane * 8 + 2 * j + 1]);
     __syncthreads();
     const int c = blockIdx.x * 256 + threadIdx.x;
     if (c < a.cols) {
