@@ -590,7 +590,7 @@ db_status db_contract_f32(const float* A, int64_t a_row, int64_t a_k,
  * zero).  Calls on one stream may share a workspace, calls that may overlap on the device
  * (captured graphs of such calls too) need distinct ones.  Launches: forward 1 (linear), 2
  * (block), backward 2 to 4 (linear), 3 (block), one more for each product whose reduction is
- * split and for each operand off the grid; rows = 0: memsets.
+ * split and for operands off the grid; rows = 0: memsets.
  * ------------------------------------------------------------------------ */
 typedef enum {
     DB_ACT_NONE = 0,
@@ -698,7 +698,8 @@ db_status db_checkpoint_unpack(const void* codes, const void* scale,
  *           by calls on one stream, distinct for calls that may overlap
  * Any alignment down to the element size; 16-byte aligned rows take wide accesses.
  * Buffers that a call writes must not overlap others (DB_ERR_ARG).  Launches: lookup 1;
- * gradient 3 up to 8192 rows, beyond that 2 for each 9 bits of vocab and 2 more.
+ * gradient 2 up to 256 rows, 3 up to 65536, beyond that 2 for each 9 bits of vocab and 2
+ * more.
  * ------------------------------------------------------------------------ */
 db_status db_embedding(const int32_t* tokens, const void* table,
                        db_dtype table_dtype, float scale, int64_t rows,

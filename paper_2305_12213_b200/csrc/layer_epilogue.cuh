@@ -117,6 +117,24 @@ __device__ __forceinline__ void load_bytes(const UNIT* p, int valid, uint32_t (&
 #pragma unroll
             for (int i = 0; i < BYTES / 16; ++i) load16(reinterpret_cast<const char*>(p) + 16 * i, q + 4 * i);
         }
+    } else if (valid == BYTES / static_cast<int>(sizeof(UNIT))) {
+        // off the 16-byte grid: whole words from the first word boundary on, the bytes before and behind them one by one
+        const unsigned char* b = reinterpret_cast<const unsigned char*>(p);
+        const int lead = static_cast<int>((4 - (reinterpret_cast<uintptr_t>(p) & 3)) & 3);
+        uint32_t head = 0, tail = 0;
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            if (j < lead) head |= static_cast<uint32_t>(b[j]) << (8 * (4 - lead + j));     // at the word's top
+            if (lead && j < 4 - lead) tail |= static_cast<uint32_t>(b[BYTES - 4 + lead + j]) << (8 * j);
+        }
+        uint32_t before = head;
+#pragma unroll
+        for (int i = 0; i < BYTES / 4; ++i) {
+            uint32_t word = tail;
+            if (i < BYTES / 4 - 1 || lead == 0) word = *reinterpret_cast<const uint32_t*>(b + lead + 4 * i);
+            q[i] = lead ? __funnelshift_r(before, word, 8 * (4 - lead)) : word;
+            before = word;
+        }
     } else {
         constexpr int kPer = 4 / sizeof(UNIT);
 #pragma unroll
@@ -138,6 +156,18 @@ __device__ __forceinline__ void store_bytes(UNIT* p, int valid, const uint32_t (
 #pragma unroll
             for (int i = 0; i < BYTES / 16; ++i) store16(reinterpret_cast<char*>(p) + 16 * i, q + 4 * i);
         }
+    } else if (valid == BYTES / static_cast<int>(sizeof(UNIT))) {
+        unsigned char* b = reinterpret_cast<unsigned char*>(p);
+        const int lead = static_cast<int>((4 - (reinterpret_cast<uintptr_t>(p) & 3)) & 3);
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            if (j < lead) b[j] = static_cast<unsigned char>(q[0] >> (8 * j));
+            if (lead && j < 4 - lead) b[BYTES - 4 + lead + j] = static_cast<unsigned char>(q[BYTES / 4 - 1] >> (8 * (lead + j)));
+        }
+#pragma unroll
+        for (int i = 0; i < BYTES / 4; ++i)
+            if (i < BYTES / 4 - 1 || lead == 0)
+                *reinterpret_cast<uint32_t*>(b + lead + 4 * i) = lead ? __funnelshift_r(q[i], q[i + 1 < BYTES / 4 ? i + 1 : i], 8 * lead) : q[i];
     } else {
         constexpr int kPer = 4 / sizeof(UNIT);
 #pragma unroll
@@ -226,6 +256,75 @@ __device__ __forceinline__ void fetch_row(const Kept& k, int e4m3, long long row
     for (int i = 0; i < 8; ++i) r.q[i] = c[i];
     r.scale = k.scale[row * ((N + kChunk - 1) / kChunk) + col / kChunk];
 }
+
+// ------------------------------------------------------------------------------------------------ eight values of a row
+// As loaded, so that a load under way holds no more registers than it has bytes.
+template <class T> struct Raw8;
+template <> struct Raw8<__nv_bfloat16> {
+    uint4 q;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, int n) {
+        if (n == 8 && aligned_to(p, 16)) {
+            q = *reinterpret_cast<const uint4*>(p);
+        } else {
+            uint32_t w[4];
+            const unsigned short* u = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                w[j] = (2 * j < n ? u[2 * j] : 0u) | (2 * j + 1 < n ? static_cast<uint32_t>(u[2 * j + 1]) << 16 : 0u);
+            q = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    __device__ __forceinline__ void values(Pair (&v)[4]) const {
+        v[0] = unpack_pair(q.x); v[1] = unpack_pair(q.y);
+        v[2] = unpack_pair(q.z); v[3] = unpack_pair(q.w);
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const {
+        unpack2(q.x, v[0], v[1]); unpack2(q.y, v[2], v[3]);
+        unpack2(q.z, v[4], v[5]); unpack2(q.w, v[6], v[7]);
+    }
+};
+template <> struct Raw8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p, int n) {
+        if (n == 8 && aligned_to(p, 16)) {
+            a = *reinterpret_cast<const float4*>(p);
+            b = *(reinterpret_cast<const float4*>(p) + 1);
+        } else {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : 0.f;
+            a = make_float4(v[0], v[1], v[2], v[3]);
+            b = make_float4(v[4], v[5], v[6], v[7]);
+        }
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const {
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+};
+// The same for codes of a checkpoint.
+struct Codes8 {
+    uint2 q;
+    __device__ __forceinline__ void load(const uint8_t* p, int n) {
+        if (n == 8 && aligned_to(p, 8)) {
+            q = *reinterpret_cast<const uint2*>(p);
+        } else {
+            uint32_t w[2] = {0, 0};
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < n) w[j / 4] |= static_cast<uint32_t>(p[j]) << (8 * (j % 4));
+            q = make_uint2(w[0], w[1]);
+        }
+    }
+    __device__ __forceinline__ void values(uint32_t scale_byte, Pair (&v)[4]) const {
+        const Pair scale = both(ck8::scale_value(scale_byte));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 t = ck8::values2((j < 2 ? q.x : q.y) >> (16 * (j % 2)));
+            v[j] = mul(pair(t.x, t.y), scale);
+        }
+    }
+};
 
 // ------------------------------------------------------------------------------------------------ activations
 // silu(z) = z s, s = 1 / (1 + e^-z);  gelu(z) = z P(z), P the normal distribution function.  The approximate exponential
@@ -317,17 +416,6 @@ __device__ __forceinline__ void act_row(Pair (&v)[16], int act) {
     if (act == DB_ACT_SILU) act_row<DB_ACT_SILU>(v);
     else if (act == DB_ACT_GELU) act_row<DB_ACT_GELU>(v);
     else if (act == DB_ACT_RELU) act_row<DB_ACT_RELU>(v);
-}
-// d *= act'(z), four pairs
-__device__ __forceinline__ void times_slope(Pair (&d)[4], const Pair (&z)[4], int act) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        Pair value, slope;
-        if (act == DB_ACT_SILU) act_pair_slope<DB_ACT_SILU>(z[i], value, slope);
-        else if (act == DB_ACT_GELU) act_pair_slope<DB_ACT_GELU>(z[i], value, slope);
-        else act_pair_slope<DB_ACT_RELU>(z[i], value, slope);
-        d[i] = mul(d[i], slope);
-    }
 }
 // Two values at a time, packed as they are done: 48 words of results instead of 96 floats.
 template <int ACT, bool E4M3>

@@ -20,34 +20,29 @@ size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 __host__ __device__ constexpr long long cdiv(long long a, long long b) { return (a + b - 1) / b; }
 
 // ---------------------------------------------------------------------------------------------- small kernels
-// Copy of a bf16 matrix to rows of `to_pitch`: what brings operands to the 16-byte grid that TMA needs.
-__global__ void __launch_bounds__(256)
-repitch_kernel(const bf16* from, long long from_pitch, bf16* to, long long to_pitch, long long rows, int cols, int* clear_status) {
+// Copies of bf16 matrices to rows of `to_pitch` (a multiple of 8): what brings operands to the 16-byte grid that TMA needs.
+struct Repitch {
+    const bf16* from; bf16* to;
+    long long from_pitch, to_pitch, rows;
+    int cols;
+};
+constexpr int kMaxCopies = 5;
+struct RepitchArgs {
+    Repitch m[kMaxCopies];       // blockIdx.y
+    int* clear_status;
+};
+__global__ void __launch_bounds__(256) repitch_kernel(const __grid_constant__ RepitchArgs a) {
     tc::griddep_wait();
     tc::griddep_launch_dependents();
-    if (clear_status && blockIdx.x == 0 && threadIdx.x == 0) *clear_status = 0;
-    const long long per_row = cdiv(cols, 8), total = rows * per_row;
+    if (a.clear_status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.clear_status = 0;
+    const Repitch& m = a.m[blockIdx.y];
+    const long long per_row = cdiv(m.cols, 8), total = m.rows * per_row;
     for (long long i = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x; i < total; i += static_cast<long long>(gridDim.x) * blockDim.x) {
         const long long r = i / per_row;
         const int c = static_cast<int>(i - r * per_row) * 8;
-        const bf16* p = from + r * from_pitch + c;
-        union { uint4 q; bf16 v[8]; } x;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x.v[j] = c + j < cols ? p[j] : __float2bfloat16_rn(0.f);
-        *reinterpret_cast<uint4*>(to + r * to_pitch + c) = x.q;
-    }
-}
-
-// Eight values of a row as pairs, n of them there.
-__device__ __forceinline__ void load8(const bf16* p, int n, Pair (&v)[4]) {
-    if (n == 8 && lg::aligned_to(p, 16)) {
-        const uint4 q = *reinterpret_cast<const uint4*>(p);
-        v[0] = lg::unpack_pair(q.x); v[1] = lg::unpack_pair(q.y);
-        v[2] = lg::unpack_pair(q.z); v[3] = lg::unpack_pair(q.w);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            v[j] = lg::pair(2 * j < n ? __bfloat162float(p[2 * j]) : 0.f, 2 * j + 1 < n ? __bfloat162float(p[2 * j + 1]) : 0.f);
+        lg::Raw8<bf16> x;
+        x.load(m.from + r * m.from_pitch + c, min(8, m.cols - c));
+        *reinterpret_cast<uint4*>(m.to + r * m.to_pitch + c) = x.q;
     }
 }
 
@@ -64,6 +59,7 @@ struct ActGradArgs {
 
 // dz = dy act'(z) and the sums of its columns.  HBM-bound.  A warp takes 256 columns of a row, eight per lane; a CTA's
 // eight warps take every eighth row of a slab and add their sums in warp order, so the result does not depend on timing.
+template <int ACT, bool E4M3>
 __global__ void __launch_bounds__(256)
 act_grad_kernel(const __grid_constant__ ActGradArgs a) {
     __shared__ float part[8][256];
@@ -77,48 +73,58 @@ act_grad_kernel(const __grid_constant__ ActGradArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) sum[j] = lg::both(0.f);
     if (n > 0) {
-        for (long long r = first + warp; r < last; r += 8) {
-            Pair d[4], z[4];
-            load8(a.dy + r * a.dy_pitch + col, n, d);
-            if (a.act != DB_ACT_NONE) {
-                if (a.z_e4m3) {
-                    const uint8_t* c = static_cast<const uint8_t*>(a.z.data) + r * a.cols + col;
-                    const Pair scale = lg::both(ck8::scale_value(a.z.scale[r * ((a.cols + 31) / 32) + col / 32]));
-                    uint32_t w[2] = {0, 0};
-                    if (n == 8 && lg::aligned_to(c, 8)) {
-                        const uint2 q = *reinterpret_cast<const uint2*>(c);
-                        w[0] = q.x; w[1] = q.y;
+        constexpr int kDeep = 4;                               // rows under way
+        for (long long r0 = first + warp; r0 < last; r0 += 8 * kDeep) {
+            lg::Raw8<bf16> dy[kDeep], z16[kDeep];
+            lg::Codes8 z8[kDeep];
+            uint32_t byte[kDeep];
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {
+                const long long r = r0 + 8 * i;
+                const int m = r < last ? n : 0;
+                dy[i].load(a.dy + r * a.dy_pitch + col, m);
+                if (ACT == DB_ACT_NONE) continue;
+                if (E4M3) {
+                    byte[i] = m ? a.z.scale[r * ((a.cols + 31) / 32) + col / 32] : 0;
+                    z8[i].load(static_cast<const uint8_t*>(a.z.data) + r * a.cols + col, m);
+                } else {
+                    z16[i].load(static_cast<const bf16*>(a.z.data) + r * a.cols + col, m);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {
+                const long long r = r0 + 8 * i;
+                if (r >= last) break;
+                Pair d[4];
+                dy[i].values(d);
+                if (ACT != DB_ACT_NONE) {
+                    Pair z[4];
+                    if (E4M3) z8[i].values(byte[i], z);
+                    else z16[i].values(z);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        Pair value, slope;
+                        lg::act_pair_slope<ACT>(z[j], value, slope);
+                        d[j] = lg::mul(d[j], slope);
+                    }
+                }
+                if (a.dz) {
+                    bf16* q = a.dz + r * a.dz_pitch + col;     // workspace rows: aligned, pitch a multiple of 32
+                    if (n == 8) {
+                        *reinterpret_cast<uint4*>(q) = make_uint4(lg::pack_pair(d[0]), lg::pack_pair(d[1]), lg::pack_pair(d[2]), lg::pack_pair(d[3]));
                     } else {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (j < n) w[j / 4] |= static_cast<uint32_t>(c[j]) << (8 * (j % 4));
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 t = ck8::values2(w[j / 2] >> (16 * (j % 2)));
-                        z[j] = lg::mul(lg::pair(t.x, t.y), scale);
-                    }
-                } else {
-                    load8(static_cast<const bf16*>(a.z.data) + r * a.cols + col, n, z);
-                }
-                lg::times_slope(d, z, a.act);
-            }
-            if (a.dz) {
-                bf16* q = a.dz + r * a.dz_pitch + col;   // workspace rows: aligned, pitch a multiple of 32
-                if (n == 8) {
-                    *reinterpret_cast<uint4*>(q) = make_uint4(lg::pack_pair(d[0]), lg::pack_pair(d[1]), lg::pack_pair(d[2]), lg::pack_pair(d[3]));
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float x, y;
-                        lg::halves(d[j], x, y);
-                        if (2 * j < n) q[2 * j] = __float2bfloat16_rn(x);
-                        if (2 * j + 1 < n) q[2 * j + 1] = __float2bfloat16_rn(y);
+                        for (int j = 0; j < 4; ++j) {
+                            float x, y;
+                            lg::halves(d[j], x, y);
+                            if (2 * j < n) q[2 * j] = __float2bfloat16_rn(x);
+                            if (2 * j + 1 < n) q[2 * j + 1] = __float2bfloat16_rn(y);
+                        }
                     }
                 }
-            }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sum[j] = lg::add(sum[j], d[j]);
+                for (int j = 0; j < 4; ++j) sum[j] = lg::add(sum[j], d[j]);
+            }
         }
     }
     if (!a.sums) return;
@@ -131,6 +137,16 @@ act_grad_kernel(const __grid_constant__ ActGradArgs a) {
 #pragma unroll
         for (int w = 0; w < 8; ++w) s += part[w][threadIdx.x];
         a.sums[blockIdx.y * a.sums_pitch + c] = s;
+    }
+}
+
+using ActGradFn = void (*)(const ActGradArgs);
+ActGradFn act_grad_fn(int act, bool e4m3) {
+    switch (act) {
+        case DB_ACT_RELU: return e4m3 ? act_grad_kernel<DB_ACT_RELU, true> : act_grad_kernel<DB_ACT_RELU, false>;
+        case DB_ACT_GELU: return e4m3 ? act_grad_kernel<DB_ACT_GELU, true> : act_grad_kernel<DB_ACT_GELU, false>;
+        case DB_ACT_SILU: return e4m3 ? act_grad_kernel<DB_ACT_SILU, true> : act_grad_kernel<DB_ACT_SILU, false>;
+        default: return act_grad_kernel<DB_ACT_NONE, false>;
     }
 }
 
@@ -393,28 +409,30 @@ struct Arena {               // hands out the workspace in pieces of whole 256 b
     }
 };
 
-// An operand for TMA: the matrix itself where it lies on the 16-byte grid, else a copy in the workspace.
+// An operand for TMA: the matrix itself where it lies on the 16-byte grid, else a copy in the workspace, made by copy_now().
 struct Operands {
     Arena& arena;
-    cudaStream_t stream;
-    int* status;
-    bool& clear;
-    db_status st = DB_OK;
+    RepitchArgs copies{};
+    int count = 0;
+    long long most = 0;
+    explicit Operands(Arena& a) : arena(a) {}
     Matrix of(const void* p, long long rows, long long cols, long long pitch) {
         Matrix m{static_cast<const bf16*>(p), rows, cols, pitch};
         if (on_grid(p, pitch)) return m;
         m.pitch = (cols + 7) / 8 * 8;
         bf16* to = reinterpret_cast<bf16*>(arena.take(static_cast<size_t>(rows * m.pitch) * 2));
-        if (arena.base && st == DB_OK) {
-            const long long pieces = rows * (m.pitch / 8);
-            Launch L(dim3(static_cast<unsigned>(std::min<long long>(cdiv(pieces, 256), 8LL * sm_count()))), dim3(256), 0, stream);
-            const cudaError_t err = cudaLaunchKernelEx(&L.cfg, repitch_kernel, m.p, pitch, to, m.pitch, rows, static_cast<int>(cols),
-                                                       clear ? status : static_cast<int*>(nullptr));
-            clear = false;
-            if (err != cudaSuccess) st = record_cuda_error(err, "repitch_kernel");
-        }
+        copies.m[count++] = {m.p, to, pitch, m.pitch, rows, static_cast<int>(cols)};
+        most = std::max(most, rows * (m.pitch / 8));
         m.p = to;
         return m;
+    }
+    db_status copy_now(int* status, bool& clear, cudaStream_t stream) {
+        if (count == 0) return DB_OK;
+        copies.clear_status = clear ? status : nullptr;
+        clear = false;
+        Launch L(dim3(static_cast<unsigned>(std::min<long long>(cdiv(most, 256), 8LL * sm_count())), count), dim3(256), 0, stream);
+        DB_CUDA_TRY(cudaLaunchKernelEx(&L.cfg, repitch_kernel, copies));
+        return DB_OK;
     }
 };
 
@@ -462,7 +480,7 @@ struct LinearArgs {
 db_status linear_forward(const LinearArgs& v, Arena& arena, cudaStream_t stream, bool aligned) {
     int* status = reinterpret_cast<int*>(arena.base);
     bool clear = true;
-    Operands ops{arena, stream, status, clear};
+    Operands ops(arena);
     Product p;
     const void* off = aligned ? nullptr : reinterpret_cast<const void*>(2);   // when counting: a pointer off the grid
     const bool count = !arena.base;
@@ -478,8 +496,9 @@ db_status linear_forward(const LinearArgs& v, Arena& arena, cudaStream_t stream,
     p.e.act = v.act;
     const Plan plan = make_plan(kForward, &p.size, 1, cdiv(v.n_in, lg::kBlockK));
     float* partials = reinterpret_cast<float*>(arena.take(static_cast<size_t>(plan.partial_floats) * 4));
-    if (count || ops.st != DB_OK) return ops.st;
-    return run_products(kForward, &p, 1, partials, status, clear, stream);
+    if (count) return DB_OK;
+    const db_status st = ops.copy_now(status, clear, stream);
+    return st != DB_OK ? st : run_products(kForward, &p, 1, partials, status, clear, stream);
 }
 
 struct LinearGradArgs {
@@ -503,7 +522,7 @@ db_status linear_backward(const LinearGradArgs& v, Arena& arena, cudaStream_t st
     const void* off = aligned ? nullptr : reinterpret_cast<const void*>(2);
     const bool has_act = count || v.act != DB_ACT_NONE, want_bias = count || v.dbias, want_dw = count || v.dw, want_dx = count || v.dx;
     Matrix dz{static_cast<const bf16*>(v.dy), v.rows, v.n_out, v.dy_pitch};
-    Operands ops{arena, stream, status, clear};
+    Operands ops(arena);
     if (has_act || want_bias) {
         ActGradArgs a{};
         a.dy = static_cast<const bf16*>(v.dy); a.dy_pitch = v.dy_pitch;
@@ -528,7 +547,7 @@ db_status linear_backward(const LinearGradArgs& v, Arena& arena, cudaStream_t st
             a.clear_status = status;
             clear = false;
             Launch L(dim3(static_cast<unsigned>(cdiv(v.n_out, 256)), used), dim3(256), 0, stream);
-            DB_CUDA_TRY(cudaLaunchKernelEx(&L.cfg, act_grad_kernel, a));
+            DB_CUDA_TRY(cudaLaunchKernelEx(&L.cfg, act_grad_fn(a.act, a.z_e4m3), a));
             if (want_bias) {
                 Launch F(dim3(static_cast<unsigned>(cdiv(v.n_out, 128))), dim3(128), 0, stream);
                 DB_CUDA_TRY(cudaLaunchKernelEx(&F.cfg, bias_fold_kernel, static_cast<const float*>(a.sums), a.sums_pitch, used, v.n_out,
@@ -542,30 +561,26 @@ db_status linear_backward(const LinearGradArgs& v, Arena& arena, cudaStream_t st
     plan_x = make_plan(kInputGrad, &size_x, 1, cdiv(v.n_out, lg::kBlockK));
     plan_w = make_plan(kWeightGrad, &size_w, 1, cdiv(v.rows, lg::kBlockK));
     float* partials = reinterpret_cast<float*>(arena.take(static_cast<size_t>(std::max(plan_x.partial_floats, plan_w.partial_floats)) * 4));
+    Product p, q;
     if (want_dx) {
-        Product p;
         p.a[0] = dz;
         p.b[0] = ops.of(count ? off : v.w, v.n_in, v.n_out, count && aligned ? (v.n_out + 7) / 8 * 8 : v.n_out);
         p.size = size_x;
         p.e.out = v.dx; p.e.out_pitch = v.dx_pitch;
         p.e.addend = static_cast<const bf16*>(v.addend); p.e.addend_pitch = v.addend_pitch;
-        if (ops.st != DB_OK) return ops.st;
-        if (!count) {
-            const db_status st = run_products(kInputGrad, &p, 1, partials, status, clear, stream);
-            if (st != DB_OK) return st;
-        }
     }
     if (want_dw) {
-        Product p;
-        p.a[0] = ops.of(count ? off : v.x, v.rows, v.n_in, count ? (aligned ? (v.n_in + 7) / 8 * 8 : v.n_in) : v.x_pitch);
-        p.b[0] = dz;
-        p.size = size_w;
-        p.e.out = v.dw; p.e.out_pitch = v.n_out;
-        p.e.out_f32 = v.grad_dtype == DB_F32;
-        if (ops.st != DB_OK) return ops.st;
-        if (!count) return run_products(kWeightGrad, &p, 1, partials, status, clear, stream);
+        q.a[0] = ops.of(count ? off : v.x, v.rows, v.n_in, count ? (aligned ? (v.n_in + 7) / 8 * 8 : v.n_in) : v.x_pitch);
+        q.b[0] = dz;
+        q.size = size_w;
+        q.e.out = v.dw; q.e.out_pitch = v.n_out;
+        q.e.out_f32 = v.grad_dtype == DB_F32;
     }
-    return DB_OK;
+    if (count) return DB_OK;
+    db_status st = ops.copy_now(status, clear, stream);
+    if (st == DB_OK && want_dx) st = run_products(kInputGrad, &p, 1, partials, status, clear, stream);
+    if (st == DB_OK && want_dw) st = run_products(kWeightGrad, &q, 1, partials, status, clear, stream);
+    return st;
 }
 
 // ---------------------------------------------------------------------------------------------- gated block
@@ -585,7 +600,7 @@ db_status gated_forward(const GatedArgs& v, Arena& arena, cudaStream_t stream, b
     int* status = reinterpret_cast<int*>(arena.base);
     bool clear = true;
     const void* off = aligned ? nullptr : reinterpret_cast<const void*>(2);
-    Operands ops{arena, stream, status, clear};
+    Operands ops(arena);
     const long long h_pitch = (v.hidden + 31LL) / 32 * 32;
     bf16* h = reinterpret_cast<bf16*>(arena.take(static_cast<size_t>(v.rows * h_pitch) * 2));
     const auto pitch = [&](long long given, long long cols) { return !count ? given : aligned ? (cols + 7) / 8 * 8 : cols; };
@@ -606,8 +621,9 @@ db_status gated_forward(const GatedArgs& v, Arena& arena, cudaStream_t stream, b
     q.e.addend = static_cast<const bf16*>(v.residual); q.e.addend_pitch = v.residual_pitch;
     const Plan a = make_plan(kGated, &p.size, 1, cdiv(v.width, lg::kBlockK)), b = make_plan(kForward, &q.size, 1, cdiv(v.hidden, lg::kBlockK));
     float* partials = reinterpret_cast<float*>(arena.take(static_cast<size_t>(std::max(a.partial_floats, b.partial_floats)) * 4));
-    if (count || ops.st != DB_OK) return ops.st;
-    const db_status st = run_products(kGated, &p, 1, partials, status, clear, stream);
+    if (count) return DB_OK;
+    db_status st = ops.copy_now(status, clear, stream);
+    if (st == DB_OK) st = run_products(kGated, &p, 1, partials, status, clear, stream);
     return st != DB_OK ? st : run_products(kForward, &q, 1, partials, status, clear, stream);
 }
 
@@ -616,7 +632,7 @@ db_status gated_backward(const GatedArgs& v, Arena& arena, cudaStream_t stream, 
     int* status = reinterpret_cast<int*>(arena.base);
     bool clear = true;
     const void* off = aligned ? nullptr : reinterpret_cast<const void*>(2);
-    Operands ops{arena, stream, status, clear};
+    Operands ops(arena);
     const long long h_pitch = (v.hidden + 31LL) / 32 * 32;
     const size_t h_bytes = static_cast<size_t>(v.rows * h_pitch) * 2;
     bf16* h = reinterpret_cast<bf16*>(arena.take(h_bytes));
@@ -680,8 +696,9 @@ db_status gated_backward(const GatedArgs& v, Arena& arena, cudaStream_t stream, 
         floats = std::max(floats, make_plan(kWeightGrad, sizes, n, cdiv(v.rows, lg::kBlockK)).partial_floats);
     }
     float* partials = reinterpret_cast<float*>(arena.take(static_cast<size_t>(floats) * 4));
-    if (count || ops.st != DB_OK) return ops.st;
-    db_status st = run_products(kGatedGrad, &p, 1, partials, status, clear, stream);
+    if (count) return DB_OK;
+    db_status st = ops.copy_now(status, clear, stream);
+    if (st == DB_OK) st = run_products(kGatedGrad, &p, 1, partials, status, clear, stream);
     if (st == DB_OK && want_dx) st = run_products(kInputGrad, &q, 1, partials, status, clear, stream);
     if (st == DB_OK && n) st = run_products(kWeightGrad, w, n, partials, status, clear, stream);
     return st;
