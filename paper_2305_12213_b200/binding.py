@@ -741,76 +741,92 @@ def adamw_scale_elems(n: int) -> int:
 
 
 # ---------------------------------------------------------------------------------------------------------------
-# layers: a call's tensors share one device, which is made current for it
+# layers.  A call's tensors share one device, which is made current for it.  Small layers' calls are bound by this side
+# (a linear layer of 256 rows: 8 us of Python and launch against 10 on the GPU), so the checks ask a tensor each thing once.
 # ---------------------------------------------------------------------------------------------------------------
-class _Call:
-    """Collects the arguments of a layer call: every tensor is on the device of the first one."""
+_BF16, _E4M3, _E8M0 = torch.bfloat16, torch.float8_e4m3fn, torch.float8_e8m0fnu
 
-    def __init__(self, first: torch.Tensor):
-        if not first.is_cuda:
-            raise TypeError("the tensors of a layer must be CUDA tensors")
-        self.device = first.device
 
-    def _here(self, t: torch.Tensor, name: str) -> None:
-        if t.device != self.device:
-            raise ValueError(f"{name} is on {t.device}, the call's first tensor on {self.device}")
+def _device_index(first: torch.Tensor) -> int:
+    index = first.get_device()
+    if index < 0:
+        raise TypeError("the tensors of a layer must be CUDA tensors")
+    return index
 
-    def rows(self, t: Optional[torch.Tensor], rows: int, cols: int, name: str, dtype: torch.dtype = torch.bfloat16):
-        """Pointer and pitch of a [rows, cols] tensor whose rows are contiguous."""
-        if t is None:
-            return None, 0
-        self._here(t, name)
-        if t.dtype != dtype:
-            raise TypeError(f"{name} must be {dtype}")
-        if tuple(t.shape) != (rows, cols):
-            raise ValueError(f"{name} must be [{rows}, {cols}]")
-        pitch = t.stride(0) if rows > 1 else cols
-        if (cols > 1 and t.stride(1) != 1) or pitch < cols:
-            raise ValueError(f"the rows of {name} must be contiguous and may not overlap")
-        return t.data_ptr(), pitch
 
-    def whole(self, t: Optional[torch.Tensor], shape, dtype: torch.dtype, name: str):
-        """Pointer of a contiguous tensor."""
-        if t is None:
-            return None
-        self._here(t, name)
-        if tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{name} must be {list(shape)}")
-        return _dev_ptr(t, dtype, name)
+def _elsewhere(t: torch.Tensor, index: int, name: str):
+    raise ValueError(f"{name} is on {t.device}, the call's first tensor on cuda:{index}")
 
-    def kept(self, t: Optional[torch.Tensor], scale: Optional[torch.Tensor], rows: int, cols: int, name: str):
-        """Pointers and type of a tensor kept for the backward pass."""
-        if t is None:
-            return None, None, DB_BF16
-        if t.dtype == torch.float8_e4m3fn:
-            if scale is None:
-                raise ValueError(f"{name} in 8 bits needs {name}_scale")
-            return (self.whole(t, (rows, cols), t.dtype, name),
-                    self.whole(scale, (rows, checkpoint_scales(cols)), torch.float8_e8m0fnu, name + "_scale"), DB_E4M3)
-        return self.whole(t, (rows, cols), torch.bfloat16, name), None, DB_BF16
 
-    def grads(self, named, dtype=None):
-        """Pointers and common type of the wanted weight gradients: named = [(tensor, shape, name), ...]."""
-        for t, _, name in named:
-            if t is not None:
-                if dtype is not None and t.dtype != dtype:
-                    raise TypeError("weight gradients must have one type")
-                dtype = t.dtype
-        code = DB_BF16 if dtype is None else _dtype_code(dtype)
-        return [self.whole(t, shape, dtype, name) for t, shape, name in named], code
+def _rows(t: Optional[torch.Tensor], rows: int, cols: int, index: int, name: str, dtype: torch.dtype = _BF16):
+    """Pointer and pitch of a [rows, cols] tensor whose rows are contiguous."""
+    if t is None:
+        return None, 0
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if t.shape != (rows, cols):
+        raise ValueError(f"{name} must be [{rows}, {cols}]")
+    if t.get_device() != index:
+        _elsewhere(t, index, name)
+    pitch, step = t.stride()
+    if rows <= 1:
+        pitch = cols
+    if pitch < cols or (step != 1 and cols > 1):
+        raise ValueError(f"the rows of {name} must be contiguous and may not overlap")
+    return t.data_ptr(), pitch
 
-    def workspace(self, t: torch.Tensor):
-        self._here(t, "workspace")
-        return t.data_ptr(), t.numel() * t.element_size()
 
-    def __call__(self, fn, *args, stream: Optional[torch.cuda.Stream] = None) -> None:
-        index = self.device.index
-        handle = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
-        if torch.cuda.current_device() == index:
-            _check(fn(*args, handle))
-        else:
-            with torch.cuda.device(self.device):
-                _check(fn(*args, handle))
+def _whole(t: Optional[torch.Tensor], shape, dtype: torch.dtype, index: int, name: str) -> Optional[int]:
+    """Pointer of a contiguous tensor."""
+    if t is None:
+        return None
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}")
+    if t.dtype != dtype or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous CUDA tensor of {dtype}")
+    if t.get_device() != index:
+        _elsewhere(t, index, name)
+    return t.data_ptr()
+
+
+def _kept(t: Optional[torch.Tensor], scale: Optional[torch.Tensor], rows: int, cols: int, index: int, name: str):
+    """Pointers and type of a tensor kept for the backward pass."""
+    if t is None:
+        return None, None, DB_BF16
+    if t.dtype == _E4M3:
+        if scale is None:
+            raise ValueError(f"{name} in 8 bits needs its scale")
+        return (_whole(t, (rows, cols), _E4M3, index, name),
+                _whole(scale, (rows, checkpoint_scales(cols)), _E8M0, index, name + "'s scale"), DB_E4M3)
+    return _whole(t, (rows, cols), _BF16, index, name), None, DB_BF16
+
+
+def _grad_code(*tensors: Optional[torch.Tensor]):
+    """The common type of the wanted weight gradients and its code."""
+    dtype = None
+    for t in tensors:
+        if t is not None:
+            if dtype is not None and t.dtype != dtype:
+                raise TypeError("weight gradients must have one type")
+            dtype = t.dtype
+    return (_BF16, DB_BF16) if dtype is None else (dtype, _dtype_code(dtype))
+
+
+def _scratch(t: torch.Tensor, index: int):
+    if t.get_device() != index:
+        _elsewhere(t, index, "workspace")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _launch(index: int, stream: Optional[torch.cuda.Stream], fn, *args) -> None:
+    handle = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() == index:
+        status = fn(*args, handle)
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, handle)
+    if status:
+        _check(status)
 
 
 def _activation(name: str) -> int:
@@ -850,16 +866,16 @@ def linear(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, workspace: torch.T
     z receives x w + bias for the backward pass: bfloat16, or float8_e4m3fn with z_scale [rows, checkpoint_scales(n_out)]
     (float8_e8m0fnu).  workspace: uint8, linear_workspace_bytes(...) bytes.
     """
-    call = _Call(x)
+    index = _device_index(x)
     rows, n_in = x.shape
     n_out = w.shape[-1]
-    xp, x_pitch = call.rows(x, rows, n_in, "x")
-    rp, r_pitch = call.rows(residual, rows, n_out, "residual")
-    yp, y_pitch = call.rows(y, rows, n_out, "y")
-    zp, sp, zt = call.kept(z, z_scale, rows, n_out, "z")
-    call(lib().db_linear, xp, x_pitch, call.whole(w, (n_in, n_out), torch.bfloat16, "w"),
-         call.whole(bias, (n_out,), torch.bfloat16, "bias"), rp, r_pitch, _activation(activation), rows, n_in, n_out, yp,
-         y_pitch, zp, sp, zt, *call.workspace(workspace), stream=stream)
+    xp, x_pitch = _rows(x, rows, n_in, index, "x")
+    rp, r_pitch = _rows(residual, rows, n_out, index, "residual")
+    yp, y_pitch = _rows(y, rows, n_out, index, "y")
+    zp, sp, zt = _kept(z, z_scale, rows, n_out, index, "z")
+    _launch(index, stream, lib().db_linear, xp, x_pitch, _whole(w, (n_in, n_out), _BF16, index, "w"),
+            _whole(bias, (n_out,), _BF16, index, "bias"), rp, r_pitch, _activation(activation), rows, n_in, n_out, yp, y_pitch,
+            zp, sp, zt, *_scratch(workspace, index))
 
 
 def linear_grad(dy: torch.Tensor, x: Optional[torch.Tensor], w: torch.Tensor, workspace: torch.Tensor,
@@ -869,18 +885,19 @@ def linear_grad(dy: torch.Tensor, x: Optional[torch.Tensor], w: torch.Tensor, wo
     """db_linear_grad: the wanted ones of dx (+ dx_addend), dw and dbias; z as db_linear kept it (needed with an
     activation).  dw and dbias are both float32 or both bfloat16; x is needed for dw.
     workspace: linear_grad_workspace_bytes(...) bytes."""
-    call = _Call(dy)
+    index = _device_index(dy)
     n_in, n_out = w.shape
     rows = dy.shape[0]
-    dyp, dy_pitch = call.rows(dy, rows, n_out, "dy")
-    xp, x_pitch = call.rows(x, rows, n_in, "x")
-    dxp, dx_pitch = call.rows(dx, rows, n_in, "dx")
-    ap, a_pitch = call.rows(dx_addend, rows, n_in, "dx_addend")
-    zp, sp, zt = call.kept(z, z_scale, rows, n_out, "z")
-    (dwp, dbp), code = call.grads([(dw, (n_in, n_out), "dw"), (dbias, (n_out,), "dbias")])
-    call(lib().db_linear_grad, dyp, dy_pitch, xp, x_pitch, call.whole(w, (n_in, n_out), torch.bfloat16, "w"), zp, sp, zt,
-         _activation(activation), rows, n_in, n_out, dxp, dx_pitch, ap, a_pitch, dwp, dbp, code,
-         *call.workspace(workspace), stream=stream)
+    dyp, dy_pitch = _rows(dy, rows, n_out, index, "dy")
+    xp, x_pitch = _rows(x, rows, n_in, index, "x")
+    dxp, dx_pitch = _rows(dx, rows, n_in, index, "dx")
+    ap, a_pitch = _rows(dx_addend, rows, n_in, index, "dx_addend")
+    zp, sp, zt = _kept(z, z_scale, rows, n_out, index, "z")
+    dtype, code = _grad_code(dw, dbias)
+    _launch(index, stream, lib().db_linear_grad, dyp, dy_pitch, xp, x_pitch, _whole(w, (n_in, n_out), _BF16, index, "w"), zp, sp,
+            zt, _activation(activation), rows, n_in, n_out, dxp, dx_pitch, ap, a_pitch,
+            _whole(dw, (n_in, n_out), dtype, index, "dw"), _whole(dbias, (n_out,), dtype, index, "dbias"), code,
+            *_scratch(workspace, index))
 
 
 def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, y: torch.Tensor,
@@ -894,21 +911,20 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
     gate and up receive x w_gate and x w_up for the backward pass, both bfloat16 or both float8_e4m3fn with their scales
     [rows, checkpoint_scales(hidden)].  workspace: gated_ffn_workspace_bytes(...) bytes.
     """
-    call = _Call(x)
+    index = _device_index(x)
     rows, width = x.shape
     hidden = w_gate.shape[-1]
-    bf16 = torch.bfloat16
-    xp, x_pitch = call.rows(x, rows, width, "x")
-    rp, r_pitch = call.rows(residual, rows, width, "residual")
-    yp, y_pitch = call.rows(y, rows, width, "y")
-    gp, gs, gt = call.kept(gate, gate_scale, rows, hidden, "gate")
-    upp, us, ut = call.kept(up, up_scale, rows, hidden, "up")
+    xp, x_pitch = _rows(x, rows, width, index, "x")
+    rp, r_pitch = _rows(residual, rows, width, index, "residual")
+    yp, y_pitch = _rows(y, rows, width, index, "y")
+    gp, gs, gt = _kept(gate, gate_scale, rows, hidden, index, "gate")
+    upp, us, ut = _kept(up, up_scale, rows, hidden, index, "up")
     if gate is not None and up is not None and gt != ut:
         raise TypeError("gate and up must have one type")
-    call(lib().db_gated_ffn, xp, x_pitch, call.whole(w_gate, (width, hidden), bf16, "w_gate"),
-         call.whole(w_up, (width, hidden), bf16, "w_up"), call.whole(w_down, (hidden, width), bf16, "w_down"), rp, r_pitch,
-         _activation(activation), rows, width, hidden, yp, y_pitch, gp, upp, gs, us, gt, *call.workspace(workspace),
-         stream=stream)
+    _launch(index, stream, lib().db_gated_ffn, xp, x_pitch, _whole(w_gate, (width, hidden), _BF16, index, "w_gate"),
+            _whole(w_up, (width, hidden), _BF16, index, "w_up"), _whole(w_down, (hidden, width), _BF16, index, "w_down"), rp,
+            r_pitch, _activation(activation), rows, width, hidden, yp, y_pitch, gp, upp, gs, us, gt,
+            *_scratch(workspace, index))
 
 
 def gated_ffn_grad(dy: torch.Tensor, x: Optional[torch.Tensor], w_gate: torch.Tensor, w_up: torch.Tensor,
@@ -920,24 +936,24 @@ def gated_ffn_grad(dy: torch.Tensor, x: Optional[torch.Tensor], w_gate: torch.Te
     """db_gated_ffn_grad: the wanted ones of dx (+ dx_addend), dw_gate, dw_up and dw_down; gate and up as db_gated_ffn kept
     them.  The weight gradients have one type, float32 or bfloat16; x is needed for dw_gate and dw_up.
     workspace: gated_ffn_grad_workspace_bytes(...) bytes."""
-    call = _Call(dy)
+    index = _device_index(dy)
     width, hidden = w_gate.shape
     rows = dy.shape[0]
-    bf16 = torch.bfloat16
-    dyp, dy_pitch = call.rows(dy, rows, width, "dy")
-    xp, x_pitch = call.rows(x, rows, width, "x")
-    dxp, dx_pitch = call.rows(dx, rows, width, "dx")
-    ap, a_pitch = call.rows(dx_addend, rows, width, "dx_addend")
-    gp, gs, gt = call.kept(gate, gate_scale, rows, hidden, "gate")
-    upp, us, ut = call.kept(up, up_scale, rows, hidden, "up")
+    dyp, dy_pitch = _rows(dy, rows, width, index, "dy")
+    xp, x_pitch = _rows(x, rows, width, index, "x")
+    dxp, dx_pitch = _rows(dx, rows, width, index, "dx")
+    ap, a_pitch = _rows(dx_addend, rows, width, index, "dx_addend")
+    gp, gs, gt = _kept(gate, gate_scale, rows, hidden, index, "gate")
+    upp, us, ut = _kept(up, up_scale, rows, hidden, index, "up")
     if gt != ut:
         raise TypeError("gate and up must have one type")
-    (dgp, dup, ddp), code = call.grads([(dw_gate, (width, hidden), "dw_gate"), (dw_up, (width, hidden), "dw_up"),
-                                        (dw_down, (hidden, width), "dw_down")])
-    call(lib().db_gated_ffn_grad, dyp, dy_pitch, xp, x_pitch, call.whole(w_gate, (width, hidden), bf16, "w_gate"),
-         call.whole(w_up, (width, hidden), bf16, "w_up"), call.whole(w_down, (hidden, width), bf16, "w_down"), gp, upp, gs, us,
-         gt, _activation(activation), rows, width, hidden, dxp, dx_pitch, ap, a_pitch, dgp, dup, ddp, code,
-         *call.workspace(workspace), stream=stream)
+    dtype, code = _grad_code(dw_gate, dw_up, dw_down)
+    _launch(index, stream, lib().db_gated_ffn_grad, dyp, dy_pitch, xp, x_pitch,
+            _whole(w_gate, (width, hidden), _BF16, index, "w_gate"), _whole(w_up, (width, hidden), _BF16, index, "w_up"),
+            _whole(w_down, (hidden, width), _BF16, index, "w_down"), gp, upp, gs, us, gt, _activation(activation), rows, width,
+            hidden, dxp, dx_pitch, ap, a_pitch, _whole(dw_gate, (width, hidden), dtype, index, "dw_gate"),
+            _whole(dw_up, (width, hidden), dtype, index, "dw_up"), _whole(dw_down, (hidden, width), dtype, index, "dw_down"),
+            code, *_scratch(workspace, index))
 
 
 def layer_status(workspace: torch.Tensor) -> int:
@@ -949,38 +965,38 @@ def checkpoint_pack(x: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor,
                     stream: Optional[torch.cuda.Stream] = None) -> None:
     """db_checkpoint_pack: x [rows, cols] bfloat16 (rows contiguous) to codes [rows, cols] float8_e4m3fn and scale
     [rows, checkpoint_scales(cols)] float8_e8m0fnu."""
-    call = _Call(x)
+    index = _device_index(x)
     rows, cols = x.shape
-    xp, pitch = call.rows(x, rows, cols, "x")
-    cp, sp, _ = call.kept(codes, scale, rows, cols, "codes") if codes.dtype == torch.float8_e4m3fn else (None, None, None)
-    if cp is None and rows:
+    if codes.dtype != _E4M3:
         raise TypeError("codes must be float8_e4m3fn")
-    call(lib().db_checkpoint_pack, xp, pitch, rows, cols, cp, sp, stream=stream)
+    xp, pitch = _rows(x, rows, cols, index, "x")
+    cp, sp, _ = _kept(codes, scale, rows, cols, index, "codes")
+    _launch(index, stream, lib().db_checkpoint_pack, xp, pitch, rows, cols, cp, sp)
 
 
 def checkpoint_unpack(codes: torch.Tensor, scale: torch.Tensor, x: torch.Tensor,
                       stream: Optional[torch.cuda.Stream] = None) -> None:
     """db_checkpoint_unpack: the values that codes and scale stand for, rounded to bfloat16, into x."""
-    call = _Call(codes)
+    index = _device_index(codes)
     rows, cols = codes.shape
-    if codes.dtype != torch.float8_e4m3fn:
+    if codes.dtype != _E4M3:
         raise TypeError("codes must be float8_e4m3fn")
-    xp, pitch = call.rows(x, rows, cols, "x")
-    cp, sp, _ = call.kept(codes, scale, rows, cols, "codes")
-    call(lib().db_checkpoint_unpack, cp, sp, rows, cols, xp, pitch, stream=stream)
+    xp, pitch = _rows(x, rows, cols, index, "x")
+    cp, sp, _ = _kept(codes, scale, rows, cols, index, "codes")
+    _launch(index, stream, lib().db_checkpoint_unpack, cp, sp, rows, cols, xp, pitch)
 
 
 def embedding(tokens: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
               stream: Optional[torch.cuda.Stream] = None) -> None:
     """db_embedding: out[t] = scale * table[tokens[t]]; tokens int32 (outside the table: zeros), table and out float32 or
     bfloat16, out's rows contiguous."""
-    call = _Call(tokens)
+    index = _device_index(tokens)
     vocab, width = table.shape
     rows = tokens.numel()
-    op, pitch = call.rows(out, rows, width, "out", out.dtype)
-    call(lib().db_embedding, call.whole(tokens, tokens.shape, torch.int32, "tokens"),
-         call.whole(table, (vocab, width), table.dtype, "table"), _dtype_code(table.dtype), float(scale), rows, vocab, width,
-         op, pitch, _dtype_code(out.dtype), stream=stream)
+    op, pitch = _rows(out, rows, width, index, "out", out.dtype)
+    _launch(index, stream, lib().db_embedding, _whole(tokens, tokens.shape, torch.int32, index, "tokens"),
+            _whole(table, (vocab, width), table.dtype, index, "table"), _dtype_code(table.dtype), float(scale), rows, vocab,
+            width, op, pitch, _dtype_code(out.dtype))
 
 
 def embedding_grad_workspace_bytes(rows: int, vocab: int, width: int) -> int:
@@ -991,10 +1007,11 @@ def embedding_grad(tokens: torch.Tensor, dy: torch.Tensor, dtable: torch.Tensor,
                    scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> None:
     """db_embedding_grad: dtable[v] = scale * sum of dy[t] with tokens[t] == v, every row written.  dy and dtable float32 or
     bfloat16; workspace: embedding_grad_workspace_bytes(rows, vocab, width) bytes."""
-    call = _Call(tokens)
+    index = _device_index(tokens)
     vocab, width = dtable.shape
     rows = tokens.numel()
-    dp, pitch = call.rows(dy, rows, width, "dy", dy.dtype)
-    call(lib().db_embedding_grad, call.whole(tokens, tokens.shape, torch.int32, "tokens"), dp, pitch, _dtype_code(dy.dtype),
-         float(scale), rows, vocab, width, call.whole(dtable, (vocab, width), dtable.dtype, "dtable"),
-         _dtype_code(dtable.dtype), *call.workspace(workspace), stream=stream)
+    dp, pitch = _rows(dy, rows, width, index, "dy", dy.dtype)
+    _launch(index, stream, lib().db_embedding_grad, _whole(tokens, tokens.shape, torch.int32, index, "tokens"), dp, pitch,
+            _dtype_code(dy.dtype), float(scale), rows, vocab, width,
+            _whole(dtable, (vocab, width), dtable.dtype, index, "dtable"), _dtype_code(dtable.dtype),
+            *_scratch(workspace, index))

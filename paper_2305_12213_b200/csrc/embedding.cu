@@ -24,7 +24,7 @@ constexpr int kPart = kBlock * kSteps;           // entries a CTA sorts at a tim
 constexpr int kMaxSortBlocks = 512;              // every CTA reads all CTAs' counts, so their number is bounded
 constexpr int kClusterWarps = 32, kMaxSteps = 8, kMaxCluster = 8;   // sorting in one launch: up to 65536 rows
 constexpr long long kClusterRows = 32LL * kClusterWarps * kMaxSteps * kMaxCluster;
-constexpr int kAloneRows = 256;                  // up to here no run is cut
+constexpr int kFewRows = 256;                    // up to here nothing is sorted
 constexpr long long kMaxRows = 1LL << 28, kMaxVocab = 1LL << 26, kMaxWidth = 1LL << 20;
 
 long long cdiv(long long a, long long b) { return (a + b - 1) / b; }
@@ -168,16 +168,18 @@ __device__ __forceinline__ void rank_entries(const int (&key)[STEPS], int shift,
         if (s * 32 >= entries_left) break;                     // the same for the whole warp
         const bool in = s * 32 + lane < entries_left;
         const unsigned live = __ballot_sync(0xFFFFFFFFu, in);
-        rank[s] = 0;
-        if (in) {
-            const int d = digit_of(key[s], shift);
-            const unsigned same = __match_any_sync(live, d);
-            const int below = __popc(same & ((1u << lane) - 1));
-            const int before = mine[d];
-            __syncwarp(live);
-            if (below == 0) mine[d] = static_cast<unsigned short>(before + __popc(same));
-            rank[s] = before + below;
+        const int d = digit_of(key[s], shift);
+        unsigned same = live;                                  // lanes with this digit, a vote for each bit (the match
+#pragma unroll                                                 // instruction takes four times as long)
+        for (int b = 0; b < kDigitBits; ++b) {
+            const unsigned set = __ballot_sync(0xFFFFFFFFu, (d >> b) & 1);
+            same &= (d >> b) & 1 ? set : ~set;
         }
+        const int below = __popc(same & ((1u << lane) - 1));
+        const int before = mine[d];
+        rank[s] = before + below;
+        __syncwarp();
+        if (in && below == 0) mine[d] = static_cast<unsigned short>(before + __popc(same));
         __syncwarp();
     }
 }
@@ -304,11 +306,13 @@ __global__ void __launch_bounds__(kClusterThreads) cluster_sort_kernel(const __g
         if (ctas > 1) cluster_sync(); else __syncthreads();
         int before = 0;
         if (tid < kBins) {
-            int all = 0;
-            for (int c = 0; c < ctas; ++c) {
-                const int x = ctas > 1 ? load_cluster(&counts[tid], c) : counts[tid];
-                all += x;
-                if (c < rank) before += x;
+            int all = 0, x[kMaxCluster];
+#pragma unroll
+            for (int c = 0; c < kMaxCluster; ++c) x[c] = c >= ctas ? 0 : ctas > 1 ? load_cluster(&counts[tid], c) : counts[tid];
+#pragma unroll
+            for (int c = 0; c < kMaxCluster; ++c) {
+                all += x[c];
+                if (c < rank) before += x[c];
             }
             base[tid] = all;
         }
@@ -357,7 +361,6 @@ struct SumArgs {
     int* joins; int* join_list;   // units in which a cut run begins
     int rows, vocab, width;
     int unit, units;              // sorted entries per unit
-    int whole;                    // no run is cut: a unit finishes whatever begins in it
     int threads_shift;            // log2 of the threads that take a row, 8 columns each
     int zero_turns;               // CTAs that write zero rows for each one that adds
     float scale;
@@ -397,11 +400,11 @@ __global__ void __launch_bounds__(kBlock, sizeof(DT) == 2 ? 4 : 3) embedding_sum
     const int beyond = end < a.rows ? a.keys[end] : -1;
     // the run at the beginning: its own, another unit's (skipped), or cut
     const bool from_before = begin > 0 && a.keys[begin - 1] == head;
-    const bool head_cut = from_before && !a.whole && ((begin > a.unit && a.keys[begin - a.unit - 1] == head) || beyond == head);
+    const bool head_cut = from_before && ((begin > a.unit && a.keys[begin - a.unit - 1] == head) || beyond == head);
     const int skip = from_before && !head_cut ? head : -1;
     // the run at the end, if it begins here and goes on
     const bool goes_on = beyond == last && !(from_before && last == head);
-    const bool tail_cut = goes_on && !a.whole && end + a.unit < a.rows && a.keys[end + a.unit] == last;
+    const bool tail_cut = goes_on && end + a.unit < a.rows && a.keys[end + a.unit] == last;
     const int stop = goes_on && !tail_cut ? a.rows : end;
     int current = head;
     float sum[8];
@@ -461,6 +464,59 @@ __global__ void __launch_bounds__(kBlock, sizeof(DT) == 2 ? 4 : 3) embedding_sum
         if (over) break;
     }
     flush(tail_cut);
+}
+
+// Few rows: no sort.  A warp holds all tokens, eight a lane, and asks for each of its rows of the table which of them are
+// that row's token (at most eight votes); 256 columns a warp.  One launch, bound by its latency and the table's rows.
+struct FewArgs {
+    const int* tokens;
+    const void* dy; long long dy_pitch;
+    void* out;
+    int rows, vocab, width;
+    float scale;
+};
+template <class DT, class OT>
+__global__ void __launch_bounds__(kBlock) embedding_few_kernel(const __grid_constant__ FewArgs a) {
+    constexpr int kHeld = kFewRows / 32, kDeep = 4;
+    tc::griddep_wait();
+    tc::griddep_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int col = (blockIdx.y * 32 + lane) * 8, n = max(0, min(8, a.width - col));
+    int token[kHeld];
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) token[j] = j * 32 + lane < a.rows ? a.tokens[j * 32 + lane] : -1;
+    const int stride = gridDim.x * (kBlock / 32);
+    for (int v = blockIdx.x * (kBlock / 32) + warp; v < a.vocab; v += stride) {
+        float sum[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) {
+            unsigned found = __ballot_sync(0xFFFFFFFFu, token[h] == v);
+            while (found) {                                     // the same for the whole warp; ascending rows
+                Raw8<DT> x[kDeep];
+                bool in[kDeep];
+#pragma unroll
+                for (int d = 0; d < kDeep; ++d) {
+                    in[d] = found != 0;
+                    const int row = in[d] ? h * 32 + __ffs(found) - 1 : 0;
+                    found &= found - 1;
+                    x[d].load(static_cast<const DT*>(a.dy) + row * a.dy_pitch + col, in[d] ? n : 0);
+                }
+#pragma unroll
+                for (int d = 0; d < kDeep; ++d) {
+                    if (!in[d]) break;
+                    float y[8];
+                    x[d].values(y);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum[j] += y[j];
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] *= a.scale;
+        if (n > 0) store8(static_cast<OT*>(a.out) + static_cast<long long>(v) * a.width + col, n, sum);
+    }
 }
 
 // Cut runs: the beginning's sum, then the units' in a fixed order (eight warps, each every eighth unit).
@@ -595,7 +651,7 @@ template <class DT, class OT>
 db_status launch_sum(const SumArgs& a, dim3 grid, cudaStream_t stream) {
     Launch S(grid, kBlock, 0, stream);
     DB_CUDA_TRY(cudaLaunchKernelEx(&S.cfg, embedding_sum_kernel<DT, OT>, a));
-    if (!a.whole) {
+    if (a.units > 2) {                                          // a cut run is longer than a unit
         Launch J(dim3(static_cast<unsigned>(std::min<long long>(4LL * sm_count(), static_cast<long long>(a.units) * cdiv(a.width, 256)))), kBlock, 0, stream);
         DB_CUDA_TRY(cudaLaunchKernelEx(&J.cfg, embedding_join_kernel<OT>, a));
     }
@@ -658,6 +714,15 @@ extern "C" db_status db_embedding_grad(const int32_t* tokens, const void* dy, in
         DB_CUDA_TRY(cudaMemsetAsync(dtable, 0, static_cast<size_t>(ng), stream));
         return DB_OK;
     }
+    if (rows <= kFewRows) {
+        const FewArgs f{tokens, dy, dy_pitch, dtable, static_cast<int>(rows), vocab, width, scale};
+        Launch F(dim3(static_cast<unsigned>(std::min<long long>(cdiv(vocab, kBlock / 32), 8LL * sm_count())), static_cast<unsigned>(cdiv(width, 256))),
+                 kBlock, 0, stream);
+        void (*fn)(const FewArgs) = dy_dtype == DB_F32 ? (grad_dtype == DB_F32 ? embedding_few_kernel<float, float> : embedding_few_kernel<float, bf16>)
+                                                       : (grad_dtype == DB_F32 ? embedding_few_kernel<bf16, float> : embedding_few_kernel<bf16, bf16>);
+        DB_CUDA_TRY(cudaLaunchKernelEx(&F.cfg, fn, f));
+        return DB_OK;
+    }
     char* base = static_cast<char*>(workspace);
     const auto ints = [&](size_t at) { return reinterpret_cast<int*>(base + at); };
     // digits of 9 bits until the largest key, vocab (a token outside the table), is covered
@@ -707,7 +772,6 @@ extern "C" db_status db_embedding_grad(const int32_t* tokens, const void* dy, in
     a.joins = ints(L.joins); a.join_list = ints(L.join_list);
     a.rows = static_cast<int>(rows); a.vocab = vocab; a.width = width;
     a.unit = L.unit; a.units = L.units; a.scale = scale;
-    a.whole = rows <= kAloneRows;
     a.threads_shift = shift_of(width);
     const int groups = kBlock >> a.threads_shift;
     const long long sum_ctas = cdiv(L.units, groups), zero_ctas = cdiv(vocab, static_cast<long long>(kZeroRows) * groups);

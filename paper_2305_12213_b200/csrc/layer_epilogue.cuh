@@ -344,115 +344,164 @@ __device__ __forceinline__ float reciprocal_fast(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ Pair exp2_pair(Pair x) {
-    float a, b;
-    halves(x, a, b);
-    return pair(exp2_fast(a), exp2_fast(b));
-}
-__device__ __forceinline__ Pair reciprocal_pair(Pair x) {
-    float a, b;
-    halves(x, a, b);
-    return pair(reciprocal_fast(a), reciprocal_fast(b));
-}
 constexpr float kLog2e = 1.44269504f;
-__device__ __forceinline__ Pair sigmoid(Pair z) { return reciprocal_pair(add(exp2_pair(mul(z, both(-kLog2e))), both(1.f))); }
-__device__ __forceinline__ Pair magnitude(Pair z) { return z & 0x7FFFFFFF7FFFFFFFull; }
+constexpr Pair kSigns = 0x8000000080000000ull;
+// Four pairs at a time, step by step: an epilogue warp has its scheduler almost to itself, and a chain of twenty dependent
+// instructions, one pair after the other, left it idle for most of their latencies.
+constexpr int kBatch = 4;
+using Batch = Pair[kBatch];
+#define DB_EACH _Pragma("unroll") for (int i = 0; i < kBatch; ++i)
+__device__ __forceinline__ void exp2_batch(Batch& x) {
+    DB_EACH {
+        float a, b;
+        halves(x[i], a, b);
+        x[i] = pair(exp2_fast(a), exp2_fast(b));
+    }
+}
+__device__ __forceinline__ void reciprocal_batch(Batch& x) {
+    DB_EACH {
+        float a, b;
+        halves(x[i], a, b);
+        x[i] = pair(reciprocal_fast(a), reciprocal_fast(b));
+    }
+}
+__device__ __forceinline__ void sigmoid(const Batch& z, Batch& s) {
+    DB_EACH s[i] = mul(z[i], both(-kLog2e));
+    exp2_batch(s);
+    DB_EACH s[i] = add(s[i], both(1.f));
+    reciprocal_batch(s);
+}
+__device__ __forceinline__ Pair magnitude(Pair z) { return z & ~kSigns; }
 __device__ __forceinline__ Pair positive_part(Pair z) {       // a NaN stays one
     float a, b;
     halves(z, a, b);
     return pair(a < 0.f ? 0.f : a, b < 0.f ? 0.f : b);
 }
-// bell = e^(-z^2 / 2); returns erfc(|z| / sqrt(2)) / 2
-__device__ __forceinline__ Pair normal_tail(Pair z, Pair& bell) {
-    const Pair t = reciprocal_pair(mul_add(magnitude(z), both(0.23164190f), both(1.f)));   // 0.3275911 / sqrt(2)
-    bell = exp2_pair(mul(mul(z, both(-0.5f * kLog2e)), z));
-    Pair poly = mul_add(both(0.5f * 1.061405429f), t, both(-0.5f * 1.453152027f));
-    poly = mul_add(poly, t, both(0.5f * 1.421413741f));
-    poly = mul_add(poly, t, both(-0.5f * 0.284496736f));
-    poly = mul_add(poly, t, both(0.5f * 0.254829592f));
-    return mul(mul(poly, t), bell);
+// bell = e^(-z^2 / 2), tail = erfc(|z| / sqrt(2)) / 2
+__device__ __forceinline__ void normal_tail(const Batch& z, Batch& bell, Batch& tail) {
+    Batch t;
+    DB_EACH t[i] = mul_add(magnitude(z[i]), both(0.23164190f), both(1.f));   // 0.3275911 / sqrt(2)
+    DB_EACH bell[i] = mul(mul(z[i], both(-0.5f * kLog2e)), z[i]);
+    reciprocal_batch(t);
+    exp2_batch(bell);
+    DB_EACH tail[i] = mul_add(both(0.5f * 1.061405429f), t[i], both(-0.5f * 1.453152027f));
+    DB_EACH tail[i] = mul_add(tail[i], t[i], both(0.5f * 1.421413741f));
+    DB_EACH tail[i] = mul_add(tail[i], t[i], both(-0.5f * 0.284496736f));
+    DB_EACH tail[i] = mul_add(tail[i], t[i], both(0.5f * 0.254829592f));
+    DB_EACH t[i] = mul(t[i], bell[i]);
+    DB_EACH tail[i] = mul(tail[i], t[i]);
 }
 template <int ACT>
-__device__ __forceinline__ Pair act_pair(Pair z) {
-    if (ACT == DB_ACT_SILU) return mul(z, sigmoid(z));
-    if (ACT == DB_ACT_GELU) {
-        Pair bell;
-        const Pair tail = normal_tail(z, bell);
-        return mul_add(magnitude(z) ^ 0x8000000080000000ull, tail, positive_part(z));
-    }
-    if (ACT == DB_ACT_RELU) return positive_part(z);
-    return z;
-}
-template <int ACT>
-__device__ __forceinline__ void act_pair_slope(Pair z, Pair& value, Pair& slope) {
+__device__ __forceinline__ void act_batch(Batch& z) {
     if (ACT == DB_ACT_SILU) {
-        const Pair s = sigmoid(z);
-        value = mul(z, s);
-        slope = mul_add(value, mul_add(s, both(-1.f), both(1.f)), s);
+        Batch s;
+        sigmoid(z, s);
+        DB_EACH z[i] = mul(z[i], s[i]);
     } else if (ACT == DB_ACT_GELU) {
-        Pair bell;
-        const Pair tail = normal_tail(z, bell);
-        value = mul_add(magnitude(z) ^ 0x8000000080000000ull, tail, positive_part(z));
-        // P(z) - 1/2 has z's sign and the magnitude 1/2 - tail
-        const Pair centred = mul_add(tail, both(-1.f), both(0.5f)) ^ (z & 0x8000000080000000ull);
-        slope = mul_add(mul(z, both(0.39894228f)), bell, add(centred, both(0.5f)));
+        Batch bell, tail;
+        normal_tail(z, bell, tail);
+        DB_EACH z[i] = mul_add(magnitude(z[i]) ^ kSigns, tail[i], positive_part(z[i]));
     } else if (ACT == DB_ACT_RELU) {
-        value = positive_part(z);
-        float a, b;
-        halves(z, a, b);
-        slope = pair(a <= 0.f ? 0.f : 1.f, b <= 0.f ? 0.f : 1.f);
+        DB_EACH z[i] = positive_part(z[i]);
+    }
+}
+template <int ACT>
+__device__ __forceinline__ void act_batch_slope(const Batch& z, Batch& value, Batch& slope) {
+    if (ACT == DB_ACT_SILU) {
+        Batch s;
+        sigmoid(z, s);
+        DB_EACH value[i] = mul(z[i], s[i]);
+        DB_EACH slope[i] = mul_add(s[i], both(-1.f), both(1.f));
+        DB_EACH slope[i] = mul_add(value[i], slope[i], s[i]);
+    } else if (ACT == DB_ACT_GELU) {
+        Batch bell, tail;
+        normal_tail(z, bell, tail);
+        DB_EACH value[i] = mul_add(magnitude(z[i]) ^ kSigns, tail[i], positive_part(z[i]));
+        // P(z) - 1/2 has z's sign and the magnitude 1/2 - tail
+        DB_EACH slope[i] = mul_add(tail[i], both(-1.f), both(0.5f)) ^ (z[i] & kSigns);
+        DB_EACH slope[i] = add(slope[i], both(0.5f));
+        DB_EACH tail[i] = mul(z[i], both(0.39894228f));
+        DB_EACH slope[i] = mul_add(tail[i], bell[i], slope[i]);
+    } else if (ACT == DB_ACT_RELU) {
+        DB_EACH {
+            value[i] = positive_part(z[i]);
+            float a, b;
+            halves(z[i], a, b);
+            slope[i] = pair(a <= 0.f ? 0.f : 1.f, b <= 0.f ? 0.f : 1.f);
+        }
     } else {
-        value = z;
-        slope = both(1.f);
+        DB_EACH {
+            value[i] = z[i];
+            slope[i] = both(1.f);
+        }
     }
 }
 // The branch on the activation is taken once for a row, not for each value.
 template <int ACT>
 __device__ __forceinline__ void act_row(Pair (&v)[16]) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = act_pair<ACT>(v[i]);
+    for (int j = 0; j < 16; j += kBatch) {
+        Batch b;
+        DB_EACH b[i] = v[j + i];
+        act_batch<ACT>(b);
+        DB_EACH v[j + i] = b[i];
+    }
 }
 __device__ __forceinline__ void act_row(Pair (&v)[16], int act) {
     if (act == DB_ACT_SILU) act_row<DB_ACT_SILU>(v);
     else if (act == DB_ACT_GELU) act_row<DB_ACT_GELU>(v);
     else if (act == DB_ACT_RELU) act_row<DB_ACT_RELU>(v);
 }
-// Two values at a time, packed as they are done: 48 words of results instead of 96 floats.
+// Sixteen columns at a time, stored as they are done, so that few results wait in registers.
 template <int ACT, bool E4M3>
-__device__ __forceinline__ void gated_grad_row(const Pair (&dh)[16], const RawRow& gate, const RawRow& up, uint32_t (&d_gate)[16],
-                                               uint32_t (&d_up)[16], uint32_t (&h)[16]) {
+__device__ __forceinline__ void gated_grad_row(const Pair (&dh)[16], const RawRow& gate, const RawRow& up, __nv_bfloat16* d_gate,
+                                               __nv_bfloat16* d_up, __nv_bfloat16* h, int n) {
     const Pair gate_scale = both(E4M3 ? ck8::scale_value(gate.scale) : 1.f), up_scale = both(E4M3 ? ck8::scale_value(up.scale) : 1.f);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        Pair z, u, a, s;
-        if (E4M3) {
-            const float2 x = ck8::values2(gate.q[i / 2] >> (16 * (i % 2))), y = ck8::values2(up.q[i / 2] >> (16 * (i % 2)));
-            z = mul(pair(x.x, x.y), gate_scale);
-            u = mul(pair(y.x, y.y), up_scale);
-        } else {
-            z = unpack_pair(gate.q[i]);
-            u = unpack_pair(up.q[i]);
+    for (int half = 0; half < 2; ++half) {
+        uint32_t qg[8], qu[8], qh[8];
+#pragma unroll
+        for (int j = 0; j < 8; j += kBatch) {
+            Batch z, u, a, s;
+            DB_EACH {
+                const int w = 8 * half + j + i;
+                if (E4M3) {
+                    const float2 x = ck8::values2(gate.q[w / 2] >> (16 * (w % 2))), y = ck8::values2(up.q[w / 2] >> (16 * (w % 2)));
+                    z[i] = mul(pair(x.x, x.y), gate_scale);
+                    u[i] = mul(pair(y.x, y.y), up_scale);
+                } else {
+                    z[i] = unpack_pair(gate.q[w]);
+                    u[i] = unpack_pair(up.q[w]);
+                }
+            }
+            act_batch_slope<ACT>(z, a, s);
+            DB_EACH qh[j + i] = pack_pair(mul(a[i], u[i]));
+            DB_EACH qu[j + i] = pack_pair(mul(dh[8 * half + j + i], a[i]));
+            DB_EACH s[i] = mul(s[i], u[i]);
+            DB_EACH qg[j + i] = pack_pair(mul(dh[8 * half + j + i], s[i]));
         }
-        act_pair_slope<ACT>(z, a, s);
-        h[i] = pack_pair(mul(a, u));
-        d_gate[i] = pack_pair(mul(mul(dh[i], u), s));
-        d_up[i] = pack_pair(mul(dh[i], a));
+        const int valid = min(16, n - 16 * half);
+        if (valid > 0) {
+            store_bytes<32>(reinterpret_cast<unsigned short*>(d_gate) + 16 * half, valid, qg);
+            store_bytes<32>(reinterpret_cast<unsigned short*>(d_up) + 16 * half, valid, qu);
+            store_bytes<32>(reinterpret_cast<unsigned short*>(h) + 16 * half, valid, qh);
+        }
     }
 }
 template <bool E4M3>
-__device__ __forceinline__ void gated_grad_row(int act, const Pair (&dh)[16], const RawRow& gate, const RawRow& up, uint32_t (&d_gate)[16],
-                                               uint32_t (&d_up)[16], uint32_t (&h)[16]) {
-    if (act == DB_ACT_SILU) gated_grad_row<DB_ACT_SILU, E4M3>(dh, gate, up, d_gate, d_up, h);
-    else if (act == DB_ACT_GELU) gated_grad_row<DB_ACT_GELU, E4M3>(dh, gate, up, d_gate, d_up, h);
-    else if (act == DB_ACT_RELU) gated_grad_row<DB_ACT_RELU, E4M3>(dh, gate, up, d_gate, d_up, h);
-    else gated_grad_row<DB_ACT_NONE, E4M3>(dh, gate, up, d_gate, d_up, h);
+__device__ __forceinline__ void gated_grad_row(int act, const Pair (&dh)[16], const RawRow& gate, const RawRow& up, __nv_bfloat16* d_gate,
+                                               __nv_bfloat16* d_up, __nv_bfloat16* h, int n) {
+    if (act == DB_ACT_SILU) gated_grad_row<DB_ACT_SILU, E4M3>(dh, gate, up, d_gate, d_up, h, n);
+    else if (act == DB_ACT_GELU) gated_grad_row<DB_ACT_GELU, E4M3>(dh, gate, up, d_gate, d_up, h, n);
+    else if (act == DB_ACT_RELU) gated_grad_row<DB_ACT_RELU, E4M3>(dh, gate, up, d_gate, d_up, h, n);
+    else gated_grad_row<DB_ACT_NONE, E4M3>(dh, gate, up, d_gate, d_up, h, n);
 }
 
 // ------------------------------------------------------------------------------------------------ the epilogue of a row
-// What the epilogue of 32 columns reads: fetched ahead, while the accumulator of the columns before is worked on.
+// What the epilogue of 32 columns reads.
 template <int EPI>
 struct Fetched {
-    uint32_t addend[16];
+    uint32_t bias[16], addend[16];
 };
 template <>
 struct Fetched<kEpiGated> {};
@@ -464,6 +513,7 @@ template <int EPI>
 __device__ __forceinline__ void epilogue_fetch(const EpilogueArgs& e, long long row, int col, int N, Fetched<EPI>& f) {
     const int n = min(kChunk, N - col);
     if constexpr (EPI == kEpiStore) {
+        if (e.bias) load_raw(e.bias + col, n, f.bias);
         if (e.addend) load_raw(e.addend + row * e.addend_pitch + col, n, f.addend);
     } else if constexpr (EPI == kEpiGatedGrad) {
         fetch_row(e.kept[0], e.kept_e4m3, row, col, N, n, f.gate);
@@ -477,10 +527,8 @@ __device__ __forceinline__ void epilogue_row(const EpilogueArgs& e, long long ro
     const int n = min(kChunk, N - col);
     if constexpr (EPI == kEpiStore) {
         if (e.bias) {
-            uint32_t q[16];
-            load_raw(e.bias + col, n, q);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = add(v[i], unpack_pair(q[i]));
+            for (int i = 0; i < 16; ++i) v[i] = add(v[i], unpack_pair(f.bias[i]));
         }
         if (e.kept[0].data) keep_row(e.kept[0], e.kept_e4m3, row, col, N, n, v);
         act_row(v, e.act);
@@ -500,14 +548,15 @@ __device__ __forceinline__ void epilogue_row(const EpilogueArgs& e, long long ro
         for (int i = 0; i < 16; ++i) v[i] = mul(v[i], u[i]);
         store_row(static_cast<__nv_bfloat16*>(e.out) + row * e.out_pitch + col, n, v);
     } else {
-        uint32_t d_gate[16], d_up[16], h[16];
-        if (e.kept_e4m3) gated_grad_row<true>(e.act, v, f.gate, f.up, d_gate, d_up, h);
-        else gated_grad_row<false>(e.act, v, f.gate, f.up, d_gate, d_up, h);
-        store_bytes<64>(reinterpret_cast<unsigned short*>(e.d_gate + row * e.d_pitch + col), n, d_gate);
-        store_bytes<64>(reinterpret_cast<unsigned short*>(e.d_up + row * e.d_pitch + col), n, d_up);
-        store_bytes<64>(static_cast<unsigned short*>(e.out) + row * e.out_pitch + col, n, h);
+        __nv_bfloat16* d_gate = e.d_gate + row * e.d_pitch + col;
+        __nv_bfloat16* d_up = e.d_up + row * e.d_pitch + col;
+        __nv_bfloat16* h = static_cast<__nv_bfloat16*>(e.out) + row * e.out_pitch + col;
+        if (e.kept_e4m3) gated_grad_row<true>(e.act, v, f.gate, f.up, d_gate, d_up, h, n);
+        else gated_grad_row<false>(e.act, v, f.gate, f.up, d_gate, d_up, h, n);
     }
 }
+
+#undef DB_EACH
 
 }  // namespace lg
 }  // namespace dynbatch

@@ -338,28 +338,30 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
         __syncwarp();
     } else {
         const int quarter = warp & 3, part = (warp - 2) >> 2;
+        constexpr int kPerWarp = kTileN * 4 / S::kEpilogueWarps;
         int n = 0;
         for (int t = worker; t < total; t += workers, ++n) {
             const Tile tile = decode(g, t);
             const Problem& p = g.p[tile.problem];
             const int buf = n & 1, N = p.N;
-            constexpr int kPerWarp = kTileN * 4 / S::kEpilogueWarps;
             const long long row = static_cast<long long>(tile.m) * S::kTileM + rank * kRows + quarter * 32 + lane;
             const int first = tile.n * kTileN + part * kPerWarp, columns = min(kPerWarp, N - first);   // may be none
             const bool in = row < p.M && g.splits == 1;       // the epilogue is applied here, or to the joined sum
-            Fetched<EPI> now, next;
-            if (in && columns > 0) epilogue_fetch<EPI>(p.e, row, first, N, now);
-            // one lane asks: 256 threads asking at once slow the two that feed the tensor cores (0.32 us a block, not 0.2)
+            Fetched<EPI> fetched;                              // of the first columns: while the products still run
+            if (in && columns > 0) epilogue_fetch<EPI>(p.e, row, first, N, fetched);
+            // one lane asks: 256 threads asking at once slow the two that feed the tensor cores
             bool ready = false;
             if (lane == 0) ready = tc::mbar_wait(&ready_bar[buf], (n >> 1) & 1, &abort_flag, g.status, 0x305);
             if (!__shfl_sync(0xFFFFFFFFu, ready, 0)) break;
             tc::tc_fence_after();
             const uint32_t acc = tmem + buf * BN + (static_cast<uint32_t>(quarter * 32) << 16) + part * kPerWarp;
+            // Fetching the next columns' rows into a second set of registers gained nothing (the arithmetic then has fewer),
+            // nor did asking the L2 for them a tile ahead (161 against 193 us for the block's first backward product).
 #pragma unroll 1
             for (int c = 0; c < columns; c += kChunk) {
                 __syncwarp();                                  // rows past the end rejoin for the next read
                 const int col = first + c;
-                if (in && c + kChunk < columns) epilogue_fetch<EPI>(p.e, row, col + kChunk, N, next);
+                if (in && c > 0) epilogue_fetch<EPI>(p.e, row, col, N, fetched);
                 uint32_t raw[kChunk];
                 Pair v[kChunk / 2], u[kChunk / 2];
                 tc::tmem_load32(acc + c, raw);
@@ -371,14 +373,13 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
                     for (int i = 0; i < kChunk / 2; ++i) u[i] = pair(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1]));
                 }
                 if (in) {
-                    epilogue_row<EPI>(p.e, row, col, N, now, v, u);
+                    epilogue_row<EPI>(p.e, row, col, N, fetched, v, u);
                 } else if (row < p.M) {
                     const long long pitch = partial_pitch(N), plane = p.M * pitch;
                     float* to = g.partials + p.partial + tile.split * plane * (EPI == kEpiGated ? 2 : 1) + row * pitch + col;
                     store_row(to, kChunk, v);
                     if (EPI == kEpiGated) store_row(to + plane, kChunk, u);
                 }
-                now = next;
             }
             tc::tc_fence_before();
             __syncwarp();

@@ -101,12 +101,10 @@ act_grad_kernel(const __grid_constant__ ActGradArgs a) {
                     Pair z[4];
                     if (E4M3) z8[i].values(byte[i], z);
                     else z16[i].values(z);
+                    lg::Batch value, slope;
+                    lg::act_batch_slope<ACT>(z, value, slope);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        Pair value, slope;
-                        lg::act_pair_slope<ACT>(z[j], value, slope);
-                        d[j] = lg::mul(d[j], slope);
-                    }
+                    for (int j = 0; j < 4; ++j) d[j] = lg::mul(d[j], slope[j]);
                 }
                 if (a.dz) {
                     bf16* q = a.dz + r * a.dz_pitch + col;     // workspace rows: aligned, pitch a multiple of 32
@@ -150,16 +148,23 @@ ActGradFn act_grad_fn(int act, bool e4m3) {
     }
 }
 
-// Column sums: the slabs' sums added in slab order.
-__global__ void __launch_bounds__(128)
+// Column sums: each warp adds every eighth slab's sums of 32 columns, then the warps' are added in order.
+__global__ void __launch_bounds__(256)
 bias_fold_kernel(const float* sums, long long pitch, int slabs, int cols, void* out, int out_f32) {
+    __shared__ float part[8][32];
     tc::griddep_wait();
     tc::griddep_launch_dependents();
-    const int c = blockIdx.x * blockDim.x + threadIdx.x;
-    if (c >= cols) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 32 + lane;
     float s = 0.f;
-#pragma unroll 8
-    for (int i = 0; i < slabs; ++i) s += sums[i * pitch + c];
+    if (c < cols) {
+#pragma unroll 10
+        for (int i = warp; i < slabs; i += 8) s += sums[i * pitch + c];
+    }
+    part[warp][lane] = s;
+    __syncthreads();
+    if (warp != 0 || c >= cols) return;
+#pragma unroll
+    for (int w = 1; w < 8; ++w) s += part[w][lane];
     if (out_f32) static_cast<float*>(out)[c] = s;
     else static_cast<bf16*>(out)[c] = __float2bfloat16_rn(s);
 }
@@ -549,7 +554,7 @@ db_status linear_backward(const LinearGradArgs& v, Arena& arena, cudaStream_t st
             Launch L(dim3(static_cast<unsigned>(cdiv(v.n_out, 256)), used), dim3(256), 0, stream);
             DB_CUDA_TRY(cudaLaunchKernelEx(&L.cfg, act_grad_fn(a.act, a.z_e4m3), a));
             if (want_bias) {
-                Launch F(dim3(static_cast<unsigned>(cdiv(v.n_out, 128))), dim3(128), 0, stream);
+                Launch F(dim3(static_cast<unsigned>(cdiv(v.n_out, 32))), dim3(256), 0, stream);
                 DB_CUDA_TRY(cudaLaunchKernelEx(&F.cfg, bias_fold_kernel, static_cast<const float*>(a.sums), a.sums_pitch, used, v.n_out,
                                                v.dbias, v.grad_dtype == DB_F32 ? 1 : 0));
             }
