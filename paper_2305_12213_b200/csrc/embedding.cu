@@ -99,8 +99,8 @@ __global__ void __launch_bounds__(kBlock) embedding_kernel(const __grid_constant
 // ---------------------------------------------------------------------------------------------- sorting positions by token
 struct SortArgs {
     const int* tokens;            // first pass; tokens outside the table sort behind it, as key `vocab`
-    const int* keys_in; const int* pos_in;
-    int* keys_out; int* pos_out;
+    const int2* in;               // entries (key, position)
+    int2* out;
     int* counts;                  // [CTA][bin]
     uint8_t* present;             // [vocab] 1 where a token occurs: zeroed by the first pass, set by the last
     int* joins;                   // number of runs to join, zeroed by the first pass
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kBlock) sort_count_kernel(const __grid_constan
     __syncthreads();
     const int begin = blockIdx.x * a.per_block, end = min(a.rows, begin + a.per_block);
     for (int i = begin + threadIdx.x; i < end; i += kBlock)
-        atomicAdd(&bins[digit_of(a.first ? key_of(a.tokens, a.vocab, i) : a.keys_in[i], a.shift)], 1);
+        atomicAdd(&bins[digit_of(a.first ? key_of(a.tokens, a.vocab, i) : a.in[i].x, a.shift)], 1);
     __syncthreads();
     for (int b = threadIdx.x; b < kBins; b += kBlock) a.counts[blockIdx.x * kBins + b] = bins[b];
 }
@@ -214,8 +214,10 @@ __global__ void __launch_bounds__(kBlock) sort_scatter_kernel(const __grid_const
         for (int s = 0; s < kSteps; ++s) {
             const int i = first + s * 32 + lane;
             const bool in = s * 32 + lane < left;
-            key[s] = in ? (a.first ? key_of(a.tokens, a.vocab, i) : a.keys_in[i]) : 0;
-            pos[s] = in ? (a.first ? i : a.pos_in[i]) : 0;
+            int2 x = make_int2(0, 0);
+            if (in) x = a.first ? make_int2(key_of(a.tokens, a.vocab, i), i) : a.in[i];
+            key[s] = x.x;
+            pos[s] = x.y;
         }
         rank_entries<kSortWarps, kSteps>(key, a.shift, left, counters, rank);
         __syncthreads();
@@ -235,8 +237,7 @@ __global__ void __launch_bounds__(kBlock) sort_scatter_kernel(const __grid_const
             if (s * 32 + lane < left) {
                 const int d = digit_of(key[s], a.shift);
                 const int to = base[d] + counters[warp * kBins + d] + rank[s];
-                a.keys_out[to] = key[s];
-                a.pos_out[to] = pos[s];
+                a.out[to] = make_int2(key[s], pos[s]);
                 if (a.last && key[s] < a.vocab) a.present[key[s]] = 1;
             }
         }
@@ -252,8 +253,7 @@ __global__ void __launch_bounds__(kBlock) sort_scatter_kernel(const __grid_const
 // four launches.)
 struct ClusterSortArgs {
     const int* tokens;
-    int2* between[2];             // entries (key, position) from pass to pass
-    int* keys_out; int* pos_out;
+    int2* between[2];             // entries (key, position) from pass to pass; the last pass writes [0]
     uint8_t* present;
     int* joins;
     int rows, vocab, passes, steps;   // a CTA has 1024 * steps entries
@@ -321,19 +321,14 @@ __global__ void __launch_bounds__(kClusterThreads) cluster_sort_kernel(const __g
         if (tid < kBins) base[tid] += before;
         __syncthreads();
         const bool last = pass + 1 == a.passes;
-        int2* to = ctas > 1 ? a.between[pass & 1] : own;
+        int2* to = last || ctas > 1 ? a.between[(a.passes - 1 - pass) & 1] : own;
 #pragma unroll
         for (int s = 0; s < kMaxSteps; ++s) {
             if (s * 32 + lane < left) {
                 const int d = digit_of(key[s], shift);
                 const int at = base[d] + counters[warp * kBins + d] + where[s];
-                if (last) {
-                    a.keys_out[at] = key[s];
-                    a.pos_out[at] = pos[s];
-                    if (key[s] < a.vocab) a.present[key[s]] = 1;
-                } else {
-                    to[at] = make_int2(key[s], pos[s]);
-                }
+                to[at] = make_int2(key[s], pos[s]);
+                if (last && key[s] < a.vocab) a.present[key[s]] = 1;
             }
         }
         if (last) break;
@@ -353,7 +348,7 @@ __global__ void __launch_bounds__(kClusterThreads) cluster_sort_kernel(const __g
 
 // ---------------------------------------------------------------------------------------------- sums of runs
 struct SumArgs {
-    const int* keys; const int* pos;
+    const int2* entries;          // (key, position), sorted
     const uint8_t* present;
     const void* dy; long long dy_pitch;
     void* out;
@@ -396,15 +391,15 @@ __global__ void __launch_bounds__(kBlock, sizeof(DT) == 2 ? 4 : 3) embedding_sum
     if (unit >= a.units) return;
     const int begin = unit * a.unit, end = min(a.rows, begin + a.unit);
     const DT* dy = static_cast<const DT*>(a.dy);
-    const int head = a.keys[begin], last = a.keys[end - 1];
-    const int beyond = end < a.rows ? a.keys[end] : -1;
+    const int head = a.entries[begin].x, last = a.entries[end - 1].x;
+    const int beyond = end < a.rows ? a.entries[end].x : -1;
     // the run at the beginning: its own, another unit's (skipped), or cut
-    const bool from_before = begin > 0 && a.keys[begin - 1] == head;
-    const bool head_cut = from_before && ((begin > a.unit && a.keys[begin - a.unit - 1] == head) || beyond == head);
+    const bool from_before = begin > 0 && a.entries[begin - 1].x == head;
+    const bool head_cut = from_before && ((begin > a.unit && a.entries[begin - a.unit - 1].x == head) || beyond == head);
     const int skip = from_before && !head_cut ? head : -1;
     // the run at the end, if it begins here and goes on
     const bool goes_on = beyond == last && !(from_before && last == head);
-    const bool tail_cut = goes_on && end + a.unit < a.rows && a.keys[end + a.unit] == last;
+    const bool tail_cut = goes_on && end + a.unit < a.rows && a.entries[end + a.unit].x == last;
     const int stop = goes_on && !tail_cut ? a.rows : end;
     int current = head;
     float sum[8];
@@ -429,8 +424,9 @@ __global__ void __launch_bounds__(kBlock, sizeof(DT) == 2 ? 4 : 3) embedding_sum
 #pragma unroll
         for (int d = 0; d < kDeep; ++d) {
             const bool in = i + d < stop;
-            key[d] = in ? a.keys[i + d] : -1;
-            pos[d] = in ? a.pos[i + d] : 0;
+            const int2 x = in ? a.entries[i + d] : make_int2(-1, 0);
+            key[d] = x.x;
+            pos[d] = x.y;
         }
     };
     entries(begin);
@@ -530,7 +526,7 @@ __global__ void __launch_bounds__(kBlock) embedding_join_kernel(const __grid_con
     const int slices = (a.width + 255) / 256, joins = *a.joins;
     for (long long i = blockIdx.x; i < static_cast<long long>(joins) * slices; i += gridDim.x) {
         const int unit = a.join_list[i / slices], col = static_cast<int>(i % slices) * 256 + lane * 8, n = max(0, min(8, a.width - col));
-        const int key = a.keys[min(a.rows, (unit + 1) * a.unit) - 1];
+        const int key = a.entries[min(a.rows, (unit + 1) * a.unit) - 1].x;
         float sum[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] = 0.f;
@@ -546,7 +542,7 @@ __global__ void __launch_bounds__(kBlock) embedding_join_kernel(const __grid_con
 #pragma unroll
             for (int d = 0; d < kDeep; ++d) {
                 const int w = u + d * kWarps;
-                in[d] = w < a.units && a.keys[static_cast<long long>(w) * a.unit] == key;
+                in[d] = w < a.units && a.entries[static_cast<long long>(w) * a.unit].x == key;
                 v[d].load(a.head + static_cast<long long>(w < a.units ? w : unit) * a.width + col, w < a.units ? n : 0);
             }
 #pragma unroll
@@ -605,7 +601,7 @@ bool valid_size(long long rows, long long vocab, long long width) {
 int unit_of(long long rows) { return rows <= 4096 ? 8 : rows <= 16384 ? 16 : 32; }
 
 struct GradLayout {
-    size_t keys[2], pos[2], between[2], counts, present, joins, join_list, head, tail, total;
+    size_t entries[2], counts, present, joins, join_list, head, tail, total;
     int unit, units;
 };
 GradLayout grad_layout(long long rows, long long vocab, long long width) {
@@ -619,9 +615,7 @@ GradLayout grad_layout(long long rows, long long vocab, long long width) {
     L.unit = unit_of(rows);
     L.units = static_cast<int>(cdiv(rows, L.unit));
     for (int i = 0; i < 2; ++i) {
-        L.keys[i] = take(4 * rows);
-        L.pos[i] = take(4 * rows);
-        L.between[i] = take(rows <= kClusterRows ? 8 * rows : 0);
+        L.entries[i] = take(8 * rows);
     }
     L.counts = take(4LL * kBins * std::min<long long>(kMaxSortBlocks, cdiv(rows, kPart)));
     L.present = take(vocab);
@@ -725,6 +719,7 @@ extern "C" db_status db_embedding_grad(const int32_t* tokens, const void* dy, in
     }
     char* base = static_cast<char*>(workspace);
     const auto ints = [&](size_t at) { return reinterpret_cast<int*>(base + at); };
+    const auto entries = [&](int i) { return reinterpret_cast<int2*>(base + L.entries[i]); };
     // digits of 9 bits until the largest key, vocab (a token outside the table), is covered
     int passes = 1;
     while (vocab >> (passes * kDigitBits)) ++passes;
@@ -735,9 +730,8 @@ extern "C" db_status db_embedding_grad(const int32_t* tokens, const void* dy, in
         while (ctas < kMaxCluster && ctas * kClusterThreads < rows) ctas *= 2;
         ClusterSortArgs s{};
         s.tokens = tokens;
-        s.between[0] = reinterpret_cast<int2*>(base + L.between[0]);
-        s.between[1] = reinterpret_cast<int2*>(base + L.between[1]);
-        s.keys_out = ints(L.keys[0]); s.pos_out = ints(L.pos[0]);
+        s.between[0] = entries(0);
+        s.between[1] = entries(1);
         s.present = reinterpret_cast<uint8_t*>(base + L.present);
         s.joins = ints(L.joins);
         s.rows = static_cast<int>(rows); s.vocab = vocab; s.passes = passes;
@@ -756,8 +750,8 @@ extern "C" db_status db_embedding_grad(const int32_t* tokens, const void* dy, in
         const int used = static_cast<int>(cdiv(rows, s.per_block));
         for (int p = 0; p < passes; ++p) {
             s.first = p == 0; s.last = p + 1 == passes; s.shift = p * kDigitBits;
-            s.keys_in = ints(L.keys[(p + 1) & 1]); s.pos_in = ints(L.pos[(p + 1) & 1]);
-            s.keys_out = ints(L.keys[p & 1]); s.pos_out = ints(L.pos[p & 1]);
+            s.in = entries((p + 1) & 1);
+            s.out = entries(p & 1);
             sorted = p & 1;
             Launch C(dim3(used), kBlock, 0, stream), S(dim3(used), kBlock, 0, stream);
             DB_CUDA_TRY(cudaLaunchKernelEx(&C.cfg, sort_count_kernel, s));
@@ -765,7 +759,7 @@ extern "C" db_status db_embedding_grad(const int32_t* tokens, const void* dy, in
         }
     }
     SumArgs a{};
-    a.keys = ints(L.keys[sorted]); a.pos = ints(L.pos[sorted]);
+    a.entries = entries(sorted);
     a.present = reinterpret_cast<uint8_t*>(base + L.present);
     a.dy = dy; a.dy_pitch = dy_pitch; a.out = dtable;
     a.head = reinterpret_cast<float*>(base + L.head); a.tail = reinterpret_cast<float*>(base + L.tail);

@@ -105,7 +105,8 @@ __device__ __forceinline__ uint32_t in_first_cta(const void* p) {
     return a;
 }
 __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    // no wider release than the default: it would wait for the warp's stores, which nobody here reads
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void expect_tx(uint64_t* bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(tc::smem_u32(bar)), "r"(bytes) : "memory");
@@ -357,6 +358,14 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
             const uint32_t acc = tmem + buf * BN + (static_cast<uint32_t>(quarter * 32) << 16) + part * kPerWarp;
             // Fetching the next columns' rows into a second set of registers gained nothing (the arithmetic then has fewer),
             // nor did asking the L2 for them a tile ahead (161 against 193 us for the block's first backward product).
+            const auto release = [&] {                         // the accumulator has been read: the next products may have it
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (CG == 2) arrive_cluster(in_first_cta(&taken_bar[buf]));
+                    else tc::mbar_arrive(&taken_bar[buf]);
+                }
+            };
 #pragma unroll 1
             for (int c = 0; c < columns; c += kChunk) {
                 __syncwarp();                                  // rows past the end rejoin for the next read
@@ -372,6 +381,7 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
 #pragma unroll
                     for (int i = 0; i < kChunk / 2; ++i) u[i] = pair(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1]));
                 }
+                if (c + kChunk >= columns) release();
                 if (in) {
                     epilogue_row<EPI>(p.e, row, col, N, fetched, v, u);
                 } else if (row < p.M) {
@@ -381,12 +391,7 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
                     if (EPI == kEpiGated) store_row(to + plane, kChunk, u);
                 }
             }
-            tc::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if (CG == 2) arrive_cluster(in_first_cta(&taken_bar[buf]));
-                else tc::mbar_arrive(&taken_bar[buf]);
-            }
+            if (columns <= 0) release();
         }
         __syncwarp();
     }

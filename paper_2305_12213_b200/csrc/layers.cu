@@ -283,9 +283,12 @@ long long tiles_of(Kind kind, TileShape shape, const Size& s) {
 
 // The tile shape and the number of pieces of the reduction with the least estimated time, in SM cycles.
 // A 64-deep block of a tile costs its products or its copies (about 57 bytes a cycle reach an SM), whichever is longer,
-// a tile something for its start and end, and a reduction in pieces a second kernel and the traffic of the partial sums.
+// more for each of two CTAs on an SM; a tile something for its start and end; and a reduction in pieces a second kernel and
+// the traffic of the partial sums.  (256 x 2048 x 1000 in 64-column tiles, us: one piece 11.9, four 10.8, eight 9.3, sixteen
+// 11.9; 1024 x 1024 x 1024: one 8.3, two 14.4; pairs of 256 columns there 11.4.)
 Plan make_plan(Kind kind, const Size* sizes, int n, long long blocks) {
-    constexpr double kBlock[kTileShapes] = {560, 430, 560, 420}, kTile[kTileShapes] = {2600, 2000, 1700, 1300}, kCombine = 4000;
+    constexpr double kBlock[kTileShapes] = {560, 430, 560, 380}, kShared[kTileShapes] = {560, 430, 900, 550};
+    constexpr double kTile[kTileShapes] = {4700, 3100, 1500, 1300}, kCombine = 3500;
     Plan best;
     if (blocks == 0 || n == 0) return best;                  // no rows: nothing is launched
     for (int j = 0; j < n; ++j)
@@ -295,16 +298,16 @@ Plan make_plan(Kind kind, const Size* sizes, int n, long long blocks) {
     for (int i = 0; i < kTileShapes; ++i) {
         const TileShape shape = static_cast<TileShape>(i);
         if (!gemm_fn(kind, shape)) continue;
-        const long long workers = std::max(1, sms / kShapes[i].cg);
+        const long long alone = std::max(1, sms / kShapes[i].cg), workers = alone * kShapes[i].ctas;
         long long tiles = 0, outputs = 0;
         for (int j = 0; j < n; ++j) {
             tiles += tiles_of(kind, shape, sizes[j]);
             outputs += sizes[j].M * lg::partial_pitch(sizes[j].N) * (kind == kGated ? 2 : 1);
         }
         for (long long want = std::min(blocks, std::max(1LL, workers / tiles));; want = (want + 1) / 2) {
-            const long long per = cdiv(blocks, want), splits = cdiv(blocks, per);
-            const double time = static_cast<double>(cdiv(tiles * splits, workers)) * (per * kBlock[i]) + kTile[i] +
-                                (splits > 1 ? kCombine + outputs * (splits + 1) * 4 / 2500.0 : 0);
+            const long long per = cdiv(blocks, want), splits = cdiv(blocks, per), ctas = tiles * splits;
+            const double time = static_cast<double>(cdiv(ctas, workers)) * per * (ctas > alone ? kShared[i] : kBlock[i]) + kTile[i] +
+                                (splits > 1 ? kCombine + outputs * (splits + 1) * 4 / 6000.0 : 0);
             if (least == 0 || time < least) {
                 least = time;
                 best.shape = shape;
