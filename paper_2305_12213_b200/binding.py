@@ -820,7 +820,7 @@ def _scratch(t: torch.Tensor, index: int):
 
 def _launch(index: int, stream: Optional[torch.cuda.Stream], fn, *args) -> None:
     handle = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
-    if torch.cuda.current_device() == index:
+    if torch._C._cuda_getDevice() == index:
         status = fn(*args, handle)
     else:
         with torch.cuda.device(index):

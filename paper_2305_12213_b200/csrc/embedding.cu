@@ -147,7 +147,8 @@ __device__ __forceinline__ void scan_bins(int* total, int* warp_sum) {
     __syncthreads();
     if (tid < kBins / 2) {
         int before = s - x - y;
-        for (int w = 0; w < warp; ++w) before += warp_sum[w];
+#pragma unroll
+        for (int w = 0; w < kBins / 64; ++w) before += w < warp ? warp_sum[w] : 0;
         total[2 * tid] = before;
         total[2 * tid + 1] = before + x;
     }
@@ -161,7 +162,7 @@ __device__ __forceinline__ void rank_entries(const int (&key)[STEPS], int shift,
                                              int (&rank)[STEPS]) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     unsigned short* mine = counters + warp * kBins;
-    for (int b = lane; b < kBins; b += 32) mine[b] = 0;
+    for (int b = lane; b < kBins / 8; b += 32) reinterpret_cast<uint4*>(mine)[b] = make_uint4(0, 0, 0, 0);
     __syncwarp();
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
@@ -185,7 +186,7 @@ __device__ __forceinline__ void rank_entries(const int (&key)[STEPS], int shift,
 }
 
 __global__ void __launch_bounds__(kBlock) sort_scatter_kernel(const __grid_constant__ SortArgs a) {
-    __shared__ unsigned short counters[kSortWarps * kBins];
+    __shared__ __align__(16) unsigned short counters[kSortWarps * kBins];
     __shared__ int base[kBins], total[kBins], warp_sum[kSortWarps];
     tc::griddep_wait();
     tc::griddep_launch_dependents();
@@ -222,12 +223,14 @@ __global__ void __launch_bounds__(kBlock) sort_scatter_kernel(const __grid_const
         rank_entries<kSortWarps, kSteps>(key, a.shift, left, counters, rank);
         __syncthreads();
         for (int b = tid; b < kBins; b += kBlock) {       // counts become the start of each warp's entries
+            unsigned short c[kSortWarps];
             int at = 0;
 #pragma unroll
+            for (int w = 0; w < kSortWarps; ++w) c[w] = counters[w * kBins + b];
+#pragma unroll
             for (int w = 0; w < kSortWarps; ++w) {
-                const int c = counters[w * kBins + b];
                 counters[w * kBins + b] = static_cast<unsigned short>(at);
-                at += c;
+                at += c[w];
             }
             total[b] = at;
         }
@@ -294,12 +297,14 @@ __global__ void __launch_bounds__(kClusterThreads) cluster_sort_kernel(const __g
         rank_entries<kClusterWarps, kMaxSteps>(key, shift, left, counters, where);
         __syncthreads();
         if (tid < kBins) {
+            unsigned short c[kClusterWarps];                   // read first: a chain of reads and writes costs 0.6 us
             int at = 0;
 #pragma unroll
+            for (int w = 0; w < kClusterWarps; ++w) c[w] = counters[w * kBins + tid];
+#pragma unroll
             for (int w = 0; w < kClusterWarps; ++w) {
-                const int c = counters[w * kBins + tid];
                 counters[w * kBins + tid] = static_cast<unsigned short>(at);
-                at += c;
+                at += c[w];
             }
             counts[tid] = at;
         }
