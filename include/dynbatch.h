@@ -582,7 +582,7 @@ db_status db_contract_f32(const float* A, int64_t a_row, int64_t a_k,
  *                The query depends on the current device's number of SMs.
  *
  * Buffers that a call writes must not overlap any other it touches, but as said above
- * (DB_ERR_ARG).  Any alignment down to the element size is accepted; outputs with
+ * (DB_ERR_ARG); different columns of one wider tensor (equal pitches) do not overlap.  Any alignment down to the element size is accepted; outputs with
  * 16-byte aligned rows take wide stores.  NaN and Inf in a row of x stay in that row of
  * y; in a weight gradient they spread to their feature.  The order of every sum depends
  * on sizes and device alone: the same call gives the same bits.  fp32 weight gradients:
@@ -663,7 +663,7 @@ db_status db_gated_ffn_grad(const void* dy, int64_t dy_pitch, const void* x,
  *           unpacked values are rounded to bf16, which is exact but below 2^-126
  *   codes   device, [rows, cols] contiguous e4m3
  *   scale   device, [rows, ceil(cols / 32)] contiguous bytes e + 127 (255: NaN)
- *   rows >= 0 (0: DB_OK, nothing enqueued), 1 <= cols <= 2^24, at most 2^40 values
+ *   rows    0 .. 2^38 (0: nothing is enqueued), cols 1 .. 2^24, at most 2^40 values
  * Any alignment down to the element size; 16-byte aligned rows of x and 8-byte aligned
  * rows of codes take wide accesses.  The buffers must not overlap.
  * ------------------------------------------------------------------------ */

@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(kBlock) checkpoint_unpack_kernel(const __grid_
     }
 }
 
-bool valid(long long rows, long long cols) { return rows >= 0 && rows <= (1LL << 40) && cols >= 1 && cols <= (1LL << 24) && rows * cols <= (1LL << 40); }
+bool valid(long long rows, long long cols) { return rows >= 0 && rows <= (1LL << 38) && cols >= 1 && cols <= (1LL << 24) && rows * cols <= (1LL << 40); }
 
 // Threads that take a row: a power of two from four (a group of 32 values) to a CTA's.
 int shift_of(long long cols) {
@@ -133,7 +133,6 @@ template <class Args>
 db_status launch(void (*fn)(const Args), const Args& a, cudaStream_t stream) {
     const long long per_cta = static_cast<long long>(kRowsAtOnce) * (kBlock >> a.threads_shift), across = 8LL << a.threads_shift;
     const long long ctas = (a.rows + per_cta - 1) / per_cta;
-    if (ctas > 0x7FFFFFFF) return DB_ERR_ARG;
     cudaLaunchConfig_t cfg;
     std::memset(&cfg, 0, sizeof cfg);
     cudaLaunchAttribute attr;

@@ -6,6 +6,7 @@
 // units are joined by a second small kernel from the units' partial sums.  No float atomics: the same call gives the
 // same bits.
 #include <algorithm>
+#include <atomic>
 #include <cstring>
 
 #include "common.h"
@@ -639,6 +640,19 @@ bool apart(const void* a, long long na, const void* b, long long nb) {
 int size_of(db_dtype t) { return t == DB_F32 ? 4 : 2; }
 bool valid_type(db_dtype t) { return t == DB_F32 || t == DB_BF16; }
 
+// Once per device: the attribute call costs a microsecond.
+db_status allow_sort_smem() {
+    constexpr int kDevices = 64;
+    static std::atomic<unsigned char> done[kDevices];
+    int device = 0;
+    DB_CUDA_TRY(cudaGetDevice(&device));
+    const bool known = device >= 0 && device < kDevices;
+    if (known && done[device].load(std::memory_order_relaxed)) return DB_OK;
+    DB_CUDA_TRY(cudaFuncSetAttribute(cluster_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kClusterSmem));
+    if (known) done[device].store(1, std::memory_order_relaxed);
+    return DB_OK;
+}
+
 // log2 of the threads that take a row, 8 values each
 int shift_of(long long width) {
     int s = 0;
@@ -741,7 +755,8 @@ extern "C" db_status db_embedding_grad(const int32_t* tokens, const void* dy, in
         s.joins = ints(L.joins);
         s.rows = static_cast<int>(rows); s.vocab = vocab; s.passes = passes;
         s.steps = static_cast<int>(cdiv(rows, static_cast<long long>(ctas) * kClusterThreads));
-        DB_CUDA_TRY(cudaFuncSetAttribute(cluster_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kClusterSmem));
+        const db_status st = allow_sort_smem();
+        if (st != DB_OK) return st;
         Launch S(dim3(ctas), kClusterThreads, kClusterSmem, stream, ctas);
         DB_CUDA_TRY(cudaLaunchKernelEx(&S.cfg, cluster_sort_kernel, s));
     } else {

@@ -372,6 +372,14 @@ __device__ __forceinline__ void sigmoid(const Batch& z, Batch& s) {
     reciprocal_batch(s);
 }
 __device__ __forceinline__ Pair magnitude(Pair z) { return z & ~kSigns; }
+// -min(|z|, the largest finite value): an infinity times a tail of zero is to be zero; a NaN stays one
+__device__ __forceinline__ Pair minus_finite_magnitude(Pair z) {
+    float a, b;
+    halves(magnitude(z), a, b);
+    asm("min.NaN.f32 %0, %0, 0f7F7FFFFF;" : "+f"(a));
+    asm("min.NaN.f32 %0, %0, 0f7F7FFFFF;" : "+f"(b));
+    return pair(-a, -b);
+}
 __device__ __forceinline__ Pair positive_part(Pair z) {       // a NaN stays one
     float a, b;
     halves(z, a, b);
@@ -400,7 +408,7 @@ __device__ __forceinline__ void act_batch(Batch& z) {
     } else if (ACT == DB_ACT_GELU) {
         Batch bell, tail;
         normal_tail(z, bell, tail);
-        DB_EACH z[i] = mul_add(magnitude(z[i]) ^ kSigns, tail[i], positive_part(z[i]));
+        DB_EACH z[i] = mul_add(minus_finite_magnitude(z[i]), tail[i], positive_part(z[i]));
     } else if (ACT == DB_ACT_RELU) {
         DB_EACH z[i] = positive_part(z[i]);
     }
@@ -416,7 +424,7 @@ __device__ __forceinline__ void act_batch_slope(const Batch& z, Batch& value, Ba
     } else if (ACT == DB_ACT_GELU) {
         Batch bell, tail;
         normal_tail(z, bell, tail);
-        DB_EACH value[i] = mul_add(magnitude(z[i]) ^ kSigns, tail[i], positive_part(z[i]));
+        DB_EACH value[i] = mul_add(minus_finite_magnitude(z[i]), tail[i], positive_part(z[i]));
         // P(z) - 1/2 has z's sign and the magnitude 1/2 - tail
         DB_EACH slope[i] = mul_add(tail[i], both(-1.f), both(0.5f)) ^ (z[i] & kSigns);
         DB_EACH slope[i] = add(slope[i], both(0.5f));

@@ -444,17 +444,32 @@ struct Operands {
     }
 };
 
-struct Extent { const void* p; long long bytes; bool written; };
-long long extent_bytes(long long rows, long long cols, long long pitch, int size) { return rows > 0 ? ((rows - 1) * pitch + cols) * size : 0; }
+// Rows of `row` bytes, `pitch` bytes apart.
+struct Extent {
+    const void* p;
+    long long rows, row, pitch;
+    bool written;
+};
+Extent matrix(const void* p, long long rows, long long cols, long long pitch, int size, bool written) { return {p, rows, cols * size, pitch * size, written}; }
+Extent block(const void* p, long long bytes, bool written) { return {p, bytes > 0 ? 1 : 0, bytes, bytes, written}; }
 
+bool overlap(const Extent& x, const Extent& y) {
+    if (!x.p || !y.p || x.rows < 1 || y.rows < 1) return false;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
+    if (a >= b + static_cast<uintptr_t>((y.rows - 1) * y.pitch + y.row) || b >= a + static_cast<uintptr_t>((x.rows - 1) * x.pitch + x.row)) return false;
+    if (x.pitch == y.pitch && x.rows > 1 && y.rows > 1) {      // columns of one tensor: apart if they are in every row
+        const long long ahead = b >= a ? static_cast<long long>((b - a) % static_cast<uintptr_t>(x.pitch))
+                                       : (x.pitch - static_cast<long long>((a - b) % static_cast<uintptr_t>(x.pitch))) % x.pitch;
+        return ahead < x.row || ahead + y.row > x.pitch;
+    }
+    return true;
+}
 // Whether something that a call writes overlaps anything else it touches.
-bool overlaps(const Extent* x, int n) {
-    for (int i = 0; i < n; ++i)
-        for (int j = i + 1; j < n; ++j) {
-            if (!x[i].p || !x[j].p || !(x[i].written || x[j].written) || x[i].bytes <= 0 || x[j].bytes <= 0) continue;
-            const uintptr_t a = reinterpret_cast<uintptr_t>(x[i].p), b = reinterpret_cast<uintptr_t>(x[j].p);
-            if (a < b + static_cast<uintptr_t>(x[j].bytes) && b < a + static_cast<uintptr_t>(x[i].bytes)) return true;
-        }
+template <int N>
+bool overlaps(const Extent (&x)[N]) {
+    for (int i = 0; i < N; ++i)
+        for (int j = i + 1; j < N; ++j)
+            if ((x[i].written || x[j].written) && overlap(x[i], x[j])) return true;
     return false;
 }
 
@@ -744,11 +759,11 @@ extern "C" db_status db_linear(const void* x, int64_t x_pitch, const void* w, co
     const bool e4m3 = z && z_dtype == DB_E4M3;
     const bool in_place = residual == y && residual_pitch == y_pitch;
     const Extent touched[] = {
-        {x, extent_bytes(rows, n_in, x_pitch, 2), false}, {w, extent_bytes(n_in, n_out, n_out, 2), false},
-        {bias, 2LL * n_out, false}, {in_place ? nullptr : residual, extent_bytes(rows, n_out, residual_pitch, 2), false},
-        {y, extent_bytes(rows, n_out, y_pitch, 2), true}, {z, z ? rows * n_out * kept_size(z_dtype) : 0, true},
-        {e4m3 ? z_scale : nullptr, rows * scales_of(n_out), true}, {workspace, static_cast<long long>(workspace_bytes), true}};
-    if (overlaps(touched, static_cast<int>(sizeof touched / sizeof touched[0]))) return DB_ERR_ARG;
+        matrix(x, rows, n_in, x_pitch, 2, false), matrix(w, n_in, n_out, n_out, 2, false),
+        block(bias, 2LL * n_out, false), matrix(in_place ? nullptr : residual, rows, n_out, residual_pitch, 2, false),
+        matrix(y, rows, n_out, y_pitch, 2, true), block(z, z ? rows * n_out * kept_size(z_dtype) : 0, true),
+        block(e4m3 ? z_scale : nullptr, rows * scales_of(n_out), true), block(workspace, static_cast<long long>(workspace_bytes), true)};
+    if (overlaps(touched)) return DB_ERR_ARG;
     const bool aligned = on_grid(x, x_pitch) && on_grid(w, n_out);
     LinearArgs v{x, w, bias, residual, x_pitch, residual_pitch, rows, n_in, n_out, act, y, y_pitch, z, z_scale, z_dtype};
     Arena need(nullptr);
@@ -795,15 +810,15 @@ extern "C" db_status db_linear_grad(const void* dy, int64_t dy_pitch, const void
         return DB_ERR_ARG;
     const bool in_place = dx_addend == dx && dx_addend_pitch == dx_pitch;
     const Extent touched[] = {
-        {dy, extent_bytes(rows, n_out, dy_pitch, 2), false}, {dw ? x : nullptr, extent_bytes(rows, n_in, x_pitch, 2), false},
-        {dx ? w : nullptr, extent_bytes(n_in, n_out, n_out, 2), false},
-        {with_z ? z : nullptr, rows * n_out * kept_size(z_dtype), false},
-        {with_z && z_dtype == DB_E4M3 ? z_scale : nullptr, rows * scales_of(n_out), false},
-        {in_place ? nullptr : dx_addend, extent_bytes(rows, n_in, dx_addend_pitch, 2), false},
-        {dx, extent_bytes(rows, n_in, dx_pitch, 2), true}, {dw, static_cast<long long>(n_in) * n_out * g, true},
-        {dbias, static_cast<long long>(n_out) * g, true}, {workspace, static_cast<long long>(workspace_bytes), true}};
-    if (overlaps(touched, static_cast<int>(sizeof touched / sizeof touched[0]))) return DB_ERR_ARG;
-    const bool aligned = (with_z || on_grid(dy, dy_pitch)) && (!dw || on_grid(x, x_pitch)) && (!dx || on_grid(w, n_out));
+        matrix(dy, rows, n_out, dy_pitch, 2, false), matrix(dw ? x : nullptr, rows, n_in, x_pitch, 2, false),
+        matrix(dx ? w : nullptr, n_in, n_out, n_out, 2, false),
+        block(with_z ? z : nullptr, rows * n_out * kept_size(z_dtype), false),
+        block(with_z && z_dtype == DB_E4M3 ? z_scale : nullptr, rows * scales_of(n_out), false),
+        matrix(in_place ? nullptr : dx_addend, rows, n_in, dx_addend_pitch, 2, false),
+        matrix(dx, rows, n_in, dx_pitch, 2, true), block(dw, static_cast<long long>(n_in) * n_out * g, true),
+        block(dbias, static_cast<long long>(n_out) * g, true), block(workspace, static_cast<long long>(workspace_bytes), true)};
+    if (overlaps(touched)) return DB_ERR_ARG;
+    const bool aligned = (with_z || (!dx && !dw) || on_grid(dy, dy_pitch)) && (!dw || on_grid(x, x_pitch)) && (!dx || on_grid(w, n_out));
     LinearGradArgs v{dy, x, w, z, z_scale, dx_addend, dy_pitch, x_pitch, dx_addend_pitch, rows, z_dtype, grad_dtype,
                      n_in, n_out, act, dx, dw, dbias, dx_pitch};
     Arena need(nullptr);
@@ -851,12 +866,12 @@ extern "C" db_status db_gated_ffn(const void* x, int64_t x_pitch, const void* w_
     const long long weight = 2LL * width * hidden, kept = gate ? rows * hidden * kept_size(kept_dtype) : 0, scales = rows * scales_of(hidden);
     const bool in_place = residual == y && residual_pitch == y_pitch;
     const Extent touched[] = {
-        {x, extent_bytes(rows, width, x_pitch, 2), false}, {w_gate, weight, false}, {w_up, weight, false}, {w_down, weight, false},
-        {in_place ? nullptr : residual, extent_bytes(rows, width, residual_pitch, 2), false},
-        {y, extent_bytes(rows, width, y_pitch, 2), true}, {gate, kept, true}, {up, kept, true},
-        {e4m3 ? gate_scale : nullptr, scales, true}, {e4m3 ? up_scale : nullptr, scales, true},
-        {workspace, static_cast<long long>(workspace_bytes), true}};
-    if (overlaps(touched, static_cast<int>(sizeof touched / sizeof touched[0]))) return DB_ERR_ARG;
+        matrix(x, rows, width, x_pitch, 2, false), block(w_gate, weight, false), block(w_up, weight, false), block(w_down, weight, false),
+        matrix(in_place ? nullptr : residual, rows, width, residual_pitch, 2, false),
+        matrix(y, rows, width, y_pitch, 2, true), block(gate, kept, true), block(up, kept, true),
+        block(e4m3 ? gate_scale : nullptr, scales, true), block(e4m3 ? up_scale : nullptr, scales, true),
+        block(workspace, static_cast<long long>(workspace_bytes), true)};
+    if (overlaps(touched)) return DB_ERR_ARG;
     const bool aligned = on_grid(x, x_pitch) && on_grid(w_gate, hidden) && on_grid(w_up, hidden) && on_grid(w_down, width);
     GatedArgs v{};
     v.x = x; v.x_pitch = x_pitch; v.w_gate = w_gate; v.w_up = w_up; v.w_down = w_down;
@@ -912,13 +927,13 @@ extern "C" db_status db_gated_ffn_grad(const void* dy, int64_t dy_pitch, const v
     const long long kept = rows * hidden * kept_size(kept_dtype), scales = rows * scales_of(hidden);
     const bool in_place = dx_addend == dx && dx_addend_pitch == dx_pitch;
     const Extent touched[] = {
-        {dy, extent_bytes(rows, width, dy_pitch, 2), false}, {needs_x ? x : nullptr, extent_bytes(rows, width, x_pitch, 2), false},
-        {dx ? w_gate : nullptr, weight, false}, {dx ? w_up : nullptr, weight, false}, {w_down, weight, false},
-        {gate, kept, false}, {up, kept, false}, {e4m3 ? gate_scale : nullptr, scales, false}, {e4m3 ? up_scale : nullptr, scales, false},
-        {in_place ? nullptr : dx_addend, extent_bytes(rows, width, dx_addend_pitch, 2), false},
-        {dx, extent_bytes(rows, width, dx_pitch, 2), true}, {dw_gate, grad, true}, {dw_up, grad, true}, {dw_down, grad, true},
-        {workspace, static_cast<long long>(workspace_bytes), true}};
-    if (overlaps(touched, static_cast<int>(sizeof touched / sizeof touched[0]))) return DB_ERR_ARG;
+        matrix(dy, rows, width, dy_pitch, 2, false), matrix(needs_x ? x : nullptr, rows, width, x_pitch, 2, false),
+        block(dx ? w_gate : nullptr, weight, false), block(dx ? w_up : nullptr, weight, false), block(w_down, weight, false),
+        block(gate, kept, false), block(up, kept, false), block(e4m3 ? gate_scale : nullptr, scales, false), block(e4m3 ? up_scale : nullptr, scales, false),
+        matrix(in_place ? nullptr : dx_addend, rows, width, dx_addend_pitch, 2, false),
+        matrix(dx, rows, width, dx_pitch, 2, true), block(dw_gate, grad, true), block(dw_up, grad, true), block(dw_down, grad, true),
+        block(workspace, static_cast<long long>(workspace_bytes), true)};
+    if (overlaps(touched)) return DB_ERR_ARG;
     const bool aligned = on_grid(dy, dy_pitch) && (!needs_x || on_grid(x, x_pitch)) && on_grid(w_down, width) &&
                          (!dx || (on_grid(w_gate, hidden) && on_grid(w_up, hidden)));
     GatedArgs v{};

@@ -435,7 +435,8 @@ def test_embedding(rows, vocab, n, pad, shift, table_dtype, out_dtype):
 GRADS = [  # rows, vocab, width, distribution of the tokens
     (1, 1, 1, "all"), (1, 300, 64, "all"), (200, 800, 64, "zipf"), (9, 5, 33, "all"), (500, 3, 40, "all"), (8192, 511, 72, "zipf"),
     (8192, 512, 8, "zipf"), (8193, 513, 16, "zipf"), (5000, 40000, 264, "zipf"), (20000, 3000, 136, "zipf"), (16385, 100, 24, "one"),
-    (30000, 300000, 24, "all"), (4097, 64, 2056, "zipf"), (3000, 70, 8, "outside"), (1100000, 1500, 8, "zipf"),
+    (30000, 300000, 24, "all"), (1500, 400, 40, "zipf"), (257, 5000, 24, "zipf"), (256, 5000, 24, "zipf"), (70000, 300000, 8, "zipf"),
+    (4097, 64, 2056, "zipf"), (3000, 70, 8, "outside"), (1100000, 1500, 8, "zipf"),
 ]
 
 
@@ -498,3 +499,43 @@ def test_embedding_grad_without_rows_and_in_a_graph():
     assert (out[:7] == 0).all() and (out[8:] == 0).all()
     want = f64(dy).sum(0)
     assert ((f64(out)[7] - want).abs() <= 20002 * 2.0**-24 * f64(dy).abs().sum(0)).all()
+
+
+def test_columns_of_one_tensor():
+    """x, y, the residual, dy and dx as columns of one tensor: the columns between them stay."""
+    rows, n, m = 150, 64, 72
+    wide = normal(1, rows, n + 3 * m + n + 16)
+    x, y, r, dy, dx = (wide[:, a:a + k] for a, k in ((0, n), (n, m), (n + m, m), (n + 2 * m, m), (n + 3 * m, n)))
+    before = wide.clone()
+    w = normal(2, n, m, std=0.1)
+    ws = workspace(max(binding.linear_workspace_bytes(rows, n, m), binding.linear_grad_workspace_bytes(rows, n, m)))
+    binding.linear(x, w, y, ws, residual=r, activation="gelu")
+    binding.linear_grad(dy, x, w, ws, dx=dx)
+    want_y, want_dx = torch.empty(rows, m, dtype=bf16, device="cuda"), torch.empty(rows, n, dtype=bf16, device="cuda")
+    binding.linear(x.contiguous(), w, want_y, ws, residual=r.contiguous(), activation="gelu")
+    binding.linear_grad(dy.contiguous(), None, w, ws, dx=want_dx)
+    assert torch.equal(y, want_y) and torch.equal(dx, want_dx)
+    before[:, n:n + m], before[:, n + 3 * m:n + 3 * m + n] = want_y, want_dx
+    assert torch.equal(wide, before)
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+def test_activations_far_out(act):
+    """z = x w with a 1 x 1 weight of one: the activation of every kind of value."""
+    v = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 1e-40, 3.0, -3.0, 9.0, -9.0, 30.0, -30.0, 200.0, -200.0, 3e38, -3e38, float("inf"), float("nan")])
+    x = v.to(bf16).cuda()[:, None].contiguous()
+    y = torch.empty_like(x)
+    ws = workspace(max(binding.linear_workspace_bytes(len(v), 1, 1), binding.linear_grad_workspace_bytes(len(v), 1, 1)))
+    one = torch.ones(1, 1, dtype=bf16, device="cuda")
+    z = torch.empty_like(x)
+    binding.linear(x, one, y, ws, activation=act, z=z)
+    xd = f64(x)[:, 0]
+    want = ref.act(xd, act)
+    got = f64(y)[:, 0]
+    assert got[-1].isnan() and torch.isinf(got[-2]) and got[-2] > 0
+    assert ((got - want).abs() <= BF16 * want.abs() + 2 * FAST * xd.abs().clamp(max=1) + 1e-37)[:-2].all()
+    dx = torch.empty_like(x)
+    binding.linear_grad(torch.ones_like(x), None, one, ws, z=z, activation=act, dx=dx)
+    slope = ref.slope(xd, act)
+    # dz is rounded to bf16, and again as dx
+    assert ((f64(dx)[:, 0] - slope).abs() <= 2.01 * BF16 * slope.abs() + 4 * FAST)[:-2].all()

@@ -124,6 +124,14 @@ def test_linear_refusals(lib):
         assert _linear(lib, **bad) == E.DB_ERR_UNSUPPORTED, bad
 
 
+def test_columns_of_one_tensor_overlap_where_they_do(lib):
+    wide = _A[0]
+    apart = dict(x=wide, xp=400, y=wide + 2 * 64, yp=400, r=wide + 2 * 192, rp=400)
+    for bad in (dict(y=wide + 2 * 63), dict(y=wide + 2 * 65), dict(r=wide + 2 * 191), dict(yp=336), dict(y=wide + 2 * 300),
+                dict(y=wide + 2 * (400 * 99 - 64))):
+        assert _linear(lib, **{**apart, **bad}) == E.DB_ERR_ARG, bad
+
+
 def test_linear_grad_refusals(lib):
     for bad in (dict(dy=None), dict(x=None), dict(w=None), dict(z=None), dict(zs=None), dict(ws=None),
                 dict(dx=None, add=None, dw=None, db=None)):
@@ -167,7 +175,7 @@ def test_checkpoint_refusals(lib):
             assert f(lib, **{name: None}) == E.DB_ERR_NULL
             assert f(lib, rows=0, **{name: None}) == E.DB_OK
         for bad in (dict(rows=-1), dict(n=0), dict(n=2**24 + 1), dict(xp=63), dict(x=_A[0] + 1), dict(c=_A[0]),
-                    dict(s=_A[0] + 2 * 640 - 1), dict(rows=2**40, n=2)):
+                    dict(s=_A[0] + 2 * 640 - 1), dict(rows=2**38, n=8), dict(rows=2**38 + 1, n=1)):
             assert f(lib, **bad) == E.DB_ERR_ARG, bad
     assert _pack(lib, s=_A[1] + 639) == E.DB_ERR_ARG
 
