@@ -698,7 +698,7 @@ db_status db_checkpoint_unpack(const void* codes, const void* scale,
  *           by calls on one stream, distinct for calls that may overlap
  * Any alignment down to the element size; 16-byte aligned rows take wide accesses.
  * Buffers that a call writes must not overlap others (DB_ERR_ARG).  Launches: lookup 1;
- * gradient 1 up to 256 rows, 3 up to 65536, beyond that 2 for each 9 bits of vocab and 2
+ * gradient 1 up to 256 rows, 4 up to 65536, beyond that 2 for each 9 bits of vocab and 3
  * more.
  * ------------------------------------------------------------------------ */
 db_status db_embedding(const int32_t* tokens, const void* table,
