@@ -4,13 +4,22 @@
 // products (y = x W, dx = dz W^T, dW = x^T dz) read x, W and dz from where they lie, W stored [in, out].
 //
 // One persistent CTA (or pair of CTAs) per SM (pair) walks the output tiles:
-//   warp 0   (one lane) copies 64-deep operand blocks into a ring of shared-memory stages by TMA
-//   warp 1   owns the tensor memory; one lane issues four tcgen05.mma a stage (of the pair's first CTA alone)
+//   warp 0   copies 64-deep operand blocks into a ring of shared-memory stages by TMA
+//   warp 1   owns the tensor memory and issues four tcgen05.mma a stage (of the pair's first CTA alone)
+//            Both walk their loops as whole warps, one elected lane issues: the operands of the instructions are then
+//            known to be uniform.  With one lane walking alone a 64-deep block took 0.32 us instead of 0.22.
 //   the others take the finished accumulator out of tensor memory, 32 columns of a row per thread, apply the epilogue
 //            and store; two accumulators, so that this runs under the next tile's products.
 // A pair (cta_group::2) computes 256 rows x BN columns: each CTA holds its own 128 rows of A and half of B's, and the
 // tensor cores of both read both halves, so an operand byte in shared memory serves twice as many products.
 // Copies that serve a pair signal the first CTA's barrier; no multicast copies are used.
+//
+// Bound by the tensor cores where there are tiles for all pairs and the epilogue is plain: 16384 x 2048 x 2048, y 93 us,
+// dx 89, dW 97 (64 tiles on 74 pairs), the tensor pipe 85 to 90 % active.  1024-deep products with more to do for each
+// column are bound by the epilogue: 8191 x 1024 x 4096 48 us as it is, 55 with gelu, 59 with bias and gelu.  Its loads and
+// stores are 32 bytes of a row for each thread, and the load/store unit takes each row as an access of its own.  Single CTAs
+// start and end 1 us sooner than pairs; a first block costs them 4.7 us from the predecessor's end to their own, each further
+// one 0.2.
 //
 // Every wait is bounded (2 s): whoever gives up sets the call's status word and its CTA's flag, all roles stop, copies
 // and products under way are waited for (again with a limit), tensor memory is freed and the kernel returns.
@@ -240,7 +249,6 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
     if (g.clear_status && blockIdx.x == 0 && tid == 0) *g.status = 0;
 
     if (warp == 0) {
-        // The whole warp walks the loop and one elected lane issues: what is uniform stays in uniform registers.
         int stage = 0, it = 0;
         uint32_t phase = 0;
         bool ok = true;
@@ -350,7 +358,7 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
             const bool in = row < p.M && g.splits == 1;       // the epilogue is applied here, or to the joined sum
             Fetched<EPI> fetched;                              // of the first columns: while the products still run
             if (in && columns > 0) epilogue_fetch<EPI>(p.e, row, first, N, fetched);
-            // one lane asks: 256 threads asking at once slow the two that feed the tensor cores
+            // one lane asks for all
             bool ready = false;
             if (lane == 0) ready = tc::mbar_wait(&ready_bar[buf], (n >> 1) & 1, &abort_flag, g.status, 0x305);
             if (!__shfl_sync(0xFFFFFFFFu, ready, 0)) break;
