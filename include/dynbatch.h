@@ -589,7 +589,7 @@ db_status db_contract_f32(const float* A, int64_t a_row, int64_t a_k,
  * adding into the accumulator truncates (up to about 4e-9 * rows, relative, towards
  * zero).  Calls on one stream may share a workspace, calls that may overlap on the device
  * (captured graphs of such calls too) need distinct ones.  Launches: forward 1 (linear), 2
- * (block), backward 2 to 4 (linear), 3 (block), one more for each product whose reduction is
+ * (block), backward 2 or 3 (linear), 3 (block), one more for each product whose reduction is
  * split and for operands off the grid; rows = 0: memsets.
  * ------------------------------------------------------------------------ */
 typedef enum {

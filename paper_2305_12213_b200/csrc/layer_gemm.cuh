@@ -46,6 +46,24 @@ struct Problem {
     EpilogueArgs e;
 };
 
+// Column sums to be finished on the side: out[c] = sum over i of sums[i][c], i ascending.
+struct BiasFold {
+    const float* sums = nullptr;        // [slabs][pitch]; nullptr: none
+    long long pitch = 0;
+    int slabs = 0, cols = 0, out_f32 = 0;
+    void* out = nullptr;
+};
+// 32 columns a warp
+__device__ __forceinline__ void fold_bias(const BiasFold& f, long long warp, long long warps, int lane) {
+    for (long long c = warp * 32 + lane; c < f.cols; c += warps * 32) {
+        float s = 0.f;
+#pragma unroll 8
+        for (int i = 0; i < f.slabs; ++i) s += f.sums[i * f.pitch + c];
+        if (f.out_f32) static_cast<float*>(f.out)[c] = s;
+        else static_cast<__nv_bfloat16*>(f.out)[c] = __float2bfloat16_rn(s);
+    }
+}
+
 struct GemmArgs {
     Problem p[kMaxProblems];
     int tile_start[kMaxProblems + 1];   // first tile of a problem, and their number; a tile for each split
@@ -54,6 +72,7 @@ struct GemmArgs {
     float* partials;                    // [problem][split][gate, up][M][columns rounded up to 32]
     int* status;
     int clear_status;                   // the first CTA zeroes *status
+    BiasFold bias;                      // kEpiStore: done by the epilogue's warps while they have no accumulator yet
 };
 
 // ------------------------------------------------------------------------------------------------ PTX wrappers
@@ -348,6 +367,8 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
     } else {
         const int quarter = warp & 3, part = (warp - 2) >> 2;
         constexpr int kPerWarp = kTileN * 4 / S::kEpilogueWarps;
+        if (EPI == kEpiStore && g.bias.sums)
+            fold_bias(g.bias, static_cast<long long>(blockIdx.x) * S::kEpilogueWarps + warp - 2, static_cast<long long>(gridDim.x) * S::kEpilogueWarps, lane);
         int n = 0;
         for (int t = worker; t < total; t += workers, ++n) {
             const Tile tile = decode(g, t);

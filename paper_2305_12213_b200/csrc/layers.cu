@@ -149,25 +149,11 @@ ActGradFn act_grad_fn(int act, bool e4m3) {
     }
 }
 
-// Column sums: each warp adds every eighth slab's sums of 32 columns, then the warps' are added in order.
-__global__ void __launch_bounds__(256)
-bias_fold_kernel(const float* sums, long long pitch, int slabs, int cols, void* out, int out_f32) {
-    __shared__ float part[8][32];
+// The column sums where no product follows that would finish them on the side.
+__global__ void __launch_bounds__(128) bias_fold_kernel(const __grid_constant__ lg::BiasFold f) {
     tc::griddep_wait();
     tc::griddep_launch_dependents();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = blockIdx.x * 32 + lane;
-    float s = 0.f;
-    if (c < cols) {
-#pragma unroll 10
-        for (int i = warp; i < slabs; i += 8) s += sums[i * pitch + c];
-    }
-    part[warp][lane] = s;
-    __syncthreads();
-    if (warp != 0 || c >= cols) return;
-#pragma unroll
-    for (int w = 1; w < 8; ++w) s += part[w][lane];
-    if (out_f32) static_cast<float*>(out)[c] = s;
-    else static_cast<bf16*>(out)[c] = __float2bfloat16_rn(s);
+    lg::fold_bias(f, (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) / 32, gridDim.x * (blockDim.x / 32), threadIdx.x & 31);
 }
 
 // ---------------------------------------------------------------------------------------------- launches
@@ -345,7 +331,8 @@ struct Product {
 
 long long depth(Kind kind, const Matrix& a) { return kind == kWeightGrad ? a.rows : a.cols; }
 
-db_status run_products(Kind kind, const Product* products, int n, float* partials, int* status, bool& clear, cudaStream_t stream) {
+db_status run_products(Kind kind, const Product* products, int n, float* partials, int* status, bool& clear, cudaStream_t stream,
+                       const lg::BiasFold& bias = {}) {
     const bool a_mn = kind == kWeightGrad, b_mn = kind != kInputGrad && kind != kGatedGrad;
     lg::GemmArgs g;
     std::memset(static_cast<void*>(&g), 0, sizeof g);
@@ -387,6 +374,7 @@ db_status run_products(Kind kind, const Product* products, int n, float* partial
     g.partials = partials;
     g.status = status;
     g.clear_status = clear;
+    g.bias = bias;
     clear = false;
     const GemmFn fn = gemm_fn(kind, plan.shape);
     const db_status st = allow_smem(kind, plan.shape, fn, shape.smem);
@@ -546,6 +534,7 @@ db_status linear_backward(const LinearGradArgs& v, Arena& arena, cudaStream_t st
     const void* off = aligned ? nullptr : reinterpret_cast<const void*>(2);
     const bool has_act = count || v.act != DB_ACT_NONE, want_bias = count || v.dbias, want_dw = count || v.dw, want_dx = count || v.dx;
     Matrix dz{static_cast<const bf16*>(v.dy), v.rows, v.n_out, v.dy_pitch};
+    lg::BiasFold bias;
     Operands ops(arena);
     if (has_act || want_bias) {
         ActGradArgs a{};
@@ -572,10 +561,10 @@ db_status linear_backward(const LinearGradArgs& v, Arena& arena, cudaStream_t st
             clear = false;
             Launch L(dim3(static_cast<unsigned>(cdiv(v.n_out, 256)), used), dim3(256), 0, stream);
             DB_CUDA_TRY(cudaLaunchKernelEx(&L.cfg, act_grad_fn(a.act, a.z_e4m3), a));
-            if (want_bias) {
-                Launch F(dim3(static_cast<unsigned>(cdiv(v.n_out, 32))), dim3(256), 0, stream);
-                DB_CUDA_TRY(cudaLaunchKernelEx(&F.cfg, bias_fold_kernel, static_cast<const float*>(a.sums), a.sums_pitch, used, v.n_out,
-                                               v.dbias, v.grad_dtype == DB_F32 ? 1 : 0));
+            if (want_bias) bias = {a.sums, a.sums_pitch, used, v.n_out, v.grad_dtype == DB_F32 ? 1 : 0, v.dbias};
+            if (want_bias && !want_dx && !want_dw) {
+                Launch F(dim3(static_cast<unsigned>(cdiv(v.n_out, 128))), dim3(128), 0, stream);
+                DB_CUDA_TRY(cudaLaunchKernelEx(&F.cfg, bias_fold_kernel, bias));
             }
         }
     }
@@ -602,8 +591,8 @@ db_status linear_backward(const LinearGradArgs& v, Arena& arena, cudaStream_t st
     }
     if (count) return DB_OK;
     db_status st = ops.copy_now(status, clear, stream);
-    if (st == DB_OK && want_dx) st = run_products(kInputGrad, &p, 1, partials, status, clear, stream);
-    if (st == DB_OK && want_dw) st = run_products(kWeightGrad, &q, 1, partials, status, clear, stream);
+    if (st == DB_OK && want_dx) st = run_products(kInputGrad, &p, 1, partials, status, clear, stream, bias);
+    if (st == DB_OK && want_dw) st = run_products(kWeightGrad, &q, 1, partials, status, clear, stream, want_dx ? lg::BiasFold{} : bias);
     return st;
 }
 
