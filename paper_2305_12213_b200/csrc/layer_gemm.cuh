@@ -449,10 +449,15 @@ combine_kernel(const __grid_constant__ GemmArgs g) {
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-            for (int s = 0; s < g.splits; ++s) {
-                const float4 q = *reinterpret_cast<const float4*>(from + s * step + part * plane);
-                sum.x += q.x; sum.y += q.y; sum.z += q.z; sum.w += q.w;
+            for (int s0 = 0; s0 < g.splits; s0 += 8) {
+                float4 q[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    q[j] = s0 + j < g.splits ? *reinterpret_cast<const float4*>(from + (s0 + j) * step + part * plane) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    sum.x += q[j].x; sum.y += q[j].y; sum.z += q[j].z; sum.w += q[j].w;
+                }
             }
             sums[part][threadIdx.x / 8][threadIdx.x % 8] = sum;
         }

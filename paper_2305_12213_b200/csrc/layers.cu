@@ -270,12 +270,13 @@ long long tiles_of(Kind kind, TileShape shape, const Size& s) {
 
 // The tile shape and the number of pieces of the reduction with the least estimated time, in SM cycles.
 // A 64-deep block of a tile costs its products or its copies (about 57 bytes a cycle reach an SM), whichever is longer,
-// more for each of two CTAs on an SM; a tile something for its start and end; and a reduction in pieces a second kernel and
-// the traffic of the partial sums.  (256 x 2048 x 1000 in 64-column tiles, us: one piece 11.9, four 10.8, eight 9.3, sixteen
-// 11.9; 1024 x 1024 x 1024: one 8.3, two 14.4; pairs of 256 columns there 11.4.)
+// more for each of two CTAs on an SM; a tile something for its start and end; and a reduction in pieces a second kernel,
+// which reads eight pieces at a time, and the traffic of the partial sums.  In 64-column tiles, us by pieces 1, 4, 8, 16:
+// 256 x 2048 x 1000 11.9, 10.2, 9.3, 11.9; 16 x 2048 x 512 above 7.4, 7.3, 6.7, 6.8 (32: 8.4); 1000 x 1024 x 256 7.7, 8.7, 8.8;
+// 1024 x 1024 x 1024 8.3, in two 14.4, in pairs of 256 columns 11.4.
 Plan make_plan(Kind kind, const Size* sizes, int n, long long blocks) {
     constexpr double kBlock[kTileShapes] = {560, 430, 560, 380}, kShared[kTileShapes] = {560, 430, 900, 550};
-    constexpr double kTile[kTileShapes] = {4700, 3100, 1500, 1300}, kCombine = 3500;
+    constexpr double kTile[kTileShapes] = {4700, 3100, 1500, 1300}, kCombine = 4500, kEight = 1000;
     Plan best;
     if (blocks == 0 || n == 0) return best;                  // no rows: nothing is launched
     for (int j = 0; j < n; ++j)
@@ -294,7 +295,7 @@ Plan make_plan(Kind kind, const Size* sizes, int n, long long blocks) {
         for (long long want = std::min(blocks, std::max(1LL, workers / tiles));; want = (want + 1) / 2) {
             const long long per = cdiv(blocks, want), splits = cdiv(blocks, per), ctas = tiles * splits;
             const double time = static_cast<double>(cdiv(ctas, workers)) * per * (ctas > alone ? kShared[i] : kBlock[i]) + kTile[i] +
-                                (splits > 1 ? kCombine + outputs * (splits + 1) * 4 / 6000.0 : 0);
+                                (splits > 1 ? kCombine + kEight * cdiv(splits, 8) + outputs * (splits + 1) * 4 / 6000.0 : 0);
             if (least == 0 || time < least) {
                 least = time;
                 best.shape = shape;
