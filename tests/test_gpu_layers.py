@@ -539,3 +539,101 @@ def test_activations_far_out(act):
     slope = ref.slope(xd, act)
     # dz is rounded to bf16, and again as dx
     assert ((f64(dx)[:, 0] - slope).abs() <= 2.01 * BF16 * slope.abs() + 4 * FAST)[:-2].all()
+
+
+@pytest.mark.parametrize("rows,n,m,aligned", [(5, 16, 24, True), (130, 33, 70, False), (256, 2048, 1000, True), (40, 4096, 64, True),
+                                              (3000, 64, 264, True), (333, 1001, 777, False)])
+def test_nothing_is_written_behind_the_workspace(rows, n, m, aligned):
+    def scratch(nbytes):
+        whole = torch.full((nbytes + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+        return whole[:nbytes], whole[nbytes:]
+
+    x, w, dy = normal(1, rows, n), normal(2, n, m, std=0.05), normal(3, rows, m)
+    z, y = torch.empty(rows, m, dtype=bf16, device="cuda"), torch.empty(rows, m, dtype=bf16, device="cuda")
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(m, dtype=bf16, device="cuda")
+    ws, behind = scratch(binding.linear_workspace_bytes(rows, n, m, aligned))
+    binding.linear(x, w, y, ws, activation="silu", z=z)
+    assert (behind == 0xA5).all() and binding.layer_status(ws) == 0
+    ws, behind = scratch(binding.linear_grad_workspace_bytes(rows, n, m, aligned))
+    binding.linear_grad(dy, x, w, ws, z=z, activation="silu", dx=dx, dw=dw, dbias=db)
+    assert (behind == 0xA5).all() and binding.layer_status(ws) == 0
+    wd, yn = normal(4, m, n, std=0.05), torch.empty_like(x)
+    ws, behind = scratch(binding.gated_ffn_workspace_bytes(rows, n, m, aligned))
+    binding.gated_ffn(x, w, w, wd, yn, ws, gate=z, up=y)
+    assert (behind == 0xA5).all() and binding.layer_status(ws) == 0
+    ws, behind = scratch(binding.gated_ffn_grad_workspace_bytes(rows, n, m, aligned))
+    binding.gated_ffn_grad(yn, x, w, w, wd, z, y, ws, dx=dx, dw_gate=dw, dw_up=torch.empty_like(w), dw_down=torch.empty_like(wd))
+    assert (behind == 0xA5).all() and binding.layer_status(ws) == 0
+    tokens = torch.randint(-1, m, (rows,), generator=gen(5), device="cuda", dtype=torch.int32)
+    ws, behind = scratch(binding.embedding_grad_workspace_bytes(rows, m, n))
+    table = torch.full((m + 1, n), 7.0, dtype=bf16, device="cuda")
+    binding.embedding_grad(tokens, x, table[:m], ws)
+    assert (behind == 0xA5).all() and (table[m] == 7).all()
+
+
+def test_linear_gradients_against_differences():
+    rows, n, m = 24, 16, 40
+    x, w, dy = normal(1, rows, n, std=0.5), normal(2, n, m, std=0.5), normal(3, rows, m, std=0.5)
+    b = normal(4, m, std=0.5)
+    z, y = torch.empty(rows, m, dtype=bf16, device="cuda"), torch.empty(rows, m, dtype=bf16, device="cuda")
+    ws = workspace(max(binding.linear_workspace_bytes(rows, n, m), binding.linear_grad_workspace_bytes(rows, n, m)))
+    binding.linear(x, w, y, ws, bias=b, activation="silu", z=z)
+    got = {"x": torch.empty_like(x), "w": torch.empty_like(w), "b": torch.empty_like(b)}
+    binding.linear_grad(dy, x, w, ws, z=z, activation="silu", dx=got["x"], dw=got["w"], dbias=got["b"])
+    v = {"x": f64(x), "w": f64(w), "b": f64(b)}
+    loss = lambda v: float((ref.act(v["x"] @ v["w"] + v["b"], "silu") * f64(dy)).sum())  # noqa: E731
+    g = torch.Generator().manual_seed(4)
+    for name in v:
+        d = torch.randn(v[name].shape, generator=g, dtype=torch.float64)
+        e = 1e-5
+        slope = (loss({**v, name: v[name] + e * d}) - loss({**v, name: v[name] - e * d})) / (2 * e)
+        mine = float((f64(got[name]) * d).sum())
+        # three roundings of 2^-8 an element (z, dz, itself), with signs of their own
+        assert abs(mine - slope) <= 3 * BF16 * float((f64(got[name]) * d).norm()) * 3 + 1e-6 * abs(slope), name
+
+
+def test_host_threads_with_streams_and_workspaces_of_their_own():
+    import threading
+
+    rows, n, m = 300, 128, 256
+    w, wd = normal(1, n, m, std=0.1), normal(2, m, n, std=0.06)
+    tokens = torch.randint(-1, 50, (rows,), generator=gen(3), device="cuda", dtype=torch.int32)
+    inputs = [normal(10 + i, rows, n) for i in range(4)]
+
+    def work(x, ws, out, keep):
+        binding.gated_ffn(x, w, w, wd, out["y"], ws, residual=x, **keep)
+        binding.gated_ffn_grad(out["y"], x, w, w, wd, workspace=ws, **keep, dx=out["dx"], dw_down=out["dw"])
+        binding.embedding_grad(tokens, out["dx"], out["table"], ws)
+
+    def buffers():
+        size = max(binding.gated_ffn_workspace_bytes(rows, n, m), binding.gated_ffn_grad_workspace_bytes(rows, n, m),
+                   binding.embedding_grad_workspace_bytes(rows, 50, n))
+        out = {"y": torch.zeros(rows, n, dtype=bf16, device="cuda"), "dx": torch.zeros(rows, n, dtype=bf16, device="cuda"),
+               "dw": torch.zeros(m, n, device="cuda"), "table": torch.zeros(50, n, device="cuda")}
+        return workspace(size), out, kept_buffers(rows, m, "e4m3", ["gate", "up"])
+
+    alone = [buffers() for _ in inputs]
+    for x, b in zip(inputs, alone):
+        work(x, *b)
+    torch.cuda.synchronize()
+    together, failed = [buffers() for _ in inputs], []
+
+    def thread(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    work(inputs[i], *together[i])
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=thread, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed
+    for a, b in zip(alone, together):
+        for k in a[1]:
+            assert torch.equal(a[1][k], b[1][k]), k
