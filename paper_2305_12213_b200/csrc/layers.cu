@@ -212,9 +212,19 @@ db_status make_map(CUtensorMap* map, const Matrix& m, int box_rows) {
     const cuuint64_t strides[1] = {static_cast<cuuint64_t>(m.pitch) * 2};
     const cuuint32_t box[2] = {lg::kBlockK, static_cast<cuuint32_t>(box_rows)};
     const cuuint32_t elem[2] = {1, 1};
-    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<bf16*>(m.p), dims, strides, box, elem,
-                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const auto encode = [&] {
+        return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<bf16*>(m.p), dims, strides, box, elem,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = encode();
+    if (r != CUDA_SUCCESS) {
+        // a host thread that has not yet called the runtime for its device has no context, which the driver's call needs
+        int device = 0;
+        DB_CUDA_TRY(cudaGetDevice(&device));
+        DB_CUDA_TRY(cudaSetDevice(device));
+        r = encode();
+    }
     if (r != CUDA_SUCCESS) {
         record_message("cuTensorMapEncodeTiled rejected an operand of a layer");
         return DB_ERR_CUDA;
