@@ -76,8 +76,11 @@ struct GemmArgs {
 };
 
 // ------------------------------------------------------------------------------------------------ PTX wrappers
+// Instructions marked .aligned want all lanes of the warp at the same instruction.  Code that lanes leave and rejoin (rows past
+// the end, a row's own alignment) may stand before any of them, so each wrapper converges its warp itself.
 template <int CG>
 __device__ __forceinline__ void tmem_alloc(uint32_t* slot, uint32_t columns) {
+    __syncwarp();
     if (CG == 2) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(slot)), "r"(columns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -87,8 +90,14 @@ __device__ __forceinline__ void tmem_alloc(uint32_t* slot, uint32_t columns) {
 }
 template <int CG>
 __device__ __forceinline__ void tmem_dealloc(uint32_t base, uint32_t columns) {
+    __syncwarp();
     if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns) : "memory");
     else tc::tmem_dealloc(base, columns);
+}
+// 32 columns of the warp's 32 rows of an accumulator, a row for each lane.
+__device__ __forceinline__ void load_accumulator(uint32_t at, uint32_t (&raw)[32]) {
+    __syncwarp();
+    tc::tmem_load32(at, raw);
 }
 template <int CG>
 __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
@@ -124,6 +133,7 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     return r;
 }
 __device__ __forceinline__ void cluster_sync() {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // Address of the same shared-memory word in the pair's first CTA.
@@ -397,16 +407,15 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
             };
 #pragma unroll 1
             for (int c = 0; c < columns; c += kChunk) {
-                __syncwarp();                                  // rows past the end rejoin for the next read
                 const int col = first + c;
                 if (in && c > 0) epilogue_fetch<EPI>(p.e, row, col, N, fetched);
                 uint32_t raw[kChunk];
                 Pair v[kChunk / 2], u[kChunk / 2];
-                tc::tmem_load32(acc + c, raw);
+                load_accumulator(acc + c, raw);
 #pragma unroll
                 for (int i = 0; i < kChunk / 2; ++i) v[i] = pair(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1]));
                 if (EPI == kEpiGated) {
-                    tc::tmem_load32(acc + kTileN + c, raw);
+                    load_accumulator(acc + kTileN + c, raw);
 #pragma unroll
                     for (int i = 0; i < kChunk / 2; ++i) u[i] = pair(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1]));
                 }
