@@ -330,6 +330,7 @@ constexpr int kClusterThreads = 32 * kClusterWarps;
 constexpr int kClusterSmem = 2 * kClusterThreads * kMaxSteps * 4 + kClusterWarps * kBins * 2;
 
 __device__ __forceinline__ void cluster_sync() {
+    __syncwarp();                                  // .aligned: behind stores that only lanes with an entry made
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ int load_cluster(const int* p, int rank) {
