@@ -121,6 +121,11 @@ __device__ __forceinline__ void mma_commit(uint64_t* bar) {
     else
         tc::mma_commit(bar);
 }
+// A whole warp's bounded wait.  Lanes that poll on their own may differ where the limit runs out or the other warps give up, and
+// those that went on would wait at the next full-warp instruction for those that left: all go on, or all leave.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
+    return __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar, parity, abort_flag, status, code));
+}
 // True in one lane of a converged warp, always the same one.
 __device__ __forceinline__ bool elect_one() {
     uint32_t mine;
@@ -291,7 +296,7 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
             // what this CTA holds of B: gated, a pair's CTAs take one weight each, a single CTA half of both
             const int n0 = tile.n * kTileN + (EPI == kEpiGated ? 0 : static_cast<int>(rank) * S::kBRows);
             for (; k < k_end; ++k, ++it) {
-                if (!(ok = tc::mbar_wait(&empty_bar[stage], phase ^ 1, &abort_flag, g.status, 0x301))) break;
+                if (!(ok = warp_wait(&empty_bar[stage], phase ^ 1, &abort_flag, g.status, 0x301))) break;
                 if (elect_one()) {
                     const uint32_t bar = CG == 2 ? in_first_cta(&full_bar[stage]) : tc::smem_u32(&full_bar[stage]);
                     if (rank == 0) expect_tx(&full_bar[stage], CG * S::kStageBytes);
@@ -323,7 +328,7 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
         // every product that reads this CTA's stages has finished, and its arrival has reached this CTA
         for (int i = 0; i < S::kStages && ok && i < it; ++i) {
             if (--stage < 0) { stage = S::kStages - 1; phase ^= 1; }
-            ok = tc::mbar_wait(&empty_bar[stage], phase, &abort_flag, g.status, 0x302);
+            ok = warp_wait(&empty_bar[stage], phase, &abort_flag, g.status, 0x302);
         }
         if (!ok) {
             // copies under way land within microseconds; their barrier may be the other CTA's
@@ -344,12 +349,12 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
                 int k, k_end;
                 k_range(g, tile, k, k_end);
                 const int buf = n & 1;
-                if (!(ok = tc::mbar_wait(&taken_bar[buf], ((n >> 1) & 1) ^ 1, &abort_flag, g.status, 0x303))) break;
+                if (!(ok = warp_wait(&taken_bar[buf], ((n >> 1) & 1) ^ 1, &abort_flag, g.status, 0x303))) break;
                 tc::tc_fence_after();
                 const uint32_t acc = tmem + buf * BN;
                 uint32_t accumulate = 0;
                 for (; k < k_end; ++k) {
-                    if (!(ok = tc::mbar_wait(&full_bar[stage], phase, &abort_flag, g.status, 0x304))) break;
+                    if (!(ok = warp_wait(&full_bar[stage], phase, &abort_flag, g.status, 0x304))) break;
                     tc::tc_fence_after();
                     if (elect_one()) {
                         const uint32_t a = base + stage * S::kStageBytes;

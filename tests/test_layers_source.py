@@ -1,5 +1,5 @@
 """Rules of the layers' kernels that no run can show to be broken, checked in their source: a warp-wide .aligned instruction is
-reached by a converged warp."""
+reached by a converged warp, and a wait's verdict is the same in all lanes of a warp that goes on as one."""
 import os
 import re
 
@@ -38,3 +38,16 @@ def test_aligned_instructions_are_reached_by_converged_warps(name, at_least):
             assert len(re.findall(r"\bfor\b|\bwhile\b", body[before:at])) == 0, function
             found += 1
     assert found >= at_least
+
+
+def test_waits_have_one_verdict_for_a_warp():
+    """A time-limited wait ends in each lane on its own: its result is shared by the warp before anything branches on it."""
+    waits = 0
+    for function, body in functions("layer_gemm.cuh"):
+        for line in body.splitlines():
+            if "tc::mbar_wait(" in line:
+                shared = "__all_sync(0xFFFFFFFFu, tc::mbar_wait(" in line
+                one_lane = "if (lane == 0) ready = tc::mbar_wait(" in line and "__shfl_sync(0xFFFFFFFFu, ready, 0)" in body
+                assert shared or one_lane, (function, line.strip())
+            waits += line.count("mbar_wait(") + line.count("warp_wait(")
+    assert waits >= 6
