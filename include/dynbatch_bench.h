@@ -63,6 +63,29 @@ db_status db_bench_aggregate_variant(db_bench_variant variant, int32_t stage_flo
 db_status db_bench_wait_timeout(int32_t* status, int32_t code, uint64_t limit_ns,
                                 void* cuda_stream);
 
+/* Which kernel a product of the layers (db_linear and the others) runs on the
+ * current device (148 SMs where there is none): CTAs that share a tile (1, or
+ * 2 for a pair), columns of its accumulator, and the pieces its reduction is cut into
+ * (above 1 a second kernel joins them).  The calls take their plan from the same
+ * functions, so a test can pick sizes that reach a kernel, and fails once the
+ * plan no longer picks it.  n_in and n_out are width and hidden for the gated
+ * block; DB_BENCH_GATED_DW is all three weight gradients at once. */
+typedef enum {
+    DB_BENCH_LINEAR_Y = 0,
+    DB_BENCH_LINEAR_DX = 1,
+    DB_BENCH_LINEAR_DW = 2,
+    DB_BENCH_GATED_H = 3,  /* gate, up and h */
+    DB_BENCH_GATED_Y = 4,
+    DB_BENCH_GATED_DH = 5, /* dh with d_gate, d_up and h */
+    DB_BENCH_GATED_DX = 6,
+    DB_BENCH_GATED_DW = 7
+} db_bench_layer_product;
+
+db_status db_bench_layer_plan(db_bench_layer_product product, int64_t rows,
+                              int32_t n_in, int32_t n_out,
+                              int32_t* ctas_per_tile, int32_t* tile_columns,
+                              int32_t* pieces);
+
 #if defined(__GNUC__)
 #pragma GCC visibility pop
 #endif

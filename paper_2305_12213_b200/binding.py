@@ -72,6 +72,7 @@ _SIGNATURES = {
     "db_bench_read_probe_sink_bytes": (c_size_t, [c_size_t]),
     "db_bench_read_probe": (c_int32, [c_void_p, c_size_t, c_void_p, c_void_p]),
     "db_bench_wait_timeout": (c_int32, [c_void_p, c_int32, ctypes.c_uint64, c_void_p]),
+    "db_bench_layer_plan": (c_int32, [c_int32, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_void_p]),
     "db_bench_aggregate_variant": (c_int32, [c_int32, c_int32, c_void_p, c_void_p, c_int32, c_int64, c_void_p,
                                              c_void_p, c_float, c_float, c_void_p, c_void_p]),
     "db_host_pipeline_create": (c_int32, [c_void_p]),
@@ -309,6 +310,18 @@ def bench_wait_timeout(status: torch.Tensor, code: int, limit_ns: int,
     """db_bench_wait_timeout: run the kernels' bounded wait until it gives up and reports `code`."""
     _check(lib().db_bench_wait_timeout(_dev_ptr(status, torch.int32, "status"), int(code), int(limit_ns),
                                        _stream_ptr(stream)))
+
+
+DB_BENCH_LAYER_PRODUCTS = {"linear_y": 0, "linear_dx": 1, "linear_dw": 2, "gated_h": 3, "gated_y": 4, "gated_dh": 5,
+                           "gated_dx": 6, "gated_dw": 7}
+
+
+def bench_layer_plan(product: str, rows: int, n_in: int, n_out: int):
+    """db_bench_layer_plan: (CTAs that share a tile, columns of a tile, pieces of the reduction) of a layer's product."""
+    out = (c_int32 * 3)()
+    at = ctypes.addressof(out)
+    _check(lib().db_bench_layer_plan(DB_BENCH_LAYER_PRODUCTS[product], int(rows), int(n_in), int(n_out), at, at + 4, at + 8))
+    return tuple(out)
 
 
 def bench_aggregate_variant(variant: int, stage_floats: int, grads: Sequence[torch.Tensor], b: Sequence[int],

@@ -5,6 +5,7 @@
 #include <cstring>
 
 #include "common.h"
+#include "dynbatch_bench.h"
 #include "layer_gemm.cuh"
 
 namespace dynbatch {
@@ -319,6 +320,27 @@ Plan make_plan(Kind kind, const Size* sizes, int n, long long blocks) {
     return best;
 }
 
+// The products of the layers.  A call's workspace, its launches and db_bench_layer_plan take a product's plan from here.
+Plan plan_forward(long long rows, long long n_in, long long n_out) {                // x w; h w_down
+    const Size size{rows, n_out};
+    return make_plan(kForward, &size, 1, cdiv(n_in, lg::kBlockK));
+}
+Plan plan_input_grad(long long rows, long long n_in, long long n_out, int sources) {   // dz w^T, or the sum of two of them
+    const Size size{rows, n_in};
+    return make_plan(kInputGrad, &size, 1, sources * cdiv(n_out, lg::kBlockK));
+}
+Plan plan_gated(long long rows, long long width, long long hidden) {                // gate and up
+    const Size size{rows, hidden};
+    return make_plan(kGated, &size, 1, cdiv(width, lg::kBlockK));
+}
+Plan plan_gated_grad(long long rows, long long width, long long hidden) {           // dh
+    const Size size{rows, hidden};
+    return make_plan(kGatedGrad, &size, 1, cdiv(width, lg::kBlockK));
+}
+Plan plan_weight_grad(const Size* sizes, int n, long long rows) {                   // x^T dz, up to three at once
+    return make_plan(kWeightGrad, sizes, n, cdiv(rows, lg::kBlockK));
+}
+
 // Once per kernel and device: the attribute call costs a microsecond.
 db_status allow_smem(Kind kind, TileShape shape, GemmFn fn, int bytes) {
     constexpr int kDevices = 64;
@@ -342,24 +364,19 @@ struct Product {
 
 long long depth(Kind kind, const Matrix& a) { return kind == kWeightGrad ? a.rows : a.cols; }
 
-db_status run_products(Kind kind, const Product* products, int n, float* partials, int* status, bool& clear, cudaStream_t stream,
-                       const lg::BiasFold& bias = {}) {
+db_status run_products(Kind kind, const Plan& plan, const Product* products, int n, float* partials, int* status, bool& clear,
+                       cudaStream_t stream, const lg::BiasFold& bias = {}) {
     const bool a_mn = kind == kWeightGrad, b_mn = kind != kInputGrad && kind != kGatedGrad;
     lg::GemmArgs g;
     std::memset(static_cast<void*>(&g), 0, sizeof g);
-    Size sizes[lg::kMaxProblems];
-    long long blocks = 0;
     for (int i = 0; i < n; ++i) {
-        sizes[i] = products[i].size;
         lg::Problem& p = g.p[i];
-        p.M = static_cast<int>(sizes[i].M);
-        p.N = static_cast<int>(sizes[i].N);
+        p.M = static_cast<int>(products[i].size.M);
+        p.N = static_cast<int>(products[i].size.N);
         p.blocks0 = static_cast<int>(cdiv(depth(kind, products[i].a[0]), lg::kBlockK));
         p.blocks = p.blocks0 + (products[i].sources > 1 ? static_cast<int>(cdiv(depth(kind, products[i].a[1]), lg::kBlockK)) : 0);
-        blocks = std::max<long long>(blocks, p.blocks);
         p.e = products[i].e;
     }
-    const Plan plan = make_plan(kind, sizes, n, blocks);
     const ShapeInfo& shape = kShapes[plan.shape];
     const int tile_n = kind == kGated ? shape.bn / 2 : shape.bn;
     long long tiles = 0, floats = 0;
@@ -517,11 +534,11 @@ db_status linear_forward(const LinearArgs& v, Arena& arena, cudaStream_t stream,
     p.e.kept[0] = {v.z, static_cast<uint8_t*>(v.z_scale)};
     p.e.kept_e4m3 = v.z_dtype == DB_E4M3;
     p.e.act = v.act;
-    const Plan plan = make_plan(kForward, &p.size, 1, cdiv(v.n_in, lg::kBlockK));
+    const Plan plan = plan_forward(v.rows, v.n_in, v.n_out);
     float* partials = reinterpret_cast<float*>(arena.take(static_cast<size_t>(plan.partial_floats) * 4));
     if (count) return DB_OK;
     const db_status st = ops.copy_now(status, clear, stream);
-    return st != DB_OK ? st : run_products(kForward, &p, 1, partials, status, clear, stream);
+    return st != DB_OK ? st : run_products(kForward, plan, &p, 1, partials, status, clear, stream);
 }
 
 struct LinearGradArgs {
@@ -580,10 +597,8 @@ db_status linear_backward(const LinearGradArgs& v, Arena& arena, cudaStream_t st
         }
     }
     if (count ? !aligned : !has_act && (want_dx || want_dw)) dz = ops.of(count ? off : v.dy, v.rows, v.n_out, count ? v.n_out : v.dy_pitch);
-    Plan plan_x, plan_w;
     const Size size_x{v.rows, v.n_in}, size_w{v.n_in, v.n_out};
-    plan_x = make_plan(kInputGrad, &size_x, 1, cdiv(v.n_out, lg::kBlockK));
-    plan_w = make_plan(kWeightGrad, &size_w, 1, cdiv(v.rows, lg::kBlockK));
+    const Plan plan_x = plan_input_grad(v.rows, v.n_in, v.n_out, 1), plan_w = plan_weight_grad(&size_w, 1, v.rows);
     float* partials = reinterpret_cast<float*>(arena.take(static_cast<size_t>(std::max(plan_x.partial_floats, plan_w.partial_floats)) * 4));
     Product p, q;
     if (want_dx) {
@@ -602,8 +617,8 @@ db_status linear_backward(const LinearGradArgs& v, Arena& arena, cudaStream_t st
     }
     if (count) return DB_OK;
     db_status st = ops.copy_now(status, clear, stream);
-    if (st == DB_OK && want_dx) st = run_products(kInputGrad, &p, 1, partials, status, clear, stream, bias);
-    if (st == DB_OK && want_dw) st = run_products(kWeightGrad, &q, 1, partials, status, clear, stream, want_dx ? lg::BiasFold{} : bias);
+    if (st == DB_OK && want_dx) st = run_products(kInputGrad, plan_x, &p, 1, partials, status, clear, stream, bias);
+    if (st == DB_OK && want_dw) st = run_products(kWeightGrad, plan_w, &q, 1, partials, status, clear, stream, want_dx ? lg::BiasFold{} : bias);
     return st;
 }
 
@@ -643,12 +658,12 @@ db_status gated_forward(const GatedArgs& v, Arena& arena, cudaStream_t stream, b
     q.size = {v.rows, v.width};
     q.e.out = v.y; q.e.out_pitch = v.y_pitch;
     q.e.addend = static_cast<const bf16*>(v.residual); q.e.addend_pitch = v.residual_pitch;
-    const Plan a = make_plan(kGated, &p.size, 1, cdiv(v.width, lg::kBlockK)), b = make_plan(kForward, &q.size, 1, cdiv(v.hidden, lg::kBlockK));
+    const Plan a = plan_gated(v.rows, v.width, v.hidden), b = plan_forward(v.rows, v.hidden, v.width);
     float* partials = reinterpret_cast<float*>(arena.take(static_cast<size_t>(std::max(a.partial_floats, b.partial_floats)) * 4));
     if (count) return DB_OK;
     db_status st = ops.copy_now(status, clear, stream);
-    if (st == DB_OK) st = run_products(kGated, &p, 1, partials, status, clear, stream);
-    return st != DB_OK ? st : run_products(kForward, &q, 1, partials, status, clear, stream);
+    if (st == DB_OK) st = run_products(kGated, a, &p, 1, partials, status, clear, stream);
+    return st != DB_OK ? st : run_products(kForward, b, &q, 1, partials, status, clear, stream);
 }
 
 db_status gated_backward(const GatedArgs& v, Arena& arena, cudaStream_t stream, bool aligned) {
@@ -677,7 +692,7 @@ db_status gated_backward(const GatedArgs& v, Arena& arena, cudaStream_t stream, 
     p.e.kept[1] = {v.up, static_cast<uint8_t*>(v.up_scale)};
     p.e.kept_e4m3 = v.kept_dtype == DB_E4M3;
     p.e.act = v.act;
-    const Plan plan_p = make_plan(kGatedGrad, &p.size, 1, cdiv(v.width, lg::kBlockK));
+    const Plan plan_p = plan_gated_grad(v.rows, v.width, v.hidden);
 
     if (want_dx) {
         q.a[0] = mg; q.a[1] = mu;
@@ -688,7 +703,7 @@ db_status gated_backward(const GatedArgs& v, Arena& arena, cudaStream_t stream, 
         q.e.out = v.y; q.e.out_pitch = v.y_pitch;
         q.e.addend = static_cast<const bf16*>(v.residual); q.e.addend_pitch = v.residual_pitch;
     }
-    const Plan plan_q = make_plan(kInputGrad, &q.size, want_dx ? 1 : 0, 2 * cdiv(v.hidden, lg::kBlockK));
+    const Plan plan_q = want_dx ? plan_input_grad(v.rows, v.width, v.hidden, 2) : Plan{};
 
     int n = 0;
     Size sizes[3];
@@ -712,19 +727,18 @@ db_status gated_backward(const GatedArgs& v, Arena& arena, cudaStream_t stream, 
     // which weight gradients a call wants decides how its reduction is split: room for any choice
     if (count) {
         const Size up{v.width, v.hidden}, down{v.hidden, v.width};
-        const Size choices[6][3] = {{up}, {down}, {up, up}, {up, down}, {up, up, down}, {up}};
-        const int counts[6] = {1, 1, 2, 2, 3, 1};
-        for (int i = 0; i < 6; ++i)
-            floats = std::max(floats, make_plan(kWeightGrad, choices[i], counts[i], cdiv(v.rows, lg::kBlockK)).partial_floats);
-    } else if (n) {
-        floats = std::max(floats, make_plan(kWeightGrad, sizes, n, cdiv(v.rows, lg::kBlockK)).partial_floats);
+        const Size choices[5][3] = {{up}, {down}, {up, up}, {up, down}, {up, up, down}};
+        const int counts[5] = {1, 1, 2, 2, 3};
+        for (int i = 0; i < 5; ++i) floats = std::max(floats, plan_weight_grad(choices[i], counts[i], v.rows).partial_floats);
     }
+    const Plan plan_w = plan_weight_grad(sizes, n, v.rows);
+    floats = std::max(floats, plan_w.partial_floats);
     float* partials = reinterpret_cast<float*>(arena.take(static_cast<size_t>(floats) * 4));
     if (count) return DB_OK;
     db_status st = ops.copy_now(status, clear, stream);
-    if (st == DB_OK) st = run_products(kGatedGrad, &p, 1, partials, status, clear, stream);
-    if (st == DB_OK && want_dx) st = run_products(kInputGrad, &q, 1, partials, status, clear, stream);
-    if (st == DB_OK && n) st = run_products(kWeightGrad, w, n, partials, status, clear, stream);
+    if (st == DB_OK) st = run_products(kGatedGrad, plan_p, &p, 1, partials, status, clear, stream);
+    if (st == DB_OK && want_dx) st = run_products(kInputGrad, plan_q, &q, 1, partials, status, clear, stream);
+    if (st == DB_OK && n) st = run_products(kWeightGrad, plan_w, w, n, partials, status, clear, stream);
     return st;
 }
 
@@ -958,4 +972,28 @@ extern "C" db_status db_gated_ffn_grad(const void* dy, int64_t dy_pitch, const v
     }
     Arena arena(workspace);
     return gated_backward(v, arena, stream, aligned);
+}
+
+extern "C" db_status db_bench_layer_plan(db_bench_layer_product product, int64_t rows, int32_t n_in, int32_t n_out,
+                                         int32_t* ctas_per_tile, int32_t* tile_columns, int32_t* pieces) {
+    using namespace dynbatch;
+    if (!ctas_per_tile || !tile_columns || !pieces) return DB_ERR_NULL;
+    if (!valid_size(rows, n_in, n_out) || rows == 0) return DB_ERR_ARG;
+    const Size up{n_in, n_out}, down{n_out, n_in}, all[3] = {up, up, down};
+    Plan p;
+    switch (product) {
+        case DB_BENCH_LINEAR_Y: p = plan_forward(rows, n_in, n_out); break;
+        case DB_BENCH_LINEAR_DX: p = plan_input_grad(rows, n_in, n_out, 1); break;
+        case DB_BENCH_LINEAR_DW: p = plan_weight_grad(&up, 1, rows); break;
+        case DB_BENCH_GATED_H: p = plan_gated(rows, n_in, n_out); break;
+        case DB_BENCH_GATED_Y: p = plan_forward(rows, n_out, n_in); break;
+        case DB_BENCH_GATED_DH: p = plan_gated_grad(rows, n_in, n_out); break;
+        case DB_BENCH_GATED_DX: p = plan_input_grad(rows, n_in, n_out, 2); break;
+        case DB_BENCH_GATED_DW: p = plan_weight_grad(all, 3, rows); break;
+        default: return DB_ERR_UNSUPPORTED;
+    }
+    *ctas_per_tile = kShapes[p.shape].cg;
+    *tile_columns = kShapes[p.shape].bn;
+    *pieces = p.splits;
+    return DB_OK;
 }
