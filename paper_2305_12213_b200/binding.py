@@ -826,8 +826,11 @@ def _grad_code(*tensors: Optional[torch.Tensor]):
 
 
 def _scratch(t: torch.Tensor, index: int):
+    """Pointer and size of a workspace: contiguous, so that its elements are the memory behind its pointer."""
     if t.get_device() != index:
         _elsewhere(t, index, "workspace")
+    if not t.is_contiguous():
+        raise TypeError("workspace must be a contiguous CUDA tensor")
     return t.data_ptr(), t.numel() * t.element_size()
 
 
