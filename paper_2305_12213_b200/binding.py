@@ -760,6 +760,12 @@ def adamw_scale_elems(n: int) -> int:
 _BF16, _E4M3, _E8M0 = torch.bfloat16, torch.float8_e4m3fn, torch.float8_e8m0fnu
 
 
+def _size(n: int, bits: int = 31) -> int:
+    """A size for an int32 (int64: bits = 63) argument, which ctypes would cut to its lowest bits: one past the type's range
+    is passed as -1, which every call refuses."""
+    return n if 0 <= n >> bits < 1 else -1
+
+
 def _device_index(first: torch.Tensor) -> int:
     index = first.get_device()
     if index < 0:
@@ -858,19 +864,19 @@ def checkpoint_scales(n: int) -> int:
 
 
 def linear_workspace_bytes(rows: int, n_in: int, n_out: int, aligned: bool = True) -> int:
-    return int(lib().db_linear_workspace_bytes(int(rows), int(n_in), int(n_out), int(aligned)))
+    return int(lib().db_linear_workspace_bytes(_size(int(rows), 63), _size(int(n_in)), _size(int(n_out)), bool(aligned)))
 
 
 def linear_grad_workspace_bytes(rows: int, n_in: int, n_out: int, aligned: bool = True) -> int:
-    return int(lib().db_linear_grad_workspace_bytes(int(rows), int(n_in), int(n_out), int(aligned)))
+    return int(lib().db_linear_grad_workspace_bytes(_size(int(rows), 63), _size(int(n_in)), _size(int(n_out)), bool(aligned)))
 
 
 def gated_ffn_workspace_bytes(rows: int, width: int, hidden: int, aligned: bool = True) -> int:
-    return int(lib().db_gated_ffn_workspace_bytes(int(rows), int(width), int(hidden), int(aligned)))
+    return int(lib().db_gated_ffn_workspace_bytes(_size(int(rows), 63), _size(int(width)), _size(int(hidden)), bool(aligned)))
 
 
 def gated_ffn_grad_workspace_bytes(rows: int, width: int, hidden: int, aligned: bool = True) -> int:
-    return int(lib().db_gated_ffn_grad_workspace_bytes(int(rows), int(width), int(hidden), int(aligned)))
+    return int(lib().db_gated_ffn_grad_workspace_bytes(_size(int(rows), 63), _size(int(width)), _size(int(hidden)), bool(aligned)))
 
 
 def linear(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, workspace: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -890,7 +896,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, workspace: torch.T
     yp, y_pitch = _rows(y, rows, n_out, index, "y")
     zp, sp, zt = _kept(z, z_scale, rows, n_out, index, "z")
     _launch(index, stream, lib().db_linear, xp, x_pitch, _whole(w, (n_in, n_out), _BF16, index, "w"),
-            _whole(bias, (n_out,), _BF16, index, "bias"), rp, r_pitch, _activation(activation), rows, n_in, n_out, yp, y_pitch,
+            _whole(bias, (n_out,), _BF16, index, "bias"), rp, r_pitch, _activation(activation), rows, _size(n_in), _size(n_out), yp, y_pitch,
             zp, sp, zt, *_scratch(workspace, index))
 
 
@@ -911,7 +917,7 @@ def linear_grad(dy: torch.Tensor, x: Optional[torch.Tensor], w: torch.Tensor, wo
     zp, sp, zt = _kept(z, z_scale, rows, n_out, index, "z")
     dtype, code = _grad_code(dw, dbias)
     _launch(index, stream, lib().db_linear_grad, dyp, dy_pitch, xp, x_pitch, _whole(w, (n_in, n_out), _BF16, index, "w"), zp, sp,
-            zt, _activation(activation), rows, n_in, n_out, dxp, dx_pitch, ap, a_pitch,
+            zt, _activation(activation), rows, _size(n_in), _size(n_out), dxp, dx_pitch, ap, a_pitch,
             _whole(dw, (n_in, n_out), dtype, index, "dw"), _whole(dbias, (n_out,), dtype, index, "dbias"), code,
             *_scratch(workspace, index))
 
@@ -939,7 +945,7 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
         raise TypeError("gate and up must have one type")
     _launch(index, stream, lib().db_gated_ffn, xp, x_pitch, _whole(w_gate, (width, hidden), _BF16, index, "w_gate"),
             _whole(w_up, (width, hidden), _BF16, index, "w_up"), _whole(w_down, (hidden, width), _BF16, index, "w_down"), rp,
-            r_pitch, _activation(activation), rows, width, hidden, yp, y_pitch, gp, upp, gs, us, gt,
+            r_pitch, _activation(activation), rows, _size(width), _size(hidden), yp, y_pitch, gp, upp, gs, us, gt,
             *_scratch(workspace, index))
 
 
@@ -966,8 +972,8 @@ def gated_ffn_grad(dy: torch.Tensor, x: Optional[torch.Tensor], w_gate: torch.Te
     dtype, code = _grad_code(dw_gate, dw_up, dw_down)
     _launch(index, stream, lib().db_gated_ffn_grad, dyp, dy_pitch, xp, x_pitch,
             _whole(w_gate, (width, hidden), _BF16, index, "w_gate"), _whole(w_up, (width, hidden), _BF16, index, "w_up"),
-            _whole(w_down, (hidden, width), _BF16, index, "w_down"), gp, upp, gs, us, gt, _activation(activation), rows, width,
-            hidden, dxp, dx_pitch, ap, a_pitch, _whole(dw_gate, (width, hidden), dtype, index, "dw_gate"),
+            _whole(w_down, (hidden, width), _BF16, index, "w_down"), gp, upp, gs, us, gt, _activation(activation), rows,
+            _size(width), _size(hidden), dxp, dx_pitch, ap, a_pitch, _whole(dw_gate, (width, hidden), dtype, index, "dw_gate"),
             _whole(dw_up, (width, hidden), dtype, index, "dw_up"), _whole(dw_down, (hidden, width), dtype, index, "dw_down"),
             code, *_scratch(workspace, index))
 
@@ -987,7 +993,7 @@ def checkpoint_pack(x: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor,
         raise TypeError("codes must be float8_e4m3fn")
     xp, pitch = _rows(x, rows, cols, index, "x")
     cp, sp, _ = _kept(codes, scale, rows, cols, index, "codes")
-    _launch(index, stream, lib().db_checkpoint_pack, xp, pitch, rows, cols, cp, sp)
+    _launch(index, stream, lib().db_checkpoint_pack, xp, pitch, rows, _size(cols), cp, sp)
 
 
 def checkpoint_unpack(codes: torch.Tensor, scale: torch.Tensor, x: torch.Tensor,
@@ -999,7 +1005,7 @@ def checkpoint_unpack(codes: torch.Tensor, scale: torch.Tensor, x: torch.Tensor,
         raise TypeError("codes must be float8_e4m3fn")
     xp, pitch = _rows(x, rows, cols, index, "x")
     cp, sp, _ = _kept(codes, scale, rows, cols, index, "codes")
-    _launch(index, stream, lib().db_checkpoint_unpack, cp, sp, rows, cols, xp, pitch)
+    _launch(index, stream, lib().db_checkpoint_unpack, cp, sp, rows, _size(cols), xp, pitch)
 
 
 def embedding(tokens: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
@@ -1011,12 +1017,12 @@ def embedding(tokens: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scal
     rows = tokens.numel()
     op, pitch = _rows(out, rows, width, index, "out", out.dtype)
     _launch(index, stream, lib().db_embedding, _whole(tokens, tokens.shape, torch.int32, index, "tokens"),
-            _whole(table, (vocab, width), table.dtype, index, "table"), _dtype_code(table.dtype), float(scale), rows, vocab,
-            width, op, pitch, _dtype_code(out.dtype))
+            _whole(table, (vocab, width), table.dtype, index, "table"), _dtype_code(table.dtype), float(scale), rows, _size(vocab),
+            _size(width), op, pitch, _dtype_code(out.dtype))
 
 
 def embedding_grad_workspace_bytes(rows: int, vocab: int, width: int) -> int:
-    return int(lib().db_embedding_grad_workspace_bytes(int(rows), int(vocab), int(width)))
+    return int(lib().db_embedding_grad_workspace_bytes(_size(int(rows), 63), _size(int(vocab)), _size(int(width))))
 
 
 def embedding_grad(tokens: torch.Tensor, dy: torch.Tensor, dtable: torch.Tensor, workspace: torch.Tensor,
@@ -1028,6 +1034,6 @@ def embedding_grad(tokens: torch.Tensor, dy: torch.Tensor, dtable: torch.Tensor,
     rows = tokens.numel()
     dp, pitch = _rows(dy, rows, width, index, "dy", dy.dtype)
     _launch(index, stream, lib().db_embedding_grad, _whole(tokens, tokens.shape, torch.int32, index, "tokens"), dp, pitch,
-            _dtype_code(dy.dtype), float(scale), rows, vocab, width,
+            _dtype_code(dy.dtype), float(scale), rows, _size(vocab), _size(width),
             _whole(dtable, (vocab, width), dtable.dtype, index, "dtable"), _dtype_code(dtable.dtype),
             *_scratch(workspace, index))
