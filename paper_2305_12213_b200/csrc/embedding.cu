@@ -92,8 +92,10 @@ __global__ void __launch_bounds__(kBlock) embedding_kernel(const __grid_constant
         if (row >= a.rows) break;
         float x[8];
         v[d].values(x);
+        if (token[d] >= 0 && token[d] < a.vocab) {             // else zeros whatever the scale is
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= a.scale;
+            for (int j = 0; j < 8; ++j) x[j] *= a.scale;
+        }
         store8(static_cast<OT*>(a.out) + row * a.out_pitch + col, n, x);
     }
 }
@@ -539,9 +541,11 @@ __global__ void __launch_bounds__(kBlock) embedding_few_kernel(const __grid_cons
         float sum[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+        bool named = false;                                     // a row that no token names is zeros whatever the scale is
 #pragma unroll
         for (int h = 0; h < kHeld; ++h) {
             unsigned found = __ballot_sync(0xFFFFFFFFu, token[h] == v);
+            named = named || found;
             while (found) {                                     // the same for the whole warp; ascending rows
                 Raw8<DT> x[kDeep];
                 bool in[kDeep];
@@ -562,8 +566,10 @@ __global__ void __launch_bounds__(kBlock) embedding_few_kernel(const __grid_cons
                 }
             }
         }
+        if (named) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] *= a.scale;
+            for (int j = 0; j < 8; ++j) sum[j] *= a.scale;
+        }
         if (n > 0) store8(static_cast<OT*>(a.out) + static_cast<long long>(v) * a.width + col, n, sum);
     }
 }

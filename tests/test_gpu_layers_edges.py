@@ -1,5 +1,5 @@
 """Calls of the layers that their documentation allows and that are easily got wrong: buffers at any element of a flat one, offsets
-past 32 bits, in-place sums and rows that are not finite in the kernels of CTA pairs."""
+past 32 bits, scales that are not finite, in-place sums and rows that are not finite in the kernels of CTA pairs."""
 import pytest
 import torch
 
@@ -237,3 +237,29 @@ def test_whole_tensors_past_32_bits():
     want = 140 / 128 * last                                     # 140 equal terms: each sum is off by half a step of fp32
     assert ((x[-1].float() - want).abs() <= (ref.BF16 + 141 * 2.0**-24) * want.abs()).all()
     assert (x[1:-1] == 0).all()
+
+
+# ------------------------------------------------------------------------------------------------ scales
+@pytest.mark.parametrize("scale", [float("inf"), float("nan"), -2.0, 0.0])
+@pytest.mark.parametrize("rows", [40, 700])
+def test_rows_without_a_token_are_zeros_whatever_the_scale(rows, scale):
+    vocab, n = 90, 24
+    tokens = torch.randint(0, vocab // 2, (rows,), generator=gen(1), device="cuda", dtype=torch.int32) * 2 - 1     # -1, 1, 3, ...
+    table, dy = normal(2, vocab, n, dtype=torch.float32), normal(3, rows, n, dtype=torch.float32)
+    out = torch.full((rows, n), 7.0, device="cuda")
+    binding.embedding(tokens, table, out, scale=scale)
+    t = tokens.cpu().long()
+    want = torch.where((t >= 0)[:, None], table.cpu()[t.clamp_min(0)] * scale, torch.zeros(()))
+    assert torch.equal(out.cpu().nan_to_num(1e9), want.nan_to_num(1e9))
+    assert (out.view(torch.int32)[tokens < 0] == 0).all()
+    grad = torch.full((vocab, n), 7.0, device="cuda")
+    binding.embedding_grad(tokens, dy, grad, workspace(binding.embedding_grad_workspace_bytes(rows, vocab, n)), scale=scale)
+    used = torch.zeros(vocab, dtype=torch.bool, device="cuda")
+    used[tokens[tokens >= 0].long()] = True
+    assert (grad.view(torch.int32)[~used] == 0).all()
+    if scale != scale or scale in (float("inf"),):
+        assert not grad[used].isfinite().any()
+    else:
+        want = ref.embedding_grad(tokens, dy.cpu(), vocab, scale)
+        size = ref.embedding_grad(tokens, dy.cpu().abs(), vocab, abs(scale))
+        assert ((f64(grad) - want).abs() <= (rows + 2) * 2.0**-24 * size + 1e-300).all()
