@@ -7,6 +7,7 @@
 #include "common.h"
 #include "dynbatch_bench.h"
 #include "layer_gemm.cuh"
+#include "tensor_map.h"
 
 namespace dynbatch {
 namespace {
@@ -180,21 +181,6 @@ struct Launch {
     Launch& operator=(const Launch&) = delete;
 };
 
-using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledFn encode_tiled() {
-    static EncodeTiledFn fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return reinterpret_cast<EncodeTiledFn>(p);
-    }();
-    return fn;
-}
-
 struct Matrix {              // bf16, row-major
     const bf16* p = nullptr;
     long long rows = 0, cols = 0, pitch = 0;
@@ -204,33 +190,12 @@ bool on_grid(const void* p, long long pitch) { return reinterpret_cast<uintptr_t
 
 // Boxes of box_rows rows x 64 columns with the 128-byte swizzle; what lies outside the matrix reads as zero.
 db_status make_map(CUtensorMap* map, const Matrix& m, int box_rows) {
-    EncodeTiledFn enc = encode_tiled();
-    if (!enc) {
-        record_message("cuTensorMapEncodeTiled is not available from this driver");
-        return DB_ERR_CUDA;
-    }
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(m.cols), static_cast<cuuint64_t>(m.rows)};
-    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(m.pitch) * 2};
-    const cuuint32_t box[2] = {lg::kBlockK, static_cast<cuuint32_t>(box_rows)};
-    const cuuint32_t elem[2] = {1, 1};
-    const auto encode = [&] {
-        return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<bf16*>(m.p), dims, strides, box, elem,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    };
-    CUresult r = encode();
-    if (r != CUDA_SUCCESS) {
-        // a host thread that has not yet called the runtime for its device has no context, which the driver's call needs
-        int device = 0;
-        DB_CUDA_TRY(cudaGetDevice(&device));
-        DB_CUDA_TRY(cudaSetDevice(device));
-        r = encode();
-    }
-    if (r != CUDA_SUCCESS) {
-        record_message("cuTensorMapEncodeTiled rejected an operand of a layer");
-        return DB_ERR_CUDA;
-    }
-    return DB_OK;
+    const TensorMapSpec spec{CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m.p,
+                             {static_cast<cuuint64_t>(m.cols), static_cast<cuuint64_t>(m.rows)},
+                             {static_cast<cuuint64_t>(m.pitch) * 2},
+                             {lg::kBlockK, static_cast<cuuint32_t>(box_rows)},
+                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B};
+    return encode_tensor_map(map, spec, "cuTensorMapEncodeTiled rejected an operand of a layer");
 }
 
 // ---------------------------------------------------------------------------------------------- the products' plan

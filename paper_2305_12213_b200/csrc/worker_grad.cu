@@ -26,6 +26,7 @@
 #include "tc_gemm.cuh"
 #include "tc_grad.cuh"
 #include "tc_logits.cuh"
+#include "tensor_map.h"
 
 namespace dynbatch {
 namespace {
@@ -616,47 +617,19 @@ bool valid_group_shape(long long rows, int K, int D, int C) {
     return K >= 1 && K <= DB_MAX_K && rows >= K && rows <= (1 << 22) && D >= 1 && C >= 1;
 }
 
-// cuTensorMapEncodeTiled, looked up through the runtime so that the library needs no link against the driver.
-using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_tiled() {
-    static EncodeTiledFn fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) !=
-                cudaSuccess || q != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return reinterpret_cast<EncodeTiledFn>(p);
-    }();
-    return fn;
-}
-
 // Tensor map of a row-major fp32 array [rows, cols] with `pitch` floats per row, read in boxes of
 // box_rows rows x 32 columns; elements outside [rows, cols] read as zero.  Operands that are contiguous
 // along the output index need the 128-byte swizzle of 32-byte pieces (the only one the tensor core takes
 // for 32-bit operands in that orientation), operands contiguous along the reduction the ordinary one.
 db_status make_operand_map(CUtensorMap* map, const float* base, long long rows, long long cols, long long pitch,
                            int box_rows, bool output_index_major) {
-    EncodeTiledFn enc = encode_tiled();
-    if (!enc) {
-        record_message("cuTensorMapEncodeTiled is not available from this driver");
-        return DB_ERR_CUDA;
-    }
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
-    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(pitch) * sizeof(float)};
-    const cuuint32_t box[2] = {32, static_cast<cuuint32_t>(box_rows)};
-    const cuuint32_t elem[2] = {1, 1};
-    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<float*>(base), dims, strides, box, elem,
-                           CU_TENSOR_MAP_INTERLEAVE_NONE,
-                           output_index_major ? CU_TENSOR_MAP_SWIZZLE_128B_ATOM_32B : CU_TENSOR_MAP_SWIZZLE_128B,
-                           CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) {
-        record_message("cuTensorMapEncodeTiled rejected an operand layout of the worker gradient");
-        return DB_ERR_CUDA;
-    }
-    return DB_OK;
+    const TensorMapSpec spec{CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base,
+                             {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)},
+                             {static_cast<cuuint64_t>(pitch) * sizeof(float)},
+                             {32, static_cast<cuuint32_t>(box_rows)},
+                             output_index_major ? CU_TENSOR_MAP_SWIZZLE_128B_ATOM_32B : CU_TENSOR_MAP_SWIZZLE_128B,
+                             CU_TENSOR_MAP_L2_PROMOTION_L2_128B};
+    return encode_tensor_map(map, spec, "cuTensorMapEncodeTiled rejected an operand layout of the worker gradient");
 }
 
 // Tensor map of a row-major fp32 array [rows, pitch] (pitch a multiple of 32 floats) seen as
@@ -667,23 +640,12 @@ db_status make_operand_map(CUtensorMap* map, const float* base, long long rows, 
 // stored.
 db_status make_chunked_map(CUtensorMap* map, const float* base, long long rows, long long pitch, int box_rows,
                            int box_chunks) {
-    EncodeTiledFn enc = encode_tiled();
-    if (!enc) {
-        record_message("cuTensorMapEncodeTiled is not available from this driver");
-        return DB_ERR_CUDA;
-    }
-    const cuuint64_t dims[3] = {32, static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(pitch / 32)};
-    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(pitch) * sizeof(float), 128};
-    const cuuint32_t box[3] = {32, static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(box_chunks)};
-    const cuuint32_t elem[3] = {1, 1, 1};
-    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<float*>(base), dims, strides, box, elem,
-                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B_ATOM_32B,
-                           CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) {
-        record_message("cuTensorMapEncodeTiled rejected the chunked layout of a gradient operand");
-        return DB_ERR_CUDA;
-    }
-    return DB_OK;
+    const TensorMapSpec spec{CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, base,
+                             {32, static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(pitch / 32)},
+                             {static_cast<cuuint64_t>(pitch) * sizeof(float), 128},
+                             {32, static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(box_chunks)},
+                             CU_TENSOR_MAP_SWIZZLE_128B_ATOM_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B};
+    return encode_tensor_map(map, spec, "cuTensorMapEncodeTiled rejected the chunked layout of a gradient operand");
 }
 
 // out(n, c) = sum_d X(n, d) W(d, c) with both operands copied by TMA from where the caller left them
