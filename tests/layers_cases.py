@@ -18,6 +18,8 @@ LINEAR = [  # rows, n_in, n_out, bias, residual, activation, kept, pitch, shift
     (2050, 1096, 2184, True, True, "silu", "e4m3", 1112, 5),    # x copied onto the grid, the weights not
     (3000, 1032, 1544, True, True, "gelu", "bf16", 1048, 8),
     (8200, 264, 1544, False, True, "none", "none", 0, 0),
+    (515, 96, 32000, True, False, "none", "none", 0, 0),        # a vocabulary's columns
+    (70, 72, 32001, False, True, "gelu", "e4m3", 0, 0),
 ]
 FFN = [  # rows, width, hidden, residual, activation, kept, pitch, shift
     (5016, 920, 9, True, "silu", "bf16", 0, 0),
