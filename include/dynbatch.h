@@ -548,7 +548,9 @@ db_status db_contract_f32(const float* A, int64_t a_row, int64_t a_k,
  *                       dw_gate = x^T d_gate;  dw_up = x^T d_up;  dw_down = h^T dy
  *
  * act is one of db_activation: none, max(z, 0) with slope 0 at 0, z P(z) with P the
- * normal distribution function, z / (1 + e^-z).
+ * normal distribution function, z / (1 + e^-z).  P is off by about 1e-7 at most, and less
+ * than half a bf16 step of z P(z) as far down as z = -6, where that is -6e-9; e^v by about
+ * 2^-23 (1 + |v|) and a quotient by 2^-23, relative.
  *
  * What is kept for the backward pass (z; gate and up) is written by the forward
  * call, where wanted, as bf16 or as 8-bit checkpoints (below): rounded from the
@@ -582,9 +584,10 @@ db_status db_contract_f32(const float* A, int64_t a_row, int64_t a_k,
  *                The query depends on the current device's number of SMs.
  *
  * Buffers that a call writes must not overlap any other it touches, but as said above
- * (DB_ERR_ARG); different columns of one wider tensor (equal pitches) do not overlap.  Any alignment down to the element size is accepted; outputs with
- * 16-byte aligned rows take wide stores.  NaN and Inf in a row of x stay in that row of
- * y; in a weight gradient they spread to their feature.  The order of every sum depends
+ * (DB_ERR_ARG); different columns of one wider tensor (equal pitches) do not overlap.  Any
+ * alignment down to the element size is accepted; outputs with 16-byte aligned rows take
+ * wide stores.  NaN and Inf in a row of x stay in that row of y; in a weight gradient
+ * they spread to their feature.  The order of every sum depends
  * on sizes and device alone: the same call gives the same bits.  fp32 weight gradients:
  * adding into the accumulator truncates (up to about 4e-9 * rows, relative, towards
  * zero).  Calls on one stream may share a workspace, calls that may overlap on the device
@@ -686,7 +689,8 @@ db_status db_checkpoint_unpack(const void* codes, const void* scale,
  * zeros and has no gradient, as a label outside the classes has none in the worker
  * gradient.  Sums are fp32, in the order of a stable sort of the tokens cut into units
  * whose length depends on rows alone; no atomics on values: the same call gives the
- * same bits.  Rows of dtable whose token does not occur are written as zeros.
+ * same bits.  Rows of dtable whose token does not occur are written as zeros, whatever
+ * the scale.
  *
  *   tokens  device, rows int32
  *   table, dtable   device, [vocab, width] contiguous, fp32 or bf16

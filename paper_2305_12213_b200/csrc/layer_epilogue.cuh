@@ -327,10 +327,12 @@ struct Codes8 {
 };
 
 // ------------------------------------------------------------------------------------------------ activations
-// silu(z) = z s, s = 1 / (1 + e^-z);  gelu(z) = z P(z), P the normal distribution function.  The approximate exponential
-// and reciprocal are off by a few 2^-23 of a value that is rounded to 2^-9; arguments and results below 2^-126 count as 0.
+// silu(z) = z s, s = 1 / (1 + e^-z);  gelu(z) = z P(z), P the normal distribution function.  The approximate exponential of v
+// is off by about 2^-23 (1 + |v|), the reciprocal by 2^-23, relative, of a value that is rounded to 2^-9; arguments and results
+// below 2^-126 count as 0.
 // P by formula 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions: for x >= 0
-//     erfc(x) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) e^(-x^2),  t = 1 / (1 + 0.3275911 x),  off by at most 1.5e-7,
+//     erfc(x) = t (a1 + t (a2 + t (a3 + t (a4 + t a5)))) e^(-x^2),  t = 1 / (1 + 0.3275911 x),  off by at most 1.5e-7
+// (relative to it 5e-4 at z = -4, 1.6e-3 at -5, 3.6e-3 at -6, where half a bf16 step is 3.9e-3 and gelu -6e-9),
 // with x = |z| / sqrt(2): P is erfc / 2 below zero and 1 - erfc / 2 above, so gelu = max(z, 0) - |z| erfc / 2.  Two
 // special-function instructions, and the e^(-z^2 / 2) is the one that the slope needs.  With erff the epilogue, not the
 // products, set the time of a 1024-deep layer (8191 x 1024 to 4096: 92 us).

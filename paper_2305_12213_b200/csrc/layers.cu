@@ -249,7 +249,15 @@ long long tiles_of(Kind kind, TileShape shape, const Size& s) {
 // more for each of two CTAs on an SM; a tile something for its start and end; and a reduction in pieces a second kernel,
 // which reads eight pieces at a time, and the traffic of the partial sums.  In 64-column tiles, us by pieces 1, 4, 8, 16:
 // 256 x 2048 x 1000 11.9, 10.2, 9.3, 11.9; 16 x 2048 x 512 above 7.4, 7.3, 6.7, 6.8 (32: 8.4); 1000 x 1024 x 256 7.7, 8.7, 8.8;
-// 1024 x 1024 x 1024 8.3, in two 14.4, in pairs of 256 columns 11.4.
+// 1024 x 1024 x 1024 8.3, in two 14.4.  Replayed from a graph, us in pairs of 256 and 128 columns and single CTAs of 128 and 64
+// (rows x n_in x n_out, each in its best number of pieces, the picked one in brackets):
+//   y   256 x 2048 x 1000 11.8, 9.5, 11.6, [9.2]     1024 x 1024 x 1024 10.5, 8.8, 9.1, [8.4]     2048 x 1024 x 1024 10.9, [9.6], 9.7, 9.1
+//       150 x 5536 x 1704 13.4, [12.6], 16.0, 15.2   4100 x 320 x 640 7.5, 7.5, [6.8], 7.0        3000 x 1032 x 1544 [21.1], 22.2, 30.8, 32.9
+//       2000 x 4096 x 1024 25.3, [22.2], 24.3, 23.1  8191 x 1024 x 4096 [48.4], 69.0, 64.1, 84.2
+//   dx  9236 x 136 x 1088 11.4, [9.8], 10.1, 10.3    2050 x 1096 x 2184 [20.4], 23.7, 31.5, 35.9  8191 x 1024 x 4096 [50.3], 71.5, 61.8, 82.1
+//   dW  129 x 1568 x 4608 9.5, 10.6, [9.1], 10.1     3000 x 1032 x 1544 24.6, [20.7], 24.4, 31.8  8191 x 1024 x 4096 [49.9], 72.4, 62.6, 83.8
+// Of 39 products looked at this way the pick was within 7 % of the best but for one: dW of 5000 x 520 x 1032 took 22.2 in single
+// CTAs of 128 columns and six pieces, 19.7 in pairs of 256 and four.  What follows the product is not in the estimate.
 Plan make_plan(Kind kind, const Size* sizes, int n, long long blocks) {
     constexpr double kBlock[kTileShapes] = {560, 430, 560, 380}, kShared[kTileShapes] = {560, 430, 900, 550};
     constexpr double kTile[kTileShapes] = {4700, 3100, 1500, 1300}, kCombine = 4500, kEight = 1000;
