@@ -121,6 +121,14 @@ __device__ __forceinline__ void mma_commit(uint64_t* bar) {
     else
         tc::mma_commit(bar);
 }
+// The same, in this CTA alone: what gives up must leave nothing on its way to the other CTA, which may have left by then.
+template <int CG>
+__device__ __forceinline__ void mma_commit_here(uint64_t* bar) {
+    if (CG == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(tc::smem_u32(bar)) : "memory");
+    else
+        tc::mma_commit(bar);
+}
 // A whole warp's bounded wait.  Lanes that poll on their own may differ where the limit runs out or the other warps give up, and
 // those that went on would wait at the next full-warp instruction for those that left: all go on, or all leave.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
@@ -372,7 +380,7 @@ layer_gemm_kernel(const __grid_constant__ GemmArgs g) {
                 __syncwarp();
             }
             if (!ok) {
-                if (elect_one()) mma_commit<CG>(&drain_bar);
+                if (elect_one()) mma_commit_here<CG>(&drain_bar);
                 __syncwarp();
                 const unsigned long long t0 = tc::global_ns();
                 while (!tc::mbar_try_wait(&drain_bar, 0) && tc::global_ns() - t0 < tc::kWaitLimitNs) {}

@@ -51,3 +51,16 @@ def test_waits_have_one_verdict_for_a_warp():
                 assert shared or one_lane, (function, line.strip())
             waits += line.count("mbar_wait(") + line.count("warp_wait(")
     assert waits >= 6
+
+
+def test_giving_up_leaves_no_arrival_for_the_other_cta():
+    """Every barrier that the products arrive on in both CTAs of a pair is waited for in both; the one that only the CTA that gives
+    up waits for is arrived on there alone."""
+    body = dict(functions("layer_gemm.cuh"))["layer_gemm_kernel"]
+    both = re.findall(r"mma_commit<CG>\(&(\w+)", body)
+    assert sorted(both) == ["empty_bar", "ready_bar"]
+    waited = re.findall(r"(?:warp_wait|tc::mbar_wait)\(&(\w+)", body)
+    assert all(waited.count(b) >= 1 for b in both)
+    assert re.findall(r"mma_commit_here<CG>\(&(\w+)", body) == ["drain_bar"]
+    here = dict(functions("layer_gemm.cuh"))["mma_commit_here"]
+    assert "multicast" not in here and "cta_group::2" in here
